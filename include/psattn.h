@@ -75,6 +75,9 @@ typedef enum {
 
 typedef enum { PSATTN_F32 = 0, PSATTN_BF16 = 1 } psattn_dtype;
 
+/* activation of the gated feed-forward block: g / (1 + exp(-g)), or g Phi(g) with the normal distribution's Phi (no tanh form) */
+typedef enum { PSATTN_ACT_SILU = 0, PSATTN_ACT_GELU = 1 } psattn_act;
+
 /* tile classes of the block mask */
 enum { PSATTN_TILE_SKIPPED = 0, PSATTN_TILE_PARTIAL = 1, PSATTN_TILE_FULL = 2 };
 
@@ -380,6 +383,59 @@ int psattn_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t vocab, co
                        void* dlogits, void* hip_stream);
 int psattn_dpo_loss(int32_t n_pairs, float beta, const float* logp_policy, const float* logp_ref,
                     float* loss, float* d_logp, void* hip_stream);
+
+/*
+ * What stands beside attention and the loss head in a model: the rows that enter it, the norm in front of each part of a
+ * block, and the block's feed-forward part.  They act on single tokens, so prefix sharing saves the same share of them as of
+ * the projections (Section 4.2 times such parts with the attention).  A packed buffer of T tokens is T rows; padding is
+ * computed like any row, and keeps to itself.  All tensors are contiguous, row-major, of element type dt unless said otherwise;
+ * they may start wherever an element may and have any width, 16-byte boundaries and widths that are whole 16-byte groups
+ * being faster.  Any value is taken: inf and NaN reach the rows that read them and no others.  All sums are fp32, in an order
+ * that depends on the sizes alone: the same call gives the same bits.  Workspaces are the caller's device memory, of at least
+ * the bytes that the call of that name gives (never 0 for valid arguments), contents undefined on entry and exit, one for
+ * each call in flight.  No call allocates or blocks, and all may be captured into a graph.  No rows: the forward calls
+ * do nothing, the backward calls write zeros as the gradients of weights.
+ *
+ * psattn_embed_fwd: X[t, :] = scale * W[token_ids[t], :], W [vocab, hidden], X [n_tokens, hidden], token_ids device int32.  An
+ * id outside [0, vocab) (padding) gives a row of zeros.
+ * psattn_embed_bwd: dW[v, :] = scale * sum of dX[t, :] over the tokens with id v, taken in order of the tokens; dW
+ * [vocab, hidden] is written as a whole, zeros included.  Ids outside [0, vocab) give nothing, and their rows of dX are not read.
+ */
+int psattn_embed_fwd(int32_t dt, int32_t n_tokens, int32_t vocab, int32_t hidden, float scale, const int32_t* token_ids,
+                     const void* W, void* X, void* hip_stream);
+size_t psattn_embed_bwd_workspace_bytes(int32_t dt, int32_t n_tokens, int32_t vocab, int32_t hidden);
+int psattn_embed_bwd(int32_t dt, int32_t n_tokens, int32_t vocab, int32_t hidden, float scale, const int32_t* token_ids,
+                     const void* dX, void* dW, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * psattn_layernorm_fwd: with S = X + R rounded to dt (the residual stream after another part of the block; R = S = NULL: S
+ * is X), Y = (S - mean) * rstd * weight + bias over each row, rstd = 1 / sqrt(mean((S - mean)^2) + eps), the mean square of the
+ * centred values.  weight, bias: [hidden] of dt; bias may be NULL.  mean, rstd: device float [n_rows], for the backward.
+ * psattn_layernorm_bwd: from the forward's S (X where there was no R), mean and rstd: dX = the gradient with respect to S, to which
+ * dS is added where it is not NULL (what reaches S by the residual stream); it is that of X and of R.  dweight, dbias [hidden]
+ * of dt; dbias may be NULL.
+ */
+int psattn_layernorm_fwd(int32_t dt, int32_t n_rows, int32_t hidden, float eps, const void* X, const void* R,
+                         const void* weight, const void* bias, void* S, void* Y, float* mean, float* rstd, void* hip_stream);
+size_t psattn_layernorm_bwd_workspace_bytes(int32_t n_rows, int32_t hidden);
+int psattn_layernorm_bwd(int32_t dt, int32_t n_rows, int32_t hidden, const void* S, const void* weight, const float* mean,
+                         const float* rstd, const void* dY, const void* dS, void* dX, void* dweight, void* dbias,
+                         void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * psattn_ffn_fwd: G = X Wg^T, U = X Wu^T, H = act(G) o U, Y = H Wd^T.  X, Y [n_tokens, hidden]; Wg, Wu [inner, hidden] and Wd
+ * [hidden, inner], the [out_features, in_features] convention of the attention layer.  G, U, H [n_tokens, inner] are kept for the
+ * backward; G and U may both be NULL if none follows, H is needed either way.  H is rounded once, from the fp32 sums.
+ * psattn_ffn_bwd: dX, dWg, dWu, dWd from the forward's G, U, H and dY.
+ */
+int psattn_ffn_fwd(int32_t dt, int32_t act, int32_t n_tokens, int32_t hidden, int32_t inner, const void* X, const void* Wg,
+                   const void* Wu, const void* Wd, void* G, void* U, void* H, void* Y, void* workspace,
+                   size_t workspace_bytes, void* hip_stream);
+size_t psattn_ffn_fwd_workspace_bytes(int32_t dt, int32_t n_tokens, int32_t hidden, int32_t inner);
+int psattn_ffn_bwd(int32_t dt, int32_t act, int32_t n_tokens, int32_t hidden, int32_t inner, const void* X, const void* Wg,
+                   const void* Wu, const void* Wd, const void* G, const void* U, const void* H, const void* dY, void* dX,
+                   void* dWg, void* dWu, void* dWd, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t psattn_ffn_bwd_workspace_bytes(int32_t dt, int32_t n_tokens, int32_t hidden, int32_t inner);
 
 /*
  * Measurement aid (no part of the computation): issues the memory operations that a

@@ -10,5 +10,6 @@ from .binding import (  # noqa: F401
     load_library, psattn_build_meta, psattn_bwd, psattn_bwd_workspace_bytes, psattn_fwd,
     psattn_kernel_name, psattn_profile_enable, psattn_profile_read, psattn_trim_pool, BF16, F32,
     psattn_bwd_static, psattn_bwd_static_max_rows, psattn_probe_dq_atomics, psattn_pack_ffd, psattn_build_meta_multi, Rope, psattn_fwd_rope, psattn_bwd_rope,
-    LogprobPlan, psattn_logprob_fwd, psattn_logprob_bwd, psattn_dpo_loss,
+    LogprobPlan, psattn_logprob_fwd, psattn_logprob_bwd, psattn_dpo_loss, ACT_SILU, ACT_GELU,
+    psattn_embed_fwd, psattn_embed_bwd, psattn_layernorm_fwd, psattn_layernorm_bwd, psattn_ffn_fwd, psattn_ffn_bwd,
 )

@@ -1,0 +1,14 @@
+// The feed-forward block's products: what psattn_ffn.hip (arguments, order of the products) calls.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "psattn_gemm.h"
+
+namespace psattn {
+namespace gemm {
+
+// One product, enqueued on s.  pkc, qkc: k is the contiguous axis of P, Q.  Returns a psattn_status.
+int product_any(int dt, Pass pass, int act, bool pkc, bool qkc, const Product& d, hipStream_t s);
+
+}  // namespace gemm
+}  // namespace psattn

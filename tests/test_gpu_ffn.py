@@ -1,0 +1,224 @@
+"""Gated feed-forward block: forward and backward against the 64-bit oracle, exactly where whole numbers allow it."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2410_20305_amd as ps
+from block_util import HALF, TINY, Guarded, close, hold, np64, rnd, same
+from oracle import psattn_block_oracle as blk
+
+pytestmark = pytest.mark.gpu
+
+EPS32 = 2.0 ** -24
+# fp32 functions of the activation: exp, erfc and the arithmetic around them, in roundings
+ACT = 24 * EPS32
+
+
+def _inputs(rng, T, h, n, dtype):
+    return (rnd(rng, T, h, dtype=dtype), rnd(rng, n, h, scale=h ** -0.5, dtype=dtype), rnd(rng, n, h, scale=h ** -0.5, dtype=dtype),
+            rnd(rng, h, n, scale=n ** -0.5, dtype=dtype), rnd(rng, T, h, dtype=dtype))
+
+
+def _call(dev, ins, act, kept=None):
+    """Forward and backward on guarded buffers; `kept`: (G, U, H) for the backward instead of the forward's."""
+    X, Wg, Wu, Wd, dY = ins
+    (T, h), n = X.shape, Wg.shape[0]
+    t = [dev.put(a) for a in (X, Wg, Wu, Wd)]
+    Y, own = ps.psattn_ffn_fwd(*t, act=act, Y=dev.empty(T, h), kept=tuple(dev.empty(T, n) for _ in range(3)))
+    kept = own if kept is None else tuple(dev.put(a) for a in kept)
+    grads = ps.psattn_ffn_bwd(*t, kept, dev.put(dY), act=act, dX=dev.empty(T, h), dWg=dev.empty(n, h), dWu=dev.empty(n, h), dWd=dev.empty(h, n))
+    dev.check()
+    return Y, own, grads
+
+
+def _prod(a, b, err_a, k):
+    """What |a| |b| sums of k fp32 additions may be off by, a itself being off by err_a."""
+    return (k + 2) * EPS32 * (np.abs(a) @ np.abs(b)) + err_a @ np.abs(b)
+
+
+SHAPES = [(1, 1, 1), (1, 8, 8), (1, 64, 128), (2, 7, 3), (3, 130, 65), (16, 64, 64), (17, 96, 200), (31, 256, 129), (33, 72, 264), (64, 128, 256), (65, 64, 136),
+          (100, 1, 40), (127, 200, 96), (128, 128, 128), (129, 264, 40), (130, 257, 131), (221, 192, 512), (256, 512, 256), (257, 520, 264), (300, 33, 1000),
+          (512, 136, 72), (520, 640, 328), (1, 4096, 72), (5, 1000, 2731), (48, 768, 1024), (700, 64, 2048)]
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,h,n", SHAPES)
+def test_against_oracle(T, h, n, dtype, act):
+    """Every result against the oracle's on the library's own kept G, U, H, so that each bound counts its own roundings only."""
+    rng = np.random.default_rng(T * 7 + h * 3 + n)
+    ins = _inputs(rng, T, h, n, dtype)
+    X, Wg, Wu, Wd, dY = ins
+    half = HALF[dtype]
+    Y, kept, (dX, dWg, dWu, dWd) = _call(Guarded(dtype), ins, act)
+    g, u = X @ Wg.T, X @ Wu.T
+    eg, eu = (h + 2) * EPS32 * (np.abs(X) @ np.abs(Wg.T)), (h + 2) * EPS32 * (np.abs(X) @ np.abs(Wu.T))
+    close(kept[0], g, half * np.abs(g) + (1 + half) * eg, "G")
+    close(kept[1], u, half * np.abs(u) + (1 + half) * eu, "U")
+    a, da = blk.act(g, act)
+    # |act'| <= 1.13, |act''| <= 0.8: the error of g goes through them
+    ea = 1.13 * eg + ACT * np.abs(a) + ACT * TINY
+    close(kept[2], a * u, half * np.abs(a * u) + (1 + half) * (ea * np.abs(u) + (np.abs(a) + ea) * eu + 2 * EPS32 * np.abs(a * u)) + TINY, "H")
+    G, U, H = (np64(t) for t in kept)
+    ref = H @ Wd.T
+    close(Y, ref, half * np.abs(ref) + (1 + half) * _prod(H, Wd.T, np.zeros_like(H), n), "Y")
+    rX, rWg, rWu, rWd, _, _ = blk.ffn_grad(X, Wg, Wu, Wd, G, U, H, dY, act)
+    close(dWd, rWd, half * np.abs(rWd) + (1 + half) * _prod(dY.T, H, np.zeros_like(dY.T), T), "dWd")
+    a, da = blk.act(G, act)
+    dH = dY @ Wd
+    eh = (h + 2) * EPS32 * (np.abs(dY) @ np.abs(Wd))
+    dG, dU = dH * U * da, dH * a
+    eda = ACT * (np.abs(da) + 1)
+    eG = (half + 3 * EPS32) * np.abs(dG) + (1 + half) * np.abs(U) * (eh * (np.abs(da) + eda) + np.abs(dH) * eda) + TINY
+    eU = (half + 3 * EPS32) * np.abs(dU) + (1 + half) * (eh * np.abs(a) + ACT * np.abs(dU)) + TINY
+    close(dX, rX, half * np.abs(rX) + (1 + half) * (_prod(dG, Wg, eG, 2 * n) + _prod(dU, Wu, eU, 2 * n)), "dX")
+    close(dWg, rWg, half * np.abs(rWg) + (1 + half) * _prod(dG.T, X, eG.T, T), "dWg")
+    close(dWu, rWu, half * np.abs(rWu) + (1 + half) * _prod(dU.T, X, eU.T, T), "dWu")
+
+
+def _whole(rng, *shape, most=1, share=0.25):
+    return np.where(rng.uniform(size=shape) < share, rng.integers(-most, most + 1, shape), 0).astype(np.float64)
+
+
+EXACT = SHAPES + [(1000, 264, 520), (1, 2048, 4096), (8, 4104, 520), (24, 1024, 3000), (64, 2048, 1032), (260, 1032, 2056), (1031, 520, 776), (2000, 256, 264), (384, 2048, 4096)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,h,n", EXACT)
+def test_whole_numbers_are_exact(T, h, n, dtype):
+    """Small whole numbers: every sum is exact in fp32, so that one term too many or too few shows.  Gates of 64 are open
+    (SiLU(64 k) = 64 k for k > 0, and all but nothing, below 1e-24, for k < 0), a gate of 0 has the derivative 1/2."""
+    rng = np.random.default_rng(T + h + n)
+    X, Wg, Wu = _whole(rng, T, h), _whole(rng, n, h) * 64, _whole(rng, n, h)
+    Wd, dY = _whole(rng, h, n), _whole(rng, T, h)
+    kG = np.where(rng.uniform(size=(T, n)) < 0.5, 64.0, 0.0)
+    kU = rng.choice([-2.0, 2.0], (T, n))
+    kH = _whole(rng, T, n, most=2)
+    Y, kept, (dX, dWg, dWu, dWd) = _call(Guarded(dtype), (X, Wg, Wu, Wd, dY), "silu", kept=(kG, kU, kH))
+    r = hold(dtype)
+    g, u = X @ Wg.T, X @ Wu.T
+    same(kept[0], r(g), "G")
+    same(kept[1], r(u), "U")
+    H = np.where(g > 0, r(g * u), 0.0)
+    got = np64(kept[2])
+    assert np.array_equal(np.where(np.abs(got) < 1e-20, 0.0, got), H), "H"
+    # Y alone has terms that are no whole numbers: closed gates', below 1e-20 in all.  A matrix instruction may let such a term
+    # cost the sum that it joins its last bit, 2^-23 of what is summed; a whole term too many or too few is 64 at least.
+    y = H @ Wd.T
+    closed = ((g < 0) & (u != 0)).astype(np.float64) @ (np.abs(Wd.T) > 0)
+    close(Y, y, np.where(closed > 0, HALF[dtype] * np.abs(y) + 1.01 * closed * 2.0 ** -23 * (np.abs(H) @ np.abs(Wd.T)) + 1e-20, np.abs(r(y) - y)), "Y")
+    same(dWd, r(dY.T @ kH), "dWd")
+    dH = dY @ Wd
+    dG, dU = r(dH * kU * np.where(kG > 0, 1.0, 0.5)), r(dH * kG)
+    same(dWg, r(dG.T @ X), "dWg")
+    same(dWu, r(dU.T @ X), "dWu")
+    same(dX, r(dG @ Wg + dU @ Wu), "dX")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,h,n,shift", [(33, 64, 128, 1), (130, 256, 264, 3), (300, 512, 136, 2), (4, 128, 64, 1)])
+def test_unaligned_tensors(T, h, n, shift, dtype):
+    rng = np.random.default_rng(9)
+    X, Wg, Wu, Wd, dY = _whole(rng, T, h), _whole(rng, n, h) * 64, _whole(rng, n, h), _whole(rng, h, n), _whole(rng, T, h)
+    ins = (X, Wg, Wu, Wd, dY)
+    a, b = _call(Guarded(dtype), ins, "gelu"), _call(Guarded(dtype, shift), ins, "gelu")
+    for x, y in zip((a[0], *a[1], *a[2]), (b[0], *b[1], *b[2])):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("T,h,n", [(1, 256, 512), (40, 192, 320), (300, 264, 130)])
+def test_forward_without_backward(T, h, n):
+    rng = np.random.default_rng(4)
+    t = [torch.from_numpy(a).to(torch.bfloat16).cuda() for a in _inputs(rng, T, h, n, "bf16")[:4]]
+    Y, kept = ps.psattn_ffn_fwd(*t)
+    Y2, none = ps.psattn_ffn_fwd(*t, keep=False)
+    H = torch.empty(T, n, dtype=torch.bfloat16, device="cuda")
+    Y3, _ = ps.psattn_ffn_fwd(*t, keep=False, kept=(None, None, H))
+    assert none is None and torch.equal(Y, Y2) and torch.equal(Y, Y3) and torch.equal(H, kept[2])
+
+
+@pytest.mark.parametrize("T,h,n", [(5, 64, 128), (200, 256, 520), (33, 65, 130)])
+def test_not_finite_keeps_to_its_rows(T, h, n):
+    """A row of X that is not finite reaches its own rows of G, U, H, Y; one of dY its row of dX and its column sums."""
+    rng = np.random.default_rng(6)
+    X, Wg, Wu, Wd, dY = (torch.from_numpy(a).to(torch.bfloat16).cuda() for a in _inputs(rng, T, h, n, "bf16"))
+    Y, kept = ps.psattn_ffn_fwd(X, Wg, Wu, Wd)
+    dX = ps.psattn_ffn_bwd(X, Wg, Wu, Wd, kept, dY)[0]
+    bad = X.clone()
+    bad[T - 1] = float("nan")
+    bad[1, 0] = float("inf")
+    keep = [i for i in range(T) if i not in (1, T - 1)]
+    Y2, kept2 = ps.psattn_ffn_fwd(bad, Wg, Wu, Wd)
+    for a, b in zip((Y, *kept), (Y2, *kept2)):
+        assert torch.equal(a[keep], b[keep]) and not torch.isfinite(b[T - 1]).any()
+    dY[T - 1] = float("nan")
+    dX2, _, _, dWd = ps.psattn_ffn_bwd(X, Wg, Wu, Wd, kept, dY)
+    assert torch.equal(dX[:T - 1], dX2[:T - 1]) and torch.isnan(dX2[T - 1]).all() and torch.isnan(dWd).all()
+    Wn = Wd.clone()   # a row of Wd: its column of Y alone
+    Wn[h - 1] = float("inf")
+    Y3 = ps.psattn_ffn_fwd(X, Wg, Wu, Wn)[0]
+    assert torch.equal(Y3[:, :h - 1], Y[:, :h - 1]) and not torch.isfinite(Y3[:, h - 1]).all()
+
+
+def test_no_tokens():
+    h, n = 24, 40
+    X, W, Wd = torch.empty(0, h, device="cuda"), torch.ones(n, h, device="cuda"), torch.ones(h, n, device="cuda")
+    Y, kept = ps.psattn_ffn_fwd(X, W, W, Wd)
+    assert Y.shape == (0, h)
+    g = [torch.full_like(w, float("nan")) for w in (W, W, Wd)]
+    ps.psattn_ffn_bwd(X, W, W, Wd, kept, X, dWg=g[0], dWu=g[1], dWd=g[2])
+    assert all(torch.all(t == 0) for t in g)
+
+
+@pytest.mark.parametrize("T,h,n", [(3, 512, 1024), (200, 256, 264), (1100, 512, 768)])
+def test_repeats_bit_for_bit(T, h, n):
+    rng = np.random.default_rng(8)
+    X, Wg, Wu, Wd, dY = (torch.from_numpy(a).to(torch.bfloat16).cuda() for a in _inputs(rng, T, h, n, "bf16"))
+    def once():
+        Y, kept = ps.psattn_ffn_fwd(X, Wg, Wu, Wd, act="gelu")
+        return (Y, *kept, *ps.psattn_ffn_bwd(X, Wg, Wu, Wd, kept, dY, act="gelu"))
+    first = once()
+    for _ in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(first, once()))
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_gradient_against_differences(act):
+    """d(sum(Y dY)) along random directions of X and of the weights, in fp32."""
+    rng = np.random.default_rng(12)
+    ins = _inputs(rng, 40, 96, 136, "f32")
+    t = [torch.from_numpy(a).float().cuda() for a in ins]
+    dY = t[4]
+    _, kept = ps.psattn_ffn_fwd(*t[:4], act=act)
+    grads = ps.psattn_ffn_bwd(*t[:4], kept, dY, act=act)
+    for k in range(4):
+        v = torch.from_numpy(rng.standard_normal(ins[k].shape)).float().cuda()
+        step = 1e-2 / v.norm().item() * t[k].norm().item()
+        f = []
+        for sign in (1, -1):
+            moved = list(t[:4])
+            moved[k] = t[k] + sign * step * v
+            f.append((ps.psattn_ffn_fwd(*moved, act=act)[0].double() * dY.double()).sum().item())
+        want = (grads[k].double() * v.double()).sum().item()
+        # the third derivative's term is (1e-2)^2 of the size of the function's own changes
+        scale = (grads[k].double().norm() * v.double().norm()).item()
+        assert abs((f[0] - f[1]) / (2 * step) - want) <= 2e-3 * scale, k
+
+
+def test_refusals_on_the_device():
+    X, W, Wd = torch.zeros(4, 16, device="cuda"), torch.zeros(32, 16, device="cuda"), torch.zeros(16, 32, device="cuda")
+    with pytest.raises(ValueError, match="act"):
+        ps.psattn_ffn_fwd(X, W, W, Wd, act="relu")
+    with pytest.raises(ValueError):
+        ps.psattn_ffn_fwd(X, W, W, W)
+    with pytest.raises(ValueError):
+        ps.psattn_ffn_fwd(X, W, W[:16], Wd)
+    with pytest.raises(TypeError):
+        ps.psattn_ffn_fwd(X, W, W.bfloat16(), Wd)
+    with pytest.raises(ValueError):
+        ps.psattn_ffn_fwd(X, W, W, Wd, kept=(None, None, torch.empty(4, 32, device="cuda")))
+    Y, kept = ps.psattn_ffn_fwd(X, W, W, Wd)
+    with pytest.raises(ValueError):
+        ps.psattn_ffn_bwd(X, W, W, Wd, kept, X[:3])
+    with pytest.raises(ps.PsattnError):
+        ps.psattn_ffn_bwd(X, W, W, Wd, kept, X, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
