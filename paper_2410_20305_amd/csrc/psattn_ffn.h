@@ -1,4 +1,4 @@
-// The feed-forward block's products: what psattn_ffn.hip (arguments, order of the products) calls.
+// The feed-forward block's products: what psattn_ffn.hip (arguments, order and sizes of the products) calls.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -7,11 +7,14 @@
 namespace psattn {
 namespace gemm {
 
+// m x n of a workgroup's tile: 32 x 128, 64 x 128, 128 x 128, 256 x 256 (kGate: half the n, of two matrices)
+enum TileSize { k32, k64, k128, k256 };
+
 // One product, enqueued on s.  pkc, qkc: k is the contiguous axis of P, Q.  Returns a psattn_status.
-int product_any(int dt, Pass pass, int act, bool pkc, bool qkc, const Product& d, hipStream_t s);
-// The same for bf16 where product_mfma_ok says so.
-bool product_mfma_ok(bool pkc, bool qkc, const Product& d);
-int product_mfma(Pass pass, int act, bool pkc, bool qkc, const Product& d, hipStream_t s);
+// bf16 where every row of P, Q and what is stored is whole 16-byte groups on 16-byte boundaries; bf16; fp32
+int product_bf16(Pass pass, int act, bool pkc, bool qkc, TileSize size, const Product& d, hipStream_t s);
+int product_bf16_any(Pass pass, int act, bool pkc, bool qkc, TileSize size, const Product& d, hipStream_t s);
+int product_f32(Pass pass, int act, bool pkc, bool qkc, TileSize size, const Product& d, hipStream_t s);
 
 }  // namespace gemm
 }  // namespace psattn

@@ -36,6 +36,10 @@ struct Product {
     int64_t ldp, ldq, ldo;    // elements from one row in memory to the next
     int32_t M, N, K;          // K: of one segment
     int32_t n_seg, n_prod;
+    // k in n_split parts, whose sums go to `parts` in fp32 (rows of ld_part) and are joined by a kernel of their own
+    int32_t n_split;
+    float* parts;
+    int64_t ld_part;
 };
 
 template <typename E>
