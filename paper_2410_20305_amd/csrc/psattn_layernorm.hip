@@ -9,88 +9,26 @@
 
 #include <algorithm>
 #include <cmath>
-#include <initializer_list>
 #include <type_traits>
 
 #include "psattn.h"
-#include "psattn_gemm.h"
+#include "psattn_rows.h"
 
 namespace {
 
-using psattn::gemm::store1;
-using psattn::gemm::to_f32;
+using namespace psattn::rows;
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
-size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-
-template <typename E>
-constexpr int kVec = 16 / static_cast<int>(sizeof(E));
-
-__device__ __forceinline__ void unpack(const u32x4& u, float (&x)[8]) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        x[2 * j] = __uint_as_float(u[j] << 16);
-        x[2 * j + 1] = __uint_as_float(u[j] & 0xffff0000u);
-    }
-}
-__device__ __forceinline__ void unpack(const u32x4& u, float (&x)[4]) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = __uint_as_float(u[j]);
-}
-template <typename E>
-__device__ __forceinline__ u32x4 pack(const float* x) {
-    u32x4 u;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        if constexpr (sizeof(E) == 2) u[j] = psattn::mma::pack2(x[2 * j], x[2 * j + 1]);
-        else u[j] = __float_as_uint(x[j]);
-    }
-    return u;
-}
-struct __attribute__((packed, aligned(2))) Raw {
-    u32x4 u;
-};
-
-// kVec elements from column c of a row of `hidden`; zeros behind its end.  Rows may start anywhere: a group that is all there is one
-// load whatever its address
-template <bool WHOLE, typename E>
-__device__ __forceinline__ void load(const E* row, int c, int hidden, float (&x)[kVec<E>]) {
-    if constexpr (WHOLE) {
-        if (c < hidden) unpack(*reinterpret_cast<const u32x4*>(row + c), x);
-        else
-#pragma unroll
-            for (int j = 0; j < kVec<E>; ++j) x[j] = 0.f;
-    } else if (c + kVec<E> <= hidden) {
-        unpack(reinterpret_cast<const Raw*>(row + c)->u, x);
-    } else {
-#pragma unroll
-        for (int j = 0; j < kVec<E>; ++j) x[j] = c + j < hidden ? to_f32(row[c + j]) : 0.f;
-    }
-}
-template <bool WHOLE, typename E>
-__device__ __forceinline__ void store(E* row, int c, int hidden, const float (&x)[kVec<E>]) {
-    if constexpr (WHOLE) {
-        if (c < hidden) *reinterpret_cast<u32x4*>(row + c) = pack<E>(x);
-    } else if (c + kVec<E> <= hidden) {
-        reinterpret_cast<Raw*>(row + c)->u = pack<E>(x);
-    } else {
-#pragma unroll
-        for (int j = 0; j < kVec<E>; ++j)
-            if (c + j < hidden) store1(row + c + j, x[j]);
-    }
-}
 __device__ __forceinline__ float hold(float v, const uint16_t*) { return __uint_as_float(psattn::mma::pack2(v, 0.f) << 16); }
 __device__ __forceinline__ float hold(float v, const float*) { return v; }
 
-// sums over NW waves, the same in every lane; `sm`: N NW floats, another place for each call in flight
-template <int NW, int N>
+// sums over LANES lanes, the same in each; `sm` (more than a wave): 16 N floats, another place for each call in flight
+template <int LANES, int N>
 __device__ __forceinline__ void group_sum(float (&v)[N], float* sm) {
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1)
+    for (int off = (LANES < 64 ? LANES : 64) / 2; off > 0; off >>= 1)
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], off);
-    if constexpr (NW > 1) {
+    if constexpr (LANES > 64) {
         if ((threadIdx.x & 63) == 0)
 #pragma unroll
             for (int i = 0; i < N; ++i) sm[(threadIdx.x >> 6) * N + i] = v[i];
@@ -99,59 +37,59 @@ __device__ __forceinline__ void group_sum(float (&v)[N], float* sm) {
         for (int i = 0; i < N; ++i) {
             v[i] = sm[i];
 #pragma unroll
-            for (int w = 1; w < NW; ++w) v[i] += sm[w * N + i];
+            for (int w = 1; w < LANES / 64; ++w) v[i] += sm[w * N + i];
         }
     }
 }
 
-// A row to a group of NW waves, PER groups of 16 bytes to a lane.  NW = 1: four rows to a workgroup.
-template <int NW>
-constexpr int kThreads = NW == 1 ? 256 : 64 * NW;
+// A row to LANES lanes, PER groups of 16 bytes to each.  Rows of a wave and less share a workgroup of 256.
+template <int LANES>
+constexpr int kThreads = LANES < 256 ? 256 : LANES;
 
-template <typename E, int NW, int PER, bool WHOLE, bool RES>
-__global__ __launch_bounds__(kThreads<NW>) void psattn_ln_fwd(int n_rows, int hidden, float eps, const E* X, const E* R, const E* w, const E* b, E* S, E* Y,
-                                                              float* mean, float* rstd) {
-    constexpr int V = kVec<E>, kLanes = 64 * NW;
-    __shared__ float sm[2][NW];
-    const int row = NW == 1 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x, lane = threadIdx.x % kLanes;
+template <typename E, int LANES, int PER, bool WHOLE, bool RES>
+__global__ __launch_bounds__(kThreads<LANES>) void psattn_ln_fwd(int n_rows, int hidden, float eps, const E* X, const E* R, const E* w, const E* b, E* S, E* Y,
+                                                                 float* mean, float* rstd) {
+    constexpr int V = kVec<E>, kAt = kThreads<LANES> / LANES;
+    __shared__ float sm[2][16];
+    const int row = blockIdx.x * kAt + threadIdx.x / LANES, lane = threadIdx.x % LANES;
     if (row >= n_rows) return;
     const size_t at = static_cast<size_t>(row) * hidden;
     float x[PER][V];
     float sum[1] = {0.f};
 #pragma unroll
-    for (int p = 0; p < PER; ++p) load<WHOLE>(X + at, (p * kLanes + lane) * V, hidden, x[p]);
+    for (int p = 0; p < PER; ++p) load<WHOLE>(X + at, (p * LANES + lane) * V, hidden, x[p]);
     if constexpr (RES) {
         float r[PER][V];
 #pragma unroll
-        for (int p = 0; p < PER; ++p) load<WHOLE>(R + at, (p * kLanes + lane) * V, hidden, r[p]);
+        for (int p = 0; p < PER; ++p) load<WHOLE>(R + at, (p * LANES + lane) * V, hidden, r[p]);
 #pragma unroll
         for (int p = 0; p < PER; ++p) {
 #pragma unroll
             for (int j = 0; j < V; ++j) x[p][j] = hold(x[p][j] + r[p][j], X);
-            store<WHOLE>(S + at, (p * kLanes + lane) * V, hidden, x[p]);
+            store<WHOLE>(S + at, (p * LANES + lane) * V, hidden, x[p]);
         }
     }
 #pragma unroll
     for (int p = 0; p < PER; ++p)
 #pragma unroll
         for (int j = 0; j < V; ++j) sum[0] += x[p][j];
-    group_sum<NW>(sum, sm[0]);
+    group_sum<LANES>(sum, sm[0]);
     const float mu = sum[0] / hidden;
     float sq[1] = {0.f};
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
-        const int c = (p * kLanes + lane) * V;
+        const int c = (p * LANES + lane) * V;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             x[p][j] -= mu;
             if (WHOLE ? c < hidden : c + j < hidden) sq[0] += x[p][j] * x[p][j];
         }
     }
-    group_sum<NW>(sq, sm[1]);
+    group_sum<LANES>(sq, sm[1]);
     const float rs = 1.f / sqrtf(sq[0] / hidden + eps);
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
-        const int c = (p * kLanes + lane) * V;
+        const int c = (p * LANES + lane) * V;
         float wv[V], bv[V] = {};
         load<WHOLE>(w, c, hidden, wv);
         if (b) load<WHOLE>(b, c, hidden, bv);
@@ -165,107 +103,137 @@ __global__ __launch_bounds__(kThreads<NW>) void psattn_ln_fwd(int n_rows, int hi
     }
 }
 
-// Backward.  A workgroup takes rows first, first + gridDim.x, ... and keeps its lanes' columns of dw and db in registers; they go to
-// part[workgroup] at its end and are joined by psattn_ln_weights.  NW = 1: the four waves take rows of their own and add up in LDS.
-template <typename E, int NW, int PER, bool WHOLE>
-__global__ __launch_bounds__(kThreads<NW>) void psattn_ln_bwd(int n_rows, int hidden, const E* S, const E* w, const float* mean, const float* rstd, const E* dY,
-                                                              const E* dS, E* dX, float* part) {
-    constexpr int V = kVec<E>, kLanes = 64 * NW, kAt = NW == 1 ? 4 : 1;  // rows at a time
-    __shared__ float sm[2][2 * NW];
-    __shared__ float add[NW == 1 ? 3 * 64 * V : 1];
-    const int lane = threadIdx.x % kLanes, own = NW == 1 ? threadIdx.x >> 6 : 0;
-    float dw[PER][V] = {}, db[PER][V] = {}, wv[PER][V];
+// Backward.  A workgroup takes the rows from blockIdx.x on, gridDim.x apart, and keeps its lanes' columns of dw and db in registers;
+// they go to part[workgroup] at its end and are joined by psattn_ln_weights (rows that share a workgroup add up in LDS first).
+// Rows stay in the registers as they came and are unpacked twice, which leaves room for the next row's loads while one is
+// summed over the lanes (8 334 rows of 4 096 bf16 with dS 105 -> 70 us, 65 536 of 1 024 198 -> 84); with 1 024 lanes, 128
+// registers to each, there is none (20 000 rows of 16 384 bf16 1 792 us with, NOTE without).
+template <typename E, int LANES, int PER, bool WHOLE>
+__global__ __launch_bounds__(kThreads<LANES>) void psattn_ln_bwd(int n_rows, int hidden, const E* S, const E* w, const float* mean, const float* rstd, const E* dY,
+                                                                 const E* dS, E* dX, float* part) {
+    constexpr int V = kVec<E>, kAt = kThreads<LANES> / LANES;  // rows at a time
+    __shared__ float sm[2][32];
+    __shared__ float add[kAt > 1 ? kAt * LANES * V : 1];
+    const int lane = threadIdx.x % LANES, own = threadIdx.x / LANES;
+    float dw[PER][V] = {}, db[PER][V] = {};
+    u32x4 wr[PER];
 #pragma unroll
-    for (int p = 0; p < PER; ++p) load<WHOLE>(w, (p * kLanes + lane) * V, hidden, wv[p]);
-    int turn = 0;
-    for (int row = blockIdx.x * kAt + own; row < n_rows; row += gridDim.x * kAt, turn ^= 1) {
-        const size_t at = static_cast<size_t>(row) * hidden;
-        const float mu = mean[row], rs = rstd[row];
-        float x[PER][V], g[PER][V];
+    for (int p = 0; p < PER; ++p) wr[p] = raw<WHOLE>(w, (p * LANES + lane) * V, hidden);
+    u32x4 xr[PER], gr[PER], sr[PER];
+    float mu = 0.f, rs = 0.f;
+    constexpr bool kAhead = LANES < 1024;
+    const int step = gridDim.x * kAt;
+    int row = blockIdx.x * kAt + own;
+    auto fetch = [&](int r, u32x4 (&a)[PER], u32x4 (&b)[PER], u32x4 (&c)[PER], float& m, float& q) {
+        const size_t at = static_cast<size_t>(r) * hidden;
+        m = mean[r];
+        q = rstd[r];
 #pragma unroll
         for (int p = 0; p < PER; ++p) {
-            load<WHOLE>(S + at, (p * kLanes + lane) * V, hidden, x[p]);
-            load<WHOLE>(dY + at, (p * kLanes + lane) * V, hidden, g[p]);
+            a[p] = raw<WHOLE>(S + at, (p * LANES + lane) * V, hidden);
+            b[p] = raw<WHOLE>(dY + at, (p * LANES + lane) * V, hidden);
+            if (dS) c[p] = raw<WHOLE>(dS + at, (p * LANES + lane) * V, hidden);
         }
+    };
+    if (kAhead && row < n_rows) fetch(row, xr, gr, sr, mu, rs);
+    for (int turn = 0; row < n_rows; row += step, turn ^= 1) {
+        u32x4 xn[PER], gn[PER], sn[PER];
+        float mn = 0.f, qn = 0.f;
+        if constexpr (!kAhead) fetch(row, xr, gr, sr, mu, rs);
+        else if (row + step < n_rows) fetch(row + step, xn, gn, sn, mn, qn);
         float s[2] = {0.f, 0.f};
+        // behind the row's end dY and w are zeros
+        auto unpacked = [&](int p, float (&x)[V], float (&g)[V], float (&wv)[V]) {
+            unpack(xr[p], x);
+            unpack(gr[p], g);
+            unpack(wr[p], wv);
 #pragma unroll
-        for (int p = 0; p < PER; ++p)
-#pragma unroll
-            for (int j = 0; j < V; ++j) {  // behind the row's end dY and w are zeros
-                x[p][j] = (x[p][j] - mu) * rs;
-                if constexpr (!WHOLE)
-                    if ((p * kLanes + lane) * V + j >= hidden) x[p][j] = 0.f;
-                dw[p][j] += g[p][j] * x[p][j];
-                db[p][j] += g[p][j];
-                g[p][j] *= wv[p][j];
-                s[0] += g[p][j];
-                s[1] += g[p][j] * x[p][j];
-            }
-        group_sum<NW>(s, sm[turn]);
-        const float m1 = s[0] / hidden, m2 = s[1] / hidden;
+            for (int j = 0; j < V; ++j) x[j] = (x[j] - mu) * rs;
+        };
 #pragma unroll
         for (int p = 0; p < PER; ++p) {
-            const int c = (p * kLanes + lane) * V;
-            float o[V];
-            if (dS) {
-                load<WHOLE>(dS + at, c, hidden, o);
+            float x[V], g[V], wv[V];
+            unpacked(p, x, g, wv);
 #pragma unroll
-                for (int j = 0; j < V; ++j) o[j] += rs * (g[p][j] - m1 - x[p][j] * m2);
-            } else {
-#pragma unroll
-                for (int j = 0; j < V; ++j) o[j] = rs * (g[p][j] - m1 - x[p][j] * m2);
+            for (int j = 0; j < V; ++j) {
+                dw[p][j] += g[j] * x[j];
+                db[p][j] += g[j];
+                g[j] *= wv[j];
+                s[0] += g[j];
+                s[1] += g[j] * x[j];
             }
-            store<WHOLE>(dX + at, c, hidden, o);
+        }
+        group_sum<LANES>(s, sm[turn]);
+        const float m1 = s[0] / hidden, m2 = s[1] / hidden;
+        const size_t at = static_cast<size_t>(row) * hidden;
+#pragma unroll
+        for (int p = 0; p < PER; ++p) {
+            float x[V], g[V], wv[V], o[V] = {};
+            unpacked(p, x, g, wv);
+            if (dS) unpack(sr[p], o);
+#pragma unroll
+            for (int j = 0; j < V; ++j) o[j] += rs * (g[j] * wv[j] - m1 - x[j] * m2);
+            store<WHOLE>(dX + at, (p * LANES + lane) * V, hidden, o);
+        }
+        if constexpr (kAhead) {
+#pragma unroll
+            for (int p = 0; p < PER; ++p) { xr[p] = xn[p]; gr[p] = gn[p]; sr[p] = sn[p]; }
+            mu = mn;
+            rs = qn;
         }
     }
     float* const mine = part + 2 * static_cast<size_t>(blockIdx.x) * hidden;
     auto out = [&](float* to, const float (&v)[PER][V]) {
 #pragma unroll
         for (int p = 0; p < PER; ++p) {
-            float t[V];
-#pragma unroll
-            for (int j = 0; j < V; ++j) t[j] = v[p][j];
-            if constexpr (NW == 1) {
+            if constexpr (kAt > 1) {
                 __syncthreads();
-                if (own > 0)
 #pragma unroll
-                    for (int j = 0; j < V; ++j) add[((own - 1) * V + j) * 64 + lane] = t[j];
+                for (int j = 0; j < V; ++j) add[(own * V + j) * LANES + lane] = v[p][j];
                 __syncthreads();
-                if (own > 0) continue;
+                for (int i = threadIdx.x; i < LANES * V; i += kThreads<LANES>) {
+                    float t = 0.f;
 #pragma unroll
-                for (int o = 0; o < 3; ++o)
+                    for (int o = 0; o < kAt; ++o) t += add[(o * V + i % V) * LANES + i / V];
+                    const int c = p * LANES * V + i;
+                    if (c < hidden) to[c] = t;
+                }
+            } else {
+                const int c = (p * LANES + lane) * V;
 #pragma unroll
-                    for (int j = 0; j < V; ++j) t[j] += add[(o * V + j) * 64 + lane];
+                for (int j = 0; j < V; ++j)
+                    if (c + j < hidden) to[c + j] = v[p][j];
             }
-            const int c = (p * kLanes + lane) * V;
-#pragma unroll
-            for (int j = 0; j < V; ++j)
-                if (c + j < hidden) to[c + j] = t[j];
         }
     };
     out(mine, dw);
     out(mine + hidden, db);
 }
 
-// dw and db from the workgroups' parts: 32 columns to a workgroup, eight lanes to a column
-__global__ __launch_bounds__(256) void psattn_ln_weights(int n_parts, int hidden, const float* part, void* dw, void* db, int bf16) {
-    __shared__ float sm[8][2][33];
-    const int c = threadIdx.x & 31, k = threadIdx.x >> 5, i = blockIdx.x * 32 + c;
-    float v[2] = {0.f, 0.f};
-    if (i < hidden)
-        for (int p = k; p < n_parts; p += 8) {
-            v[0] += part[2 * static_cast<size_t>(p) * hidden + i];
-            v[1] += part[(2 * static_cast<size_t>(p) + 1) * hidden + i];
-        }
-    sm[k][0][c] = v[0];
-    sm[k][1][c] = v[1];
+// dw and db from the workgroups' parts: 64 of their 2 hidden columns to a workgroup, sixteen lanes to a column
+__global__ __launch_bounds__(1024) void psattn_ln_weights(int n_parts, int hidden, const float* part, void* dw, void* db, int bf16) {
+    __shared__ float sm[16][65];
+    const int c = threadIdx.x & 63, k = threadIdx.x >> 6;
+    const int64_t i = blockIdx.x * 64 + c, width = 2 * static_cast<int64_t>(hidden);
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    if (i < width) {
+        int p = k;
+        for (; p + 48 < n_parts; p += 64)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] += part[(p + 16 * u) * width + i];
+        for (; p < n_parts; p += 16) v[0] += part[p * width + i];
+    }
+    sm[k][c] = (v[0] + v[1]) + (v[2] + v[3]);
     __syncthreads();
-    if (k > 1 || i >= hidden || (k == 1 && !db)) return;
+    if (k > 0 || i >= width) return;
     float t = 0.f;
-    for (int o = 0; o < 8; ++o) t += sm[o][k][c];
-    void* const to = k == 0 ? dw : db;
-    if (bf16) store1(static_cast<uint16_t*>(to) + i, t);
-    else store1(static_cast<float*>(to) + i, t);
+#pragma unroll
+    for (int o = 0; o < 16; ++o) t += sm[o][c];
+    void* const to = i < hidden ? dw : db;
+    const int64_t at = i < hidden ? i : i - hidden;
+    if (!to) return;
+    if (bf16) store1(static_cast<uint16_t*>(to) + at, t);
+    else store1(static_cast<float*>(to) + at, t);
 }
 
 // ---- rows too wide for registers: read again for each step
@@ -291,7 +259,7 @@ __global__ __launch_bounds__(1024) void psattn_ln_fwd_wide(int hidden, float eps
         for (int j = 0; j < V; ++j) sum[0] += v[j];
     }
     if (R) x = S + at;  // each lane reads back what it wrote
-    group_sum<16>(sum, sm[0]);
+    group_sum<1024>(sum, sm[0]);
     const float mu = sum[0] / hidden;
     for (int c = threadIdx.x * V; c < hidden; c += kStep) {
         float v[V];
@@ -300,7 +268,7 @@ __global__ __launch_bounds__(1024) void psattn_ln_fwd_wide(int hidden, float eps
         for (int j = 0; j < V; ++j)
             if (c + j < hidden) sq[0] += (v[j] - mu) * (v[j] - mu);
     }
-    group_sum<16>(sq, sm[1]);
+    group_sum<1024>(sq, sm[1]);
     const float rs = 1.f / sqrtf(sq[0] / hidden + eps);
     for (int c = threadIdx.x * V; c < hidden; c += kStep) {
         float v[V], wv[V], bv[V] = {};
@@ -336,7 +304,7 @@ __global__ __launch_bounds__(1024) void psattn_ln_bwd_wide(int hidden, const E* 
                 s[1] += g[j] * wv[j] * ((x[j] - mu) * rs);
             }
     }
-    group_sum<16>(s, sm);
+    group_sum<1024>(s, sm);
     const float m1 = s[0] / hidden, m2 = s[1] / hidden;
     for (int c = threadIdx.x * V; c < hidden; c += kStep) {
         float x[V], g[V], wv[V], o[V] = {};
@@ -367,38 +335,33 @@ __global__ __launch_bounds__(256) void psattn_ln_columns(int n_rows, int hidden,
     mine[hidden + i] = b;
 }
 
-// ---- which kernel.  A row of up to 64 lanes' four loads is a wave's; wider ones a workgroup's, in up to two loads to a lane
-// (dw, db and w of a lane's columns live in registers in the backward), up to 1 024 lanes.
-constexpr int kMostWaves = 16, kMostPer = 2;
-template <typename E>
-constexpr int kWidest = 64 * kMostWaves * kMostPer * kVec<E>;
-
+// ---- which kernel.  Rows of up to 32 groups of 16 bytes are sixteen lanes' (of 64, half or more would have nothing to do: 65 536 rows
+// of 256 bf16 forward NOTE), of up to 128 a wave's, wider ones a workgroup's.
 template <typename E, typename F>
 bool sized(int hidden, F&& f) {
-    auto go = [&](auto nw, auto per) { return f(nw, per), true; };
-    const int g = (hidden + kVec<E> - 1) / kVec<E>;  // groups of 16 bytes
+    auto go = [&](auto lanes, auto per) { return f(lanes, per), true; };
+    const int64_t g = (static_cast<int64_t>(hidden) + kVec<E> - 1) / kVec<E>;
     using std::integral_constant;
-    if (g <= 64) return go(integral_constant<int, 1>{}, integral_constant<int, 1>{});
-    if (g <= 128) return go(integral_constant<int, 1>{}, integral_constant<int, 2>{});
-    if (g <= 256) return go(integral_constant<int, 4>{}, integral_constant<int, 1>{});
-    if (g <= 512) return go(integral_constant<int, 4>{}, integral_constant<int, 2>{});
-    if (g <= 1024) return go(integral_constant<int, 8>{}, integral_constant<int, 2>{});
-    if (g <= 2048) return go(integral_constant<int, 16>{}, integral_constant<int, 2>{});
+    using One = integral_constant<int, 1>;
+    using Two = integral_constant<int, 2>;
+    if (g <= 16) return go(integral_constant<int, 16>{}, One{});
+    if (g <= 32) return go(integral_constant<int, 16>{}, Two{});
+    if (g <= 64) return go(integral_constant<int, 64>{}, One{});
+    if (g <= 128) return go(integral_constant<int, 64>{}, Two{});
+    if (g <= 256) return go(integral_constant<int, 256>{}, One{});
+    if (g <= 512) return go(integral_constant<int, 256>{}, Two{});
+    if (g <= 1024) return go(integral_constant<int, 512>{}, Two{});
+    if (g <= 2048) return go(integral_constant<int, 1024>{}, Two{});
+    if constexpr (sizeof(E) == 4)  // as many columns to a lane as of bf16
+        if (g <= 4096) return go(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
     return false;
 }
 
-// workgroups of the backward, each with a part of dw and db: four to a CU keep enough loads in flight, and their parts are small
-// beside what they read; few rows have fewer
-int n_parts(int32_t n_rows, int32_t hidden) { return std::max(1, std::min(n_rows, 1024)); }
+// workgroups of the backward, each with a part of dw and db.  A part is written and read in fp32, and costs as much memory time
+// as some five rows of bf16: one for 26 rows, but 256 of them (one to a CU) at least and 1 024 at most
+int n_parts(int32_t n_rows) { return std::max(1, std::min({n_rows, 1024, std::max(256, n_rows / 26)})); }
 
 bool bad_shape(int32_t dt, int32_t n_rows, int32_t hidden) { return (dt != PSATTN_F32 && dt != PSATTN_BF16) || n_rows < 0 || hidden <= 0; }
-
-template <typename E>
-bool whole(int32_t hidden, std::initializer_list<const void*> p) {
-    uintptr_t a = 0;
-    for (const void* x : p) a |= reinterpret_cast<uintptr_t>(x);
-    return a % 16 == 0 && hidden % kVec<E> == 0;
-}
 
 template <typename E>
 void fwd(int32_t n_rows, int32_t hidden, float eps, const void* X_, const void* R_, const void* w_, const void* b_, void* S_, void* Y_, float* mean,
@@ -406,12 +369,12 @@ void fwd(int32_t n_rows, int32_t hidden, float eps, const void* X_, const void* 
     const E *X = static_cast<const E*>(X_), *R = static_cast<const E*>(R_), *w = static_cast<const E*>(w_), *b = static_cast<const E*>(b_);
     E *S = static_cast<E*>(S_), *Y = static_cast<E*>(Y_);
     const bool all = whole<E>(hidden, {X, R, w, b, S, Y});
-    const bool done = sized<E>(hidden, [&](auto nw, auto per) {
-        constexpr int NW = decltype(nw)::value, PER = decltype(per)::value;
-        const int grid = NW == 1 ? (n_rows + 3) / 4 : n_rows;
-        auto go = [&](auto kernel) { kernel<<<grid, kThreads<NW>, 0, s>>>(n_rows, hidden, eps, X, R, w, b, S, Y, mean, rstd); };
-        if (R) all ? go(psattn_ln_fwd<E, NW, PER, true, true>) : go(psattn_ln_fwd<E, NW, PER, false, true>);
-        else all ? go(psattn_ln_fwd<E, NW, PER, true, false>) : go(psattn_ln_fwd<E, NW, PER, false, false>);
+    const bool done = sized<E>(hidden, [&](auto lanes, auto per) {
+        constexpr int L = decltype(lanes)::value, PER = decltype(per)::value, kAt = kThreads<L> / L;
+        const int grid = (n_rows + kAt - 1) / kAt;
+        auto go = [&](auto kernel) { kernel<<<grid, kThreads<L>, 0, s>>>(n_rows, hidden, eps, X, R, w, b, S, Y, mean, rstd); };
+        if (R) all ? go(psattn_ln_fwd<E, L, PER, true, true>) : go(psattn_ln_fwd<E, L, PER, false, true>);
+        else all ? go(psattn_ln_fwd<E, L, PER, true, false>) : go(psattn_ln_fwd<E, L, PER, false, false>);
     });
     if (!done) psattn_ln_fwd_wide<E><<<n_rows, 1024, 0, s>>>(hidden, eps, X, R, w, b, S, Y, mean, rstd);
 }
@@ -421,14 +384,14 @@ void bwd(int32_t n_rows, int32_t hidden, const void* S_, const void* w_, const f
          void* dw, void* db, float* part, hipStream_t s) {
     const E *S = static_cast<const E*>(S_), *w = static_cast<const E*>(w_), *dY = static_cast<const E*>(dY_), *dS = static_cast<const E*>(dS_);
     E* dX = static_cast<E*>(dX_);
-    int np = n_rows > 0 ? n_parts(n_rows, hidden) : 0;
+    int np = n_rows > 0 ? n_parts(n_rows) : 0;
     if (n_rows > 0) {
         const bool all = whole<E>(hidden, {S, w, dY, dS, dX});
-        const bool done = sized<E>(hidden, [&](auto nw, auto per) {
-            constexpr int NW = decltype(nw)::value, PER = decltype(per)::value;
-            if (NW == 1) np = (np + 3) / 4;
-            auto go = [&](auto kernel) { kernel<<<np, kThreads<NW>, 0, s>>>(n_rows, hidden, S, w, mean, rstd, dY, dS, dX, part); };
-            all ? go(psattn_ln_bwd<E, NW, PER, true>) : go(psattn_ln_bwd<E, NW, PER, false>);
+        const bool done = sized<E>(hidden, [&](auto lanes, auto per) {
+            constexpr int L = decltype(lanes)::value, PER = decltype(per)::value, kAt = kThreads<L> / L;
+            np = std::min(np, (n_rows + kAt - 1) / kAt);
+            auto go = [&](auto kernel) { kernel<<<np, kThreads<L>, 0, s>>>(n_rows, hidden, S, w, mean, rstd, dY, dS, dX, part); };
+            all ? go(psattn_ln_bwd<E, L, PER, true>) : go(psattn_ln_bwd<E, L, PER, false>);
         });
         if (!done) {
             np = std::min(np, 64);
@@ -436,7 +399,7 @@ void bwd(int32_t n_rows, int32_t hidden, const void* S_, const void* w_, const f
             psattn_ln_columns<E><<<dim3((hidden + 255) / 256, np), 256, 0, s>>>(n_rows, hidden, S, mean, rstd, dY, part);
         }
     }
-    psattn_ln_weights<<<(hidden + 31) / 32, 256, 0, s>>>(np, hidden, part, dw, db, sizeof(E) == 2);
+    psattn_ln_weights<<<(2 * hidden + 63) / 64, 1024, 0, s>>>(np, hidden, part, dw, db, sizeof(E) == 2);
 }
 
 // grids of at most 2^31 threads: a row to 1 024 of them
@@ -460,7 +423,7 @@ int psattn_layernorm_fwd(int32_t dt, int32_t n_rows, int32_t hidden, float eps, 
 
 size_t psattn_layernorm_bwd_workspace_bytes(int32_t n_rows, int32_t hidden) {
     if (n_rows < 0 || hidden <= 0) return 0;
-    return align_up(2 * sizeof(float) * static_cast<size_t>(n_parts(n_rows, hidden)) * hidden, 256) + 256;
+    return align_up(2 * sizeof(float) * static_cast<size_t>(n_parts(n_rows)) * hidden, 256) + 256;
 }
 
 int psattn_layernorm_bwd(int32_t dt, int32_t n_rows, int32_t hidden, const void* S, const void* weight, const float* mean, const float* rstd,
