@@ -106,14 +106,16 @@ __global__ __launch_bounds__(kThreads<LANES>) void psattn_ln_fwd(int n_rows, int
 // Backward.  A workgroup takes the rows from blockIdx.x on, gridDim.x apart, and keeps its lanes' columns of dw and db in registers;
 // they go to part[workgroup] at its end and are joined by psattn_ln_weights (rows that share a workgroup add up in LDS first).
 // Rows stay in the registers as they came and are unpacked twice, which leaves room for the next row's loads while one is
-// summed over the lanes (8 334 rows of 4 096 bf16 with dS 105 -> 70 us, 65 536 of 1 024 198 -> 84); with 1 024 lanes, 128
-// registers to each, there is none (20 000 rows of 16 384 bf16 1 792 us with, NOTE without).
-template <typename E, int LANES, int PER, bool WHOLE>
+// summed over the lanes (8 334 rows of 4 096 bf16 with dS 105 -> 70 us, 65 536 of 1 024 198 -> 84).
+//   Without SUMS a workgroup has one row, and dw and db are left to psattn_ln_columns: 32 columns to a lane and their sums do not
+// fit beside a row (20 000 rows of 16 384 bf16, sums in registers and in part spilled 665 - 1 650 us, apart NOTE).
+template <typename E, int LANES, int PER, bool WHOLE, bool SUMS>
 __global__ __launch_bounds__(kThreads<LANES>) void psattn_ln_bwd(int n_rows, int hidden, const E* S, const E* w, const float* mean, const float* rstd, const E* dY,
                                                                  const E* dS, E* dX, float* part) {
     constexpr int V = kVec<E>, kAt = kThreads<LANES> / LANES;  // rows at a time
     __shared__ float sm[2][32];
     __shared__ float add[kAt > 1 ? kAt * LANES * V : 1];
+    static_assert(SUMS || kAt == 1, "short rows' columns are summed here");
     const int lane = threadIdx.x % LANES, own = threadIdx.x / LANES;
     float dw[PER][V] = {}, db[PER][V] = {};
     u32x4 wr[PER];
@@ -121,7 +123,7 @@ __global__ __launch_bounds__(kThreads<LANES>) void psattn_ln_bwd(int n_rows, int
     for (int p = 0; p < PER; ++p) wr[p] = raw<WHOLE>(w, (p * LANES + lane) * V, hidden);
     u32x4 xr[PER], gr[PER], sr[PER];
     float mu = 0.f, rs = 0.f;
-    constexpr bool kAhead = LANES < 1024;
+    constexpr bool kAhead = SUMS;
     const int step = gridDim.x * kAt;
     int row = blockIdx.x * kAt + own;
     auto fetch = [&](int r, u32x4 (&a)[PER], u32x4 (&b)[PER], u32x4 (&c)[PER], float& m, float& q) {
@@ -156,8 +158,10 @@ __global__ __launch_bounds__(kThreads<LANES>) void psattn_ln_bwd(int n_rows, int
             unpacked(p, x, g, wv);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                dw[p][j] += g[j] * x[j];
-                db[p][j] += g[j];
+                if constexpr (SUMS) {
+                    dw[p][j] += g[j] * x[j];
+                    db[p][j] += g[j];
+                }
                 g[j] *= wv[j];
                 s[0] += g[j];
                 s[1] += g[j] * x[j];
@@ -182,6 +186,7 @@ __global__ __launch_bounds__(kThreads<LANES>) void psattn_ln_bwd(int n_rows, int
             rs = qn;
         }
     }
+    if constexpr (!SUMS) return;
     float* const mine = part + 2 * static_cast<size_t>(blockIdx.x) * hidden;
     auto out = [&](float* to, const float (&v)[PER][V]) {
 #pragma unroll
@@ -318,30 +323,57 @@ __global__ __launch_bounds__(1024) void psattn_ln_bwd_wide(int hidden, const E* 
     }
 }
 
-// part[y]: sums of one column over rows y, y + gridDim.y, ...
+// part[y]: sums of kVec columns to a lane over rows y, y + gridDim.y, ...
 template <typename E>
 __global__ __launch_bounds__(256) void psattn_ln_columns(int n_rows, int hidden, const E* S, const float* mean, const float* rstd, const E* dY, float* part) {
-    const int i = blockIdx.x * 256 + threadIdx.x;
-    if (i >= hidden) return;
-    float w = 0.f, b = 0.f;
-    for (int r = blockIdx.y; r < n_rows; r += gridDim.y) {
-        const size_t at = static_cast<size_t>(r) * hidden + i;
-        const float dy = to_f32(dY[at]);
-        w += dy * ((to_f32(S[at]) - mean[r]) * rstd[r]);
-        b += dy;
+    constexpr int V = kVec<E>, kAtOnce = 4;
+    const int c = (blockIdx.x * 256 + threadIdx.x) * V;
+    if (c >= hidden) return;
+    float w[V] = {}, b[V] = {};
+    auto add = [&](const u32x4& s, const u32x4& d, float mu, float rs) {
+        float x[V], g[V];
+        unpack(s, x);
+        unpack(d, g);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            w[j] += g[j] * ((x[j] - mu) * rs);
+            b[j] += g[j];
+        }
+    };
+    const int step = gridDim.y;
+    int r = blockIdx.y;
+    for (; r + (kAtOnce - 1) * step < n_rows; r += kAtOnce * step) {
+        u32x4 s[kAtOnce], d[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const size_t at = static_cast<size_t>(r + u * step) * hidden;
+            s[u] = raw<false>(S + at, c, hidden);
+            d[u] = raw<false>(dY + at, c, hidden);
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) add(s[u], d[u], mean[r + u * step], rstd[r + u * step]);
     }
-    float* const mine = part + 2 * static_cast<size_t>(blockIdx.y) * hidden;
-    mine[i] = w;
-    mine[hidden + i] = b;
+    for (; r < n_rows; r += step) {
+        const size_t at = static_cast<size_t>(r) * hidden;
+        add(raw<false>(S + at, c, hidden), raw<false>(dY + at, c, hidden), mean[r], rstd[r]);
+    }
+    float* const mine = part + 2 * static_cast<size_t>(blockIdx.y) * hidden + c;
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+        if (c + j < hidden) {
+            mine[j] = w[j];
+            mine[hidden + j] = b[j];
+        }
 }
 
 // ---- which kernel.  Rows of up to 32 groups of 16 bytes are sixteen lanes' (of 64, half or more would have nothing to do: 65 536 rows
 // of 256 bf16 forward NOTE), of up to 128 a wave's, wider ones a workgroup's.
-template <typename E, typename F>
+template <typename E, bool BWD, typename F>
 bool sized(int hidden, F&& f) {
+    using std::integral_constant;
     auto go = [&](auto lanes, auto per) { return f(lanes, per), true; };
     const int64_t g = (static_cast<int64_t>(hidden) + kVec<E> - 1) / kVec<E>;
-    using std::integral_constant;
+    constexpr int kWidest = 4 * 8 / kVec<E>;  // groups of a lane: 32 columns
     using One = integral_constant<int, 1>;
     using Two = integral_constant<int, 2>;
     if (g <= 16) return go(integral_constant<int, 16>{}, One{});
@@ -351,9 +383,13 @@ bool sized(int hidden, F&& f) {
     if (g <= 256) return go(integral_constant<int, 256>{}, One{});
     if (g <= 512) return go(integral_constant<int, 256>{}, Two{});
     if (g <= 1024) return go(integral_constant<int, 512>{}, Two{});
-    if (g <= 2048) return go(integral_constant<int, 1024>{}, Two{});
-    if constexpr (sizeof(E) == 4)  // as many columns to a lane as of bf16
-        if (g <= 4096) return go(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+    if constexpr (BWD) {
+        if (g <= 2048) return go(integral_constant<int, 512>{}, integral_constant<int, 4>{});
+        if (g <= 512 * kWidest) return go(integral_constant<int, 512>{}, integral_constant<int, kWidest>{});
+    } else {
+        if (g <= 2048) return go(integral_constant<int, 1024>{}, Two{});
+        if (g <= 512 * kWidest) return go(integral_constant<int, 1024>{}, integral_constant<int, kWidest / 2>{});
+    }
     return false;
 }
 
@@ -369,7 +405,7 @@ void fwd(int32_t n_rows, int32_t hidden, float eps, const void* X_, const void* 
     const E *X = static_cast<const E*>(X_), *R = static_cast<const E*>(R_), *w = static_cast<const E*>(w_), *b = static_cast<const E*>(b_);
     E *S = static_cast<E*>(S_), *Y = static_cast<E*>(Y_);
     const bool all = whole<E>(hidden, {X, R, w, b, S, Y});
-    const bool done = sized<E>(hidden, [&](auto lanes, auto per) {
+    const bool done = sized<E, false>(hidden, [&](auto lanes, auto per) {
         constexpr int L = decltype(lanes)::value, PER = decltype(per)::value, kAt = kThreads<L> / L;
         const int grid = (n_rows + kAt - 1) / kAt;
         auto go = [&](auto kernel) { kernel<<<grid, kThreads<L>, 0, s>>>(n_rows, hidden, eps, X, R, w, b, S, Y, mean, rstd); };
@@ -387,16 +423,20 @@ void bwd(int32_t n_rows, int32_t hidden, const void* S_, const void* w_, const f
     int np = n_rows > 0 ? n_parts(n_rows) : 0;
     if (n_rows > 0) {
         const bool all = whole<E>(hidden, {S, w, dY, dS, dX});
-        const bool done = sized<E>(hidden, [&](auto lanes, auto per) {
+        bool sums = false;
+        const bool done = sized<E, true>(hidden, [&](auto lanes, auto per) {
             constexpr int L = decltype(lanes)::value, PER = decltype(per)::value, kAt = kThreads<L> / L;
-            np = std::min(np, (n_rows + kAt - 1) / kAt);
-            auto go = [&](auto kernel) { kernel<<<np, kThreads<L>, 0, s>>>(n_rows, hidden, S, w, mean, rstd, dY, dS, dX, part); };
-            all ? go(psattn_ln_bwd<E, L, PER, true>) : go(psattn_ln_bwd<E, L, PER, false>);
+            constexpr bool SUMS = PER * kVec<E> < 32;  // up to 1 024 groups
+            if (SUMS) np = std::min(np, (n_rows + kAt - 1) / kAt);
+            sums = SUMS;
+            auto go = [&](auto kernel) { kernel<<<SUMS ? np : n_rows, kThreads<L>, 0, s>>>(n_rows, hidden, S, w, mean, rstd, dY, dS, dX, part); };
+            all ? go(psattn_ln_bwd<E, L, PER, true, SUMS>) : go(psattn_ln_bwd<E, L, PER, false, SUMS>);
         });
-        if (!done) {
-            np = std::min(np, 64);
-            psattn_ln_bwd_wide<E><<<n_rows, 1024, 0, s>>>(hidden, S, w, mean, rstd, dY, dS, dX);
-            psattn_ln_columns<E><<<dim3((hidden + 255) / 256, np), 256, 0, s>>>(n_rows, hidden, S, mean, rstd, dY, part);
+        if (!done) psattn_ln_bwd_wide<E><<<n_rows, 1024, 0, s>>>(hidden, S, w, mean, rstd, dY, dS, dX);
+        if (!sums) {
+            const int cols = (hidden + 256 * kVec<E> - 1) / (256 * kVec<E>);
+            np = std::min(np, std::max(1, 2048 / cols));  // eight workgroups to a CU
+            psattn_ln_columns<E><<<dim3(cols, np), 256, 0, s>>>(n_rows, hidden, S, mean, rstd, dY, part);
         }
     }
     psattn_ln_weights<<<(2 * hidden + 63) / 64, 1024, 0, s>>>(np, hidden, part, dw, db, sizeof(E) == 2);
