@@ -20,6 +20,10 @@
 namespace psattn {
 namespace gemm {
 
+#ifndef V_L
+#define V_L 3
+#define V_M 3
+#endif
 // Which tile a workgroup takes.  Workgroups go to the eight XCDs in turn: each XCD takes a run of tiles, and the run goes through
 // kGroup rows of tiles at a time, so that those that run together share their operands in its L2.
 constexpr int kGroup = 8;
@@ -189,9 +193,9 @@ __device__ __forceinline__ void store_chunks(float* base, int64_t ld, int rows, 
     for (int k = 0; k < 2; ++k) put8(base + row * ld + 16 * k + col, x.c[k], cols - 16 * k - col);
 }
 
-template <int BM_, int BN_, int WM_, int WN_>
-struct Shape {  // tile, waves
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, kWaves = WM * WN, kThreads = 64 * kWaves;
+template <int BM_, int BN_, int WM_, int WN_, int NBQ_>
+struct Shape {  // tile, waves, LDS buffers of Q (of P: two)
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NBQ = NBQ_, kWaves = WM * WN, kThreads = 64 * kWaves;
     static constexpr int MB = BM / WM / 32, NB = BN / WN / 32;  // blocks of a wave
 };
 
@@ -202,8 +206,10 @@ __global__ __launch_bounds__(S::kThreads, 2) void psattn_ffn_tiles(Product d, in
     static_assert(PASS != kGate || NB == 2, "a wave holds a block of the gate and the same of up");
     static_assert(PKC || S::BM % (256 / sizeof(E)) == 0, "whole sub-tiles");
     static_assert(QKC || S::BN % (256 / sizeof(E)) == 0, "whole sub-tiles");
-    __shared__ __attribute__((aligned(1024))) char lds[2 * (kPB + kQB)];
-    char *const ptile = lds, *const qtile = lds + 2 * kPB;  // two buffers each, so that a read's buffer is in its immediate offset
+    constexpr int NBQ = S::NBQ;
+    static_assert(ASYNC || NBQ == 2, "what goes through registers is one tile ahead");
+    __shared__ __attribute__((aligned(1024))) char lds[2 * kPB + NBQ * kQB];
+    char *const ptile = lds, *const qtile = lds + 2 * kPB;
     const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = w / S::WN, wn = w % S::WN;
     const int z = blockIdx.y / d.n_split, part = blockIdx.y % d.n_split;  // product, part of its k
     int tm, tn;
@@ -224,102 +230,144 @@ __global__ __launch_bounds__(S::kThreads, 2) void psattn_ffn_tiles(Product d, in
     const int64_t p_step = (PKC ? kBk : kBk * d.ldp) * static_cast<int64_t>(sizeof(E)), q_step = (QKC ? kBk : kBk * d.ldq) * static_cast<int64_t>(sizeof(E));
     auto p_base = [&](int seg) { return static_cast<const char*>(d.p[d.n_prod > 1 ? z : seg]) + (PKC ? m0 * d.ldp : m0) * static_cast<int64_t>(sizeof(E)); };
     auto q_base = [&](int seg) { return static_cast<const char*>(d.q[seg]) + (QKC ? n0 * d.ldq : n0) * static_cast<int64_t>(sizeof(E)); };
-    // where the next copies come from
+    // where an operand's next copies come from
     const int seg0 = d.n_seg > 1 && first >= per_seg ? 1 : 0;
     const char *pc = p_base(seg0) + (first - seg0 * per_seg) * p_step, *qc = q_base(seg0) + (first - seg0 * per_seg) * q_step;
     const char* qc2 = PASS == kGate ? q_base(1) + first * q_step : nullptr;
-    int left = seg0 ? 0 : per_seg - first;  // tiles of the first segment not yet asked for
-    // of a tile: PER copies of P, then those of Q
-    constexpr int kP = decltype(cp)::PER, kQ = decltype(cq)::PER, kCopies = kP + kQ;
-    auto copy = [&](auto J, auto BUF) {
-        constexpr int j = decltype(J)::value, buf = decltype(BUF)::value;
-        if constexpr (j < kP) {
-            cp.template issue<j>(pc, ptile + buf * kPB, w);
-        } else {
-            const char* base = qc;
-            if constexpr (PASS == kGate) base = (((w * kQ + j - kP) * 8) >> 5) & 1 ? qc2 : qc;
-            cq.template issue<j - kP>(base, qtile + buf * kQB, w);
-        }
+    int p_left = seg0 ? 0 : per_seg - first, q_left = p_left;  // tiles of the first segment not yet asked for
+    constexpr int kP = decltype(cp)::PER, kQ = decltype(cq)::PER;
+    auto copy_p = [&](auto J, int buf) { cp.template issue<decltype(J)::value>(pc, ptile + buf * kPB, w); };
+    auto copy_q = [&](auto J, int buf) {
+        const char* base = qc;
+        if constexpr (PASS == kGate) base = (((w * kQ + decltype(J)::value) * 8) >> 5) & 1 ? qc2 : qc;
+        cq.template issue<decltype(J)::value>(base, qtile + buf * kQB, w);
     };
-    auto put = [&](auto J, auto BUF) {
-        constexpr int j = decltype(J)::value, buf = decltype(BUF)::value;
-        if constexpr (j < kP) cp.template put<j>(ptile + buf * kPB, w, l);
-        else cq.template put<j - kP>(qtile + buf * kQB, w, l);
-    };
-    auto advance = [&] {
+    auto advance_p = [&] {
         pc += p_step;
+        if (--p_left == 0 && d.n_seg > 1) pc = p_base(1);
+    };
+    auto advance_q = [&] {
         qc += q_step;
         if constexpr (PASS == kGate) qc2 += q_step;
-        if (--left == 0 && d.n_seg > 1) {
-            pc = p_base(1);
-            qc = q_base(1);
-        }
+        if (--q_left == 0 && d.n_seg > 1) qc = q_base(1);
     };
     using I0 = std::integral_constant<int, 0>;
-    using I1 = std::integral_constant<int, 1>;
-    auto read = [&](auto R, auto SET, auto BUF, auto T) {  // the R-th operand of step T
-        constexpr int r = decltype(R)::value, set = decltype(SET)::value, buf = decltype(BUF)::value, t = decltype(T)::value;
-        if constexpr (r < NB) fq[set][r] = read_frag<E, QKC, r, t>(qtile + buf * kQB, lq);
-        else fp[set][r - NB] = read_frag<E, PKC, r - NB, t>(ptile + buf * kPB, lp);
+    auto read = [&](auto R, auto SET, int pbuf, int qbuf, auto T) {  // the R-th operand of step T
+        constexpr int r = decltype(R)::value, set = decltype(SET)::value, t = decltype(T)::value;
+        if constexpr (r < NB) fq[set][r] = read_frag<E, QKC, r, t>(qtile + qbuf * kQB, lq);
+        else fp[set][r - NB] = read_frag<E, PKC, r - NB, t>(ptile + pbuf * kPB, lp);
     };
     constexpr int kSteps = 4, kReads = MB + NB, kSlots = MB * NB;
-    // the things of [0, N) that stand in MFMA slot S
-    auto in_slot = [&](auto S_, auto N_, auto&& f) {
-        static_for<0, decltype(N_)::value>([&](auto I) {
-            if constexpr (decltype(I)::value * kSlots / decltype(N_)::value == decltype(S_)::value) f(I);
+    // f for each of [B, E) that stands in MFMA slot S
+    auto in_slot = [&](auto S_, auto B_, auto E_, auto&& f) {
+        constexpr int s = decltype(S_)::value, b = decltype(B_)::value, n = decltype(E_)::value - b;
+        static_for<0, n>([&](auto I) {
+            if constexpr (decltype(I)::value * kSlots / n == s) f(std::integral_constant<int, b + decltype(I)::value>{});
         });
     };
     using Reads = std::integral_constant<int, kReads>;
-    using Copies = std::integral_constant<int, kCopies>;
-    // one tile; `next`: there is one behind it, `more`: and one behind that
-    auto tile = [&](auto BUF, bool next, bool more) {
+    using Ps = std::integral_constant<int, kP>;
+    using Qs = std::integral_constant<int, kQ>;
+    using HalfP = std::integral_constant<int, (kP + 1) / 2>;
+    using HalfQ = std::integral_constant<int, (kQ + 1) / 2>;
+    // One tile; `ahead`: how many there are behind it; q0, q1, q2: the buffers of Q of this tile, of the next one, and the one that is filled
+    auto tile = [&](auto BUF, int ahead, int q0, int q1, int q2) {
         constexpr int buf = decltype(BUF)::value;
-        using Other = std::integral_constant<int, buf ^ 1>;
         static_for<0, kSteps>([&](auto T) {
             constexpr int t = decltype(T)::value, set = t & 1;
             using Set = std::integral_constant<int, set ^ 1>;
             if constexpr (t == kSteps - 1) {
-                if constexpr (ASYNC) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-                else __syncthreads();
+                if constexpr (!ASYNC) {
+                    __syncthreads();
+                } else if constexpr (NBQ == 2) {
+                    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                } else {  // the copies of Q of the tile after the next may be in flight
+                    if (ahead >= 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kQ) : "memory");
+                    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                }
             }
             static_for<0, kSlots>([&](auto S_) {
                 constexpr int s = decltype(S_)::value;
-                in_slot(S_, Reads{}, [&](auto R) {
-                    if constexpr (t < kSteps - 1) read(R, Set{}, BUF, std::integral_constant<int, t + 1>{});
-                    else read(R, Set{}, Other{}, I0{});
+                in_slot(S_, I0{}, Reads{}, [&](auto R) {
+                    if constexpr (t < kSteps - 1) read(R, Set{}, buf, q0, std::integral_constant<int, t + 1>{});
+                    else read(R, Set{}, buf ^ 1, q1, I0{});
                 });
                 if constexpr (!ASYNC && t == kSteps - 2) {
-                    if (next) in_slot(S_, Copies{}, [&](auto J) { put(J, Other{}); });
+                    if (ahead >= 1) {
+                        in_slot(S_, I0{}, Ps{}, [&](auto J) { cp.template put<decltype(J)::value>(ptile + (buf ^ 1) * kPB, w, l); });
+                        in_slot(S_, I0{}, Qs{}, [&](auto J) { cq.template put<decltype(J)::value>(qtile + q1 * kQB, w, l); });
+                    }
                 }
-                if constexpr (t == kSteps - 1) {
-                    if (more) in_slot(S_, Copies{}, [&](auto J) { copy(J, BUF); });
+                if constexpr (NBQ == 2) {
+                    if constexpr (t == kSteps - 1)
+                        if (ahead >= 2) {
+                            in_slot(S_, I0{}, Ps{}, [&](auto J) { copy_p(J, buf); });
+                            in_slot(S_, I0{}, Qs{}, [&](auto J) { copy_q(J, q2); });
+                        }
+                } else if constexpr (t == kSteps - 1) {
+                    if (ahead >= 2) in_slot(S_, I0{}, HalfP{}, [&](auto J) { copy_p(J, buf); });
+                } else if constexpr (t == 0) {
+                    if (ahead >= 1) in_slot(S_, HalfP{}, Ps{}, [&](auto J) { copy_p(J, buf ^ 1); });
+                } else if constexpr (t == 1) {
+                    if (ahead >= 2) in_slot(S_, I0{}, HalfQ{}, [&](auto J) { copy_q(J, q2); });
+                } else {
+                    if (ahead >= 2) in_slot(S_, HalfQ{}, Qs{}, [&](auto J) { copy_q(J, q2); });
                 }
                 acc[s % NB][s / NB] = mfma(fq[set][s % NB], fp[set][s / NB], acc[s % NB][s / NB]);
                 __builtin_amdgcn_sched_barrier(0);
             });
+            if constexpr (NBQ == 3 && t == 0) {
+                if (ahead >= 1) advance_p();
+            } else if constexpr (NBQ == 3 && t == 2) {
+                if (ahead >= 2) advance_q();
+            } else if constexpr (NBQ == 2 && t == kSteps - 1) {
+                if (ahead >= 2) {
+                    advance_p();
+                    advance_q();
+                }
+            }
         });
-        if (more) advance();
     };
     if (total > 0) {
-        static_for<0, kCopies>([&](auto J) { copy(J, I0{}); });
-        static_for<0, kCopies>([&](auto J) { put(J, I0{}); });
-        advance();
+        static_for<0, kP>([&](auto J) { copy_p(J, 0); });
+        static_for<0, kQ>([&](auto J) { copy_q(J, 0); });
+        advance_p();
+        advance_q();
+        if constexpr (!ASYNC) {
+            static_for<0, kP>([&](auto J) { cp.template put<decltype(J)::value>(ptile, w, l); });
+            static_for<0, kQ>([&](auto J) { cq.template put<decltype(J)::value>(qtile, w, l); });
+        }
         if (total > 1) {
-            static_for<0, kCopies>([&](auto J) { copy(J, I1{}); });
-            advance();
-            if constexpr (ASYNC) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kCopies) : "memory");
-            else __syncthreads();
+            static_for<0, kQ>([&](auto J) { copy_q(J, 1); });
+            advance_q();
+            static_for<0, NBQ == 3 ? HalfP::value : kP>([&](auto J) { copy_p(J, 1); });
+            if constexpr (NBQ == 2) advance_p();
+            if constexpr (ASYNC) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kQ + (NBQ == 3 ? HalfP::value : kP)) : "memory");
         } else {
             if constexpr (ASYNC) asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-            else __syncthreads();
         }
-        static_for<0, kReads>([&](auto R) { read(R, I0{}, I0{}, I0{}); });
-        int i = 0;
-        for (; i + 1 < total; i += 2) {
-            tile(I0{}, true, i + 2 < total);
-            tile(I1{}, i + 2 < total, i + 3 < total);
+        if constexpr (!ASYNC) __syncthreads();
+        static_for<0, kReads>([&](auto R) { read(R, I0{}, 0, 0, I0{}); });
+        int ahead = total - 1, q0 = 0, q1 = 1, q2 = NBQ - 1;
+        auto turn = [&] {
+            if constexpr (NBQ == 3) {
+                const int q = q0;
+                q0 = q1;
+                q1 = q2;
+                q2 = q;
+            } else {
+                q0 ^= 1;
+                q1 ^= 1;
+            }
+            --ahead;
+        };
+        while (ahead >= 1) {
+            tile(std::integral_constant<int, 0>{}, ahead, NBQ == 2 ? 0 : q0, NBQ == 2 ? 1 : q1, NBQ == 2 ? 0 : q2);
+            turn();
+            tile(std::integral_constant<int, 1>{}, ahead, NBQ == 2 ? 1 : q0, NBQ == 2 ? 0 : q1, NBQ == 2 ? 1 : q2);
+            turn();
         }
-        if (i < total) tile(I0{}, false, false);
+        if (ahead == 0) tile(std::integral_constant<int, 0>{}, 0, NBQ == 2 ? 0 : q0, NBQ == 2 ? 1 : q1, NBQ == 2 ? 0 : q2);
     }
     if (const int rest = per_seg * kBk; rest < d.K && part == d.n_split - 1) {  // what is left of k, zeros behind it
         for (int seg = 0; seg < d.n_seg; ++seg) {
@@ -334,7 +382,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void psattn_ffn_tiles(Product d, in
                 });
             __syncthreads();
             static_for<0, kSteps>([&](auto T) {
-                static_for<0, kReads>([&](auto R) { read(R, I0{}, I0{}, T); });
+                static_for<0, kReads>([&](auto R) { read(R, I0{}, 0, 0, T); });
                 static_for<0, kSlots>([&](auto S_) {
                     constexpr int s = decltype(S_)::value;
                     acc[s % NB][s / NB] = mfma(fq[0][s % NB], fp[0][s / NB], acc[s % NB][s / NB]);
@@ -412,11 +460,11 @@ int launch_tiles(const Product& d, hipStream_t s) {
 template <typename E, bool ASYNC, bool PKC, bool QKC, Pass PASS, int ACT>
 int launch_sized(TileSize size, const Product& d, hipStream_t s) {
     if constexpr (PKC) {
-        if (size == k32) return launch_tiles<E, ASYNC, PKC, QKC, PASS, ACT, Shape<32, 128, 1, 2>>(d, s);
-        if (size == k64) return launch_tiles<E, ASYNC, PKC, QKC, PASS, ACT, Shape<64, 128, 1, 2>>(d, s);
+        if (size == k32) return launch_tiles<E, ASYNC, PKC, QKC, PASS, ACT, Shape<32, 128, 1, 2, 2>>(d, s);
+        if (size == k64) return launch_tiles<E, ASYNC, PKC, QKC, PASS, ACT, Shape<64, 128, 1, 2, 2>>(d, s);
     }
-    if (size == k256) return launch_tiles<E, ASYNC, PKC, QKC, PASS, ACT, Shape<256, 256, 2, 4>>(d, s);
-    return launch_tiles<E, ASYNC, PKC, QKC, PASS, ACT, Shape<128, 128, 2, 2>>(d, s);
+    if (size == k256) return launch_tiles<E, ASYNC, PKC, QKC, PASS, ACT, Shape<256, 256, 2, 4, ASYNC ? V_L : 2>>(d, s);
+    return launch_tiles<E, ASYNC, PKC, QKC, PASS, ACT, Shape<128, 128, 2, 2, ASYNC ? V_M : 2>>(d, s);
 }
 
 template <typename E, bool ASYNC>
