@@ -9,6 +9,7 @@
 
 #include <algorithm>
 #include <initializer_list>
+#include <type_traits>
 
 #include "psattn.h"
 #include "psattn_ffn.h"
@@ -43,75 +44,161 @@ struct Plan {
 
 constexpr int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-Plan plan(int32_t dt, Pass pass, bool pkc, int64_t M, int64_t N, int64_t K, int n_seg, int n_prod) {
-    static constexpr int bm[] = {32, 64, 128, 256}, bn[] = {128, 128, 128, 256}, per_cu[] = {4, 3, 2, 1};
+// How a product's operands and results are moved: kWhole in 16-byte groups on boundaries, kOdd not, kFloat fp32
+enum Move { kWhole, kOdd, kFloat };
+
+// What a product takes, in us, from the rounds of workgroups that its tiles make: which tile size, and k in how many parts.  A step is 128
+// bytes of k.  Measured, hidden 4 096, inner 14 336: 256 x 256, one workgroup to a CU, 1.6 us a step (1.25 where few CUs have one);
+// 128 x 128, two to a CU, 1.05 a step, 0.65 by itself; through registers half as much again; fp32 what its MFMAs take.  A round's start and
+// end take 3 us, or 14 (gate) and 30 (dG, dU) with 256 x 256, whose workgroups have nothing beside them to cover it, 3 and 12 with
+// 128 x 128.  The two sizes, in turn: 8 192 tokens 7.0 and 8.5 ms, 1 024 tokens 1.72 and 1.49, 256 tokens 1.16 and 0.72 (unsplit).
+// Parts have no end but their sums' way to memory, and are joined by another launch.
+double cost(Move move, Pass pass, TileSize size, int64_t tiles, int64_t steps, int64_t split, double out_bytes) {
+    const bool big = size == k256, parts = split > 1;
+    const double per_wg = static_cast<double>(cdiv(steps, split)), odd = move == kOdd ? 1.5 : 1;
+    const double full = (move == kFloat ? (big ? 6.8 : 3.4) : (big ? 1.6 : 1.05) * odd) * per_wg, few = (move == kFloat ? (big ? 6.8 : 1.7) : (big ? 1.25 : 0.65) * odd) * per_wg;
+    const double end = parts || pass == kPlain ? 3 : pass == kGate ? (big ? 14 : 3) : (big ? 30 : 12);
+    const int64_t wgs = tiles * split, slots = big ? 256 : 512, rest = wgs % slots;
+    const bool little = rest > 0 && (big ? wgs <= 128 : rest <= 256);
+    return static_cast<double>(wgs / slots) * (full + end) + (rest == 0 ? 0 : (little ? few : full) + end) + (parts ? 4 + static_cast<double>(split) * out_bytes * 1.3 / 4.5e6 : 0);
+}
+
+Plan plan(Move move, Pass pass, bool pkc, int64_t M, int64_t N, int64_t K, int n_seg, int n_prod) {
+    static constexpr int bm[] = {32, 64, 128, 256}, bn[] = {128, 128, 128, 256};
     auto tiles = [&](TileSize t) { return cdiv(M, bm[t]) * cdiv(N * (pass == kGate ? 2 : 1), bn[t]) * n_prod; };
-    Plan p{};
-    p.size = pkc && M <= 32 ? k32 : pkc && M <= 64 ? k64 : tiles(k256) >= 200 ? k256 : k128;
-    const int64_t steps = K / (dt == PSATTN_BF16 ? 64 : 32) * n_seg, n = tiles(p.size), want = 256 * per_cu[p.size];
-    p.split = static_cast<int32_t>(std::max<int64_t>(1, std::min(want / n, steps / 4)));
-    return p;
+    const int64_t steps = K / (move == kFloat ? 32 : 64) * n_seg;
+    Plan best{k128, 1};
+    if (pkc && M <= 64) {
+        // few tokens: the weights have to be read, and three or four workgroups to a CU keep enough of them in flight (one token, hidden 4 096,
+        // inner 14 336: 5.5 TB/s)
+        best.size = M <= 32 ? k32 : k64;
+        best.split = static_cast<int32_t>(std::max<int64_t>(1, std::min((M <= 32 ? 1024 : 768) / tiles(best.size), steps / 4)));
+        return best;
+    }
+    const double out = sizeof(float) * static_cast<double>(M) * N * (pass == kGate ? 2 : n_prod);
+    double least = 0;
+    for (const TileSize t : {k128, k256})
+        for (const int64_t split : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 24, 32, 48, 64}) {
+            if (split > 1 && steps / split < 4) break;
+            const double us = cost(move, pass, t, tiles(t), steps, split, out);
+            if ((t == k128 && split == 1) || us < least) {
+                least = us;
+                best = {t, static_cast<int32_t>(split)};
+            }
+        }
+    return best;
 }
 
 int64_t ld_part(int64_t N) { return (N + 7) / 8 * 8; }
 
+// room for a product's parts, whichever way its operands turn out to move
 size_t part_bytes(int32_t dt, Pass pass, bool pkc, int64_t M, int64_t N, int64_t K, int n_seg, int n_prod) {
     if (M == 0 || K == 0) return 0;  // no tokens: no products
-    const Plan p = plan(dt, pass, pkc, M, N, K, n_seg, n_prod);
-    return p.split > 1 ? sizeof(float) * p.split * (pass == kGate ? 2 : n_prod) * M * ld_part(N) : 0;
+    auto room = [&](Move move) {
+        const Plan p = plan(move, pass, pkc, M, N, K, n_seg, n_prod);
+        return p.split > 1 ? sizeof(float) * p.split * (pass == kGate ? 2 : n_prod) * M * ld_part(N) : size_t{0};
+    };
+    return dt == PSATTN_BF16 ? std::max(room(kWhole), room(kOdd)) : room(kFloat);
 }
 
-// joins the parts of a product: the epilogue of psattn_ffn_tiles on sums from memory.  grid (columns, rows, products)
-template <typename E, Pass PASS, int ACT>
+// joins the parts of a product: the epilogue of psattn_ffn_tiles on sums from memory, V columns to a lane (4 where rows allow it: 221 x
+// 14 336, dG and dU from three parts NOTE).  grid (columns, rows, products)
+template <int V, typename E>
+__device__ __forceinline__ void put(E* p, const float (&x)[V]) {
+    if constexpr (V == 1) store1(p, x[0]);
+    else if constexpr (sizeof(E) == 2) *reinterpret_cast<uint2*>(p) = make_uint2(psattn::mma::pack2(x[0], x[1]), psattn::mma::pack2(x[2], x[3]));
+    else *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+}
+template <int V, typename E>
+__device__ __forceinline__ void get(const E* p, float (&x)[V]) {
+    if constexpr (V == 1) {
+        x[0] = to_f32(*p);
+    } else if constexpr (sizeof(E) == 2) {
+        const uint2 u = *reinterpret_cast<const uint2*>(p);
+        x[0] = __uint_as_float(u.x << 16); x[1] = __uint_as_float(u.x & 0xffff0000u);
+        x[2] = __uint_as_float(u.y << 16); x[3] = __uint_as_float(u.y & 0xffff0000u);
+    } else {
+        const float4 u = *reinterpret_cast<const float4*>(p);
+        x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
+    }
+}
+
+template <typename E, Pass PASS, int ACT, int V>
 __global__ __launch_bounds__(256) void psattn_ffn_join(Product d) {
-    const int n = blockIdx.x * 256 + threadIdx.x, z = blockIdx.z;
+    const int n = (blockIdx.x * 256 + threadIdx.x) * V, z = blockIdx.z;
     if (n >= d.N) return;
+    constexpr int kOuts = PASS == kGate ? 2 : 1, kAtOnce = 4;
     const int n_out = PASS == kGate ? 2 : d.n_prod;
     for (int m = blockIdx.y; m < d.M; m += gridDim.y) {
         const float* p = d.parts + static_cast<int64_t>(m) * d.ld_part + n;
         const int64_t one = static_cast<int64_t>(d.M) * d.ld_part;
-        float x = 0.f, up = 0.f;
-        for (int i = 0; i < d.n_split; ++i) {
-            x += p[(static_cast<int64_t>(i) * n_out + z) * one];
-            if constexpr (PASS == kGate) up += p[(static_cast<int64_t>(i) * n_out + 1) * one];
-        }
+        float x[kOuts][V] = {};
+        auto add = [&](int from, auto COUNT) {  // loads together, sums in order
+            constexpr int count = decltype(COUNT)::value;
+            float a[count][kOuts][V];
+#pragma unroll
+            for (int u = 0; u < count; ++u)
+#pragma unroll
+                for (int o = 0; o < kOuts; ++o) get<V>(p + (static_cast<int64_t>(from + u) * n_out + (PASS == kGate ? o : z)) * one, a[u][o]);
+#pragma unroll
+            for (int u = 0; u < count; ++u)
+#pragma unroll
+                for (int o = 0; o < kOuts; ++o)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) x[o][j] += a[u][o][j];
+        };
+        int i = 0;
+        for (; i + kAtOnce <= d.n_split; i += kAtOnce) add(i, std::integral_constant<int, kAtOnce>{});
+        for (; i < d.n_split; ++i) add(i, std::integral_constant<int, 1>{});
         const int64_t at = m * d.ldo + n;
         if constexpr (PASS == kGate) {
-            if (d.G) store1(static_cast<E*>(d.G) + at, x);
-            if (d.U) store1(static_cast<E*>(d.U) + at, up);
-            store1(static_cast<E*>(d.H) + at, act<ACT>(x) * up);
+            if (d.G) put<V>(static_cast<E*>(d.G) + at, x[0]);
+            if (d.U) put<V>(static_cast<E*>(d.U) + at, x[1]);
+            float h[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) h[j] = act<E, ACT>(x[0][j]) * x[1][j];
+            put<V>(static_cast<E*>(d.H) + at, h);
         } else if constexpr (PASS == kDact) {
-            float a, da;
-            act_grad<ACT>(to_f32(static_cast<const E*>(d.G)[at]), a, da);
-            store1(static_cast<E*>(d.out[0]) + at, x * to_f32(static_cast<const E*>(d.U)[at]) * da);
-            store1(static_cast<E*>(d.out[1]) + at, x * a);
+            float gate[V], up[V], dg[V], du[V];
+            get<V>(static_cast<const E*>(d.G) + at, gate);
+            get<V>(static_cast<const E*>(d.U) + at, up);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                float a, da;
+                act_grad<E, ACT>(gate[j], a, da);
+                dg[j] = x[0][j] * up[j] * da;
+                du[j] = x[0][j] * a;
+            }
+            put<V>(static_cast<E*>(d.out[0]) + at, dg);
+            put<V>(static_cast<E*>(d.out[1]) + at, du);
         } else {
-            store1(static_cast<E*>(d.out[z]) + at, x);
+            put<V>(static_cast<E*>(d.out[z]) + at, x[0]);
         }
     }
 }
 
-template <typename E>
+template <typename E, int V>
 void join(Pass pass, int act, const Product& d, hipStream_t s) {
-    const dim3 grid(static_cast<uint32_t>(cdiv(d.N, 256)), std::min(d.M, 4096), pass == kPlain ? d.n_prod : 1);
+    const dim3 grid(static_cast<uint32_t>(cdiv(d.N, 256 * V)), std::min(d.M, 4096), pass == kPlain ? d.n_prod : 1);
     auto go = [&](auto kernel) { kernel<<<grid, 256, 0, s>>>(d); };
-    if (pass == kPlain) go(psattn_ffn_join<E, kPlain, 0>);
-    else if (pass == kGate) act == PSATTN_ACT_SILU ? go(psattn_ffn_join<E, kGate, 0>) : go(psattn_ffn_join<E, kGate, 1>);
-    else act == PSATTN_ACT_SILU ? go(psattn_ffn_join<E, kDact, 0>) : go(psattn_ffn_join<E, kDact, 1>);
+    if (pass == kPlain) go(psattn_ffn_join<E, kPlain, 0, V>);
+    else if (pass == kGate) act == PSATTN_ACT_SILU ? go(psattn_ffn_join<E, kGate, 0, V>) : go(psattn_ffn_join<E, kGate, 1, V>);
+    else act == PSATTN_ACT_SILU ? go(psattn_ffn_join<E, kDact, 0, V>) : go(psattn_ffn_join<E, kDact, 1, V>);
 }
 
 // `parts`: room of part_bytes()
 int product(int32_t dt, Pass pass, int act, bool pkc, bool qkc, Product d, void* parts, hipStream_t s) {
     if (std::max(d.ldp, d.ldq) * elem_bytes(dt) * 256 >= (int64_t{1} << 31)) return PSATTN_EUNSUPPORTED;  // a tile's copies have 32-bit offsets
-    const Plan p = plan(dt, pass, pkc, d.M, d.N, d.K, d.n_seg, d.n_prod);
+    const Move move = dt != PSATTN_BF16 ? kFloat : whole_rows(pkc, d) ? kWhole : kOdd;
+    const Plan p = plan(move, pass, pkc, d.M, d.N, d.K, d.n_seg, d.n_prod);
     d.n_split = p.split;
     d.parts = static_cast<float*>(parts);
     d.ld_part = ld_part(d.N);
-    const int rc = dt != PSATTN_BF16 ? product_f32(pass, act, pkc, qkc, p.size, d, s) : whole_rows(pkc, d) ? product_bf16(pass, act, pkc, qkc, p.size, d, s)
-                                                                                                  : product_bf16_any(pass, act, pkc, qkc, p.size, d, s);
+    const int rc = (move == kFloat ? product_f32 : move == kWhole ? product_bf16 : product_bf16_any)(pass, act, pkc, qkc, p.size, d, s);
     if (rc != PSATTN_OK || d.n_split == 1) return rc;
-    if (dt == PSATTN_BF16) join<uint16_t>(pass, act, d, s);
-    else join<float>(pass, act, d, s);
+    const bool four = at16({d.out[0], d.out[1], d.G, d.U, d.H}) && d.ldo % 4 == 0 && d.N % 4 == 0;
+    if (dt == PSATTN_BF16) four ? join<uint16_t, 4>(pass, act, d, s) : join<uint16_t, 1>(pass, act, d, s);
+    else four ? join<float, 4>(pass, act, d, s) : join<float, 1>(pass, act, d, s);
     return hipGetLastError() == hipSuccess ? PSATTN_OK : PSATTN_EHIP;
 }
 

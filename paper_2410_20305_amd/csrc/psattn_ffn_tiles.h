@@ -20,10 +20,6 @@
 namespace psattn {
 namespace gemm {
 
-#ifndef V_L
-#define V_L 3
-#define V_M 3
-#endif
 // Which tile a workgroup takes.  Workgroups go to the eight XCDs in turn: each XCD takes a run of tiles, and the run goes through
 // kGroup rows of tiles at a time, so that those that run together share their operands in its L2.
 constexpr int kGroup = 8;
@@ -142,32 +138,49 @@ __device__ __forceinline__ void put8(float* p, const float (&x)[8], int n) {
             if (j < n) p[j] = x[j];
     }
 }
-template <bool ALIGNED, typename E>
-__device__ __forceinline__ void get8(const E* p, float (&x)[8], int n) {
-    if (ALIGNED || n >= 8) {
+// eight elements as they lie in memory
+template <typename E>
+struct Group {
+    uint32_t w[2 * sizeof(E)];
+    template <bool ALIGNED>
+    __device__ __forceinline__ void get(const E* p, int n) {
+        constexpr int W = 2 * sizeof(E);
+        if (ALIGNED || n >= 8) {
+#pragma unroll
+            for (int i = 0; i < W; i += 4) {
+                if constexpr (ALIGNED) {
+                    const uint4 x = *reinterpret_cast<const uint4*>(p + i * 4 / sizeof(E));
+                    w[i] = x.x; w[i + 1] = x.y; w[i + 2] = x.z; w[i + 3] = x.w;
+                } else {
+                    const Raw16 x = *reinterpret_cast<const Raw16*>(p + i * 4 / sizeof(E));
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) w[i + j] = x.w[j];
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < W; ++i) w[i] = 0;
+#pragma unroll
+            for (int j = 0; j < 7; ++j)
+                if (j < n) {
+                    if constexpr (sizeof(E) == 2) w[j / 2] |= static_cast<uint32_t>(p[j]) << (16 * (j & 1));
+                    else w[j] = __float_as_uint(p[j]);
+                }
+        }
+    }
+    __device__ __forceinline__ void values(float (&x)[8]) const {
         if constexpr (sizeof(E) == 2) {
-            uint4 u;
-            if constexpr (ALIGNED) u = *reinterpret_cast<const uint4*>(p);
-            else { const Raw16 r = *reinterpret_cast<const Raw16*>(p); u = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]); }
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 x[2 * j] = __uint_as_float(w[j] << 16);
                 x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
             }
         } else {
-            const Raw16 a = *reinterpret_cast<const Raw16*>(p), b = *reinterpret_cast<const Raw16*>(p + 4);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                x[j] = __uint_as_float(a.w[j]);
-                x[4 + j] = __uint_as_float(b.w[j]);
-            }
+            for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(w[j]);
         }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = j < n ? to_f32(p[j]) : 0.f;
     }
-}
+};
 
 // Stores a block of 32 x 32.  bf16: 64 contiguous bytes of 16 rows at a time (rows r and r + 16 trade chunks between the 16-lane
 // halves); fp32: 32 bytes to a lane
@@ -390,6 +403,57 @@ __global__ __launch_bounds__(S::kThreads, 2) void psattn_ffn_tiles(Product d, in
             });
         }
     }
+    if (PASS == kDact && d.n_split == 1) {
+        // G and U of the wave's next block are asked for before this one's results are made.  Rows outside are read from inside and not
+        // stored; so are whole groups of columns, and blocks that have none
+        auto place = [&](int i, int& m, int& n, int& rows, int& cols) {
+            m = m0 + (wm * MB + i / NB) * 32;
+            n = n0 + (wn * NB + i % NB) * 32;
+            rows = d.M - m;
+            cols = d.N - n;
+            return rows > 0 && cols > 0;
+        };
+        constexpr int kBlocks = MB * NB;
+        Group<E> g[2][2], u[2][2];
+        auto ask = [&](int i, int set) {
+            int m, n, rows, cols;
+            if (!place(i, m, n, rows, cols)) return;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int c = min(16 * k + 8 * (l >> 5), (cols - 1) / 8 * 8);
+                const int64_t from = (m + min(l & 31, rows - 1)) * d.ldo + n + c;
+                g[set][k].template get<ASYNC>(static_cast<const E*>(d.G) + from, cols - c);
+                u[set][k].template get<ASYNC>(static_cast<const E*>(d.U) + from, cols - c);
+            }
+        };
+        ask(0, 0);
+        static_for<0, kBlocks>([&](auto I) {
+            constexpr int i = decltype(I)::value, set = i & 1;
+            if constexpr (i + 1 < kBlocks) ask(i + 1, set ^ 1);
+            int m, n, rows, cols;
+            if (!place(i, m, n, rows, cols)) return;
+            const Chunks x = chunks(acc[i % NB][i / NB]);
+            Chunks dg, du;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                float gate[8], up[8];
+                g[set][k].values(gate);
+                u[set][k].values(up);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    float a, da;
+                    act_grad<E, ACT>(gate[j], a, da);
+                    dg.c[k][j] = x.c[k][j] * up[j] * da;
+                    du.c[k][j] = x.c[k][j] * a;
+                }
+            }
+            const int64_t at = m * d.ldo + n;
+            store_chunks<ASYNC>(static_cast<E*>(d.out[0]) + at, d.ldo, rows, cols, dg, l);
+            store_chunks<ASYNC>(static_cast<E*>(d.out[1]) + at, d.ldo, rows, cols, du, l);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        return;
+    }
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
         const int m = m0 + (wm * MB + mb) * 32, rows = d.M - m;
@@ -409,40 +473,16 @@ __global__ __launch_bounds__(S::kThreads, 2) void psattn_ffn_tiles(Product d, in
             const int64_t at = m * d.ldo + n;
             f32x16 h;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) h[i] = act<ACT>(acc[0][mb][i]) * acc[1][mb][i];
+            for (int i = 0; i < 16; ++i) h[i] = act<E, ACT>(acc[0][mb][i]) * acc[1][mb][i];
             if (d.G) store_chunks<ASYNC>(static_cast<E*>(d.G) + at, d.ldo, rows, cols, chunks(acc[0][mb]), l);
             if (d.U) store_chunks<ASYNC>(static_cast<E*>(d.U) + at, d.ldo, rows, cols, chunks(acc[1][mb]), l);
             store_chunks<ASYNC>(static_cast<E*>(d.H) + at, d.ldo, rows, cols, chunks(h), l);
-        } else {
+        } else if constexpr (PASS == kPlain) {
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
                 const int n = n0 + (wn * NB + nb) * 32, cols = d.N - n;
                 if (cols <= 0) break;
-                const int64_t at = m * d.ldo + n;
-                const Chunks x = chunks(acc[nb][mb]);
-                if constexpr (PASS == kPlain) {
-                    store_chunks<ASYNC>(static_cast<E*>(d.out[d.n_prod > 1 ? z : 0]) + at, d.ldo, rows, cols, x, l);
-                } else {
-                    Chunks dg, du;
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        // rows outside are read from inside and not stored; so are whole groups of columns
-                        const int col = 16 * k + 8 * (l >> 5), c = min(col, (cols - 1) / 8 * 8);
-                        const int64_t from = at + min(l & 31, rows - 1) * d.ldo + c;
-                        float gate[8], up[8];
-                        get8<ASYNC>(static_cast<const E*>(d.G) + from, gate, cols - c);
-                        get8<ASYNC>(static_cast<const E*>(d.U) + from, up, cols - c);
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            float a, da;
-                            act_grad<ACT>(gate[j], a, da);
-                            dg.c[k][j] = x.c[k][j] * up[j] * da;
-                            du.c[k][j] = x.c[k][j] * a;
-                        }
-                    }
-                    store_chunks<ASYNC>(static_cast<E*>(d.out[0]) + at, d.ldo, rows, cols, dg, l);
-                    store_chunks<ASYNC>(static_cast<E*>(d.out[1]) + at, d.ldo, rows, cols, du, l);
-                }
+                store_chunks<ASYNC>(static_cast<E*>(d.out[d.n_prod > 1 ? z : 0]) + m * d.ldo + n, d.ldo, rows, cols, chunks(acc[nb][mb]), l);
             }
         }
     }
@@ -463,8 +503,8 @@ int launch_sized(TileSize size, const Product& d, hipStream_t s) {
         if (size == k32) return launch_tiles<E, ASYNC, PKC, QKC, PASS, ACT, Shape<32, 128, 1, 2, 2>>(d, s);
         if (size == k64) return launch_tiles<E, ASYNC, PKC, QKC, PASS, ACT, Shape<64, 128, 1, 2, 2>>(d, s);
     }
-    if (size == k256) return launch_tiles<E, ASYNC, PKC, QKC, PASS, ACT, Shape<256, 256, 2, 4, ASYNC ? V_L : 2>>(d, s);
-    return launch_tiles<E, ASYNC, PKC, QKC, PASS, ACT, Shape<128, 128, 2, 2, ASYNC ? V_M : 2>>(d, s);
+    if (size == k256) return launch_tiles<E, ASYNC, PKC, QKC, PASS, ACT, Shape<256, 256, 2, 4, ASYNC ? 3 : 2>>(d, s);
+    return launch_tiles<E, ASYNC, PKC, QKC, PASS, ACT, Shape<128, 128, 2, 2, ASYNC ? 3 : 2>>(d, s);
 }
 
 template <typename E, bool ASYNC>

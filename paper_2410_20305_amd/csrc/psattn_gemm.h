@@ -189,22 +189,33 @@ __device__ __forceinline__ uint4 fetch(int c, int64_t ld, int k0, int K, int row
 
 // ---- activation: ACT as psattn_act
 // SiLU a = g s, a' = s (1 + g (1 - s)), s = 1 / (1 + exp(-g)); GELU a = g Phi(g), a' = Phi(g) + g phi(g), Phi by erfc, which
-// keeps its relative accuracy where the gate is closed.
-template <int ACT>
+// keeps its relative accuracy where the gate is closed.  For bf16 the exponential is the hardware's (off by |g| 2^-24 relatively) and
+// so is the reciprocal (2^-23): nothing beside the result's own 2^-8.
+template <typename E>
+__device__ __forceinline__ float exp_of(float x) {
+    if constexpr (sizeof(E) == 2) return __expf(x);
+    else return expf(x);
+}
+template <typename E>
+__device__ __forceinline__ float logistic(float g) {
+    if constexpr (sizeof(E) == 2) return __builtin_amdgcn_rcpf(1.f + __expf(-g));
+    else return 1.f / (1.f + expf(-g));
+}
+template <typename E, int ACT>
 __device__ __forceinline__ float act(float g) {
-    if constexpr (ACT == 0) return g / (1.f + expf(-g));
+    if constexpr (ACT == 0) return g * logistic<E>(g);
     else return 0.5f * g * erfcf(-0.70710678118654752f * g);
 }
-template <int ACT>
+template <typename E, int ACT>
 __device__ __forceinline__ void act_grad(float g, float& a, float& da) {
     if constexpr (ACT == 0) {
-        const float s = 1.f / (1.f + expf(-g));
+        const float s = logistic<E>(g);
         a = g * s;
         da = s * (1.f + g * (1.f - s));
     } else {
         const float cdf = 0.5f * erfcf(-0.70710678118654752f * g);
         a = g * cdf;
-        da = cdf + g * 0.3989422804014327f * expf(-0.5f * g * g);
+        da = cdf + g * 0.3989422804014327f * exp_of<E>(-0.5f * g * g);
     }
 }
 
