@@ -581,23 +581,23 @@ def psattn_dpo_loss(logp_policy, logp_ref, beta, stream=None):
 
 
 # ---- what stands beside attention in a model: embedding, layer norm, feed-forward block
-def _check_rows(t, name, dtype=None):
-    """The tensor that a call takes its sizes and its device from."""
+def _check_rows(t, name):
+    """Index of the device that a call runs on: that of the tensor from which it takes its sizes."""
     if t.dim() != 2:
         raise ValueError("%s must have two dimensions, got %d" % (name, t.dim()))
-    if not t.is_cuda:
-        raise ValueError("%s must be a device tensor" % name)
-    if t.device.index != (_TORCH or _torch()).cuda.current_device():
+    _check_tensor(t, name, t.shape, None)
+    dev = t.get_device()
+    if dev != (_TORCH or _torch())._C._cuda_getDevice():
         raise ValueError("%s is on %s, which is not the current device" % (name, t.device))
-    _check_tensor(t, name, t.shape, dtype)
+    return dev
 
 
-def _check_all(like, *tensors):
-    """(tensor, name, shape, dtype) each, on the device of `like`."""
+def _check_all(dev, *tensors):
+    """(tensor, name, shape, dtype) each, on device `dev`."""
     for t, name, shape, dtype in tensors:
         _check_tensor(t, name, shape, dtype)
-        if t.device != like.device:
-            raise ValueError("%s is on %s, not on %s" % (name, t.device, like.device))
+        if t.get_device() != dev:
+            raise ValueError("%s is on %s, not on cuda:%d" % (name, t.device, dev))
 
 
 def _workspace(given, need, like, stream):
@@ -618,11 +618,11 @@ def _workspace(given, need, like, stream):
 def psattn_embed_fwd(token_ids, W, scale=1.0, X=None, stream=None):
     """X [T, hidden] = scale * rows of W [vocab, hidden] by token_ids int32 [T]; ids outside the table give rows of zeros."""
     torch, lib = _TORCH or _torch(), _LIB or load_library()
-    _check_rows(W, "W")
+    dev = _check_rows(W, "W")
     (V, h), T = W.shape, token_ids.numel()
     dt = _dtype_code(W)
     X = torch.empty((T, h), dtype=W.dtype, device=W.device) if X is None else X
-    _check_all(W, (token_ids, "token_ids", (T,), torch.int32), (X, "X", (T, h), W.dtype))
+    _check_all(dev, (token_ids, "token_ids", (T,), torch.int32), (X, "X", (T, h), W.dtype))
     st = lib.psattn_embed_fwd(dt, T, V, h, float(scale), token_ids.data_ptr(), W.data_ptr(), X.data_ptr(), _stream_ptr(stream))
     _check(st, "psattn_embed_fwd")
     return X
@@ -631,13 +631,13 @@ def psattn_embed_fwd(token_ids, W, scale=1.0, X=None, stream=None):
 def psattn_embed_bwd(token_ids, dX, vocab, scale=1.0, dW=None, workspace=None, stream=None):
     """dW [vocab, hidden]: the gradient of psattn_embed_fwd's table."""
     torch, lib = _TORCH or _torch(), _LIB or load_library()
-    _check_rows(dX, "dX")
+    dev = _check_rows(dX, "dX")
     (T, h), vocab = dX.shape, int(vocab)
     dt = _dtype_code(dX)
     if vocab <= 0:
         raise ValueError("vocab must be positive, got %d" % vocab)
     dW = torch.empty((vocab, h), dtype=dX.dtype, device=dX.device) if dW is None else dW
-    _check_all(dX, (token_ids, "token_ids", (T,), torch.int32), (dW, "dW", (vocab, h), dX.dtype))
+    _check_all(dev, (token_ids, "token_ids", (T,), torch.int32), (dW, "dW", (vocab, h), dX.dtype))
     ws = _workspace(workspace, lib.psattn_embed_bwd_workspace_bytes(dt, T, vocab, h), dX, stream)
     st = lib.psattn_embed_bwd(dt, T, vocab, h, float(scale), token_ids.data_ptr(), dX.data_ptr(), dW.data_ptr(), ws.data_ptr(),
                               ws.numel() * ws.element_size(), _stream_ptr(stream))
@@ -648,7 +648,7 @@ def psattn_embed_bwd(token_ids, dX, vocab, scale=1.0, dW=None, workspace=None, s
 def psattn_layernorm_fwd(X, weight, bias=None, eps=1e-5, residual=None, S=None, Y=None, mean=None, rstd=None, stream=None):
     """Y, S, mean, rstd = layer norm of the rows of S = X + residual (S is X itself without one)."""
     torch, lib = _TORCH or _torch(), _LIB or load_library()
-    _check_rows(X, "X")
+    dev = _check_rows(X, "X")
     (n, h), dt, dtype = X.shape, _dtype_code(X), X.dtype
     tensors = [(weight, "weight", (h,), dtype)]
     if bias is not None:
@@ -662,7 +662,7 @@ def psattn_layernorm_fwd(X, weight, bias=None, eps=1e-5, residual=None, S=None, 
     mean = torch.empty(n, dtype=torch.float32, device=X.device) if mean is None else mean
     rstd = torch.empty(n, dtype=torch.float32, device=X.device) if rstd is None else rstd
     tensors += [(Y, "Y", X.shape, dtype), (mean, "mean", (n,), torch.float32), (rstd, "rstd", (n,), torch.float32)]
-    _check_all(X, *tensors)
+    _check_all(dev, *tensors)
     st = lib.psattn_layernorm_fwd(dt, n, h, float(eps), X.data_ptr(), None if residual is None else residual.data_ptr(), weight.data_ptr(),
                                   None if bias is None else bias.data_ptr(), None if residual is None else S.data_ptr(), Y.data_ptr(),
                                   mean.data_ptr(), rstd.data_ptr(), _stream_ptr(stream))
@@ -673,7 +673,7 @@ def psattn_layernorm_fwd(X, weight, bias=None, eps=1e-5, residual=None, S=None, 
 def psattn_layernorm_bwd(S, weight, mean, rstd, dY, dS=None, bias=True, dX=None, dweight=None, dbias=None, workspace=None, stream=None):
     """dX, dweight, dbias (None where `bias` is false) from the forward's S, mean and rstd; dX has dS added to it."""
     torch, lib = _TORCH or _torch(), _LIB or load_library()
-    _check_rows(S, "S")
+    dev = _check_rows(S, "S")
     (n, h), dt, dtype = S.shape, _dtype_code(S), S.dtype
     dX = torch.empty_like(S) if dX is None else dX
     dweight = torch.empty_like(weight) if dweight is None else dweight
@@ -686,7 +686,7 @@ def psattn_layernorm_bwd(S, weight, mean, rstd, dY, dS=None, bias=True, dX=None,
         raise ValueError("dbias is given, but there is no bias")
     if dS is not None:
         tensors.append((dS, "dS", S.shape, dtype))
-    _check_all(S, *tensors)
+    _check_all(dev, *tensors)
     ws = _workspace(workspace, lib.psattn_layernorm_bwd_workspace_bytes(n, h), S, stream)
     st = lib.psattn_layernorm_bwd(dt, n, h, S.data_ptr(), weight.data_ptr(), mean.data_ptr(), rstd.data_ptr(), dY.data_ptr(),
                                   None if dS is None else dS.data_ptr(), dX.data_ptr(), dweight.data_ptr(),
@@ -696,20 +696,20 @@ def psattn_layernorm_bwd(S, weight, mean, rstd, dY, dS=None, bias=True, dX=None,
 
 
 def _ffn_shapes(X, Wg, Wu, Wd, act):
-    _check_rows(X, "X")
+    dev = _check_rows(X, "X")
     if act not in _ACTS:
         raise ValueError("act must be one of %s, got %r" % (sorted(_ACTS), act))
     if Wg.dim() != 2:
         raise ValueError("Wg must have two dimensions, got %d" % Wg.dim())
     (T, h), n, dtype = X.shape, Wg.shape[0], X.dtype
-    return T, h, n, _dtype_code(X), [(Wg, "Wg", (n, h), dtype), (Wu, "Wu", (n, h), dtype), (Wd, "Wd", (h, n), dtype)]
+    return dev, T, h, n, _dtype_code(X), [(Wg, "Wg", (n, h), dtype), (Wu, "Wu", (n, h), dtype), (Wd, "Wd", (h, n), dtype)]
 
 
 def psattn_ffn_fwd(X, Wg, Wu, Wd, act="silu", keep=True, Y=None, kept=None, workspace=None, stream=None):
     """Y, kept = (act(X Wg^T) o (X Wu^T)) Wd^T.  `kept` = (G, U, H), each [T, inner], is what the backward takes; with keep=False
     G and U are not written and None is returned in its place (`kept` may then give H alone, as (None, None, H))."""
     torch, lib = _TORCH or _torch(), _LIB or load_library()
-    T, h, n, dt, tensors = _ffn_shapes(X, Wg, Wu, Wd, act)
+    dev, T, h, n, dt, tensors = _ffn_shapes(X, Wg, Wu, Wd, act)
     G, U, H = kept if kept is not None else (None, None, None)
     if kept is None:
         G, U = (torch.empty((T, n), dtype=X.dtype, device=X.device) for _ in range(2)) if keep else (None, None)
@@ -722,7 +722,7 @@ def psattn_ffn_fwd(X, Wg, Wu, Wd, act="silu", keep=True, Y=None, kept=None, work
         G = U = None
     Y = torch.empty_like(X) if Y is None else Y
     tensors += [(t, name, (T, n), X.dtype) for t, name in ((G, "G"), (U, "U"), (H, "H")) if t is not None]
-    _check_all(X, *tensors, (Y, "Y", X.shape, X.dtype))
+    _check_all(dev, *tensors, (Y, "Y", X.shape, X.dtype))
     ws = _workspace(workspace, lib.psattn_ffn_fwd_workspace_bytes(dt, T, h, n), X, stream)
     st = lib.psattn_ffn_fwd(dt, _ACTS[act], T, h, n, X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(),
                             G.data_ptr() if keep else None, U.data_ptr() if keep else None, H.data_ptr(), Y.data_ptr(), ws.data_ptr(),
@@ -734,7 +734,7 @@ def psattn_ffn_fwd(X, Wg, Wu, Wd, act="silu", keep=True, Y=None, kept=None, work
 def psattn_ffn_bwd(X, Wg, Wu, Wd, kept, dY, act="silu", dX=None, dWg=None, dWu=None, dWd=None, workspace=None, stream=None):
     """dX, dWg, dWu, dWd from the forward's kept (G, U, H)."""
     torch, lib = _TORCH or _torch(), _LIB or load_library()
-    T, h, n, dt, tensors = _ffn_shapes(X, Wg, Wu, Wd, act)
+    dev, T, h, n, dt, tensors = _ffn_shapes(X, Wg, Wu, Wd, act)
     G, U, H = kept
     dX = torch.empty_like(X) if dX is None else dX
     dWg = torch.empty_like(Wg) if dWg is None else dWg
@@ -743,7 +743,7 @@ def psattn_ffn_bwd(X, Wg, Wu, Wd, kept, dY, act="silu", dX=None, dWg=None, dWu=N
     tensors += [(t, name, (T, n), X.dtype) for t, name in ((G, "G"), (U, "U"), (H, "H"))]
     tensors += [(dY, "dY", X.shape, X.dtype), (dX, "dX", X.shape, X.dtype), (dWg, "dWg", (n, h), X.dtype), (dWu, "dWu", (n, h), X.dtype),
                 (dWd, "dWd", (h, n), X.dtype)]
-    _check_all(X, *tensors)
+    _check_all(dev, *tensors)
     ws = _workspace(workspace, lib.psattn_ffn_bwd_workspace_bytes(dt, T, h, n), X, stream)
     st = lib.psattn_ffn_bwd(dt, _ACTS[act], T, h, n, X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(), G.data_ptr(), U.data_ptr(),
                             H.data_ptr(), dY.data_ptr(), dX.data_ptr(), dWg.data_ptr(), dWu.data_ptr(), dWd.data_ptr(), ws.data_ptr(),

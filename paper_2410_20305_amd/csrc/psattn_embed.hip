@@ -39,17 +39,18 @@ __global__ __launch_bounds__(kThreads) void psattn_embed_rows(int n_tokens, int 
     for (int64_t b = blockIdx.x; b < n; b += gridDim.x) {
         const int t0 = static_cast<int>(b / per) * at_once + sub * AT, c = ((static_cast<int>(b % per) << lanes) + l) * V;
         if (c >= hidden) continue;
+        const Place pl = place<WHOLE, E>(c, hidden);
         u32x4 r[AT];
 #pragma unroll
         for (int u = 0; u < AT; ++u) {
             const int id = t0 + u < n_tokens ? ids[t0 + u] : -1;
             r[u] = u32x4{0, 0, 0, 0};
-            if (id >= 0 && id < vocab) r[u] = raw<WHOLE>(W + static_cast<int64_t>(id) * hidden, c, hidden);
+            if (id >= 0 && id < vocab) r[u] = raw<WHOLE>(W + static_cast<int64_t>(id) * hidden, pl, hidden);
         }
 #pragma unroll
         for (int u = 0; u < AT; ++u) {
             float x[V];
-            unpack(r[u], x);
+            unpack(settled<WHOLE>(r[u], pl.down), x);
 #pragma unroll
             for (int j = 0; j < V; ++j) x[j] *= scale;
             if (t0 + u < n_tokens) store<WHOLE>(X + static_cast<int64_t>(t0 + u) * hidden, c, hidden, x);
@@ -214,6 +215,7 @@ __global__ __launch_bounds__(kThreads) void psattn_embed_sum(int n, int vocab, i
     __syncthreads();
     const int c = ((static_cast<int>(blockIdx.x) % per << lanes) + l) * V;
     if (c >= hidden) return;
+    const Place pl = place<WHOLE, E>(c, hidden);
     for (int i = 0; i < m;) {
         const int v = key[i + 1];
         if (v >= vocab) return;  // padding, behind all others
@@ -224,11 +226,11 @@ __global__ __launch_bounds__(kThreads) void psattn_embed_sum(int n, int vocab, i
         for (; j + 8 <= end; j += 8) {
             u32x4 x[8];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) x[u] = raw<WHOLE>(dX + static_cast<int64_t>(tok[j + u]) * hidden, c, hidden);
+            for (int u = 0; u < 8; ++u) x[u] = raw<WHOLE>(dX + static_cast<int64_t>(tok[j + u]) * hidden, pl, hidden);
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
                 float y[V];
-                unpack(x[u], y);
+                unpack(settled<WHOLE>(x[u], pl.down), y);
 #pragma unroll
                 for (int k = 0; k < V; ++k) sum[k] += y[k];
             }

@@ -101,8 +101,8 @@ size_t part_bytes(int32_t dt, Pass pass, bool pkc, int64_t M, int64_t N, int64_t
     return dt == PSATTN_BF16 ? std::max(room(kWhole), room(kOdd)) : room(kFloat);
 }
 
-// joins the parts of a product: the epilogue of psattn_ffn_tiles on sums from memory, V columns to a lane (4 where rows allow it: 221 x
-// 14 336, dG and dU from three parts NOTE).  grid (columns, rows, products)
+// joins the parts of a product: the epilogue of psattn_ffn_tiles on sums from memory, V columns to a lane (4 where rows allow it: dG and dU of
+// 500 x 14 336 44 -> 20 us).  grid (columns, rows, products)
 template <int V, typename E>
 __device__ __forceinline__ void put(E* p, const float (&x)[V]) {
     if constexpr (V == 1) store1(p, x[0]);

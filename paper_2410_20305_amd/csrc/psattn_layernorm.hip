@@ -54,19 +54,26 @@ __global__ __launch_bounds__(kThreads<LANES>) void psattn_ln_fwd(int n_rows, int
     const int row = blockIdx.x * kAt + threadIdx.x / LANES, lane = threadIdx.x % LANES;
     if (row >= n_rows) return;
     const size_t at = static_cast<size_t>(row) * hidden;
+    const int from = lane * V - (WHOLE ? 0 : misalignment(X + at));  // this lane's first column
     float x[PER][V];
     float sum[1] = {0.f};
+    u32x4 xr[PER], rr[RES ? PER : 1];
+    Place pl[PER];
 #pragma unroll
-    for (int p = 0; p < PER; ++p) load<WHOLE>(X + at, (p * LANES + lane) * V, hidden, x[p]);
-    if constexpr (RES) {
-        float r[PER][V];
+    for (int p = 0; p < PER; ++p) {
+        pl[p] = place<WHOLE, E>(from + p * LANES * V, hidden);
+        xr[p] = raw<WHOLE>(X + at, pl[p], hidden);
+        if constexpr (RES) rr[p] = raw<WHOLE>(R + at, pl[p], hidden);
+    }
 #pragma unroll
-        for (int p = 0; p < PER; ++p) load<WHOLE>(R + at, (p * LANES + lane) * V, hidden, r[p]);
+    for (int p = 0; p < PER; ++p) {
+        unpack(settled<WHOLE>(xr[p], pl[p].down), x[p]);
+        if constexpr (RES) {
+            float r[V];
+            unpack(settled<WHOLE>(rr[p], pl[p].down), r);
 #pragma unroll
-        for (int p = 0; p < PER; ++p) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) x[p][j] = hold(x[p][j] + r[p][j], X);
-            store<WHOLE>(S + at, (p * LANES + lane) * V, hidden, x[p]);
+            for (int j = 0; j < V; ++j) x[p][j] = hold(x[p][j] + r[j], X);
+            store<WHOLE>(S + at, from + p * LANES * V, hidden, x[p]);
         }
     }
 #pragma unroll
@@ -78,21 +85,21 @@ __global__ __launch_bounds__(kThreads<LANES>) void psattn_ln_fwd(int n_rows, int
     float sq[1] = {0.f};
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
-        const int c = (p * LANES + lane) * V;
+        const int c = from + p * LANES * V;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             x[p][j] -= mu;
-            if (WHOLE ? c < hidden : c + j < hidden) sq[0] += x[p][j] * x[p][j];
+            if (WHOLE ? c < hidden : c + j >= 0 && c + j < hidden) sq[0] += x[p][j] * x[p][j];
         }
     }
     group_sum<LANES>(sq, sm[1]);
     const float rs = 1.f / sqrtf(sq[0] / hidden + eps);
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
-        const int c = (p * LANES + lane) * V;
+        const int c = from + p * LANES * V;
         float wv[V], bv[V] = {};
-        load<WHOLE>(w, c, hidden, wv);
-        if (b) load<WHOLE>(b, c, hidden, bv);
+        unpack(settled<WHOLE>(raw<WHOLE>(w, pl[p], hidden), pl[p].down), wv);
+        if (b) unpack(settled<WHOLE>(raw<WHOLE>(b, pl[p], hidden), pl[p].down), bv);
 #pragma unroll
         for (int j = 0; j < V; ++j) x[p][j] = x[p][j] * rs * wv[j] + bv[j];
         store<WHOLE>(Y + at, c, hidden, x[p]);
@@ -108,33 +115,39 @@ __global__ __launch_bounds__(kThreads<LANES>) void psattn_ln_fwd(int n_rows, int
 // Rows stay in the registers as they came and are unpacked twice, which leaves room for the next row's loads while one is
 // summed over the lanes (8 334 rows of 4 096 bf16 with dS 105 -> 70 us, 65 536 of 1 024 198 -> 84).
 //   Without SUMS a workgroup has one row, and dw and db are left to psattn_ln_columns: 32 columns to a lane and their sums do not
-// fit beside a row (20 000 rows of 16 384 bf16, sums in registers and in part spilled 665 - 1 650 us, apart NOTE).
+// fit beside a row (20 000 rows of 16 384 bf16, sums in registers and in part spilled 665 - 1 650 us, apart 642).
 template <typename E, int LANES, int PER, bool WHOLE, bool SUMS>
 __global__ __launch_bounds__(kThreads<LANES>) void psattn_ln_bwd(int n_rows, int hidden, const E* S, const E* w, const float* mean, const float* rstd, const E* dY,
                                                                  const E* dS, E* dX, float* part) {
     constexpr int V = kVec<E>, kAt = kThreads<LANES> / LANES;  // rows at a time
     __shared__ float sm[2][32];
-    __shared__ float add[kAt > 1 ? kAt * LANES * V : 1];
+    __shared__ float add[kAt > 1 ? kAt * LANES * PER * V : 1];
     static_assert(SUMS || kAt == 1, "short rows' columns are summed here");
     const int lane = threadIdx.x % LANES, own = threadIdx.x / LANES;
     float dw[PER][V] = {}, db[PER][V] = {};
-    u32x4 wr[PER];
-#pragma unroll
-    for (int p = 0; p < PER; ++p) wr[p] = raw<WHOLE>(w, (p * LANES + lane) * V, hidden);
     u32x4 xr[PER], gr[PER], sr[PER];
     float mu = 0.f, rs = 0.f;
     constexpr bool kAhead = SUMS;
     const int step = gridDim.x * kAt;
     int row = blockIdx.x * kAt + own;
+    // this lane's first column: the same for all its rows, whose misalignment has to be
+    const int from = lane * V - (WHOLE || (step % V != 0 && hidden % V != 0) || row >= n_rows ? 0 : misalignment(S + static_cast<size_t>(row) * hidden));
+    Place pl[PER];
+    u32x4 wr[PER];
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+        pl[p] = place<WHOLE, E>(from + p * LANES * V, hidden);
+        wr[p] = settled<WHOLE>(raw<WHOLE>(w, pl[p], hidden), pl[p].down);
+    }
     auto fetch = [&](int r, u32x4 (&a)[PER], u32x4 (&b)[PER], u32x4 (&c)[PER], float& m, float& q) {
         const size_t at = static_cast<size_t>(r) * hidden;
         m = mean[r];
         q = rstd[r];
 #pragma unroll
         for (int p = 0; p < PER; ++p) {
-            a[p] = raw<WHOLE>(S + at, (p * LANES + lane) * V, hidden);
-            b[p] = raw<WHOLE>(dY + at, (p * LANES + lane) * V, hidden);
-            if (dS) c[p] = raw<WHOLE>(dS + at, (p * LANES + lane) * V, hidden);
+            a[p] = raw<WHOLE>(S + at, pl[p], hidden);
+            b[p] = raw<WHOLE>(dY + at, pl[p], hidden);
+            if (dS) c[p] = raw<WHOLE>(dS + at, pl[p], hidden);
         }
     };
     if (kAhead && row < n_rows) fetch(row, xr, gr, sr, mu, rs);
@@ -146,8 +159,8 @@ __global__ __launch_bounds__(kThreads<LANES>) void psattn_ln_bwd(int n_rows, int
         float s[2] = {0.f, 0.f};
         // behind the row's end dY and w are zeros
         auto unpacked = [&](int p, float (&x)[V], float (&g)[V], float (&wv)[V]) {
-            unpack(xr[p], x);
-            unpack(gr[p], g);
+            unpack(settled<WHOLE>(xr[p], pl[p].down), x);
+            unpack(settled<WHOLE>(gr[p], pl[p].down), g);
             unpack(wr[p], wv);
 #pragma unroll
             for (int j = 0; j < V; ++j) x[j] = (x[j] - mu) * rs;
@@ -174,10 +187,10 @@ __global__ __launch_bounds__(kThreads<LANES>) void psattn_ln_bwd(int n_rows, int
         for (int p = 0; p < PER; ++p) {
             float x[V], g[V], wv[V], o[V] = {};
             unpacked(p, x, g, wv);
-            if (dS) unpack(sr[p], o);
+            if (dS) unpack(settled<WHOLE>(sr[p], pl[p].down), o);
 #pragma unroll
             for (int j = 0; j < V; ++j) o[j] += rs * (g[j] * wv[j] - m1 - x[j] * m2);
-            store<WHOLE>(dX + at, (p * LANES + lane) * V, hidden, o);
+            store<WHOLE>(dX + at, from + p * LANES * V, hidden, o);
         }
         if constexpr (kAhead) {
 #pragma unroll
@@ -189,25 +202,24 @@ __global__ __launch_bounds__(kThreads<LANES>) void psattn_ln_bwd(int n_rows, int
     if constexpr (!SUMS) return;
     float* const mine = part + 2 * static_cast<size_t>(blockIdx.x) * hidden;
     auto out = [&](float* to, const float (&v)[PER][V]) {
+        float* const at = kAt > 1 ? add + own * LANES * PER * V : to;  // rows that share the workgroup: by column, then added up
+        if constexpr (kAt > 1) {
+            __syncthreads();
+        }
 #pragma unroll
-        for (int p = 0; p < PER; ++p) {
-            if constexpr (kAt > 1) {
-                __syncthreads();
+        for (int p = 0; p < PER; ++p)
 #pragma unroll
-                for (int j = 0; j < V; ++j) add[(own * V + j) * LANES + lane] = v[p][j];
-                __syncthreads();
-                for (int i = threadIdx.x; i < LANES * V; i += kThreads<LANES>) {
-                    float t = 0.f;
+            for (int j = 0; j < V; ++j) {
+                const int c = from + p * LANES * V + j;
+                if (c >= 0 && c < hidden) at[c] = v[p][j];
+            }
+        if constexpr (kAt > 1) {
+            __syncthreads();
+            for (int c = threadIdx.x; c < hidden; c += kThreads<LANES>) {
+                float t = 0.f;
 #pragma unroll
-                    for (int o = 0; o < kAt; ++o) t += add[(o * V + i % V) * LANES + i / V];
-                    const int c = p * LANES * V + i;
-                    if (c < hidden) to[c] = t;
-                }
-            } else {
-                const int c = (p * LANES + lane) * V;
-#pragma unroll
-                for (int j = 0; j < V; ++j)
-                    if (c + j < hidden) to[c + j] = v[p][j];
+                for (int o = 0; o < kAt; ++o) t += add[o * LANES * PER * V + c];
+                to[c] = t;
             }
         }
     };
@@ -327,52 +339,54 @@ __global__ __launch_bounds__(1024) void psattn_ln_bwd_wide(int hidden, const E* 
 template <typename E>
 __global__ __launch_bounds__(256) void psattn_ln_columns(int n_rows, int hidden, const E* S, const float* mean, const float* rstd, const E* dY, float* part) {
     constexpr int V = kVec<E>, kAtOnce = 4;
-    const int c = (blockIdx.x * 256 + threadIdx.x) * V;
+    const int step = gridDim.y;
+    const bool same = step % V == 0 || hidden % V == 0;  // all rows of this workgroup start alike
+    const int c = (blockIdx.x * 256 + threadIdx.x) * V - (same ? misalignment(S + static_cast<size_t>(blockIdx.y) * hidden) : 0);
     if (c >= hidden) return;
+    const Place pl = place<false, E>(c, hidden);
     float w[V] = {}, b[V] = {};
     auto add = [&](const u32x4& s, const u32x4& d, float mu, float rs) {
         float x[V], g[V];
-        unpack(s, x);
-        unpack(d, g);
+        unpack(settled<false>(s, pl.down), x);
+        unpack(settled<false>(d, pl.down), g);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             w[j] += g[j] * ((x[j] - mu) * rs);
             b[j] += g[j];
         }
     };
-    const int step = gridDim.y;
     int r = blockIdx.y;
     for (; r + (kAtOnce - 1) * step < n_rows; r += kAtOnce * step) {
         u32x4 s[kAtOnce], d[kAtOnce];
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) {
             const size_t at = static_cast<size_t>(r + u * step) * hidden;
-            s[u] = raw<false>(S + at, c, hidden);
-            d[u] = raw<false>(dY + at, c, hidden);
+            s[u] = raw<false>(S + at, pl, hidden);
+            d[u] = raw<false>(dY + at, pl, hidden);
         }
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) add(s[u], d[u], mean[r + u * step], rstd[r + u * step]);
     }
     for (; r < n_rows; r += step) {
         const size_t at = static_cast<size_t>(r) * hidden;
-        add(raw<false>(S + at, c, hidden), raw<false>(dY + at, c, hidden), mean[r], rstd[r]);
+        add(raw<false>(S + at, pl, hidden), raw<false>(dY + at, pl, hidden), mean[r], rstd[r]);
     }
-    float* const mine = part + 2 * static_cast<size_t>(blockIdx.y) * hidden + c;
+    float* const mine = part + 2 * static_cast<size_t>(blockIdx.y) * hidden;
 #pragma unroll
     for (int j = 0; j < V; ++j)
-        if (c + j < hidden) {
-            mine[j] = w[j];
-            mine[hidden + j] = b[j];
+        if (c + j >= 0 && c + j < hidden) {
+            mine[c + j] = w[j];
+            mine[hidden + c + j] = b[j];
         }
 }
 
 // ---- which kernel.  Rows of up to 32 groups of 16 bytes are sixteen lanes' (of 64, half or more would have nothing to do: 65 536 rows
-// of 256 bf16 forward NOTE), of up to 128 a wave's, wider ones a workgroup's.
+// of 256 bf16 with R forward 40 us, 27 with sixteen), of up to 128 a wave's, wider ones a workgroup's.
 template <typename E, bool BWD, typename F>
-bool sized(int hidden, F&& f) {
+bool sized(int hidden, bool all, F&& f) {
     using std::integral_constant;
     auto go = [&](auto lanes, auto per) { return f(lanes, per), true; };
-    const int64_t g = (static_cast<int64_t>(hidden) + kVec<E> - 1) / kVec<E>;
+    const int64_t g = (static_cast<int64_t>(hidden) + kVec<E> - 1) / kVec<E> + (all ? 0 : 1);  // rows that start off a boundary reach into one more
     constexpr int kWidest = 4 * 8 / kVec<E>;  // groups of a lane: 32 columns
     using One = integral_constant<int, 1>;
     using Two = integral_constant<int, 2>;
@@ -382,6 +396,7 @@ bool sized(int hidden, F&& f) {
     if (g <= 128) return go(integral_constant<int, 64>{}, Two{});
     if (g <= 256) return go(integral_constant<int, 256>{}, One{});
     if (g <= 512) return go(integral_constant<int, 256>{}, Two{});
+    if (g <= 768 && (all || !BWD)) return go(integral_constant<int, 256>{}, integral_constant<int, 3>{});  // ... at 1.7 TB/s instead of 2.1 where rows start anywhere
     if (g <= 1024) return go(integral_constant<int, 512>{}, Two{});
     if constexpr (BWD) {
         if (g <= 2048) return go(integral_constant<int, 512>{}, integral_constant<int, 4>{});
@@ -405,7 +420,7 @@ void fwd(int32_t n_rows, int32_t hidden, float eps, const void* X_, const void* 
     const E *X = static_cast<const E*>(X_), *R = static_cast<const E*>(R_), *w = static_cast<const E*>(w_), *b = static_cast<const E*>(b_);
     E *S = static_cast<E*>(S_), *Y = static_cast<E*>(Y_);
     const bool all = whole<E>(hidden, {X, R, w, b, S, Y});
-    const bool done = sized<E, false>(hidden, [&](auto lanes, auto per) {
+    const bool done = sized<E, false>(hidden, all, [&](auto lanes, auto per) {
         constexpr int L = decltype(lanes)::value, PER = decltype(per)::value, kAt = kThreads<L> / L;
         const int grid = (n_rows + kAt - 1) / kAt;
         auto go = [&](auto kernel) { kernel<<<grid, kThreads<L>, 0, s>>>(n_rows, hidden, eps, X, R, w, b, S, Y, mean, rstd); };
@@ -424,18 +439,19 @@ void bwd(int32_t n_rows, int32_t hidden, const void* S_, const void* w_, const f
     if (n_rows > 0) {
         const bool all = whole<E>(hidden, {S, w, dY, dS, dX});
         bool sums = false;
-        const bool done = sized<E, true>(hidden, [&](auto lanes, auto per) {
+        const bool done = sized<E, true>(hidden, all, [&](auto lanes, auto per) {
             constexpr int L = decltype(lanes)::value, PER = decltype(per)::value, kAt = kThreads<L> / L;
             constexpr bool SUMS = PER * kVec<E> < 32;  // up to 1 024 groups
             if (SUMS) np = std::min(np, (n_rows + kAt - 1) / kAt);
+            if (np > 8) np -= np % 8;  // a workgroup's rows start alike
             sums = SUMS;
             auto go = [&](auto kernel) { kernel<<<SUMS ? np : n_rows, kThreads<L>, 0, s>>>(n_rows, hidden, S, w, mean, rstd, dY, dS, dX, part); };
             all ? go(psattn_ln_bwd<E, L, PER, true, SUMS>) : go(psattn_ln_bwd<E, L, PER, false, SUMS>);
         });
         if (!done) psattn_ln_bwd_wide<E><<<n_rows, 1024, 0, s>>>(hidden, S, w, mean, rstd, dY, dS, dX);
         if (!sums) {
-            const int cols = (hidden + 256 * kVec<E> - 1) / (256 * kVec<E>);
-            np = std::min(np, std::max(1, 2048 / cols));  // eight workgroups to a CU
+            const int cols = (hidden + kVec<E> - 1 + 256 * kVec<E> - 1) / (256 * kVec<E>);
+            np = std::min(np, std::max(8, 2048 / cols / 8 * 8));  // eight workgroups to a CU
             psattn_ln_columns<E><<<dim3(cols, np), 256, 0, s>>>(n_rows, hidden, S, mean, rstd, dY, part);
         }
     }
