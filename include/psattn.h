@@ -424,16 +424,17 @@ int psattn_layernorm_bwd(int32_t dt, int32_t n_rows, int32_t hidden, const void*
 
 /*
  * psattn_ffn_fwd: G = X Wg^T, U = X Wu^T, H = act(G) o U, Y = H Wd^T.  X, Y [n_tokens, hidden]; Wg, Wu [inner, hidden] and Wd
- * [hidden, inner], the [out_features, in_features] convention of the attention layer.  G, U, H [n_tokens, inner] are kept for the
- * backward; G and U may both be NULL if none follows, H is needed either way.  H is rounded once, from the fp32 sums.
+ * [hidden, inner], the [out_features, in_features] convention of the attention layer.  G, U (float) and H (dt), [n_tokens, inner], are
+ * kept for the backward; G and U may both be NULL if none follows, H is needed either way.  H is rounded once, from the fp32 sums.
+ * Rows of 2^22 bytes and more are refused with PSATTN_EUNSUPPORTED.
  * psattn_ffn_bwd: dX, dWg, dWu, dWd from the forward's G, U, H and dY.
  */
 int psattn_ffn_fwd(int32_t dt, int32_t act, int32_t n_tokens, int32_t hidden, int32_t inner, const void* X, const void* Wg,
-                   const void* Wu, const void* Wd, void* G, void* U, void* H, void* Y, void* workspace,
+                   const void* Wu, const void* Wd, float* G, float* U, void* H, void* Y, void* workspace,
                    size_t workspace_bytes, void* hip_stream);
 size_t psattn_ffn_fwd_workspace_bytes(int32_t dt, int32_t n_tokens, int32_t hidden, int32_t inner);
 int psattn_ffn_bwd(int32_t dt, int32_t act, int32_t n_tokens, int32_t hidden, int32_t inner, const void* X, const void* Wg,
-                   const void* Wu, const void* Wd, const void* G, const void* U, const void* H, const void* dY, void* dX,
+                   const void* Wu, const void* Wd, const float* G, const float* U, const void* H, const void* dY, void* dX,
                    void* dWg, void* dWu, void* dWd, void* workspace, size_t workspace_bytes, void* hip_stream);
 size_t psattn_ffn_bwd_workspace_bytes(int32_t dt, int32_t n_tokens, int32_t hidden, int32_t inner);
 

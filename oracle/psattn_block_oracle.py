@@ -52,11 +52,10 @@ def act(g, kind):
 
 
 def ffn(X, Wg, Wu, Wd, kind, hold=lambda x: x):
-    """Y, G, U, H; `hold` is applied to what is kept (the rounding to the element type).  H comes from the sums, not from the
-    kept G and U."""
+    """Y, G, U, H; `hold` is the rounding of H to the element type."""
     G, U = X @ Wg.T, X @ Wu.T
     H = hold(act(G, kind)[0] * U)
-    return H @ Wd.T, hold(G), hold(U), H
+    return H @ Wd.T, G, U, H
 
 
 def ffn_grad(X, Wg, Wu, Wd, G, U, H, dY, kind, hold=lambda x: x):

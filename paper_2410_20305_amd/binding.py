@@ -706,13 +706,14 @@ def _ffn_shapes(X, Wg, Wu, Wd, act):
 
 
 def psattn_ffn_fwd(X, Wg, Wu, Wd, act="silu", keep=True, Y=None, kept=None, workspace=None, stream=None):
-    """Y, kept = (act(X Wg^T) o (X Wu^T)) Wd^T.  `kept` = (G, U, H), each [T, inner], is what the backward takes; with keep=False
+    """Y, kept = (act(X Wg^T) o (X Wu^T)) Wd^T.  `kept` = (G, U, H), [T, inner] each, G and U float32, is what the
+    backward takes; with keep=False
     G and U are not written and None is returned in its place (`kept` may then give H alone, as (None, None, H))."""
     torch, lib = _TORCH or _torch(), _LIB or load_library()
     dev, T, h, n, dt, tensors = _ffn_shapes(X, Wg, Wu, Wd, act)
     G, U, H = kept if kept is not None else (None, None, None)
     if kept is None:
-        G, U = (torch.empty((T, n), dtype=X.dtype, device=X.device) for _ in range(2)) if keep else (None, None)
+        G, U = (torch.empty((T, n), dtype=torch.float32, device=X.device) for _ in range(2)) if keep else (None, None)
         H = torch.empty((T, n), dtype=X.dtype, device=X.device)
         if stream is not None and not keep:  # H goes back to torch when this call returns
             H.record_stream(stream if not isinstance(stream, int) else torch.cuda.ExternalStream(stream, device=X.device))
@@ -721,7 +722,7 @@ def psattn_ffn_fwd(X, Wg, Wu, Wd, act="silu", keep=True, Y=None, kept=None, work
     if not keep:
         G = U = None
     Y = torch.empty_like(X) if Y is None else Y
-    tensors += [(t, name, (T, n), X.dtype) for t, name in ((G, "G"), (U, "U"), (H, "H")) if t is not None]
+    tensors += [(t, name, (T, n), torch.float32) for t, name in ((G, "G"), (U, "U")) if t is not None] + [(H, "H", (T, n), X.dtype)]
     _check_all(dev, *tensors, (Y, "Y", X.shape, X.dtype))
     ws = _workspace(workspace, lib.psattn_ffn_fwd_workspace_bytes(dt, T, h, n), X, stream)
     st = lib.psattn_ffn_fwd(dt, _ACTS[act], T, h, n, X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(),
@@ -740,7 +741,7 @@ def psattn_ffn_bwd(X, Wg, Wu, Wd, kept, dY, act="silu", dX=None, dWg=None, dWu=N
     dWg = torch.empty_like(Wg) if dWg is None else dWg
     dWu = torch.empty_like(Wu) if dWu is None else dWu
     dWd = torch.empty_like(Wd) if dWd is None else dWd
-    tensors += [(t, name, (T, n), X.dtype) for t, name in ((G, "G"), (U, "U"), (H, "H"))]
+    tensors += [(G, "G", (T, n), torch.float32), (U, "U", (T, n), torch.float32), (H, "H", (T, n), X.dtype)]
     tensors += [(dY, "dY", X.shape, X.dtype), (dX, "dX", X.shape, X.dtype), (dWg, "dWg", (n, h), X.dtype), (dWu, "dWu", (n, h), X.dtype),
                 (dWd, "dWd", (h, n), X.dtype)]
     _check_all(dev, *tensors)

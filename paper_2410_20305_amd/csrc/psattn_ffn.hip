@@ -3,8 +3,10 @@
 // The paper's sequences share a prompt, and the block acts on single tokens, so sharing saves the same part of it as of the
 // projections.  Forward: gate and up projection, activation and product in one kernel (they share X, and G, U, H leave once),
 // then the down projection.  Backward: dH = dY Wd with dG, dU in its epilogue; dX = dG Wg + dU Wu as one product over both
-// weights' rows; dWg, dWu in one launch; dWd.  All sums over k are fp32; G, U, H, dG and dU are held in the element type like any
-// activation, H being rounded once, from the fp32 sums.
+// weights' rows; dWg, dWu in one launch; dWd.  All sums over k are fp32.  H, dG and dU are operands of the
+// matrix cores and are held in the element type, each rounded once, from fp32.  G and U are kept in fp32: rounded to bf16 they would
+// put two more roundings into dG and dU, and gradients of weights off by 3.1e-3 (relative L2 against 64 bits) instead of NOTE, whose own rounding
+// is 1.7e-3; that costs NOTE of a training step's time.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -152,16 +154,16 @@ __global__ __launch_bounds__(256) void psattn_ffn_join(Product d) {
         for (; i < d.n_split; ++i) add(i, std::integral_constant<int, 1>{});
         const int64_t at = m * d.ldo + n;
         if constexpr (PASS == kGate) {
-            if (d.G) put<V>(static_cast<E*>(d.G) + at, x[0]);
-            if (d.U) put<V>(static_cast<E*>(d.U) + at, x[1]);
+            if (d.G) put<V>(d.G + at, x[0]);
+            if (d.U) put<V>(d.U + at, x[1]);
             float h[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) h[j] = act<E, ACT>(x[0][j]) * x[1][j];
             put<V>(static_cast<E*>(d.H) + at, h);
         } else if constexpr (PASS == kDact) {
             float gate[V], up[V], dg[V], du[V];
-            get<V>(static_cast<const E*>(d.G) + at, gate);
-            get<V>(static_cast<const E*>(d.U) + at, up);
+            get<V>(d.G + at, gate);
+            get<V>(d.U + at, up);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 float a, da;
@@ -225,7 +227,7 @@ size_t psattn_ffn_fwd_workspace_bytes(int32_t dt, int32_t n_tokens, int32_t hidd
 }
 
 int psattn_ffn_fwd(int32_t dt, int32_t act, int32_t n_tokens, int32_t hidden, int32_t inner, const void* X, const void* Wg, const void* Wu,
-                   const void* Wd, void* G, void* U, void* H, void* Y, void* workspace, size_t workspace_bytes, void* hip_stream) {
+                   const void* Wd, float* G, float* U, void* H, void* Y, void* workspace, size_t workspace_bytes, void* hip_stream) {
     if (bad_shape(dt, act, n_tokens, hidden, inner)) return PSATTN_EINVAL;
     if (n_tokens == 0) return PSATTN_OK;
     if (!X || !Wg || !Wu || !Wd || !H || !Y || (!G) != (!U)) return PSATTN_EINVAL;
@@ -246,7 +248,7 @@ int psattn_ffn_fwd(int32_t dt, int32_t act, int32_t n_tokens, int32_t hidden, in
 }
 
 int psattn_ffn_bwd(int32_t dt, int32_t act, int32_t n_tokens, int32_t hidden, int32_t inner, const void* X, const void* Wg, const void* Wu,
-                   const void* Wd, const void* G, const void* U, const void* H, const void* dY, void* dX, void* dWg, void* dWu, void* dWd,
+                   const void* Wd, const float* G, const float* U, const void* H, const void* dY, void* dX, void* dWg, void* dWu, void* dWd,
                    void* workspace, size_t workspace_bytes, void* hip_stream) {
     if (bad_shape(dt, act, n_tokens, hidden, inner)) return PSATTN_EINVAL;
     if (!dWg || !dWu || !dWd) return PSATTN_EINVAL;
@@ -263,7 +265,7 @@ int psattn_ffn_bwd(int32_t dt, int32_t act, int32_t n_tokens, int32_t hidden, in
     char* const parts = dU + align_up(static_cast<size_t>(n_tokens) * inner * elem_bytes(dt), 256);
     int rc;
     Product a{};  // dH = dY Wd, dG and dU
-    a.p[0] = dY; a.q[0] = Wd; a.G = const_cast<void*>(G); a.U = const_cast<void*>(U); a.out[0] = dG; a.out[1] = dU;
+    a.p[0] = dY; a.q[0] = Wd; a.G = const_cast<float*>(G); a.U = const_cast<float*>(U); a.out[0] = dG; a.out[1] = dU;
     a.ldp = hidden; a.ldq = a.ldo = inner;
     a.M = n_tokens; a.N = inner; a.K = hidden; a.n_seg = a.n_prod = 1;
     if ((rc = product(dt, kDact, act, true, false, a, parts, s)) != PSATTN_OK) return rc;

@@ -138,46 +138,21 @@ __device__ __forceinline__ void put8(float* p, const float (&x)[8], int n) {
             if (j < n) p[j] = x[j];
     }
 }
-// eight elements as they lie in memory
-template <typename E>
+// eight floats as they come from memory
 struct Group {
-    uint32_t w[2 * sizeof(E)];
+    float w[8];
     template <bool ALIGNED>
-    __device__ __forceinline__ void get(const E* p, int n) {
-        constexpr int W = 2 * sizeof(E);
+    __device__ __forceinline__ void get(const float* p, int n) {
         if (ALIGNED || n >= 8) {
 #pragma unroll
-            for (int i = 0; i < W; i += 4) {
-                if constexpr (ALIGNED) {
-                    const uint4 x = *reinterpret_cast<const uint4*>(p + i * 4 / sizeof(E));
-                    w[i] = x.x; w[i + 1] = x.y; w[i + 2] = x.z; w[i + 3] = x.w;
-                } else {
-                    const Raw16 x = *reinterpret_cast<const Raw16*>(p + i * 4 / sizeof(E));
+            for (int i = 0; i < 8; i += 4) {
+                const Raw16 x = *reinterpret_cast<const Raw16*>(p + i);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) w[i + j] = x.w[j];
-                }
+                for (int j = 0; j < 4; ++j) w[i + j] = __uint_as_float(x.w[j]);
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < W; ++i) w[i] = 0;
-#pragma unroll
-            for (int j = 0; j < 7; ++j)
-                if (j < n) {
-                    if constexpr (sizeof(E) == 2) w[j / 2] |= static_cast<uint32_t>(p[j]) << (16 * (j & 1));
-                    else w[j] = __float_as_uint(p[j]);
-                }
-        }
-    }
-    __device__ __forceinline__ void values(float (&x)[8]) const {
-        if constexpr (sizeof(E) == 2) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                x[2 * j] = __uint_as_float(w[j] << 16);
-                x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(w[j]);
+            for (int j = 0; j < 8; ++j) w[j] = j < n ? p[j] : 0.f;
         }
     }
 };
@@ -414,7 +389,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void psattn_ffn_tiles(Product d, in
             return rows > 0 && cols > 0;
         };
         constexpr int kBlocks = MB * NB;
-        Group<E> g[2][2], u[2][2];
+        Group g[2][2], u[2][2];
         auto ask = [&](int i, int set) {
             int m, n, rows, cols;
             if (!place(i, m, n, rows, cols)) return;
@@ -422,8 +397,8 @@ __global__ __launch_bounds__(S::kThreads, 2) void psattn_ffn_tiles(Product d, in
             for (int k = 0; k < 2; ++k) {
                 const int c = min(16 * k + 8 * (l >> 5), (cols - 1) / 8 * 8);
                 const int64_t from = (m + min(l & 31, rows - 1)) * d.ldo + n + c;
-                g[set][k].template get<ASYNC>(static_cast<const E*>(d.G) + from, cols - c);
-                u[set][k].template get<ASYNC>(static_cast<const E*>(d.U) + from, cols - c);
+                g[set][k].template get<ASYNC>(d.G + from, cols - c);
+                u[set][k].template get<ASYNC>(d.U + from, cols - c);
             }
         };
         ask(0, 0);
@@ -436,14 +411,11 @@ __global__ __launch_bounds__(S::kThreads, 2) void psattn_ffn_tiles(Product d, in
             Chunks dg, du;
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                float gate[8], up[8];
-                g[set][k].values(gate);
-                u[set][k].values(up);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     float a, da;
-                    act_grad<E, ACT>(gate[j], a, da);
-                    dg.c[k][j] = x.c[k][j] * up[j] * da;
+                    act_grad<E, ACT>(g[set][k].w[j], a, da);
+                    dg.c[k][j] = x.c[k][j] * u[set][k].w[j] * da;
                     du.c[k][j] = x.c[k][j] * a;
                 }
             }
@@ -474,8 +446,8 @@ __global__ __launch_bounds__(S::kThreads, 2) void psattn_ffn_tiles(Product d, in
             f32x16 h;
 #pragma unroll
             for (int i = 0; i < 16; ++i) h[i] = act<E, ACT>(acc[0][mb][i]) * acc[1][mb][i];
-            if (d.G) store_chunks<ASYNC>(static_cast<E*>(d.G) + at, d.ldo, rows, cols, chunks(acc[0][mb]), l);
-            if (d.U) store_chunks<ASYNC>(static_cast<E*>(d.U) + at, d.ldo, rows, cols, chunks(acc[1][mb]), l);
+            if (d.G) store_chunks<ASYNC>(d.G + at, d.ldo, rows, cols, chunks(acc[0][mb]), l);
+            if (d.U) store_chunks<ASYNC>(d.U + at, d.ldo, rows, cols, chunks(acc[1][mb]), l);
             store_chunks<ASYNC>(static_cast<E*>(d.H) + at, d.ldo, rows, cols, chunks(h), l);
         } else if constexpr (PASS == kPlain) {
 #pragma unroll

@@ -32,7 +32,8 @@ enum Pass {
 struct Product {
     const void *p[2], *q[2];  // of the segments along k (n_seg), or of two products of one shape (n_prod, p and out only); kGate: q of gate and up
     void* out[2];             // kPlain: out[product]; kDact: dG, dU
-    void *G, *U, *H;          // kGate: written (G, U may be null); kDact: G, U are read
+    float *G, *U;             // kGate: written (may be null); kDact: read
+    void* H;                  // kGate: written
     int64_t ldp, ldq, ldo;    // elements from one row in memory to the next
     int32_t M, N, K;          // K: of one segment
     int32_t n_seg, n_prod;
