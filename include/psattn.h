@@ -400,6 +400,7 @@ int psattn_dpo_loss(int32_t n_pairs, float beta, const float* logp_policy, const
  * id outside [0, vocab) (padding) gives a row of zeros.
  * psattn_embed_bwd: dW[v, :] = scale * sum of dX[t, :] over the tokens with id v, taken in order of the tokens; dW
  * [vocab, hidden] is written as a whole, zeros included.  Ids outside [0, vocab) give nothing, and their rows of dX are not read.
+ * PSATTN_EUNSUPPORTED: more than 2^24 tokens, hidden over 2^23, or sizes whose grids would have 2^31 threads.
  */
 int psattn_embed_fwd(int32_t dt, int32_t n_tokens, int32_t vocab, int32_t hidden, float scale, const int32_t* token_ids,
                      const void* W, void* X, void* hip_stream);
@@ -413,7 +414,7 @@ int psattn_embed_bwd(int32_t dt, int32_t n_tokens, int32_t vocab, int32_t hidden
  * centred values.  weight, bias: [hidden] of dt; bias may be NULL.  mean, rstd: device float [n_rows], for the backward.
  * psattn_layernorm_bwd: from the forward's S (X where there was no R), mean and rstd: dX = the gradient with respect to S, to which
  * dS is added where it is not NULL (what reaches S by the residual stream); it is that of X and of R.  dweight, dbias [hidden]
- * of dt; dbias may be NULL.
+ * of dt; dbias may be NULL.  PSATTN_EUNSUPPORTED: 2^21 rows and more, or hidden over 2^24.
  */
 int psattn_layernorm_fwd(int32_t dt, int32_t n_rows, int32_t hidden, float eps, const void* X, const void* R,
                          const void* weight, const void* bias, void* S, void* Y, float* mean, float* rstd, void* hip_stream);
@@ -426,7 +427,7 @@ int psattn_layernorm_bwd(int32_t dt, int32_t n_rows, int32_t hidden, const void*
  * psattn_ffn_fwd: G = X Wg^T, U = X Wu^T, H = act(G) o U, Y = H Wd^T.  X, Y [n_tokens, hidden]; Wg, Wu [inner, hidden] and Wd
  * [hidden, inner], the [out_features, in_features] convention of the attention layer.  G, U (float) and H (dt), [n_tokens, inner], are
  * kept for the backward; G and U may both be NULL if none follows, H is needed either way.  H is rounded once, from the fp32 sums.
- * Rows of 2^22 bytes and more are refused with PSATTN_EUNSUPPORTED.
+ * Rows of 2^23 bytes and more are refused with PSATTN_EUNSUPPORTED.
  * psattn_ffn_bwd: dX, dWg, dWu, dWd from the forward's G, U, H and dY.
  */
 int psattn_ffn_fwd(int32_t dt, int32_t act, int32_t n_tokens, int32_t hidden, int32_t inner, const void* X, const void* Wg,

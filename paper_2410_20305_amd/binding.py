@@ -585,6 +585,8 @@ def _check_rows(t, name):
     """Index of the device that a call runs on: that of the tensor from which it takes its sizes."""
     if t.dim() != 2:
         raise ValueError("%s must have two dimensions, got %d" % (name, t.dim()))
+    if max(t.shape) >= 1 << 31:
+        raise ValueError("%s has shape %s: sizes are 32-bit" % (name, tuple(t.shape)))
     _check_tensor(t, name, t.shape, None)
     dev = t.get_device()
     if dev != (_TORCH or _torch())._C._cuda_getDevice():
@@ -593,11 +595,12 @@ def _check_rows(t, name):
 
 
 def _check_all(dev, *tensors):
-    """(tensor, name, shape, dtype) each, on device `dev`."""
+    """(tensor, name, shape, dtype) each, on device `dev`.  None: an output that the call makes itself."""
     for t, name, shape, dtype in tensors:
+        if t is None or (t.get_device() == dev and t.is_contiguous() and t.shape == shape and t.dtype == dtype):
+            continue
         _check_tensor(t, name, shape, dtype)
-        if t.get_device() != dev:
-            raise ValueError("%s is on %s, not on cuda:%d" % (name, t.device, dev))
+        raise ValueError("%s is on %s, not on cuda:%d" % (name, t.device, dev))
 
 
 def _workspace(given, need, like, stream):
@@ -621,8 +624,8 @@ def psattn_embed_fwd(token_ids, W, scale=1.0, X=None, stream=None):
     dev = _check_rows(W, "W")
     (V, h), T = W.shape, token_ids.numel()
     dt = _dtype_code(W)
-    X = torch.empty((T, h), dtype=W.dtype, device=W.device) if X is None else X
     _check_all(dev, (token_ids, "token_ids", (T,), torch.int32), (X, "X", (T, h), W.dtype))
+    X = torch.empty((T, h), dtype=W.dtype, device=W.device) if X is None else X
     st = lib.psattn_embed_fwd(dt, T, V, h, float(scale), token_ids.data_ptr(), W.data_ptr(), X.data_ptr(), _stream_ptr(stream))
     _check(st, "psattn_embed_fwd")
     return X
@@ -634,10 +637,10 @@ def psattn_embed_bwd(token_ids, dX, vocab, scale=1.0, dW=None, workspace=None, s
     dev = _check_rows(dX, "dX")
     (T, h), vocab = dX.shape, int(vocab)
     dt = _dtype_code(dX)
-    if vocab <= 0:
-        raise ValueError("vocab must be positive, got %d" % vocab)
-    dW = torch.empty((vocab, h), dtype=dX.dtype, device=dX.device) if dW is None else dW
+    if not 0 < vocab < 1 << 31:
+        raise ValueError("vocab must be a positive 32-bit number, got %d" % vocab)
     _check_all(dev, (token_ids, "token_ids", (T,), torch.int32), (dW, "dW", (vocab, h), dX.dtype))
+    dW = torch.empty((vocab, h), dtype=dX.dtype, device=dX.device) if dW is None else dW
     ws = _workspace(workspace, lib.psattn_embed_bwd_workspace_bytes(dt, T, vocab, h), dX, stream)
     st = lib.psattn_embed_bwd(dt, T, vocab, h, float(scale), token_ids.data_ptr(), dX.data_ptr(), dW.data_ptr(), ws.data_ptr(),
                               ws.numel() * ws.element_size(), _stream_ptr(stream))
@@ -649,20 +652,17 @@ def psattn_layernorm_fwd(X, weight, bias=None, eps=1e-5, residual=None, S=None, 
     """Y, S, mean, rstd = layer norm of the rows of S = X + residual (S is X itself without one)."""
     torch, lib = _TORCH or _torch(), _LIB or load_library()
     dev = _check_rows(X, "X")
-    (n, h), dt, dtype = X.shape, _dtype_code(X), X.dtype
-    tensors = [(weight, "weight", (h,), dtype)]
-    if bias is not None:
-        tensors.append((bias, "bias", (h,), dtype))
-    if residual is not None:
-        S = torch.empty_like(X) if S is None else S
-        tensors += [(residual, "residual", X.shape, dtype), (S, "S", X.shape, dtype)]
-    elif S is not None:
+    shape, dt, dtype, f32 = X.shape, _dtype_code(X), X.dtype, torch.float32
+    n, h = shape
+    if S is not None and residual is None:
         raise ValueError("S is an output of the residual sum: without a residual it is X")
+    _check_all(dev, (weight, "weight", (h,), dtype), (bias, "bias", (h,), dtype), (residual, "residual", shape, dtype), (S, "S", shape, dtype),
+               (Y, "Y", shape, dtype), (mean, "mean", (n,), f32), (rstd, "rstd", (n,), f32))
+    if residual is not None and S is None:
+        S = torch.empty_like(X)
     Y = torch.empty_like(X) if Y is None else Y
-    mean = torch.empty(n, dtype=torch.float32, device=X.device) if mean is None else mean
-    rstd = torch.empty(n, dtype=torch.float32, device=X.device) if rstd is None else rstd
-    tensors += [(Y, "Y", X.shape, dtype), (mean, "mean", (n,), torch.float32), (rstd, "rstd", (n,), torch.float32)]
-    _check_all(dev, *tensors)
+    mean = torch.empty(n, dtype=f32, device=X.device) if mean is None else mean
+    rstd = torch.empty(n, dtype=f32, device=X.device) if rstd is None else rstd
     st = lib.psattn_layernorm_fwd(dt, n, h, float(eps), X.data_ptr(), None if residual is None else residual.data_ptr(), weight.data_ptr(),
                                   None if bias is None else bias.data_ptr(), None if residual is None else S.data_ptr(), Y.data_ptr(),
                                   mean.data_ptr(), rstd.data_ptr(), _stream_ptr(stream))
@@ -674,19 +674,19 @@ def psattn_layernorm_bwd(S, weight, mean, rstd, dY, dS=None, bias=True, dX=None,
     """dX, dweight, dbias (None where `bias` is false) from the forward's S, mean and rstd; dX has dS added to it."""
     torch, lib = _TORCH or _torch(), _LIB or load_library()
     dev = _check_rows(S, "S")
-    (n, h), dt, dtype = S.shape, _dtype_code(S), S.dtype
+    shape, dt, dtype, f32 = S.shape, _dtype_code(S), S.dtype, torch.float32
+    n, h = shape
+    if dbias is not None and not bias:
+        raise ValueError("dbias is given, but there is no bias")
+    for t, name in ((weight, "weight"), (mean, "mean"), (rstd, "rstd"), (dY, "dY")):
+        if t is None:
+            raise ValueError("%s is missing" % name)
+    _check_all(dev, (weight, "weight", (h,), dtype), (mean, "mean", (n,), f32), (rstd, "rstd", (n,), f32), (dY, "dY", shape, dtype),
+               (dS, "dS", shape, dtype), (dX, "dX", shape, dtype), (dweight, "dweight", (h,), dtype), (dbias, "dbias", (h,), dtype))
     dX = torch.empty_like(S) if dX is None else dX
     dweight = torch.empty_like(weight) if dweight is None else dweight
-    tensors = [(weight, "weight", (h,), dtype), (mean, "mean", (n,), torch.float32), (rstd, "rstd", (n,), torch.float32),
-               (dY, "dY", S.shape, dtype), (dX, "dX", S.shape, dtype), (dweight, "dweight", (h,), dtype)]
-    if bias:
-        dbias = torch.empty_like(weight) if dbias is None else dbias
-        tensors.append((dbias, "dbias", (h,), dtype))
-    elif dbias is not None:
-        raise ValueError("dbias is given, but there is no bias")
-    if dS is not None:
-        tensors.append((dS, "dS", S.shape, dtype))
-    _check_all(dev, *tensors)
+    if bias and dbias is None:
+        dbias = torch.empty_like(weight)
     ws = _workspace(workspace, lib.psattn_layernorm_bwd_workspace_bytes(n, h), S, stream)
     st = lib.psattn_layernorm_bwd(dt, n, h, S.data_ptr(), weight.data_ptr(), mean.data_ptr(), rstd.data_ptr(), dY.data_ptr(),
                                   None if dS is None else dS.data_ptr(), dX.data_ptr(), dweight.data_ptr(),
@@ -701,14 +701,15 @@ def _ffn_shapes(X, Wg, Wu, Wd, act):
         raise ValueError("act must be one of %s, got %r" % (sorted(_ACTS), act))
     if Wg.dim() != 2:
         raise ValueError("Wg must have two dimensions, got %d" % Wg.dim())
+    if Wu is None or Wd is None:
+        raise ValueError("Wu and Wd are needed")
     (T, h), n, dtype = X.shape, Wg.shape[0], X.dtype
     return dev, T, h, n, _dtype_code(X), [(Wg, "Wg", (n, h), dtype), (Wu, "Wu", (n, h), dtype), (Wd, "Wd", (h, n), dtype)]
 
 
 def psattn_ffn_fwd(X, Wg, Wu, Wd, act="silu", keep=True, Y=None, kept=None, workspace=None, stream=None):
-    """Y, kept = (act(X Wg^T) o (X Wu^T)) Wd^T.  `kept` = (G, U, H), [T, inner] each, G and U float32, is what the
-    backward takes; with keep=False
-    G and U are not written and None is returned in its place (`kept` may then give H alone, as (None, None, H))."""
+    """Y, kept = (act(X Wg^T) o (X Wu^T)) Wd^T.  `kept` = (G, U, H), [T, inner] each, G and U float32, is what the backward takes;
+    with keep=False G and U are not written and None is returned in its place (`kept` may then give H alone, as (None, None, H))."""
     torch, lib = _TORCH or _torch(), _LIB or load_library()
     dev, T, h, n, dt, tensors = _ffn_shapes(X, Wg, Wu, Wd, act)
     G, U, H = kept if kept is not None else (None, None, None)
@@ -721,9 +722,10 @@ def psattn_ffn_fwd(X, Wg, Wu, Wd, act="silu", keep=True, Y=None, kept=None, work
         raise ValueError("kept must hold G, U and H, or with keep=False H alone")
     if not keep:
         G = U = None
-    Y = torch.empty_like(X) if Y is None else Y
-    tensors += [(t, name, (T, n), torch.float32) for t, name in ((G, "G"), (U, "U")) if t is not None] + [(H, "H", (T, n), X.dtype)]
+    if kept is not None:
+        tensors += [(G, "G", (T, n), torch.float32), (U, "U", (T, n), torch.float32), (H, "H", (T, n), X.dtype)]
     _check_all(dev, *tensors, (Y, "Y", X.shape, X.dtype))
+    Y = torch.empty_like(X) if Y is None else Y
     ws = _workspace(workspace, lib.psattn_ffn_fwd_workspace_bytes(dt, T, h, n), X, stream)
     st = lib.psattn_ffn_fwd(dt, _ACTS[act], T, h, n, X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(),
                             G.data_ptr() if keep else None, U.data_ptr() if keep else None, H.data_ptr(), Y.data_ptr(), ws.data_ptr(),
@@ -737,14 +739,14 @@ def psattn_ffn_bwd(X, Wg, Wu, Wd, kept, dY, act="silu", dX=None, dWg=None, dWu=N
     torch, lib = _TORCH or _torch(), _LIB or load_library()
     dev, T, h, n, dt, tensors = _ffn_shapes(X, Wg, Wu, Wd, act)
     G, U, H = kept
+    if any(t is None for t in (G, U, H, dY)):
+        raise ValueError("kept G, U, H and dY are needed")
+    _check_all(dev, *tensors, (G, "G", (T, n), torch.float32), (U, "U", (T, n), torch.float32), (H, "H", (T, n), X.dtype), (dY, "dY", X.shape, X.dtype),
+               (dX, "dX", X.shape, X.dtype), (dWg, "dWg", (n, h), X.dtype), (dWu, "dWu", (n, h), X.dtype), (dWd, "dWd", (h, n), X.dtype))
     dX = torch.empty_like(X) if dX is None else dX
     dWg = torch.empty_like(Wg) if dWg is None else dWg
     dWu = torch.empty_like(Wu) if dWu is None else dWu
     dWd = torch.empty_like(Wd) if dWd is None else dWd
-    tensors += [(G, "G", (T, n), torch.float32), (U, "U", (T, n), torch.float32), (H, "H", (T, n), X.dtype)]
-    tensors += [(dY, "dY", X.shape, X.dtype), (dX, "dX", X.shape, X.dtype), (dWg, "dWg", (n, h), X.dtype), (dWu, "dWu", (n, h), X.dtype),
-                (dWd, "dWd", (h, n), X.dtype)]
-    _check_all(dev, *tensors)
     ws = _workspace(workspace, lib.psattn_ffn_bwd_workspace_bytes(dt, T, h, n), X, stream)
     st = lib.psattn_ffn_bwd(dt, _ACTS[act], T, h, n, X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(), G.data_ptr(), U.data_ptr(),
                             H.data_ptr(), dY.data_ptr(), dX.data_ptr(), dWg.data_ptr(), dWu.data_ptr(), dWd.data_ptr(), ws.data_ptr(),

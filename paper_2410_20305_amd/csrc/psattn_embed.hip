@@ -60,7 +60,7 @@ __global__ __launch_bounds__(kThreads) void psattn_embed_rows(int n_tokens, int 
 
 // ---- tokens sorted by id
 // Up to kRankMost tokens: a token's place is the number of tokens that come before it, counted by sixteen lanes over all keys, which
-// fit LDS.  One launch instead of six, and no chain of barriers.
+// fit LDS: one launch instead of four (2 000 tokens 6 us, 6 000 16, 8 334 28, where the sort below takes 20 whatever their number up to 16 000).
 //
 // More: passes over the id's digits, least first, each stable: the digits' counts in every block of tokens, then each token to its
 // place, for which a workgroup adds up the counts of all blocks itself (at most kMostBlocks; longer inputs have longer blocks).  Ids
@@ -145,7 +145,7 @@ __global__ __launch_bounds__(kSortThreads) void psattn_embed_place(int n, int vo
     }
 }
 
-constexpr int kRankMost = 4096;
+constexpr int kRankMost = 6144;
 
 __global__ __launch_bounds__(kThreads) void psattn_embed_rank(int n, int vocab, const int32_t* ids, int32_t* out_keys, int32_t* out_tokens) {
     __shared__ __attribute__((aligned(16))) uint32_t key[kRankMost];

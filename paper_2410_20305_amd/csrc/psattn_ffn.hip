@@ -190,7 +190,6 @@ void join(Pass pass, int act, const Product& d, hipStream_t s) {
 
 // `parts`: room of part_bytes()
 int product(int32_t dt, Pass pass, int act, bool pkc, bool qkc, Product d, void* parts, hipStream_t s) {
-    if (std::max(d.ldp, d.ldq) * elem_bytes(dt) * 256 >= (int64_t{1} << 31)) return PSATTN_EUNSUPPORTED;  // a tile's copies have 32-bit offsets
     const Move move = dt != PSATTN_BF16 ? kFloat : whole_rows(pkc, d) ? kWhole : kOdd;
     const Plan p = plan(move, pass, pkc, d.M, d.N, d.K, d.n_seg, d.n_prod);
     d.n_split = p.split;
@@ -202,6 +201,13 @@ int product(int32_t dt, Pass pass, int act, bool pkc, bool qkc, Product d, void*
     if (dt == PSATTN_BF16) four ? join<uint16_t, 4>(pass, act, d, s) : join<uint16_t, 1>(pass, act, d, s);
     else four ? join<float, 4>(pass, act, d, s) : join<float, 1>(pass, act, d, s);
     return hipGetLastError() == hipSuccess ? PSATTN_OK : PSATTN_EHIP;
+}
+
+// a tile's copies have 32-bit offsets, and grids stay below 2^31 threads
+bool too_large(int32_t dt, int64_t n_tokens, int64_t hidden, int64_t inner) {
+    if (std::max(hidden, inner) * static_cast<int64_t>(elem_bytes(dt)) * 256 >= (int64_t{1} << 31)) return true;
+    const int64_t t = cdiv(n_tokens, 128), h = cdiv(hidden, 128), i = cdiv(inner, 128);
+    return std::max({t * (2 * i + 1), t * h, 2 * i * h}) >= (int64_t{1} << 23);
 }
 
 // zeros without a memset, which a captured graph would not replay faithfully
@@ -232,6 +238,7 @@ int psattn_ffn_fwd(int32_t dt, int32_t act, int32_t n_tokens, int32_t hidden, in
     if (n_tokens == 0) return PSATTN_OK;
     if (!X || !Wg || !Wu || !Wd || !H || !Y || (!G) != (!U)) return PSATTN_EINVAL;
     if (!workspace || workspace_bytes < psattn_ffn_fwd_workspace_bytes(dt, n_tokens, hidden, inner)) return PSATTN_EINVAL;
+    if (too_large(dt, n_tokens, hidden, inner)) return PSATTN_EUNSUPPORTED;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     char* const parts = reinterpret_cast<char*>(align_up(reinterpret_cast<uintptr_t>(workspace), 256));
     Product gate{};
@@ -260,6 +267,7 @@ int psattn_ffn_bwd(int32_t dt, int32_t act, int32_t n_tokens, int32_t hidden, in
     }
     if (!X || !Wg || !Wu || !Wd || !G || !U || !H || !dY || !dX || !workspace) return PSATTN_EINVAL;
     if (workspace_bytes < psattn_ffn_bwd_workspace_bytes(dt, n_tokens, hidden, inner)) return PSATTN_EINVAL;
+    if (too_large(dt, n_tokens, hidden, inner)) return PSATTN_EUNSUPPORTED;
     char* const dG = reinterpret_cast<char*>(align_up(reinterpret_cast<uintptr_t>(workspace), 256));
     char* const dU = dG + align_up(static_cast<size_t>(n_tokens) * inner * elem_bytes(dt), 256);
     char* const parts = dU + align_up(static_cast<size_t>(n_tokens) * inner * elem_bytes(dt), 256);

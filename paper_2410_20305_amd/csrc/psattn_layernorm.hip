@@ -458,8 +458,8 @@ void bwd(int32_t n_rows, int32_t hidden, const void* S_, const void* w_, const f
     psattn_ln_weights<<<(2 * hidden + 63) / 64, 1024, 0, s>>>(np, hidden, part, dw, db, sizeof(E) == 2);
 }
 
-// grids of at most 2^31 threads: a row to 1 024 of them
-constexpr int32_t kMostRows = (1 << 21) - 1;
+// grids of at most 2^31 threads: a row to 1 024 of them, or 64 columns of dw and db
+constexpr int32_t kMostRows = (1 << 21) - 1, kMostHidden = 1 << 24;
 
 }  // namespace
 
@@ -470,7 +470,7 @@ int psattn_layernorm_fwd(int32_t dt, int32_t n_rows, int32_t hidden, float eps, 
     if (bad_shape(dt, n_rows, hidden) || !(eps >= 0.f) || std::isinf(eps)) return PSATTN_EINVAL;
     if (n_rows == 0) return PSATTN_OK;
     if (!X || !weight || !Y || !mean || !rstd || (!R) != (!S)) return PSATTN_EINVAL;
-    if (n_rows > kMostRows || hidden > INT32_MAX / 2) return PSATTN_EUNSUPPORTED;
+    if (n_rows > kMostRows || hidden > kMostHidden) return PSATTN_EUNSUPPORTED;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     if (dt == PSATTN_BF16) fwd<uint16_t>(n_rows, hidden, eps, X, R, weight, bias, S, Y, mean, rstd, s);
     else fwd<float>(n_rows, hidden, eps, X, R, weight, bias, S, Y, mean, rstd, s);
@@ -488,7 +488,7 @@ int psattn_layernorm_bwd(int32_t dt, int32_t n_rows, int32_t hidden, const void*
     if (bad_shape(dt, n_rows, hidden) || !dweight) return PSATTN_EINVAL;
     if (n_rows > 0 && (!S || !weight || !mean || !rstd || !dY || !dX || !workspace)) return PSATTN_EINVAL;
     if (n_rows > 0 && workspace_bytes < psattn_layernorm_bwd_workspace_bytes(n_rows, hidden)) return PSATTN_EINVAL;
-    if (n_rows > kMostRows || hidden > INT32_MAX / 2) return PSATTN_EUNSUPPORTED;
+    if (n_rows > kMostRows || hidden > kMostHidden) return PSATTN_EUNSUPPORTED;
     float* const part = reinterpret_cast<float*>(align_up(reinterpret_cast<uintptr_t>(workspace), 256));
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     if (dt == PSATTN_BF16) bwd<uint16_t>(n_rows, hidden, S, weight, mean, rstd, dY, dS, dX, dweight, dbias, part, s);

@@ -59,6 +59,16 @@ def test_library_refuses(call, args):
     assert call(**args) == -1, args
 
 
+@pytest.mark.parametrize("call,args", [
+    (_embed_fwd, dict(T=(1 << 24) + 1)), (_embed_fwd, dict(h=(1 << 23) + 1)), (_embed_bwd, dict(T=(1 << 24) + 1, n=1 << 62)), (_embed_bwd, dict(V=(1 << 31) - 1, n=1 << 62)),
+    (_embed_bwd, dict(V=1 << 28, n=1 << 62)), (_ln_fwd, dict(n=1 << 21)), (_ln_fwd, dict(h=(1 << 24) + 1)), (_ln_bwd, dict(n=1 << 21, size=1 << 62)),
+    (_ln_bwd, dict(h=(1 << 24) + 8, size=1 << 62)), (_ffn_fwd, dict(h=1 << 22, size=1 << 62)), (_ffn_fwd, dict(dt=F32, h=1 << 21, size=1 << 62)),
+    (_ffn_bwd, dict(h=1 << 22, size=1 << 62)), (_ffn_bwd, dict(n=1 << 22, size=1 << 62)),
+])
+def test_library_has_no_kernel_for(call, args):
+    assert call(**args) == -6, args
+
+
 def test_no_rows_is_no_error_forward():
     assert _embed_fwd(T=0, ids=None, X=None) == 0
     assert _ln_fwd(n=0, X=None, Y=None, mean=None, rstd=None) == 0
