@@ -5,8 +5,8 @@
 // then the down projection.  Backward: dH = dY Wd with dG, dU in its epilogue; dX = dG Wg + dU Wu as one product over both
 // weights' rows; dWg, dWu in one launch; dWd.  All sums over k are fp32.  H, dG and dU are operands of the
 // matrix cores and are held in the element type, each rounded once, from fp32.  G and U are kept in fp32: rounded to bf16 they would
-// put two more roundings into dG and dU, and gradients of weights off by 3.1e-3 (relative L2 against 64 bits) instead of NOTE, whose own rounding
-// is 1.7e-3; that costs NOTE of a training step's time.
+// put two more roundings into dG and dU, and gradients of weights off by 3.1e-3 (relative L2 against 64 bits) instead of 2.3e-3 (their
+// own rounding alone is 1.7e-3); that costs 1 % of a large step's time.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -15,6 +15,7 @@
 
 #include "psattn.h"
 #include "psattn_ffn.h"
+#include "psattn_rows.h"
 
 namespace {
 
@@ -162,8 +163,9 @@ __global__ __launch_bounds__(256) void psattn_ffn_join(Product d) {
             put<V>(static_cast<E*>(d.H) + at, h);
         } else if constexpr (PASS == kDact) {
             float gate[V], up[V], dg[V], du[V];
-            get<V>(d.G + at, gate);
-            get<V>(d.U + at, up);
+            const int64_t kept = m * d.ld_kept + n;
+            get<V>(d.G + kept, gate);
+            get<V>(d.U + kept, up);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 float a, da;
@@ -190,17 +192,85 @@ void join(Pass pass, int act, const Product& d, hipStream_t s) {
 
 // `parts`: room of part_bytes()
 int product(int32_t dt, Pass pass, int act, bool pkc, bool qkc, Product d, void* parts, hipStream_t s) {
-    const Move move = dt != PSATTN_BF16 ? kFloat : whole_rows(pkc, d) ? kWhole : kOdd;
+    if (!d.odd) {
+        d.m_load = d.M;
+        d.n_load = d.N;
+    }
+    const Move move = dt != PSATTN_BF16 ? kFloat : d.odd || whole_rows(pkc, d) ? kWhole : kOdd;
     const Plan p = plan(move, pass, pkc, d.M, d.N, d.K, d.n_seg, d.n_prod);
     d.n_split = p.split;
     d.parts = static_cast<float*>(parts);
     d.ld_part = ld_part(d.N);
     const int rc = (move == kFloat ? product_f32 : move == kWhole ? product_bf16 : product_bf16_any)(pass, act, pkc, qkc, p.size, d, s);
     if (rc != PSATTN_OK || d.n_split == 1) return rc;
-    const bool four = at16({d.out[0], d.out[1], d.G, d.U, d.H}) && d.ldo % 4 == 0 && d.N % 4 == 0;
+    const bool four = at16({d.out[0], d.out[1], d.G, d.U, d.H}) && d.ldo % 4 == 0 && d.N % 4 == 0 && (pass != kDact || d.ld_kept % 4 == 0);
     if (dt == PSATTN_BF16) four ? join<uint16_t, 4>(pass, act, d, s) : join<uint16_t, 1>(pass, act, d, s);
     else four ? join<float, 4>(pass, act, d, s) : join<float, 1>(pass, act, d, s);
     return hipGetLastError() == hipSuccess ? PSATTN_OK : PSATTN_EHIP;
+}
+
+// ---- bf16 rows that are not whole 16-byte groups, made so in the workspace.  The asynchronous copies need such rows; the way through registers
+// does not, but takes 1.5 - 1.7 times as long.  What the rows' copies cost is made good from some 300 tokens on.  Through registers / made
+// whole, forward and backward in us: hidden 4 095, inner 14 335, 300 tokens 1 079 / 1 074, 700 1 638 / 1 396, 1 200 2 659 / 1 921; hidden 1 001,
+// inner 2 731, 150 tokens 116 / 114, 300 137 / 129, 1 037 238 / 187; hidden 2 047, inner 6 001, 3 001 tokens 1 500 / 1 030 (890 on rows that are whole).
+constexpr int32_t kPadTokens = 320;
+
+struct Pad {
+    const uint16_t* src;
+    uint16_t* dst;
+    int32_t rows, width;
+};
+struct Pads {
+    Pad p[6];
+};
+constexpr int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
+
+// dst[row][0 .. up8(width)) = src[row][0 .. width), zeros behind
+__global__ __launch_bounds__(256) void psattn_ffn_pad(Pads pads) {
+    const Pad p = pads.p[blockIdx.y];
+    const int groups = (p.width + 7) / 8;
+    const int64_t n = static_cast<int64_t>(p.rows) * groups;
+    for (int64_t i = blockIdx.x * int64_t{256} + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * 256) {
+        const int64_t row = i / groups;
+        const int c = static_cast<int>(i - row * groups) * 8;
+        const auto at = psattn::rows::place<false, uint16_t>(c, p.width);
+        const auto u = psattn::rows::settled<false>(psattn::rows::raw<false>(p.src + row * p.width, at, p.width), at.down);
+        *reinterpret_cast<psattn::rows::u32x4*>(p.dst + (row * groups + i - row * groups) * 8) = u;
+    }
+}
+
+int pad(std::initializer_list<Pad> list, hipStream_t s) {
+    Pads pads{};
+    int n = 0;
+    for (const Pad& p : list) pads.p[n++] = p;
+    psattn_ffn_pad<<<dim3(2048, n), 256, 0, s>>>(pads);
+    return hipGetLastError() == hipSuccess ? PSATTN_OK : PSATTN_EHIP;
+}
+
+// Whether a call's rows are made whole: by sizes alone, for the workspace, and by the tensors' addresses
+bool may_pad(int32_t dt, int32_t n_tokens) { return dt == PSATTN_BF16 && n_tokens >= kPadTokens; }
+
+// Carves a workspace
+struct Carver {
+    char* p;
+    explicit Carver(void* base) : p(reinterpret_cast<char*>(align_up(reinterpret_cast<uintptr_t>(base), 256))) {}
+    uint16_t* take(int64_t rows, int64_t width) {
+        char* const r = p;
+        p += align_up(static_cast<size_t>(rows) * static_cast<size_t>(up8(width)) * 2, 256);
+        return reinterpret_cast<uint16_t*>(r);
+    }
+};
+size_t fwd_pad_bytes(int32_t dt, int64_t n_tokens, int64_t hidden, int64_t inner) {
+    if (!may_pad(dt, static_cast<int32_t>(n_tokens))) return 0;
+    Carver c(nullptr);
+    c.take(n_tokens, hidden), c.take(inner, hidden), c.take(inner, hidden), c.take(hidden, inner), c.take(n_tokens, inner);
+    return reinterpret_cast<uintptr_t>(c.p);
+}
+size_t bwd_pad_bytes(int32_t dt, int64_t n_tokens, int64_t hidden, int64_t inner) {
+    if (!may_pad(dt, static_cast<int32_t>(n_tokens))) return 0;
+    Carver c(nullptr);
+    c.take(n_tokens, hidden), c.take(n_tokens, hidden), c.take(inner, hidden), c.take(inner, hidden), c.take(hidden, inner), c.take(n_tokens, inner);
+    return reinterpret_cast<uintptr_t>(c.p);
 }
 
 // a tile's copies have 32-bit offsets, and grids stay below 2^31 threads
@@ -223,13 +293,13 @@ size_t psattn_ffn_bwd_workspace_bytes(int32_t dt, int32_t n_tokens, int32_t hidd
     if (bad_shape(dt, PSATTN_ACT_SILU, n_tokens, hidden, inner)) return 0;
     const size_t parts = std::max({part_bytes(dt, kDact, true, n_tokens, inner, hidden, 1, 1), part_bytes(dt, kPlain, true, n_tokens, hidden, inner, 2, 1),
                                    part_bytes(dt, kPlain, false, inner, hidden, n_tokens, 1, 2), part_bytes(dt, kPlain, false, hidden, inner, n_tokens, 1, 1)});
-    return 2 * align_up(static_cast<size_t>(n_tokens) * inner * elem_bytes(dt), 256) + align_up(parts, 256) + 256;
+    return 2 * align_up(static_cast<size_t>(n_tokens) * static_cast<size_t>(up8(inner)) * elem_bytes(dt), 256) + align_up(parts, 256) + bwd_pad_bytes(dt, n_tokens, hidden, inner) + 256;
 }
 
 size_t psattn_ffn_fwd_workspace_bytes(int32_t dt, int32_t n_tokens, int32_t hidden, int32_t inner) {
     if (bad_shape(dt, PSATTN_ACT_SILU, n_tokens, hidden, inner)) return 0;
     const size_t parts = std::max(part_bytes(dt, kGate, true, n_tokens, inner, hidden, 1, 1), part_bytes(dt, kPlain, true, n_tokens, hidden, inner, 1, 1));
-    return align_up(parts, 256) + 256;
+    return align_up(parts, 256) + fwd_pad_bytes(dt, n_tokens, hidden, inner) + 256;
 }
 
 int psattn_ffn_fwd(int32_t dt, int32_t act, int32_t n_tokens, int32_t hidden, int32_t inner, const void* X, const void* Wg, const void* Wu,
@@ -240,17 +310,29 @@ int psattn_ffn_fwd(int32_t dt, int32_t act, int32_t n_tokens, int32_t hidden, in
     if (!workspace || workspace_bytes < psattn_ffn_fwd_workspace_bytes(dt, n_tokens, hidden, inner)) return PSATTN_EINVAL;
     if (too_large(dt, n_tokens, hidden, inner)) return PSATTN_EUNSUPPORTED;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    char* const parts = reinterpret_cast<char*>(align_up(reinterpret_cast<uintptr_t>(workspace), 256));
+    const bool odd = may_pad(dt, n_tokens) && !(hidden % 8 == 0 && inner % 8 == 0 && at16({X, Wg, Wu, Wd, G, U, H, Y}));
+    Carver room(workspace);
+    const int64_t hp = odd ? up8(hidden) : hidden, ip = odd ? up8(inner) : inner;
+    const uint16_t* Hp = nullptr;
+    int rc;
+    if (odd) {
+        uint16_t *x = room.take(n_tokens, hidden), *g = room.take(inner, hidden), *u = room.take(inner, hidden), *w = room.take(hidden, inner);
+        Hp = room.take(n_tokens, inner);
+        auto from = [](const void* p) { return static_cast<const uint16_t*>(p); };
+        if ((rc = pad({{from(X), x, n_tokens, hidden}, {from(Wg), g, inner, hidden}, {from(Wu), u, inner, hidden}, {from(Wd), w, hidden, inner}}, s)) != PSATTN_OK) return rc;
+        X = x; Wg = g; Wu = u; Wd = w;
+    }
+    void* const parts = room.p;
     Product gate{};
     gate.p[0] = X; gate.q[0] = Wg; gate.q[1] = Wu; gate.G = G; gate.U = U; gate.H = H;
-    gate.ldp = gate.ldq = hidden; gate.ldo = inner;
-    gate.M = n_tokens; gate.N = inner; gate.K = hidden; gate.n_seg = gate.n_prod = 1;
-    int rc = product(dt, kGate, act, true, true, gate, parts, s);
-    if (rc != PSATTN_OK) return rc;
+    gate.ldp = gate.ldq = hp; gate.ldo = inner; gate.odd = odd;
+    gate.M = gate.m_load = n_tokens; gate.N = gate.n_load = inner; gate.K = hidden; gate.n_seg = gate.n_prod = 1;
+    if ((rc = product(dt, kGate, act, true, true, gate, parts, s)) != PSATTN_OK) return rc;
+    if (odd && (rc = pad({{static_cast<const uint16_t*>(H), const_cast<uint16_t*>(Hp), n_tokens, inner}}, s)) != PSATTN_OK) return rc;
     Product down{};
-    down.p[0] = H; down.q[0] = Wd; down.out[0] = Y;
-    down.ldp = down.ldq = inner; down.ldo = hidden;
-    down.M = n_tokens; down.N = hidden; down.K = inner; down.n_seg = down.n_prod = 1;
+    down.p[0] = odd ? Hp : H; down.q[0] = Wd; down.out[0] = Y;
+    down.ldp = down.ldq = ip; down.ldo = hidden; down.odd = odd;
+    down.M = down.m_load = n_tokens; down.N = down.n_load = hidden; down.K = inner; down.n_seg = down.n_prod = 1;
     return product(dt, kPlain, act, true, true, down, parts, s);
 }
 
@@ -268,29 +350,41 @@ int psattn_ffn_bwd(int32_t dt, int32_t act, int32_t n_tokens, int32_t hidden, in
     if (!X || !Wg || !Wu || !Wd || !G || !U || !H || !dY || !dX || !workspace) return PSATTN_EINVAL;
     if (workspace_bytes < psattn_ffn_bwd_workspace_bytes(dt, n_tokens, hidden, inner)) return PSATTN_EINVAL;
     if (too_large(dt, n_tokens, hidden, inner)) return PSATTN_EUNSUPPORTED;
-    char* const dG = reinterpret_cast<char*>(align_up(reinterpret_cast<uintptr_t>(workspace), 256));
-    char* const dU = dG + align_up(static_cast<size_t>(n_tokens) * inner * elem_bytes(dt), 256);
-    char* const parts = dU + align_up(static_cast<size_t>(n_tokens) * inner * elem_bytes(dt), 256);
+    const bool odd = may_pad(dt, n_tokens) && !(hidden % 8 == 0 && inner % 8 == 0 && at16({X, Wg, Wu, Wd, G, U, H, dY, dX, dWg, dWu, dWd}));
+    const int64_t hp = odd ? up8(hidden) : hidden, ip = odd ? up8(inner) : inner;
+    Carver room(workspace);
+    char* const dG = room.p;
+    char* const dU = dG + align_up(static_cast<size_t>(n_tokens) * static_cast<size_t>(up8(inner)) * elem_bytes(dt), 256);
+    room.p = dU + align_up(static_cast<size_t>(n_tokens) * static_cast<size_t>(up8(inner)) * elem_bytes(dt), 256);
     int rc;
-    Product a{};  // dH = dY Wd, dG and dU
+    if (odd) {
+        uint16_t *x = room.take(n_tokens, hidden), *y = room.take(n_tokens, hidden), *g = room.take(inner, hidden), *u = room.take(inner, hidden), *w = room.take(hidden, inner),
+                 *k = room.take(n_tokens, inner);
+        auto from = [](const void* p) { return static_cast<const uint16_t*>(p); };
+        rc = pad({{from(X), x, n_tokens, hidden}, {from(dY), y, n_tokens, hidden}, {from(Wg), g, inner, hidden}, {from(Wu), u, inner, hidden}, {from(Wd), w, hidden, inner}, {from(H), k, n_tokens, inner}}, s);
+        if (rc != PSATTN_OK) return rc;
+        X = x; dY = y; Wg = g; Wu = u; Wd = w; H = k;
+    }
+    void* const parts = room.p;
+    Product a{};  // dH = dY Wd, dG and dU.  G and U have rows of `inner`, dG and dU rows of ip
     a.p[0] = dY; a.q[0] = Wd; a.G = const_cast<float*>(G); a.U = const_cast<float*>(U); a.out[0] = dG; a.out[1] = dU;
-    a.ldp = hidden; a.ldq = a.ldo = inner;
-    a.M = n_tokens; a.N = inner; a.K = hidden; a.n_seg = a.n_prod = 1;
+    a.ldp = hp; a.ldq = a.ldo = ip; a.ld_kept = inner; a.odd = odd;
+    a.M = a.m_load = n_tokens; a.N = inner; a.n_load = static_cast<int32_t>(ip); a.K = hidden; a.n_seg = a.n_prod = 1;
     if ((rc = product(dt, kDact, act, true, false, a, parts, s)) != PSATTN_OK) return rc;
     Product x{};  // dX = dG Wg + dU Wu
     x.p[0] = dG; x.p[1] = dU; x.q[0] = Wg; x.q[1] = Wu; x.out[0] = dX;
-    x.ldp = inner; x.ldq = x.ldo = hidden;
-    x.M = n_tokens; x.N = hidden; x.K = inner; x.n_seg = 2; x.n_prod = 1;
+    x.ldp = ip; x.ldq = hp; x.ldo = hidden; x.odd = odd;
+    x.M = x.m_load = n_tokens; x.N = hidden; x.n_load = static_cast<int32_t>(hp); x.K = inner; x.n_seg = 2; x.n_prod = 1;
     if ((rc = product(dt, kPlain, act, true, false, x, parts, s)) != PSATTN_OK) return rc;
     Product gu{};  // dWg = dG^T X, dWu = dU^T X
     gu.p[0] = dG; gu.p[1] = dU; gu.q[0] = X; gu.out[0] = dWg; gu.out[1] = dWu;
-    gu.ldp = inner; gu.ldq = gu.ldo = hidden;
-    gu.M = inner; gu.N = hidden; gu.K = n_tokens; gu.n_seg = 1; gu.n_prod = 2;
+    gu.ldp = ip; gu.ldq = hp; gu.ldo = hidden; gu.odd = odd;
+    gu.M = inner; gu.m_load = static_cast<int32_t>(ip); gu.N = hidden; gu.n_load = static_cast<int32_t>(hp); gu.K = n_tokens; gu.n_seg = 1; gu.n_prod = 2;
     if ((rc = product(dt, kPlain, act, false, false, gu, parts, s)) != PSATTN_OK) return rc;
     Product wd{};  // dWd = dY^T H
     wd.p[0] = dY; wd.q[0] = H; wd.out[0] = dWd;
-    wd.ldp = hidden; wd.ldq = wd.ldo = inner;
-    wd.M = hidden; wd.N = inner; wd.K = n_tokens; wd.n_seg = wd.n_prod = 1;
+    wd.ldp = hp; wd.ldq = ip; wd.ldo = inner; wd.odd = odd;
+    wd.M = hidden; wd.m_load = static_cast<int32_t>(hp); wd.N = inner; wd.n_load = static_cast<int32_t>(ip); wd.K = n_tokens; wd.n_seg = wd.n_prod = 1;
     return product(dt, kPlain, act, false, false, wd, parts, s);
 }
 

@@ -49,8 +49,8 @@ struct Copy {
     uint4 r[ASYNC ? 1 : PER];
     bool edge, tiny;  // the tile reaches past the rows' ends; rows shorter than a chunk
     int in_row;
-    // r0: first m or n of the tile, n_rows: how many there are in all.  What lies behind them is read again from the last one: those
-    // results are not stored
+    // r0: first m or n of the tile, n_rows: how many there are in all (KS: in a row in memory).  What lies behind them is read again from the
+    // last one: those results are not stored
     __device__ __forceinline__ void set(int64_t ld, int r0, int n_rows, int w, int l) {
         edge = !KC && r0 + ROWS > n_rows;
         tiny = !KC && n_rows < EPC;
@@ -141,9 +141,8 @@ __device__ __forceinline__ void put8(float* p, const float (&x)[8], int n) {
 // eight floats as they come from memory
 struct Group {
     float w[8];
-    template <bool ALIGNED>
     __device__ __forceinline__ void get(const float* p, int n) {
-        if (ALIGNED || n >= 8) {
+        if (n >= 8) {
 #pragma unroll
             for (int i = 0; i < 8; i += 4) {
                 const Raw16 x = *reinterpret_cast<const Raw16*>(p + i);
@@ -181,6 +180,13 @@ __device__ __forceinline__ void store_chunks(float* base, int64_t ld, int rows, 
     for (int k = 0; k < 2; ++k) put8(base + row * ld + 16 * k + col, x.c[k], cols - 16 * k - col);
 }
 
+// ... by rows of whole groups or not, which the launch knows
+template <bool ASYNC, typename E>
+__device__ __forceinline__ void store_out(E* base, int64_t ld, int rows, int cols, const Chunks& x, int l, int odd) {
+    if (ASYNC && !odd) store_chunks<true>(base, ld, rows, cols, x, l);
+    else store_chunks<false>(base, ld, rows, cols, x, l);
+}
+
 template <int BM_, int BN_, int WM_, int WN_, int NBQ_>
 struct Shape {  // tile, waves, LDS buffers of Q (of P: two)
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NBQ = NBQ_, kWaves = WM * WN, kThreads = 64 * kWaves;
@@ -205,8 +211,8 @@ __global__ __launch_bounds__(S::kThreads, 2) void psattn_ffn_tiles(Product d, in
     const int m0 = tm * S::BM, n0 = tn * kCols;
     Copy<E, PKC, S::BM, S::kWaves, false, ASYNC> cp;
     Copy<E, QKC, S::BN, S::kWaves, PASS == kGate, ASYNC> cq;
-    cp.set(d.ldp, m0, d.M, w, l);
-    cq.set(d.ldq, n0, d.N, w, l);
+    cp.set(d.ldp, m0, PKC ? d.M : d.m_load, w, l);
+    cq.set(d.ldq, n0, QKC ? d.N : d.n_load, w, l);
     const LaneRead<E, PKC> lp(l, wm * MB);
     const LaneRead<E, QKC> lq(l, wn * NB);
     f32x16 acc[NB][MB] = {};
@@ -396,9 +402,9 @@ __global__ __launch_bounds__(S::kThreads, 2) void psattn_ffn_tiles(Product d, in
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const int c = min(16 * k + 8 * (l >> 5), (cols - 1) / 8 * 8);
-                const int64_t from = (m + min(l & 31, rows - 1)) * d.ldo + n + c;
-                g[set][k].template get<ASYNC>(d.G + from, cols - c);
-                u[set][k].template get<ASYNC>(d.U + from, cols - c);
+                const int64_t from = (m + min(l & 31, rows - 1)) * d.ld_kept + n + c;
+                g[set][k].get(d.G + from, cols - c);
+                u[set][k].get(d.U + from, cols - c);
             }
         };
         ask(0, 0);
@@ -420,8 +426,8 @@ __global__ __launch_bounds__(S::kThreads, 2) void psattn_ffn_tiles(Product d, in
                 }
             }
             const int64_t at = m * d.ldo + n;
-            store_chunks<ASYNC>(static_cast<E*>(d.out[0]) + at, d.ldo, rows, cols, dg, l);
-            store_chunks<ASYNC>(static_cast<E*>(d.out[1]) + at, d.ldo, rows, cols, du, l);
+            store_out<ASYNC>(static_cast<E*>(d.out[0]) + at, d.ldo, rows, cols, dg, l, d.odd);
+            store_out<ASYNC>(static_cast<E*>(d.out[1]) + at, d.ldo, rows, cols, du, l, d.odd);
             __builtin_amdgcn_sched_barrier(0);
         });
         return;
@@ -446,15 +452,15 @@ __global__ __launch_bounds__(S::kThreads, 2) void psattn_ffn_tiles(Product d, in
             f32x16 h;
 #pragma unroll
             for (int i = 0; i < 16; ++i) h[i] = act<E, ACT>(acc[0][mb][i]) * acc[1][mb][i];
-            if (d.G) store_chunks<ASYNC>(d.G + at, d.ldo, rows, cols, chunks(acc[0][mb]), l);
-            if (d.U) store_chunks<ASYNC>(d.U + at, d.ldo, rows, cols, chunks(acc[1][mb]), l);
-            store_chunks<ASYNC>(static_cast<E*>(d.H) + at, d.ldo, rows, cols, chunks(h), l);
+            if (d.G) store_chunks<false>(d.G + at, d.ldo, rows, cols, chunks(acc[0][mb]), l);
+            if (d.U) store_chunks<false>(d.U + at, d.ldo, rows, cols, chunks(acc[1][mb]), l);
+            store_out<ASYNC>(static_cast<E*>(d.H) + at, d.ldo, rows, cols, chunks(h), l, d.odd);
         } else if constexpr (PASS == kPlain) {
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
                 const int n = n0 + (wn * NB + nb) * 32, cols = d.N - n;
                 if (cols <= 0) break;
-                store_chunks<ASYNC>(static_cast<E*>(d.out[d.n_prod > 1 ? z : 0]) + m * d.ldo + n, d.ldo, rows, cols, chunks(acc[nb][mb]), l);
+                store_out<ASYNC>(static_cast<E*>(d.out[d.n_prod > 1 ? z : 0]) + m * d.ldo + n, d.ldo, rows, cols, chunks(acc[nb][mb]), l, d.odd);
             }
         }
     }

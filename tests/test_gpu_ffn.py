@@ -39,7 +39,7 @@ def _prod(a, b, err_a, k):
 
 SHAPES = [(1, 1, 1), (1, 8, 8), (1, 64, 128), (2, 7, 3), (3, 130, 65), (16, 64, 64), (17, 96, 200), (31, 256, 129), (33, 72, 264), (64, 128, 256), (65, 64, 136),
           (100, 1, 40), (127, 200, 96), (128, 128, 128), (129, 264, 40), (130, 257, 131), (221, 192, 512), (256, 512, 256), (257, 520, 264), (300, 33, 1000),
-          (512, 136, 72), (520, 640, 328), (1, 4096, 72), (5, 1000, 2731), (48, 768, 1024), (700, 64, 2048)]
+          (512, 136, 72), (520, 640, 328), (1, 4096, 72), (5, 1000, 2731), (48, 768, 1024), (700, 64, 2048), (641, 7, 9), (640, 33, 1000), (645, 72, 131)]
 
 
 @pytest.mark.parametrize("act", ["silu", "gelu"])
@@ -81,7 +81,7 @@ def _whole(rng, *shape, most=1, share=0.25):
     return np.where(rng.uniform(size=shape) < share, rng.integers(-most, most + 1, shape), 0).astype(np.float64)
 
 
-EXACT = SHAPES + [(1000, 264, 520), (1, 2048, 4096), (8, 4104, 520), (24, 1024, 3000), (64, 2048, 1032), (260, 1032, 2056), (1031, 520, 776), (2000, 256, 264), (384, 2048, 4096)]
+EXACT = SHAPES + [(1000, 264, 520), (1, 2048, 4096), (8, 4104, 520), (24, 1024, 3000), (64, 2048, 1032), (260, 1032, 2056), (1031, 520, 776), (2000, 256, 264), (384, 2048, 4096), (800, 130, 65), (1300, 257, 131), (1037, 1001, 731), (900, 1, 1), (704, 520, 3), (2011, 15, 264)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -117,7 +117,7 @@ def test_whole_numbers_are_exact(T, h, n, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("T,h,n,shift", [(33, 64, 128, 1), (130, 256, 264, 3), (300, 512, 136, 2), (4, 128, 64, 1)])
+@pytest.mark.parametrize("T,h,n,shift", [(33, 64, 128, 1), (130, 256, 264, 3), (300, 512, 136, 2), (4, 128, 64, 1), (700, 128, 264, 1), (650, 65, 72, 3)])
 def test_unaligned_tensors(T, h, n, shift, dtype):
     rng = np.random.default_rng(9)
     X, Wg, Wu, Wd, dY = _whole(rng, T, h), _whole(rng, n, h) * 64, _whole(rng, n, h), _whole(rng, h, n), _whole(rng, T, h)
@@ -138,7 +138,7 @@ def test_forward_without_backward(T, h, n):
     assert none is None and torch.equal(Y, Y2) and torch.equal(Y, Y3) and torch.equal(H, kept[2])
 
 
-@pytest.mark.parametrize("T,h,n", [(5, 64, 128), (200, 256, 520), (33, 65, 130)])
+@pytest.mark.parametrize("T,h,n", [(5, 64, 128), (200, 256, 520), (33, 65, 130), (700, 65, 130)])
 def test_not_finite_keeps_to_its_rows(T, h, n):
     """A row of X that is not finite reaches its own rows of G, U, H, Y; one of dY its row of dX and its column sums."""
     rng = np.random.default_rng(6)
