@@ -6,7 +6,7 @@
 // weights' rows; dWg, dWu in one launch; dWd.  All sums over k are fp32.  H, dG and dU are operands of the
 // matrix cores and are held in the element type, each rounded once, from fp32.  G and U are kept in fp32: rounded to bf16 they would
 // put two more roundings into dG and dU, and gradients of weights off by 3.1e-3 (relative L2 against 64 bits) instead of 2.3e-3 (their
-// own rounding alone is 1.7e-3); that costs 1 % of a large step's time.
+// own rounding alone is 1.7e-3); that costs 3 % of a large step (16 384 tokens 13.91 -> 14.33 ms in turn: gate and up 3 023 -> 3 313 us, dG and dU 1 926 -> 2 031).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -55,7 +55,8 @@ enum Move { kWhole, kOdd, kFloat };
 // 128 x 128, two to a CU, 1.05 a step, 0.65 by itself; through registers half as much again; fp32 what its MFMAs take.  A round's start and
 // end take 3 us, or 14 (gate) and 30 (dG, dU) with 256 x 256, whose workgroups have nothing beside them to cover it, 3 and 12 with
 // 128 x 128.  The two sizes, in turn: 8 192 tokens 7.0 and 8.5 ms, 1 024 tokens 1.72 and 1.49, 256 tokens 1.16 and 0.72 (unsplit).
-// Parts have no end but their sums' way to memory, and are joined by another launch.
+// Parts have no end but their sums' way to memory, and are joined by another launch; sums that outgrow the 256 MB cache go to HBM and back
+// (dWd of 16 384 tokens, 3.5 rounds of 256 x 256: 1 602 us, in two parts 1 637; dG and dU of 4 096 tokens 556 and 669).
 double cost(Move move, Pass pass, TileSize size, int64_t tiles, int64_t steps, int64_t split, double out_bytes) {
     const bool big = size == k256, parts = split > 1;
     const double per_wg = static_cast<double>(cdiv(steps, split)), odd = move == kOdd ? 1.5 : 1;
@@ -63,7 +64,8 @@ double cost(Move move, Pass pass, TileSize size, int64_t tiles, int64_t steps, i
     const double end = parts || pass == kPlain ? 3 : pass == kGate ? (big ? 14 : 3) : (big ? 30 : 12);
     const int64_t wgs = tiles * split, slots = big ? 256 : 512, rest = wgs % slots;
     const bool little = rest > 0 && (big ? wgs <= 128 : rest <= 256);
-    return static_cast<double>(wgs / slots) * (full + end) + (rest == 0 ? 0 : (little ? few : full) + end) + (parts ? 4 + static_cast<double>(split) * out_bytes * 1.3 / 4.5e6 : 0);
+    const double bytes = static_cast<double>(split) * out_bytes, ways = bytes > 2e8 ? 2 : 1.3;
+    return static_cast<double>(wgs / slots) * (full + end) + (rest == 0 ? 0 : (little ? few : full) + end) + (parts ? 4 + bytes * ways / 4.5e6 : 0);
 }
 
 Plan plan(Move move, Pass pass, bool pkc, int64_t M, int64_t N, int64_t K, int n_seg, int n_prod) {

@@ -1,14 +1,20 @@
 // The kernel of the feed-forward block's products (psattn_gemm.h has its tiles and operands), built for bf16 with asynchronous
 // copies (psattn_ffn_bf16.hip), for bf16 of any alignment (psattn_ffn_bf16_any.hip) and for fp32 (psattn_ffn_f32.hip).
 //
-// k goes through two LDS buffers, 128 bytes of it (64 bf16, 32 fp32) at a time.  The operands of a step (16 bf16, 8 fp32) are
+// k goes through LDS buffers, 128 bytes of it (64 bf16, 32 fp32) at a time.  The operands of a step (16 bf16, 8 fp32) are
 // read while the step before is multiplied.  Ahead of a tile's last step every wave has read its last operands of it and the
 // next tile has arrived: the one barrier of a tile stands there.  Behind it the next tile's first operands are read, so that no
-// MFMA waits for LDS, and the tile after that is asked for, three steps before it is needed.
-//   ASYNC       global -> LDS copies, 16-byte groups on 16-byte boundaries
+// MFMA waits for LDS, and what follows is asked for.
+//   ASYNC       global -> LDS copies, 16-byte groups on 16-byte boundaries.  Q has a third buffer: its copies are asked for a tile earlier than
+//               P's, two to a step of either, so that the path to LDS is never without them nor flooded (8 192 tokens, hidden 4 096, inner
+//               14 336, forward and backward 7 360 us with two buffers and all copies behind the barrier, 7 085 so; 64 bytes of k in
+//               three to five buffers, which reads half lines, 7 320 - 7 410 where two buffers of 128 took 7 120)
 //   otherwise   loads into registers (16 bytes from anywhere), written to LDS a tile later, before its barrier; a group that
-//               reaches past the end of its row is read from inside it and shifted
-// Tiles, by waves of m x n: see launch_product.
+//               reaches past the end of its row is read from inside it and shifted (same sizes, 10 400 us)
+// 256 x 256 to a workgroup of eight waves (one to a CU), 128 m x 64 n to a wave: 128 accumulator registers, six operand reads for eight
+// MFMAs; 128 x 128 to four waves (two to a CU); 64 and 32 x 128 to two for few tokens.
+//   What bounds the large ones (Y of 8 192 tokens, a tile of k for all workgroups): copies by themselves 1.2 us, 54 GB/s to a CU; MFMAs by
+// themselves, on operands that never change and let the clock rise, 1.0; MFMAs and reads without copies 1.3; all of it 1.6 (1.35 PFLOP/s).
 #pragma once
 #include <hip/hip_runtime.h>
 
