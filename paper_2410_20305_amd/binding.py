@@ -738,9 +738,9 @@ def psattn_ffn_bwd(X, Wg, Wu, Wd, kept, dY, act="silu", dX=None, dWg=None, dWu=N
     """dX, dWg, dWu, dWd from the forward's kept (G, U, H)."""
     torch, lib = _TORCH or _torch(), _LIB or load_library()
     dev, T, h, n, dt, tensors = _ffn_shapes(X, Wg, Wu, Wd, act)
-    G, U, H = kept
+    G, U, H = kept if kept is not None else (None, None, None)
     if any(t is None for t in (G, U, H, dY)):
-        raise ValueError("kept G, U, H and dY are needed")
+        raise ValueError("kept G, U, H (psattn_ffn_fwd without them has keep=False) and dY are needed")
     _check_all(dev, *tensors, (G, "G", (T, n), torch.float32), (U, "U", (T, n), torch.float32), (H, "H", (T, n), X.dtype), (dY, "dY", X.shape, X.dtype),
                (dX, "dX", X.shape, X.dtype), (dWg, "dWg", (n, h), X.dtype), (dWu, "dWu", (n, h), X.dtype), (dWd, "dWd", (h, n), X.dtype))
     dX = torch.empty_like(X) if dX is None else dX
