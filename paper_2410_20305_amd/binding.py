@@ -172,6 +172,38 @@ def _stream_ptr(stream):
     return stream.cuda_stream
 
 
+# torch hands a freed block out again to the stream that was current when the block was first taken, in that stream's order.  What a
+# call makes for itself therefore has to be made on the stream that its kernels run on: memory of another stream may still
+# be in use by work queued there before it was freed.
+def _side(stream, device):
+    """The stream that a call's own tensors are made on, None where that is the current one anyway."""
+    if stream is None or _stream_ptr(stream) == _stream_ptr(None):
+        return None
+    return (_TORCH or _torch()).cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream
+
+
+def _make(side, shape, dtype, device, zero=False):
+    """A tensor that a call returns.  On another stream than the current one it is both streams': freed, it is handed out again when
+    the work that is queued on either by then is done."""
+    torch = _TORCH or _torch()
+    new = torch.zeros if zero else torch.empty
+    if side is None:
+        return new(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(side):
+        t = new(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
+def _scratch(side, shape, dtype, device):
+    """A tensor that only the call's own kernels use: freed when it returns, and handed out again behind them."""
+    torch = _TORCH or _torch()
+    if side is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(side):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 class Meta:
     """Owner of a psattn_meta handle."""
 
@@ -355,10 +387,11 @@ def psattn_fwd(meta: Meta, Q, K, V, scale, O=None, LSE=None, stream=None):
     _check_tensor(Q, "Q", (meta.total_tokens, Hq, d), None)
     _check_tensor(K, "K", (T, Hkv, d), Q.dtype)
     _check_tensor(V, "V", (T, Hkv, d), Q.dtype)
+    side = _side(stream, Q.device)
     if O is None:
-        O = torch.empty_like(Q)
+        O = _make(side, Q.shape, Q.dtype, Q.device)
     if LSE is None:
-        LSE = torch.empty((Hq, T), dtype=torch.float32, device=Q.device)
+        LSE = _make(side, (Hq, T), torch.float32, Q.device)
     _check_tensor(O, "O", Q.shape, Q.dtype)
     _check_tensor(LSE, "LSE", (Hq, T), torch.float32)
     st = lib.psattn_fwd(meta.handle, _dtype_code(Q), Hq, Hkv, d, float(scale), Q.data_ptr(), K.data_ptr(),
@@ -383,14 +416,15 @@ def psattn_bwd(meta: Meta, Q, K, V, O, dO, LSE, scale, dQ=None, dK=None, dV=None
     _check_tensor(O, "O", Q.shape, Q.dtype)
     _check_tensor(dO, "dO", Q.shape, Q.dtype)
     _check_tensor(LSE, "LSE", (Hq, T), torch.float32)
-    dQ = torch.empty_like(Q) if dQ is None else dQ
-    dK = torch.empty_like(K) if dK is None else dK
-    dV = torch.empty_like(V) if dV is None else dV
+    side = _side(stream, Q.device)
+    dQ = _make(side, Q.shape, Q.dtype, Q.device) if dQ is None else dQ
+    dK = _make(side, K.shape, Q.dtype, Q.device) if dK is None else dK
+    dV = _make(side, V.shape, Q.dtype, Q.device) if dV is None else dV
     _check_tensor(dQ, "dQ", Q.shape, Q.dtype)
     _check_tensor(dK, "dK", K.shape, Q.dtype)
     _check_tensor(dV, "dV", V.shape, Q.dtype)
     if workspace is None:
-        workspace = torch.empty(psattn_bwd_workspace_bytes(meta, Hq, Hkv, d), dtype=torch.uint8, device=Q.device)
+        workspace = _scratch(side, psattn_bwd_workspace_bytes(meta, Hq, Hkv, d), torch.uint8, Q.device)
     if not workspace.is_cuda or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous device tensor")
     ws_bytes = workspace.numel() * workspace.element_size()
@@ -458,10 +492,11 @@ def psattn_fwd_rope(meta: Meta, rope: Rope, Q, K, V, scale, O=None, LSE=None, Qr
     _check_tensor(Q, "Q", (meta.total_tokens, Hq, d), None)
     _check_tensor(K, "K", (T, Hkv, d), Q.dtype)
     _check_tensor(V, "V", (T, Hkv, d), Q.dtype)
-    O = torch.empty_like(Q) if O is None else O
-    LSE = torch.empty((Hq, T), dtype=torch.float32, device=Q.device) if LSE is None else LSE
-    Qr = torch.empty_like(Q) if Qr is None else Qr
-    Kr = torch.empty_like(K) if Kr is None else Kr
+    side = _side(stream, Q.device)
+    O = _make(side, Q.shape, Q.dtype, Q.device) if O is None else O
+    LSE = _make(side, (Hq, T), torch.float32, Q.device) if LSE is None else LSE
+    Qr = _make(side, Q.shape, Q.dtype, Q.device) if Qr is None else Qr
+    Kr = _make(side, K.shape, Q.dtype, Q.device) if Kr is None else Kr
     _check_tensor(O, "O", Q.shape, Q.dtype)
     _check_tensor(LSE, "LSE", (Hq, T), torch.float32)
     _check_tensor(Qr, "Qr", Q.shape, Q.dtype)
@@ -483,13 +518,14 @@ def psattn_bwd_rope(meta: Meta, rope: Rope, Qr, Kr, V, O, dO, LSE, scale, dQ=Non
     for t, name, shape in ((Kr, "Kr", (T, Hkv, d)), (V, "V", (T, Hkv, d)), (O, "O", Qr.shape), (dO, "dO", Qr.shape)):
         _check_tensor(t, name, shape, Qr.dtype)
     _check_tensor(LSE, "LSE", (Hq, T), torch.float32)
-    dQ = torch.empty_like(Qr) if dQ is None else dQ
-    dK = torch.empty_like(Kr) if dK is None else dK
-    dV = torch.empty_like(V) if dV is None else dV
+    side = _side(stream, Qr.device)
+    dQ = _make(side, Qr.shape, Qr.dtype, Qr.device) if dQ is None else dQ
+    dK = _make(side, Kr.shape, Qr.dtype, Qr.device) if dK is None else dK
+    dV = _make(side, V.shape, Qr.dtype, Qr.device) if dV is None else dV
     for t, name, shape in ((dQ, "dQ", Qr.shape), (dK, "dK", Kr.shape), (dV, "dV", Kr.shape)):
         _check_tensor(t, name, shape, Qr.dtype)
     if workspace is None:
-        workspace = torch.empty(psattn_bwd_workspace_bytes(meta, Hq, Hkv, d), dtype=torch.uint8, device=Qr.device)
+        workspace = _scratch(side, psattn_bwd_workspace_bytes(meta, Hq, Hkv, d), torch.uint8, Qr.device)
     st = lib.psattn_bwd_rope(meta.handle, rope.handle, _dtype_code(Qr), Hq, Hkv, d, float(scale), Qr.data_ptr(),
                              Kr.data_ptr(), V.data_ptr(), O.data_ptr(), dO.data_ptr(), LSE.data_ptr(), dQ.data_ptr(),
                              dK.data_ptr(), dV.data_ptr(), workspace.data_ptr(),
@@ -538,8 +574,9 @@ def psattn_logprob_fwd(plan: LogprobPlan, logits, token_ids, row_lse=None, resp_
     T, V = logits.shape
     _check_tensor(logits, "logits", (plan.total_tokens, V), None)
     _check_tensor(token_ids, "token_ids", (T,), torch.int32)
-    row_lse = torch.zeros(T, dtype=torch.float32, device=logits.device) if row_lse is None else row_lse
-    resp_logp = torch.empty(plan.n_responses, dtype=torch.float32, device=logits.device) if resp_logp is None else resp_logp
+    side = _side(stream, logits.device)
+    row_lse = _make(side, T, torch.float32, logits.device, zero=True) if row_lse is None else row_lse
+    resp_logp = _make(side, plan.n_responses, torch.float32, logits.device) if resp_logp is None else resp_logp
     _check_tensor(row_lse, "row_lse", (T,), torch.float32)
     _check_tensor(resp_logp, "resp_logp", (plan.n_responses,), torch.float32)
     st = load_library().psattn_logprob_fwd(plan.handle, _dtype_code(logits), V, logits.data_ptr(), token_ids.data_ptr(),
@@ -555,7 +592,7 @@ def psattn_logprob_bwd(plan: LogprobPlan, logits, token_ids, row_lse, d_resp_log
     _check_tensor(token_ids, "token_ids", (T,), torch.int32)
     _check_tensor(row_lse, "row_lse", (T,), torch.float32)
     _check_tensor(d_resp_logp, "d_resp_logp", (plan.n_responses,), torch.float32)
-    dlogits = torch.empty_like(logits) if dlogits is None else dlogits
+    dlogits = _make(_side(stream, logits.device), logits.shape, logits.dtype, logits.device) if dlogits is None else dlogits
     _check_tensor(dlogits, "dlogits", logits.shape, logits.dtype)
     st = load_library().psattn_logprob_bwd(plan.handle, _dtype_code(logits), V, logits.data_ptr(), token_ids.data_ptr(),
                                            row_lse.data_ptr(), d_resp_logp.data_ptr(), dlogits.data_ptr(),
@@ -572,8 +609,9 @@ def psattn_dpo_loss(logp_policy, logp_ref, beta, stream=None):
         raise ValueError("log-probabilities must come in (chosen, rejected) pairs")
     _check_tensor(logp_policy, "logp_policy", (n,), torch.float32)
     _check_tensor(logp_ref, "logp_ref", (n,), torch.float32)
-    loss = torch.empty(n // 2, dtype=torch.float32, device=logp_policy.device)
-    d = torch.empty(n, dtype=torch.float32, device=logp_policy.device)
+    side = _side(stream, logp_policy.device)
+    loss = _make(side, n // 2, torch.float32, logp_policy.device)
+    d = _make(side, n, torch.float32, logp_policy.device)
     st = load_library().psattn_dpo_loss(n // 2, float(beta), logp_policy.data_ptr(), logp_ref.data_ptr(), loss.data_ptr(),
                                         d.data_ptr(), _stream_ptr(stream))
     _check(st, "psattn_dpo_loss")
@@ -603,16 +641,10 @@ def _check_all(dev, *tensors):
         raise ValueError("%s is on %s, not on cuda:%d" % (name, t.device, dev))
 
 
-def _workspace(given, need, like, stream):
-    """A call's workspace: the caller's, or one that goes back to torch when the work on `stream` is done."""
-    torch = _TORCH or _torch()
+def _workspace(given, need, like, side):
+    """A call's workspace: the caller's, or one of its own."""
     if given is None:
-        ws = torch.empty(need, dtype=torch.uint8, device=like.device)
-        if stream is not None and not isinstance(stream, int):
-            ws.record_stream(stream)
-        elif stream is not None and stream != _stream_ptr(None):
-            ws.record_stream(torch.cuda.ExternalStream(stream, device=like.device))
-        return ws
+        return _scratch(side, need, (_TORCH or _torch()).uint8, like.device)
     if not given.is_cuda or not given.is_contiguous() or given.device != like.device:
         raise ValueError("workspace must be a contiguous device tensor on %s" % like.device)
     return given
@@ -625,7 +657,7 @@ def psattn_embed_fwd(token_ids, W, scale=1.0, X=None, stream=None):
     (V, h), T = W.shape, token_ids.numel()
     dt = _dtype_code(W)
     _check_all(dev, (token_ids, "token_ids", (T,), torch.int32), (X, "X", (T, h), W.dtype))
-    X = torch.empty((T, h), dtype=W.dtype, device=W.device) if X is None else X
+    X = _make(_side(stream, W.device), (T, h), W.dtype, W.device) if X is None else X
     st = lib.psattn_embed_fwd(dt, T, V, h, float(scale), token_ids.data_ptr(), W.data_ptr(), X.data_ptr(), _stream_ptr(stream))
     _check(st, "psattn_embed_fwd")
     return X
@@ -640,8 +672,9 @@ def psattn_embed_bwd(token_ids, dX, vocab, scale=1.0, dW=None, workspace=None, s
     if not 0 < vocab < 1 << 31:
         raise ValueError("vocab must be a positive 32-bit number, got %d" % vocab)
     _check_all(dev, (token_ids, "token_ids", (T,), torch.int32), (dW, "dW", (vocab, h), dX.dtype))
-    dW = torch.empty((vocab, h), dtype=dX.dtype, device=dX.device) if dW is None else dW
-    ws = _workspace(workspace, lib.psattn_embed_bwd_workspace_bytes(dt, T, vocab, h), dX, stream)
+    side = _side(stream, dX.device)
+    dW = _make(side, (vocab, h), dX.dtype, dX.device) if dW is None else dW
+    ws = _workspace(workspace, lib.psattn_embed_bwd_workspace_bytes(dt, T, vocab, h), dX, side)
     st = lib.psattn_embed_bwd(dt, T, vocab, h, float(scale), token_ids.data_ptr(), dX.data_ptr(), dW.data_ptr(), ws.data_ptr(),
                               ws.numel() * ws.element_size(), _stream_ptr(stream))
     _check(st, "psattn_embed_bwd")
@@ -658,11 +691,12 @@ def psattn_layernorm_fwd(X, weight, bias=None, eps=1e-5, residual=None, S=None, 
         raise ValueError("S is an output of the residual sum: without a residual it is X")
     _check_all(dev, (weight, "weight", (h,), dtype), (bias, "bias", (h,), dtype), (residual, "residual", shape, dtype), (S, "S", shape, dtype),
                (Y, "Y", shape, dtype), (mean, "mean", (n,), f32), (rstd, "rstd", (n,), f32))
+    side = _side(stream, X.device)
     if residual is not None and S is None:
-        S = torch.empty_like(X)
-    Y = torch.empty_like(X) if Y is None else Y
-    mean = torch.empty(n, dtype=f32, device=X.device) if mean is None else mean
-    rstd = torch.empty(n, dtype=f32, device=X.device) if rstd is None else rstd
+        S = _make(side, shape, dtype, X.device)
+    Y = _make(side, shape, dtype, X.device) if Y is None else Y
+    mean = _make(side, n, f32, X.device) if mean is None else mean
+    rstd = _make(side, n, f32, X.device) if rstd is None else rstd
     st = lib.psattn_layernorm_fwd(dt, n, h, float(eps), X.data_ptr(), None if residual is None else residual.data_ptr(), weight.data_ptr(),
                                   None if bias is None else bias.data_ptr(), None if residual is None else S.data_ptr(), Y.data_ptr(),
                                   mean.data_ptr(), rstd.data_ptr(), _stream_ptr(stream))
@@ -683,11 +717,12 @@ def psattn_layernorm_bwd(S, weight, mean, rstd, dY, dS=None, bias=True, dX=None,
             raise ValueError("%s is missing" % name)
     _check_all(dev, (weight, "weight", (h,), dtype), (mean, "mean", (n,), f32), (rstd, "rstd", (n,), f32), (dY, "dY", shape, dtype),
                (dS, "dS", shape, dtype), (dX, "dX", shape, dtype), (dweight, "dweight", (h,), dtype), (dbias, "dbias", (h,), dtype))
-    dX = torch.empty_like(S) if dX is None else dX
-    dweight = torch.empty_like(weight) if dweight is None else dweight
+    side = _side(stream, S.device)
+    dX = _make(side, shape, dtype, S.device) if dX is None else dX
+    dweight = _make(side, h, dtype, S.device) if dweight is None else dweight
     if bias and dbias is None:
-        dbias = torch.empty_like(weight)
-    ws = _workspace(workspace, lib.psattn_layernorm_bwd_workspace_bytes(n, h), S, stream)
+        dbias = _make(side, h, dtype, S.device)
+    ws = _workspace(workspace, lib.psattn_layernorm_bwd_workspace_bytes(n, h), S, side)
     st = lib.psattn_layernorm_bwd(dt, n, h, S.data_ptr(), weight.data_ptr(), mean.data_ptr(), rstd.data_ptr(), dY.data_ptr(),
                                   None if dS is None else dS.data_ptr(), dX.data_ptr(), dweight.data_ptr(),
                                   dbias.data_ptr() if bias else None, ws.data_ptr(), ws.numel() * ws.element_size(), _stream_ptr(stream))
@@ -713,11 +748,10 @@ def psattn_ffn_fwd(X, Wg, Wu, Wd, act="silu", keep=True, Y=None, kept=None, work
     torch, lib = _TORCH or _torch(), _LIB or load_library()
     dev, T, h, n, dt, tensors = _ffn_shapes(X, Wg, Wu, Wd, act)
     G, U, H = kept if kept is not None else (None, None, None)
+    side = _side(stream, X.device)
     if kept is None:
-        G, U = (torch.empty((T, n), dtype=torch.float32, device=X.device) for _ in range(2)) if keep else (None, None)
-        H = torch.empty((T, n), dtype=X.dtype, device=X.device)
-        if stream is not None and not keep:  # H goes back to torch when this call returns
-            H.record_stream(stream if not isinstance(stream, int) else torch.cuda.ExternalStream(stream, device=X.device))
+        G, U = (_make(side, (T, n), torch.float32, X.device) for _ in range(2)) if keep else (None, None)
+        H = (_make if keep else _scratch)(side, (T, n), X.dtype, X.device)  # without `keep` it ends with this call
     elif H is None or (keep and (G is None or U is None)):
         raise ValueError("kept must hold G, U and H, or with keep=False H alone")
     if not keep:
@@ -725,8 +759,8 @@ def psattn_ffn_fwd(X, Wg, Wu, Wd, act="silu", keep=True, Y=None, kept=None, work
     if kept is not None:
         tensors += [(G, "G", (T, n), torch.float32), (U, "U", (T, n), torch.float32), (H, "H", (T, n), X.dtype)]
     _check_all(dev, *tensors, (Y, "Y", X.shape, X.dtype))
-    Y = torch.empty_like(X) if Y is None else Y
-    ws = _workspace(workspace, lib.psattn_ffn_fwd_workspace_bytes(dt, T, h, n), X, stream)
+    Y = _make(side, X.shape, X.dtype, X.device) if Y is None else Y
+    ws = _workspace(workspace, lib.psattn_ffn_fwd_workspace_bytes(dt, T, h, n), X, side)
     st = lib.psattn_ffn_fwd(dt, _ACTS[act], T, h, n, X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(),
                             G.data_ptr() if keep else None, U.data_ptr() if keep else None, H.data_ptr(), Y.data_ptr(), ws.data_ptr(),
                             ws.numel() * ws.element_size(), _stream_ptr(stream))
@@ -743,11 +777,12 @@ def psattn_ffn_bwd(X, Wg, Wu, Wd, kept, dY, act="silu", dX=None, dWg=None, dWu=N
         raise ValueError("kept G, U, H (psattn_ffn_fwd without them has keep=False) and dY are needed")
     _check_all(dev, *tensors, (G, "G", (T, n), torch.float32), (U, "U", (T, n), torch.float32), (H, "H", (T, n), X.dtype), (dY, "dY", X.shape, X.dtype),
                (dX, "dX", X.shape, X.dtype), (dWg, "dWg", (n, h), X.dtype), (dWu, "dWu", (n, h), X.dtype), (dWd, "dWd", (h, n), X.dtype))
-    dX = torch.empty_like(X) if dX is None else dX
-    dWg = torch.empty_like(Wg) if dWg is None else dWg
-    dWu = torch.empty_like(Wu) if dWu is None else dWu
-    dWd = torch.empty_like(Wd) if dWd is None else dWd
-    ws = _workspace(workspace, lib.psattn_ffn_bwd_workspace_bytes(dt, T, h, n), X, stream)
+    side = _side(stream, X.device)
+    dX = _make(side, X.shape, X.dtype, X.device) if dX is None else dX
+    dWg = _make(side, (n, h), X.dtype, X.device) if dWg is None else dWg
+    dWu = _make(side, (n, h), X.dtype, X.device) if dWu is None else dWu
+    dWd = _make(side, (h, n), X.dtype, X.device) if dWd is None else dWd
+    ws = _workspace(workspace, lib.psattn_ffn_bwd_workspace_bytes(dt, T, h, n), X, side)
     st = lib.psattn_ffn_bwd(dt, _ACTS[act], T, h, n, X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(), G.data_ptr(), U.data_ptr(),
                             H.data_ptr(), dY.data_ptr(), dX.data_ptr(), dWg.data_ptr(), dWu.data_ptr(), dWd.data_ptr(), ws.data_ptr(),
                             ws.numel() * ws.element_size(), _stream_ptr(stream))
