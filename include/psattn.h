@@ -391,15 +391,18 @@ int psattn_dpo_loss(int32_t n_pairs, float beta, const float* logp_policy, const
  * computed like any row, and keeps to itself.  All tensors are contiguous, row-major, of element type dt unless said otherwise;
  * they may start wherever an element may and have any width, 16-byte boundaries and widths that are whole 16-byte groups
  * being faster.  Any value is taken: inf and NaN reach the rows that read them and no others.  All sums are fp32, in an order
- * that depends on the sizes alone: the same call gives the same bits.  Workspaces are the caller's device memory, of at least
+ * that the sizes, the token ids and the tensors' places relative to 16-byte boundaries decide: the same call gives the same bits, the
+ * same values elsewhere may differ in the last ones.  Workspaces are the caller's device memory, of at least
  * the bytes that the call of that name gives (never 0 for valid arguments), contents undefined on entry and exit, one for
  * each call in flight.  No call allocates or blocks, and all may be captured into a graph.  No rows: the forward calls
  * do nothing, the backward calls write zeros as the gradients of weights.
  *
  * psattn_embed_fwd: X[t, :] = scale * W[token_ids[t], :], W [vocab, hidden], X [n_tokens, hidden], token_ids device int32.  An
  * id outside [0, vocab) (padding) gives a row of zeros.
- * psattn_embed_bwd: dW[v, :] = scale * sum of dX[t, :] over the tokens with id v, taken in order of the tokens; dW
- * [vocab, hidden] is written as a whole, zeros included.  Ids outside [0, vocab) give nothing, and their rows of dX are not read.
+ * psattn_embed_bwd: dW[v, :] = scale * sum of dX[t, :] over the tokens with id v; dW [vocab, hidden] is written as a whole, zeros
+ * included.  Ids outside [0, vocab) give nothing, and their rows of dX are not read.  The tokens, sorted by id, are added up in
+ * pieces of one size, within a piece in their own order; the sums of a row that reaches over several pieces are then joined in a fixed
+ * order.  Where pieces are cut depends on all ids: so do the last bits of such a row.
  * PSATTN_EUNSUPPORTED: more than 2^24 tokens, hidden over 2^23, or sizes whose grids would have 2^31 threads.
  */
 int psattn_embed_fwd(int32_t dt, int32_t n_tokens, int32_t vocab, int32_t hidden, float scale, const int32_t* token_ids,

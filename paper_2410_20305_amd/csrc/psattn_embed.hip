@@ -1,10 +1,12 @@
 // Embedding rows by token id, scaled, and the gradient of the table.
-//   X[t] = scale W[id_t],  dW[v] = scale sum of dX[t] over the tokens t with id_t = v, in the order of the tokens, in fp32
+//   X[t] = scale W[id_t],  dW[v] = scale sum of dX[t] over the tokens t with id_t = v, in fp32
 // A token whose id is not in [0, vocab) (padding) has a row of zeros and gives no gradient.
 //
 // Both are bound by HBM.  The gradient sorts the tokens by id (stable, so that a row's tokens stay in their order), cuts the sorted
 // tokens into pieces of one size, whatever ids they have, and adds up runs of one id within a piece: a frequent id is many
-// pieces' work and a rare one no workgroup's own.  Runs that reach past a piece leave fp32 sums, which are joined in order.
+// pieces' work and a rare one no workgroup's own.  Within a piece a row's tokens are added one by one in their order.  Runs that reach
+// past a piece leave fp32 sums, which are joined in an order of their own (psattn_embed_join): ids and sizes decide it, and which
+// ids the other tokens have decides where pieces are cut.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -256,8 +258,8 @@ __global__ __launch_bounds__(kThreads) void psattn_embed_sum(int n, int vocab, i
     }
 }
 
-// The run that a piece's last token starts and the next pieces go on with, 256 columns of it: four waves take every fourth piece, then
-// add up in order
+// The run that a piece's last token starts and the next pieces go on with, 256 columns of it: with q_0, q_1, ... the pieces' sums of it,
+// wave w adds q_w, q_(w+4), q_(w+8), ... one by one, and the row is ((wave 0 + wave 1) + wave 2) + wave 3
 template <typename E>
 __global__ __launch_bounds__(kThreads) void psattn_embed_join(int n, int vocab, int hidden, float scale, const int32_t* keys, const float* edge, E* dW, int size) {
     __shared__ float4 sm[3][64];
