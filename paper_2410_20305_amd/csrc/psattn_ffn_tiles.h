@@ -51,7 +51,8 @@ struct Copy {
     static constexpr int PER = ROWS * 128 / 1024 / NW, EPC = kChunk<E>;
     static constexpr int kBias = ASYNC || KC ? 0 : 16;  // bytes: a chunk may be read from up to one before the tile's first column
     uint32_t off[PER];
-    int shift[ASYNC || KC ? 1 : PER];  // bits
+    static constexpr int kShifts = sizeof(E) == 2 ? 4 : 1;  // chunks whose shifts, in bits, share a register
+    uint32_t shift[ASYNC || KC ? 1 : (PER + kShifts - 1) / kShifts];
     uint4 r[ASYNC ? 1 : PER];
     bool edge, tiny;  // the tile reaches past the rows' ends; rows shorter than a chunk
     int in_row;
@@ -61,6 +62,7 @@ struct Copy {
         edge = !KC && r0 + ROWS > n_rows;
         tiny = !KC && n_rows < EPC;
         in_row = n_rows - r0;
+        for (uint32_t& s : shift) s = 0;
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
             const int q = w * PER + j;
@@ -75,7 +77,7 @@ struct Copy {
                 if constexpr (ASYNC) {
                     at = min(col, in_row / EPC * EPC - EPC);
                 } else {
-                    shift[j] = col < in_row ? (col - at) * static_cast<int>(sizeof(E)) * 8 : 0;
+                    shift[j / kShifts] |= static_cast<uint32_t>(col < in_row ? (col - at) * static_cast<int>(sizeof(E)) * 8 : 0) << (8 * (j % kShifts));
                     if (tiny) at = 0;
                 }
                 off[j] = static_cast<uint32_t>((row * ld + at) * static_cast<int64_t>(sizeof(E)) + kBias);
@@ -98,7 +100,14 @@ struct Copy {
         if constexpr (!ASYNC) {
             uint4 u = r[J];
             if constexpr (!KC)
-                if (edge && !tiny) u = shift_down(u, shift[J]);
+                if (edge && !tiny) {
+                    uint32_t s = shift[J / kShifts];
+                    if constexpr (kShifts > 1) {
+                        asm("" : "+v"(s));  // taken apart ahead of the loop, it would hold four registers there again
+                        s = s >> (8 * (J % kShifts)) & 255;
+                    }
+                    u = shift_down(u, s);
+                }
             *reinterpret_cast<uint4*>(tile + (w * PER + J) * 1024 + 16 * l) = u;
         }
     }
@@ -369,13 +378,20 @@ __global__ __launch_bounds__(S::kThreads, 2) void psattn_ffn_tiles(Product d, in
         }
         if (ahead == 0) tile(std::integral_constant<int, 0>{}, 0, NBQ == 2 ? 0 : q0, NBQ == 2 ? 1 : q1, NBQ == 2 ? 0 : q2);
     }
+    // With both operands k-major and through registers the lane is asked for again: kept over the loop, it and what is made of it would spill
+    constexpr bool kAskAgain = !ASYNC && !PKC && sizeof(E) == 2;
+    int le = l, te = threadIdx.x;
+    if constexpr (kAskAgain) {
+        le = static_cast<int>(__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0)));
+        te = 64 * w + le;
+    }
     if (const int rest = per_seg * kBk; rest < d.K && part == d.n_split - 1) {  // what is left of k, zeros behind it
         for (int seg = 0; seg < d.n_seg; ++seg) {
             __syncthreads();
-            for (int c = threadIdx.x; c < S::BM * 8; c += S::kThreads)
+            for (int c = te; c < S::BM * 8; c += S::kThreads)
                 *reinterpret_cast<uint4*>(ptile + chunk_off<E, PKC, S::BM>(c)) =
                     fetch<E, PKC, S::BM>(c, d.ldp, rest, d.K, m0, d.M, [&](int r) { return std::make_pair(d.p[d.n_prod > 1 ? z : seg], m0 + r); });
-            for (int c = threadIdx.x; c < S::BN * 8; c += S::kThreads)
+            for (int c = te; c < S::BN * 8; c += S::kThreads)
                 *reinterpret_cast<uint4*>(qtile + chunk_off<E, QKC, S::BN>(c)) = fetch<E, QKC, S::BN>(c, d.ldq, rest, d.K, n0, d.N, [&](int r) {
                     if constexpr (PASS == kGate) return std::make_pair(d.q[(r >> 5) & 1], n0 + (r >> 6) * 32 + (r & 31));
                     else return std::make_pair(d.q[seg], n0 + r);
@@ -407,8 +423,8 @@ __global__ __launch_bounds__(S::kThreads, 2) void psattn_ffn_tiles(Product d, in
             if (!place(i, m, n, rows, cols)) return;
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const int c = min(16 * k + 8 * (l >> 5), (cols - 1) / 8 * 8);
-                const int64_t from = (m + min(l & 31, rows - 1)) * d.ld_kept + n + c;
+                const int c = min(16 * k + 8 * (le >> 5), (cols - 1) / 8 * 8);
+                const int64_t from = (m + min(le & 31, rows - 1)) * d.ld_kept + n + c;
                 g[set][k].get(d.G + from, cols - c);
                 u[set][k].get(d.U + from, cols - c);
             }
@@ -432,8 +448,8 @@ __global__ __launch_bounds__(S::kThreads, 2) void psattn_ffn_tiles(Product d, in
                 }
             }
             const int64_t at = m * d.ldo + n;
-            store_out<ASYNC>(static_cast<E*>(d.out[0]) + at, d.ldo, rows, cols, dg, l, d.odd);
-            store_out<ASYNC>(static_cast<E*>(d.out[1]) + at, d.ldo, rows, cols, du, l, d.odd);
+            store_out<ASYNC>(static_cast<E*>(d.out[0]) + at, d.ldo, rows, cols, dg, le, d.odd);
+            store_out<ASYNC>(static_cast<E*>(d.out[1]) + at, d.ldo, rows, cols, du, le, d.odd);
             __builtin_amdgcn_sched_barrier(0);
         });
         return;
@@ -449,7 +465,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void psattn_ffn_tiles(Product d, in
                 const int which = PASS == kGate ? nb : z, n = n0 + (PASS == kGate ? wn : wn * NB + nb) * 32, cols = d.N - n;
                 if (cols <= 0) break;
                 const int64_t at = ((static_cast<int64_t>(part) * (PASS == kGate ? 2 : d.n_prod) + which) * d.M + m) * d.ld_part + n;
-                store_chunks<true>(d.parts + at, d.ld_part, rows, cols, chunks(acc[nb][mb]), l);
+                store_chunks<true>(d.parts + at, d.ld_part, rows, cols, chunks(acc[nb][mb]), le);
             }
         } else if constexpr (PASS == kGate) {
             const int n = n0 + wn * 32, cols = d.N - n;
@@ -458,15 +474,15 @@ __global__ __launch_bounds__(S::kThreads, 2) void psattn_ffn_tiles(Product d, in
             f32x16 h;
 #pragma unroll
             for (int i = 0; i < 16; ++i) h[i] = act<E, ACT>(acc[0][mb][i]) * acc[1][mb][i];
-            if (d.G) store_chunks<false>(d.G + at, d.ldo, rows, cols, chunks(acc[0][mb]), l);
-            if (d.U) store_chunks<false>(d.U + at, d.ldo, rows, cols, chunks(acc[1][mb]), l);
-            store_out<ASYNC>(static_cast<E*>(d.H) + at, d.ldo, rows, cols, chunks(h), l, d.odd);
+            if (d.G) store_chunks<false>(d.G + at, d.ldo, rows, cols, chunks(acc[0][mb]), le);
+            if (d.U) store_chunks<false>(d.U + at, d.ldo, rows, cols, chunks(acc[1][mb]), le);
+            store_out<ASYNC>(static_cast<E*>(d.H) + at, d.ldo, rows, cols, chunks(h), le, d.odd);
         } else if constexpr (PASS == kPlain) {
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
                 const int n = n0 + (wn * NB + nb) * 32, cols = d.N - n;
                 if (cols <= 0) break;
-                store_out<ASYNC>(static_cast<E*>(d.out[d.n_prod > 1 ? z : 0]) + m * d.ldo + n, d.ldo, rows, cols, chunks(acc[nb][mb]), l, d.odd);
+                store_out<ASYNC>(static_cast<E*>(d.out[d.n_prod > 1 ? z : 0]) + m * d.ldo + n, d.ldo, rows, cols, chunks(acc[nb][mb]), le, d.odd);
             }
         }
     }

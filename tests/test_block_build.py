@@ -1,0 +1,15 @@
+"""Static checks on the compiled kernels of what stands beside attention (CPU only: hipcc cross-compiles gfx950): none keeps a
+register in memory, where a loop would fetch it each time."""
+import pytest
+
+from test_kernel_build import _asm, _kernels
+
+
+def _nothing_in_memory(kernels):
+    for name, _, meta in kernels:
+        assert int(meta["vgpr_spill_count"]) == 0 and int(meta["private_segment_fixed_size"]) == 0, name
+
+
+@pytest.mark.parametrize("src", ["psattn_ffn_bf16_any.hip", "psattn_ffn_f32.hip"])
+def test_products_of_any_alignment_and_of_fp32(tmp_path, src):
+    _nothing_in_memory(_kernels(_asm(tmp_path, src), "psattn_ffn_tiles", 26))
