@@ -115,7 +115,7 @@ __global__ __launch_bounds__(kThreads<LANES>) void psattn_ln_fwd(int n_rows, int
 // Rows stay in the registers as they came and are unpacked twice, which leaves room for the next row's loads while one is
 // summed over the lanes (8 334 rows of 4 096 bf16 with dS 105 -> 70 us, 65 536 of 1 024 198 -> 84).
 //   Without SUMS a workgroup has one row, and dw and db are left to psattn_ln_columns: 32 columns to a lane and their sums do not
-// fit beside a row (20 000 rows of 16 384 bf16, sums in registers and in part spilled 665 - 1 650 us, apart 642).
+// fit beside a row (20 000 rows of 16 384 bf16, sums in registers and in part spilled 665 - 1 650 us, apart 616).
 template <typename E, int LANES, int PER, bool WHOLE, bool SUMS>
 __global__ __launch_bounds__(kThreads<LANES>) void psattn_ln_bwd(int n_rows, int hidden, const E* S, const E* w, const float* mean, const float* rstd, const E* dY,
                                                                  const E* dS, E* dX, float* part) {
@@ -192,6 +192,7 @@ __global__ __launch_bounds__(kThreads<LANES>) void psattn_ln_bwd(int n_rows, int
             for (int j = 0; j < V; ++j) o[j] += rs * (g[j] * wv[j] - m1 - x[j] * m2);
             store<WHOLE>(dX + at, from + p * LANES * V, hidden, o);
         }
+        if constexpr (!SUMS) return;  // its one row: nothing is kept for another
         if constexpr (kAhead) {
 #pragma unroll
             for (int p = 0; p < PER; ++p) { xr[p] = xn[p]; gr[p] = gn[p]; sr[p] = sn[p]; }
@@ -441,7 +442,7 @@ void bwd(int32_t n_rows, int32_t hidden, const void* S_, const void* w_, const f
         bool sums = false;
         const bool done = sized<E, true>(hidden, all, [&](auto lanes, auto per) {
             constexpr int L = decltype(lanes)::value, PER = decltype(per)::value, kAt = kThreads<L> / L;
-            constexpr bool SUMS = PER * kVec<E> < 32;  // up to 1 024 groups
+            constexpr bool SUMS = PER * kVec<E> < 32;  // up to 1 024 groups of bf16, 2 048 of fp32
             if (SUMS) np = std::min(np, (n_rows + kAt - 1) / kAt);
             if (np > 8) np -= np % 8;  // a workgroup's rows start alike
             sums = SUMS;

@@ -13,3 +13,8 @@ def _nothing_in_memory(kernels):
 @pytest.mark.parametrize("src", ["psattn_ffn_bf16_any.hip", "psattn_ffn_f32.hip"])
 def test_products_of_any_alignment_and_of_fp32(tmp_path, src):
     _nothing_in_memory(_kernels(_asm(tmp_path, src), "psattn_ffn_tiles", 26))
+
+
+def test_layer_norm_backward(tmp_path):
+    text = _asm(tmp_path, "psattn_layernorm.hip")
+    _nothing_in_memory(_kernels(text, "psattn_ln_bwd", text.count(".amdhsa_kernel _ZN12_GLOBAL__N_113psattn_ln_bwd")))
