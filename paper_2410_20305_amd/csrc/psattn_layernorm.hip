@@ -447,7 +447,8 @@ void bwd(int32_t n_rows, int32_t hidden, const void* S_, const void* w_, const f
             if (np > 8) np -= np % 8;  // a workgroup's rows start alike
             sums = SUMS;
             auto go = [&](auto kernel) { kernel<<<SUMS ? np : n_rows, kThreads<L>, 0, s>>>(n_rows, hidden, S, w, mean, rstd, dY, dS, dX, part); };
-            all ? go(psattn_ln_bwd<E, L, PER, true, SUMS>) : go(psattn_ln_bwd<E, L, PER, false, SUMS>);
+            if constexpr (L == 256 && PER == 3) go(psattn_ln_bwd<E, L, PER, true, SUMS>);  // whole rows alone: `sized`
+            else all ? go(psattn_ln_bwd<E, L, PER, true, SUMS>) : go(psattn_ln_bwd<E, L, PER, false, SUMS>);
         });
         if (!done) psattn_ln_bwd_wide<E><<<n_rows, 1024, 0, s>>>(hidden, S, w, mean, rstd, dY, dS, dX);
         if (!sums) {

@@ -18,3 +18,9 @@ def test_products_of_any_alignment_and_of_fp32(tmp_path, src):
 def test_layer_norm_backward(tmp_path):
     text = _asm(tmp_path, "psattn_layernorm.hip")
     _nothing_in_memory(_kernels(text, "psattn_ln_bwd", text.count(".amdhsa_kernel _ZN12_GLOBAL__N_113psattn_ln_bwd")))
+
+
+def test_no_kernel_that_no_call_reaches(tmp_path):
+    """The layer norm's rows of 513 to 768 groups have a backward of their own where they are whole groups, and no other."""
+    names = [name for name, _, _ in _kernels(_asm(tmp_path, "psattn_layernorm.hip"), "psattn_ln_bwd", 38)]
+    assert not any("Li256ELi3ELb0E" in name for name in names) and sum("Li256ELi3ELb1E" in name for name in names) == 2
