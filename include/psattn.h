@@ -391,8 +391,8 @@ int psattn_dpo_loss(int32_t n_pairs, float beta, const float* logp_policy, const
  * computed like any row, and keeps to itself.  All tensors are contiguous, row-major, of element type dt unless said otherwise;
  * they may start wherever an element may and have any width, 16-byte boundaries and widths that are whole 16-byte groups
  * being faster.  Any value is taken: inf and NaN reach the rows that read them and no others.  All sums are fp32, in an order
- * that the sizes, the token ids and the tensors' places relative to 16-byte boundaries decide: the same call gives the same bits, the
- * same values elsewhere may differ in the last ones.  Workspaces are the caller's device memory, of at least
+ * that the sizes, the token ids, the tensors' places relative to 16-byte boundaries and what a workspace has room for decide: the same
+ * call gives the same bits, the same values elsewhere may differ in the last ones.  Workspaces are the caller's device memory, of at least
  * the bytes that the call of that name gives (never 0 for valid arguments), contents undefined on entry and exit, one for
  * each call in flight.  No call allocates or blocks, and all may be captured into a graph.  No rows: the forward calls
  * do nothing, the backward calls write zeros as the gradients of weights.
@@ -431,16 +431,22 @@ int psattn_layernorm_bwd(int32_t dt, int32_t n_rows, int32_t hidden, const void*
  * [hidden, inner], the [out_features, in_features] convention of the attention layer.  G, U (float) and H (dt), [n_tokens, inner], are
  * kept for the backward; G and U may both be NULL if none follows, H is needed either way.  H is rounded once, from the fp32 sums.
  * Rows of 2^23 bytes and more are refused with PSATTN_EUNSUPPORTED.
- * psattn_ffn_bwd: dX, dWg, dWu, dWd from the forward's G, U, H and dY.
+ * psattn_ffn_bwd: dX, dWg, dWu, dWd from the forward's G, U, H and dY.  The gradients of H with respect to G and U are
+ * operands of its products, and like H they are rounded to dt once, from fp32.
+ * Workspaces: psattn_ffn_..._workspace_bytes has room for the copies that bf16 calls of 320 tokens and more make of tensors whose
+ * width is no multiple of 8.  Where tensors of other widths start off a 16-byte boundary, such calls take up to 1.5 times as long,
+ * unless the workspace has psattn_ffn_..._unaligned_workspace_bytes, which is never less: then these are copied too.
  */
 int psattn_ffn_fwd(int32_t dt, int32_t act, int32_t n_tokens, int32_t hidden, int32_t inner, const void* X, const void* Wg,
                    const void* Wu, const void* Wd, float* G, float* U, void* H, void* Y, void* workspace,
                    size_t workspace_bytes, void* hip_stream);
 size_t psattn_ffn_fwd_workspace_bytes(int32_t dt, int32_t n_tokens, int32_t hidden, int32_t inner);
+size_t psattn_ffn_fwd_unaligned_workspace_bytes(int32_t dt, int32_t n_tokens, int32_t hidden, int32_t inner);
 int psattn_ffn_bwd(int32_t dt, int32_t act, int32_t n_tokens, int32_t hidden, int32_t inner, const void* X, const void* Wg,
                    const void* Wu, const void* Wd, const float* G, const float* U, const void* H, const void* dY, void* dX,
                    void* dWg, void* dWu, void* dWd, void* workspace, size_t workspace_bytes, void* hip_stream);
 size_t psattn_ffn_bwd_workspace_bytes(int32_t dt, int32_t n_tokens, int32_t hidden, int32_t inner);
+size_t psattn_ffn_bwd_unaligned_workspace_bytes(int32_t dt, int32_t n_tokens, int32_t hidden, int32_t inner);
 
 /*
  * Measurement aid (no part of the computation): issues the memory operations that a

@@ -28,6 +28,7 @@ EXPORTS = [
     "psattn_embed_fwd", "psattn_embed_bwd", "psattn_embed_bwd_workspace_bytes",
     "psattn_layernorm_fwd", "psattn_layernorm_bwd", "psattn_layernorm_bwd_workspace_bytes",
     "psattn_ffn_fwd", "psattn_ffn_bwd", "psattn_ffn_fwd_workspace_bytes", "psattn_ffn_bwd_workspace_bytes",
+    "psattn_ffn_fwd_unaligned_workspace_bytes", "psattn_ffn_bwd_unaligned_workspace_bytes",
 ]
 
 ACT_SILU, ACT_GELU = 0, 1
@@ -82,10 +83,11 @@ def load_library():
     lib.psattn_layernorm_bwd_workspace_bytes.argtypes = [i32, i32]
     lib.psattn_ffn_fwd.argtypes = [i32] * 5 + [vp] * 9 + [C.c_size_t, vp]
     lib.psattn_ffn_bwd.argtypes = [i32] * 5 + [vp] * 13 + [C.c_size_t, vp]
-    for name in ("psattn_ffn_fwd_workspace_bytes", "psattn_ffn_bwd_workspace_bytes"):
+    ffn_bytes = ("psattn_ffn_fwd_workspace_bytes", "psattn_ffn_bwd_workspace_bytes", "psattn_ffn_fwd_unaligned_workspace_bytes",
+                 "psattn_ffn_bwd_unaligned_workspace_bytes")
+    for name in ffn_bytes:
         getattr(lib, name).argtypes = [i32] * 4
-    for name in ("psattn_embed_bwd_workspace_bytes", "psattn_layernorm_bwd_workspace_bytes", "psattn_ffn_fwd_workspace_bytes",
-                 "psattn_ffn_bwd_workspace_bytes"):
+    for name in ("psattn_embed_bwd_workspace_bytes", "psattn_layernorm_bwd_workspace_bytes", *ffn_bytes):
         getattr(lib, name).restype = C.c_size_t
     lib.psattn_free_meta.argtypes = [vp]
     lib.psattn_free_meta_async.argtypes = [vp, vp]
@@ -742,6 +744,14 @@ def _ffn_shapes(X, Wg, Wu, Wd, act):
     return dev, T, h, n, _dtype_code(X), [(Wg, "Wg", (n, h), dtype), (Wu, "Wu", (n, h), dtype), (Wd, "Wd", (h, n), dtype)]
 
 
+def _off_boundary(*tensors):
+    """Whether one of them starts off a 16-byte boundary."""
+    a = 0
+    for t in tensors:
+        a |= t.data_ptr()
+    return a & 15 != 0
+
+
 def psattn_ffn_fwd(X, Wg, Wu, Wd, act="silu", keep=True, Y=None, kept=None, workspace=None, stream=None):
     """Y, kept = (act(X Wg^T) o (X Wu^T)) Wd^T.  `kept` = (G, U, H), [T, inner] each, G and U float32, is what the backward takes;
     with keep=False G and U are not written and None is returned in its place (`kept` may then give H alone, as (None, None, H))."""
@@ -760,7 +770,8 @@ def psattn_ffn_fwd(X, Wg, Wu, Wd, act="silu", keep=True, Y=None, kept=None, work
         tensors += [(G, "G", (T, n), torch.float32), (U, "U", (T, n), torch.float32), (H, "H", (T, n), X.dtype)]
     _check_all(dev, *tensors, (Y, "Y", X.shape, X.dtype))
     Y = _make(side, X.shape, X.dtype, X.device) if Y is None else Y
-    ws = _workspace(workspace, lib.psattn_ffn_fwd_workspace_bytes(dt, T, h, n), X, side)
+    need = lib.psattn_ffn_fwd_unaligned_workspace_bytes if _off_boundary(X, Wg, Wu, Wd, H) else lib.psattn_ffn_fwd_workspace_bytes
+    ws = _workspace(workspace, need(dt, T, h, n), X, side)
     st = lib.psattn_ffn_fwd(dt, _ACTS[act], T, h, n, X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(),
                             G.data_ptr() if keep else None, U.data_ptr() if keep else None, H.data_ptr(), Y.data_ptr(), ws.data_ptr(),
                             ws.numel() * ws.element_size(), _stream_ptr(stream))
@@ -782,7 +793,8 @@ def psattn_ffn_bwd(X, Wg, Wu, Wd, kept, dY, act="silu", dX=None, dWg=None, dWu=N
     dWg = _make(side, (n, h), X.dtype, X.device) if dWg is None else dWg
     dWu = _make(side, (n, h), X.dtype, X.device) if dWu is None else dWu
     dWd = _make(side, (h, n), X.dtype, X.device) if dWd is None else dWd
-    ws = _workspace(workspace, lib.psattn_ffn_bwd_workspace_bytes(dt, T, h, n), X, side)
+    need = lib.psattn_ffn_bwd_unaligned_workspace_bytes if _off_boundary(X, Wg, Wu, Wd, H, dY) else lib.psattn_ffn_bwd_workspace_bytes
+    ws = _workspace(workspace, need(dt, T, h, n), X, side)
     st = lib.psattn_ffn_bwd(dt, _ACTS[act], T, h, n, X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(), G.data_ptr(), U.data_ptr(),
                             H.data_ptr(), dY.data_ptr(), dX.data_ptr(), dWg.data_ptr(), dWu.data_ptr(), dWd.data_ptr(), ws.data_ptr(),
                             ws.numel() * ws.element_size(), _stream_ptr(stream))

@@ -34,11 +34,11 @@ bool at16(std::initializer_list<const void*> p) {
     return a % 16 == 0;
 }
 
-// Every row of P, Q and out a whole number of 16-byte groups on 16-byte boundaries
-bool whole_rows(bool pkc, const Product& d) {
-    return at16({d.p[0], d.p[1], d.q[0], d.q[1], d.out[0], d.out[1], d.G, d.U, d.H}) && d.ldp % 8 == 0 && d.ldq % 8 == 0 && d.ldo % 8 == 0 && d.N % 8 == 0 &&
-           (pkc || d.M % 8 == 0);
+// Every row of P and Q a whole number of 16-byte groups on 16-byte boundaries; what is stored in the element type likewise
+bool whole_operands(bool pkc, bool qkc, const Product& d) {
+    return at16({d.p[0], d.p[1], d.q[0], d.q[1]}) && d.ldp % 8 == 0 && d.ldq % 8 == 0 && (pkc || d.m_load % 8 == 0) && (qkc || d.n_load % 8 == 0);
 }
+bool whole_results(const Product& d) { return at16({d.out[0], d.out[1], d.H}) && d.ldo % 8 == 0 && d.N % 8 == 0; }
 
 struct Plan {
     TileSize size;
@@ -96,14 +96,18 @@ Plan plan(Move move, Pass pass, bool pkc, int64_t M, int64_t N, int64_t K, int n
 
 int64_t ld_part(int64_t N) { return (N + 7) / 8 * 8; }
 
-// room for a product's parts, whichever way its operands turn out to move
-size_t part_bytes(int32_t dt, Pass pass, bool pkc, int64_t M, int64_t N, int64_t K, int n_seg, int n_prod) {
+// bytes of one of a product's parts
+size_t one_part(Pass pass, int64_t M, int64_t N, int n_prod) { return sizeof(float) * (pass == kGate ? 2 : n_prod) * static_cast<size_t>(M) * static_cast<size_t>(ld_part(N)); }
+
+// room for a product's parts; `any`: whichever way its operands turn out to move
+size_t part_bytes(int32_t dt, bool any, Pass pass, bool pkc, int64_t M, int64_t N, int64_t K, int n_seg, int n_prod) {
     if (M == 0 || K == 0) return 0;  // no tokens: no products
     auto room = [&](Move move) {
         const Plan p = plan(move, pass, pkc, M, N, K, n_seg, n_prod);
-        return p.split > 1 ? sizeof(float) * p.split * (pass == kGate ? 2 : n_prod) * M * ld_part(N) : size_t{0};
+        return p.split > 1 ? p.split * one_part(pass, M, N, n_prod) : size_t{0};
     };
-    return dt == PSATTN_BF16 ? std::max(room(kWhole), room(kOdd)) : room(kFloat);
+    if (dt != PSATTN_BF16) return room(kFloat);
+    return any ? std::max(room(kWhole), room(kOdd)) : room(kWhole);
 }
 
 // joins the parts of a product: the epilogue of psattn_ffn_tiles on sums from memory, V columns to a lane (4 where rows allow it: dG and dU of
@@ -192,16 +196,14 @@ void join(Pass pass, int act, const Product& d, hipStream_t s) {
     else act == PSATTN_ACT_SILU ? go(psattn_ffn_join<E, kDact, 0, V>) : go(psattn_ffn_join<E, kDact, 1, V>);
 }
 
-// `parts`: room of part_bytes()
-int product(int32_t dt, Pass pass, int act, bool pkc, bool qkc, Product d, void* parts, hipStream_t s) {
-    if (!d.odd) {
-        d.m_load = d.M;
-        d.n_load = d.N;
-    }
-    const Move move = dt != PSATTN_BF16 ? kFloat : d.odd || whole_rows(pkc, d) ? kWhole : kOdd;
+// `parts`, up to `end`: room of part_bytes(), or, where operands move another way than that was asked for, fewer parts
+int product(int32_t dt, Pass pass, int act, bool pkc, bool qkc, Product d, char* parts, const char* end, hipStream_t s) {
+    d.odd = !whole_results(d);
+    const Move move = dt != PSATTN_BF16 ? kFloat : whole_operands(pkc, qkc, d) ? kWhole : kOdd;
     const Plan p = plan(move, pass, pkc, d.M, d.N, d.K, d.n_seg, d.n_prod);
-    d.n_split = p.split;
-    d.parts = static_cast<float*>(parts);
+    const int64_t fit = (end - parts) / static_cast<int64_t>(one_part(pass, d.M, d.N, d.n_prod));
+    d.n_split = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(p.split, fit)));
+    d.parts = reinterpret_cast<float*>(parts);
     d.ld_part = ld_part(d.N);
     const int rc = (move == kFloat ? product_f32 : move == kWhole ? product_bf16 : product_bf16_any)(pass, act, pkc, qkc, p.size, d, s);
     if (rc != PSATTN_OK || d.n_split == 1) return rc;
@@ -211,10 +213,13 @@ int product(int32_t dt, Pass pass, int act, bool pkc, bool qkc, Product d, void*
     return hipGetLastError() == hipSuccess ? PSATTN_OK : PSATTN_EHIP;
 }
 
-// ---- bf16 rows that are not whole 16-byte groups, made so in the workspace.  The asynchronous copies need such rows; the way through registers
-// does not, but takes 1.5 - 1.7 times as long.  What the rows' copies cost is made good from some 300 tokens on.  Through registers / made
-// whole, forward and backward in us: hidden 4 095, inner 14 335, 300 tokens 1 079 / 1 074, 700 1 638 / 1 396, 1 200 2 659 / 1 921; hidden 1 001,
-// inner 2 731, 150 tokens 116 / 114, 300 137 / 129, 1 037 238 / 187; hidden 2 047, inner 6 001, 3 001 tokens 1 500 / 1 030 (890 on rows that are whole).
+// ---- bf16 rows that are not whole 16-byte groups on boundaries, made so in the workspace.  The asynchronous copies need such rows; the way
+// through registers does not, but takes 1.5 - 1.7 times as long.  What the rows' copies cost is made good from some 300 tokens on.  Through
+// registers / made whole, forward and backward in us: hidden 4 095, inner 14 335, 300 tokens 1 079 / 1 074, 700 1 638 / 1 396, 1 200 2 659 /
+// 1 921; hidden 1 001, inner 2 731, 150 tokens 116 / 114, 300 137 / 129, 1 037 238 / 187; hidden 2 047, inner 6 001, 3 001 tokens 1 500 / 1 030
+// (890 on rows that are whole).  Tensors of a width that is no multiple of 8 always have their room.  Others need it only where they start off a
+// boundary, which sizes do not tell: they are copied where the workspace has been made for that, and go through registers elsewhere (8 192
+// tokens, hidden 4 096, inner 14 336, forward 2 374; all tensors off a boundary 2 524 with copies, 3 881 without; X alone 2 396 and 3 187).
 constexpr int32_t kPadTokens = 320;
 
 struct Pad {
@@ -241,38 +246,55 @@ __global__ __launch_bounds__(256) void psattn_ffn_pad(Pads pads) {
     }
 }
 
-int pad(std::initializer_list<Pad> list, hipStream_t s) {
-    Pads pads{};
-    int n = 0;
-    for (const Pad& p : list) pads.p[n++] = p;
-    psattn_ffn_pad<<<dim3(2048, n), 256, 0, s>>>(pads);
-    return hipGetLastError() == hipSuccess ? PSATTN_OK : PSATTN_EHIP;
-}
+bool may_pad(int32_t dt, int64_t n_tokens) { return dt == PSATTN_BF16 && n_tokens >= kPadTokens; }
 
-// Whether a call's rows are made whole: by sizes alone, for the workspace, and by the tensors' addresses
-bool may_pad(int32_t dt, int32_t n_tokens) { return dt == PSATTN_BF16 && n_tokens >= kPadTokens; }
-
-// Carves a workspace
-struct Carver {
+// Makes rows whole: takes their room from a workspace, and copies them when told to
+struct Wholes {
     char* p;
-    explicit Carver(void* base) : p(reinterpret_cast<char*>(align_up(reinterpret_cast<uintptr_t>(base), 256))) {}
-    uint16_t* take(int64_t rows, int64_t width) {
-        char* const r = p;
-        p += align_up(static_cast<size_t>(rows) * static_cast<size_t>(up8(width)) * 2, 256);
-        return reinterpret_cast<uint16_t*>(r);
+    bool may, roomy;  // whether rows are copied at all; those of whole widths that start off a boundary too
+    Pad list[6];
+    int n = 0;
+    Wholes(void* base, bool may, bool roomy) : p(reinterpret_cast<char*>(align_up(reinterpret_cast<uintptr_t>(base), 256))), may(may), roomy(roomy) {}
+    // the tensor itself where its rows are whole, or may stay as they are; else the place of its copy
+    const void* add(const void* x, int32_t rows, int32_t width) {
+        if (!may || (width % 8 == 0 && (at16({x}) || !roomy))) return x;
+        uint16_t* const to = reinterpret_cast<uint16_t*>(p);
+        p += bytes(rows, width);
+        list[n++] = {static_cast<const uint16_t*>(x), to, rows, width};
+        return to;
+    }
+    static size_t bytes(int64_t rows, int64_t width) { return align_up(static_cast<size_t>(rows) * static_cast<size_t>(up8(width)) * 2, 256); }
+    int copy(hipStream_t s) {
+        if (n == 0) return PSATTN_OK;
+        Pads pads{};
+        std::copy(list, list + n, pads.p);
+        psattn_ffn_pad<<<dim3(2048, n), 256, 0, s>>>(pads);
+        n = 0;
+        return hipGetLastError() == hipSuccess ? PSATTN_OK : PSATTN_EHIP;
     }
 };
-size_t fwd_pad_bytes(int32_t dt, int64_t n_tokens, int64_t hidden, int64_t inner) {
-    if (!may_pad(dt, static_cast<int32_t>(n_tokens))) return 0;
-    Carver c(nullptr);
-    c.take(n_tokens, hidden), c.take(inner, hidden), c.take(inner, hidden), c.take(hidden, inner), c.take(n_tokens, inner);
-    return reinterpret_cast<uintptr_t>(c.p);
+// room for their copies: `acts` activations of width hidden (X; in the backward dY too), H and the weights
+size_t whole_bytes(int32_t dt, int64_t n_tokens, int64_t hidden, int64_t inner, bool unaligned, int acts) {
+    if (!may_pad(dt, n_tokens)) return 0;
+    size_t n = 0;
+    if (unaligned || hidden % 8) n += acts * Wholes::bytes(n_tokens, hidden) + 2 * Wholes::bytes(inner, hidden);
+    if (unaligned || inner % 8) n += Wholes::bytes(hidden, inner) + Wholes::bytes(n_tokens, inner);
+    return n;
 }
-size_t bwd_pad_bytes(int32_t dt, int64_t n_tokens, int64_t hidden, int64_t inner) {
-    if (!may_pad(dt, static_cast<int32_t>(n_tokens))) return 0;
-    Carver c(nullptr);
-    c.take(n_tokens, hidden), c.take(n_tokens, hidden), c.take(inner, hidden), c.take(inner, hidden), c.take(hidden, inner), c.take(n_tokens, inner);
-    return reinterpret_cast<uintptr_t>(c.p);
+
+size_t fwd_bytes(int32_t dt, int32_t n_tokens, int32_t hidden, int32_t inner, bool unaligned) {
+    if (bad_shape(dt, PSATTN_ACT_SILU, n_tokens, hidden, inner)) return 0;
+    const bool any = unaligned || hidden % 8 || inner % 8;
+    const size_t parts = std::max(part_bytes(dt, any, kGate, true, n_tokens, inner, hidden, 1, 1), part_bytes(dt, any, kPlain, true, n_tokens, hidden, inner, 1, 1));
+    return align_up(parts, 256) + whole_bytes(dt, n_tokens, hidden, inner, unaligned, 1) + 256;
+}
+size_t bwd_bytes(int32_t dt, int32_t n_tokens, int32_t hidden, int32_t inner, bool unaligned) {
+    if (bad_shape(dt, PSATTN_ACT_SILU, n_tokens, hidden, inner)) return 0;
+    const bool any = unaligned || hidden % 8 || inner % 8;
+    const size_t parts = std::max({part_bytes(dt, any, kDact, true, n_tokens, inner, hidden, 1, 1), part_bytes(dt, any, kPlain, true, n_tokens, hidden, inner, 2, 1),
+                                   part_bytes(dt, any, kPlain, false, inner, hidden, n_tokens, 1, 2), part_bytes(dt, any, kPlain, false, hidden, inner, n_tokens, 1, 1)});
+    return 2 * align_up(static_cast<size_t>(n_tokens) * static_cast<size_t>(up8(inner)) * elem_bytes(dt), 256) + align_up(parts, 256) +
+           whole_bytes(dt, n_tokens, hidden, inner, unaligned, 2) + 256;
 }
 
 // a tile's copies have 32-bit offsets, and grids stay below 2^31 threads
@@ -291,18 +313,13 @@ __global__ void psattn_ffn_zero(uint16_t* p, size_t n) {
 
 extern "C" {
 
-size_t psattn_ffn_bwd_workspace_bytes(int32_t dt, int32_t n_tokens, int32_t hidden, int32_t inner) {
-    if (bad_shape(dt, PSATTN_ACT_SILU, n_tokens, hidden, inner)) return 0;
-    const size_t parts = std::max({part_bytes(dt, kDact, true, n_tokens, inner, hidden, 1, 1), part_bytes(dt, kPlain, true, n_tokens, hidden, inner, 2, 1),
-                                   part_bytes(dt, kPlain, false, inner, hidden, n_tokens, 1, 2), part_bytes(dt, kPlain, false, hidden, inner, n_tokens, 1, 1)});
-    return 2 * align_up(static_cast<size_t>(n_tokens) * static_cast<size_t>(up8(inner)) * elem_bytes(dt), 256) + align_up(parts, 256) + bwd_pad_bytes(dt, n_tokens, hidden, inner) + 256;
-}
+size_t psattn_ffn_fwd_workspace_bytes(int32_t dt, int32_t n_tokens, int32_t hidden, int32_t inner) { return fwd_bytes(dt, n_tokens, hidden, inner, false); }
 
-size_t psattn_ffn_fwd_workspace_bytes(int32_t dt, int32_t n_tokens, int32_t hidden, int32_t inner) {
-    if (bad_shape(dt, PSATTN_ACT_SILU, n_tokens, hidden, inner)) return 0;
-    const size_t parts = std::max(part_bytes(dt, kGate, true, n_tokens, inner, hidden, 1, 1), part_bytes(dt, kPlain, true, n_tokens, hidden, inner, 1, 1));
-    return align_up(parts, 256) + fwd_pad_bytes(dt, n_tokens, hidden, inner) + 256;
-}
+size_t psattn_ffn_fwd_unaligned_workspace_bytes(int32_t dt, int32_t n_tokens, int32_t hidden, int32_t inner) { return fwd_bytes(dt, n_tokens, hidden, inner, true); }
+
+size_t psattn_ffn_bwd_workspace_bytes(int32_t dt, int32_t n_tokens, int32_t hidden, int32_t inner) { return bwd_bytes(dt, n_tokens, hidden, inner, false); }
+
+size_t psattn_ffn_bwd_unaligned_workspace_bytes(int32_t dt, int32_t n_tokens, int32_t hidden, int32_t inner) { return bwd_bytes(dt, n_tokens, hidden, inner, true); }
 
 int psattn_ffn_fwd(int32_t dt, int32_t act, int32_t n_tokens, int32_t hidden, int32_t inner, const void* X, const void* Wg, const void* Wu,
                    const void* Wd, float* G, float* U, void* H, void* Y, void* workspace, size_t workspace_bytes, void* hip_stream) {
@@ -312,30 +329,26 @@ int psattn_ffn_fwd(int32_t dt, int32_t act, int32_t n_tokens, int32_t hidden, in
     if (!workspace || workspace_bytes < psattn_ffn_fwd_workspace_bytes(dt, n_tokens, hidden, inner)) return PSATTN_EINVAL;
     if (too_large(dt, n_tokens, hidden, inner)) return PSATTN_EUNSUPPORTED;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    const bool odd = may_pad(dt, n_tokens) && !(hidden % 8 == 0 && inner % 8 == 0 && at16({X, Wg, Wu, Wd, G, U, H, Y}));
-    Carver room(workspace);
-    const int64_t hp = odd ? up8(hidden) : hidden, ip = odd ? up8(inner) : inner;
-    const uint16_t* Hp = nullptr;
+    const bool may = may_pad(dt, n_tokens);
+    const int64_t hp = may ? up8(hidden) : hidden, ip = may ? up8(inner) : inner;
+    Wholes room(workspace, may, workspace_bytes >= fwd_bytes(dt, n_tokens, hidden, inner, true));
+    X = room.add(X, n_tokens, hidden), Wg = room.add(Wg, inner, hidden), Wu = room.add(Wu, inner, hidden), Wd = room.add(Wd, hidden, inner);
     int rc;
-    if (odd) {
-        uint16_t *x = room.take(n_tokens, hidden), *g = room.take(inner, hidden), *u = room.take(inner, hidden), *w = room.take(hidden, inner);
-        Hp = room.take(n_tokens, inner);
-        auto from = [](const void* p) { return static_cast<const uint16_t*>(p); };
-        if ((rc = pad({{from(X), x, n_tokens, hidden}, {from(Wg), g, inner, hidden}, {from(Wu), u, inner, hidden}, {from(Wd), w, hidden, inner}}, s)) != PSATTN_OK) return rc;
-        X = x; Wg = g; Wu = u; Wd = w;
-    }
-    void* const parts = room.p;
+    if ((rc = room.copy(s)) != PSATTN_OK) return rc;
+    const void* const Hp = room.add(H, n_tokens, inner);  // copied when it is there
+    char* const parts = room.p;
+    const char* const end = static_cast<const char*>(workspace) + workspace_bytes;
     Product gate{};
     gate.p[0] = X; gate.q[0] = Wg; gate.q[1] = Wu; gate.G = G; gate.U = U; gate.H = H;
-    gate.ldp = gate.ldq = hp; gate.ldo = inner; gate.odd = odd;
+    gate.ldp = gate.ldq = hp; gate.ldo = inner;
     gate.M = gate.m_load = n_tokens; gate.N = gate.n_load = inner; gate.K = hidden; gate.n_seg = gate.n_prod = 1;
-    if ((rc = product(dt, kGate, act, true, true, gate, parts, s)) != PSATTN_OK) return rc;
-    if (odd && (rc = pad({{static_cast<const uint16_t*>(H), const_cast<uint16_t*>(Hp), n_tokens, inner}}, s)) != PSATTN_OK) return rc;
+    if ((rc = product(dt, kGate, act, true, true, gate, parts, end, s)) != PSATTN_OK) return rc;
+    if ((rc = room.copy(s)) != PSATTN_OK) return rc;
     Product down{};
-    down.p[0] = odd ? Hp : H; down.q[0] = Wd; down.out[0] = Y;
-    down.ldp = down.ldq = ip; down.ldo = hidden; down.odd = odd;
+    down.p[0] = Hp; down.q[0] = Wd; down.out[0] = Y;
+    down.ldp = down.ldq = ip; down.ldo = hidden;
     down.M = down.m_load = n_tokens; down.N = down.n_load = hidden; down.K = inner; down.n_seg = down.n_prod = 1;
-    return product(dt, kPlain, act, true, true, down, parts, s);
+    return product(dt, kPlain, act, true, true, down, parts, end, s);
 }
 
 int psattn_ffn_bwd(int32_t dt, int32_t act, int32_t n_tokens, int32_t hidden, int32_t inner, const void* X, const void* Wg, const void* Wu,
@@ -352,42 +365,38 @@ int psattn_ffn_bwd(int32_t dt, int32_t act, int32_t n_tokens, int32_t hidden, in
     if (!X || !Wg || !Wu || !Wd || !G || !U || !H || !dY || !dX || !workspace) return PSATTN_EINVAL;
     if (workspace_bytes < psattn_ffn_bwd_workspace_bytes(dt, n_tokens, hidden, inner)) return PSATTN_EINVAL;
     if (too_large(dt, n_tokens, hidden, inner)) return PSATTN_EUNSUPPORTED;
-    const bool odd = may_pad(dt, n_tokens) && !(hidden % 8 == 0 && inner % 8 == 0 && at16({X, Wg, Wu, Wd, G, U, H, dY, dX, dWg, dWu, dWd}));
-    const int64_t hp = odd ? up8(hidden) : hidden, ip = odd ? up8(inner) : inner;
-    Carver room(workspace);
-    char* const dG = room.p;
-    char* const dU = dG + align_up(static_cast<size_t>(n_tokens) * static_cast<size_t>(up8(inner)) * elem_bytes(dt), 256);
-    room.p = dU + align_up(static_cast<size_t>(n_tokens) * static_cast<size_t>(up8(inner)) * elem_bytes(dt), 256);
+    const bool may = may_pad(dt, n_tokens);
+    const int64_t hp = may ? up8(hidden) : hidden, ip = may ? up8(inner) : inner;
+    Wholes room(workspace, may, workspace_bytes >= bwd_bytes(dt, n_tokens, hidden, inner, true));
+    const size_t kept = align_up(static_cast<size_t>(n_tokens) * static_cast<size_t>(up8(inner)) * elem_bytes(dt), 256);
+    char *const dG = room.p, *const dU = dG + kept;
+    room.p = dU + kept;
+    X = room.add(X, n_tokens, hidden), dY = room.add(dY, n_tokens, hidden), Wg = room.add(Wg, inner, hidden), Wu = room.add(Wu, inner, hidden);
+    Wd = room.add(Wd, hidden, inner), H = room.add(H, n_tokens, inner);
     int rc;
-    if (odd) {
-        uint16_t *x = room.take(n_tokens, hidden), *y = room.take(n_tokens, hidden), *g = room.take(inner, hidden), *u = room.take(inner, hidden), *w = room.take(hidden, inner),
-                 *k = room.take(n_tokens, inner);
-        auto from = [](const void* p) { return static_cast<const uint16_t*>(p); };
-        rc = pad({{from(X), x, n_tokens, hidden}, {from(dY), y, n_tokens, hidden}, {from(Wg), g, inner, hidden}, {from(Wu), u, inner, hidden}, {from(Wd), w, hidden, inner}, {from(H), k, n_tokens, inner}}, s);
-        if (rc != PSATTN_OK) return rc;
-        X = x; dY = y; Wg = g; Wu = u; Wd = w; H = k;
-    }
-    void* const parts = room.p;
+    if ((rc = room.copy(s)) != PSATTN_OK) return rc;
+    char* const parts = room.p;
+    const char* const end = static_cast<const char*>(workspace) + workspace_bytes;
     Product a{};  // dH = dY Wd, dG and dU.  G and U have rows of `inner`, dG and dU rows of ip
     a.p[0] = dY; a.q[0] = Wd; a.G = const_cast<float*>(G); a.U = const_cast<float*>(U); a.out[0] = dG; a.out[1] = dU;
-    a.ldp = hp; a.ldq = a.ldo = ip; a.ld_kept = inner; a.odd = odd;
+    a.ldp = hp; a.ldq = a.ldo = ip; a.ld_kept = inner;
     a.M = a.m_load = n_tokens; a.N = inner; a.n_load = static_cast<int32_t>(ip); a.K = hidden; a.n_seg = a.n_prod = 1;
-    if ((rc = product(dt, kDact, act, true, false, a, parts, s)) != PSATTN_OK) return rc;
+    if ((rc = product(dt, kDact, act, true, false, a, parts, end, s)) != PSATTN_OK) return rc;
     Product x{};  // dX = dG Wg + dU Wu
     x.p[0] = dG; x.p[1] = dU; x.q[0] = Wg; x.q[1] = Wu; x.out[0] = dX;
-    x.ldp = ip; x.ldq = hp; x.ldo = hidden; x.odd = odd;
+    x.ldp = ip; x.ldq = hp; x.ldo = hidden;
     x.M = x.m_load = n_tokens; x.N = hidden; x.n_load = static_cast<int32_t>(hp); x.K = inner; x.n_seg = 2; x.n_prod = 1;
-    if ((rc = product(dt, kPlain, act, true, false, x, parts, s)) != PSATTN_OK) return rc;
+    if ((rc = product(dt, kPlain, act, true, false, x, parts, end, s)) != PSATTN_OK) return rc;
     Product gu{};  // dWg = dG^T X, dWu = dU^T X
     gu.p[0] = dG; gu.p[1] = dU; gu.q[0] = X; gu.out[0] = dWg; gu.out[1] = dWu;
-    gu.ldp = ip; gu.ldq = hp; gu.ldo = hidden; gu.odd = odd;
+    gu.ldp = ip; gu.ldq = hp; gu.ldo = hidden;
     gu.M = inner; gu.m_load = static_cast<int32_t>(ip); gu.N = hidden; gu.n_load = static_cast<int32_t>(hp); gu.K = n_tokens; gu.n_seg = 1; gu.n_prod = 2;
-    if ((rc = product(dt, kPlain, act, false, false, gu, parts, s)) != PSATTN_OK) return rc;
+    if ((rc = product(dt, kPlain, act, false, false, gu, parts, end, s)) != PSATTN_OK) return rc;
     Product wd{};  // dWd = dY^T H
     wd.p[0] = dY; wd.q[0] = H; wd.out[0] = dWd;
-    wd.ldp = hp; wd.ldq = ip; wd.ldo = inner; wd.odd = odd;
+    wd.ldp = hp; wd.ldq = ip; wd.ldo = inner;
     wd.M = hidden; wd.m_load = static_cast<int32_t>(hp); wd.N = inner; wd.n_load = static_cast<int32_t>(ip); wd.K = n_tokens; wd.n_seg = wd.n_prod = 1;
-    return product(dt, kPlain, act, false, false, wd, parts, s);
+    return product(dt, kPlain, act, false, false, wd, parts, end, s);
 }
 
 }  // extern "C"

@@ -39,7 +39,7 @@ struct Product {
     int32_t M, N, K;          // K: of one segment
     int32_t n_seg, n_prod;
     int32_t m_load, n_load;   // M, N, or what rows in memory have of them and more (rows padded to whole 16-byte groups)
-    int32_t odd;              // what is stored, and G and U: rows that are not whole groups on 16-byte boundaries
+    int32_t odd;              // what is stored in the element type: rows that are not whole groups on 16-byte boundaries
     // k in n_split parts, whose sums go to `parts` in fp32 (rows of ld_part) and are joined by a kernel of their own
     int32_t n_split;
     float* parts;
