@@ -175,35 +175,29 @@ def _stream_ptr(stream):
 
 
 # torch hands a freed block out again to the stream that was current when the block was first taken, in that stream's order.  What a
-# call makes for itself therefore has to be made on the stream that its kernels run on: memory of another stream may still
-# be in use by work queued there before it was freed.
-def _side(stream, device):
-    """The stream that a call's own tensors are made on, None where that is the current one anyway."""
-    if stream is None or _stream_ptr(stream) == _stream_ptr(None):
-        return None
-    return (_TORCH or _torch()).cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream
-
-
-def _make(side, shape, dtype, device, zero=False):
-    """A tensor that a call returns.  On another stream than the current one it is both streams': freed, it is handed out again when
-    the work that is queued on either by then is done."""
+# call makes for itself has to be made on the stream that its kernels run on: memory of another stream may still be in use by
+# work queued there before it was freed.
+def _elsewhere(call, args):
+    """`call` with the arguments `args` (locals() at its start) on args["stream"], which is the current stream meanwhile.  Returned
+    tensors that the call has made are both streams': freed, they are handed out again when the work queued on either by then is done."""
     torch = _TORCH or _torch()
-    new = torch.zeros if zero else torch.empty
-    if side is None:
-        return new(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(side):
-        t = new(shape, dtype=dtype, device=device)
-    t.record_stream(torch.cuda.current_stream(device))
-    return t
+    stream, args["stream"] = args["stream"], None
+    if _stream_ptr(stream) == _stream_ptr(None):
+        return call(**args)
+    here = torch.cuda.current_stream()
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
+        out = call(**args)
+    given = {id(x) for a in args.values() for x in (a if isinstance(a, (tuple, list)) else (a,))}
 
+    def record(x):
+        if isinstance(x, (tuple, list)):
+            for y in x:
+                record(y)
+        elif x is not None and id(x) not in given:
+            x.record_stream(here)
 
-def _scratch(side, shape, dtype, device):
-    """A tensor that only the call's own kernels use: freed when it returns, and handed out again behind them."""
-    torch = _TORCH or _torch()
-    if side is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(side):
-        return torch.empty(shape, dtype=dtype, device=device)
+    record(out)
+    return out
 
 
 class Meta:
@@ -383,17 +377,18 @@ def _check_tensor(t, name, shape, dtype):
 
 def psattn_fwd(meta: Meta, Q, K, V, scale, O=None, LSE=None, stream=None):
     """O, LSE = attention forward.  Q [T, Hq, d]; K, V [T, Hkv, d]; LSE [Hq, T] float32."""
+    if stream is not None:
+        return _elsewhere(psattn_fwd, locals())
     torch, lib = _TORCH or _torch(), _LIB or load_library()
     T, Hq, d = Q.shape
     Hkv = K.shape[1]
     _check_tensor(Q, "Q", (meta.total_tokens, Hq, d), None)
     _check_tensor(K, "K", (T, Hkv, d), Q.dtype)
     _check_tensor(V, "V", (T, Hkv, d), Q.dtype)
-    side = _side(stream, Q.device)
     if O is None:
-        O = _make(side, Q.shape, Q.dtype, Q.device)
+        O = torch.empty_like(Q)
     if LSE is None:
-        LSE = _make(side, (Hq, T), torch.float32, Q.device)
+        LSE = torch.empty((Hq, T), dtype=torch.float32, device=Q.device)
     _check_tensor(O, "O", Q.shape, Q.dtype)
     _check_tensor(LSE, "LSE", (Hq, T), torch.float32)
     st = lib.psattn_fwd(meta.handle, _dtype_code(Q), Hq, Hkv, d, float(scale), Q.data_ptr(), K.data_ptr(),
@@ -409,6 +404,8 @@ def psattn_bwd_workspace_bytes(meta: Meta, n_q_heads, n_kv_heads, head_dim) -> i
 def psattn_bwd(meta: Meta, Q, K, V, O, dO, LSE, scale, dQ=None, dK=None, dV=None, workspace=None,
                stream=None):
     """dQ, dK, dV = attention backward from the forward's O and LSE."""
+    if stream is not None:
+        return _elsewhere(psattn_bwd, locals())
     torch, lib = _TORCH or _torch(), _LIB or load_library()
     T, Hq, d = Q.shape
     Hkv = K.shape[1]
@@ -418,15 +415,14 @@ def psattn_bwd(meta: Meta, Q, K, V, O, dO, LSE, scale, dQ=None, dK=None, dV=None
     _check_tensor(O, "O", Q.shape, Q.dtype)
     _check_tensor(dO, "dO", Q.shape, Q.dtype)
     _check_tensor(LSE, "LSE", (Hq, T), torch.float32)
-    side = _side(stream, Q.device)
-    dQ = _make(side, Q.shape, Q.dtype, Q.device) if dQ is None else dQ
-    dK = _make(side, K.shape, Q.dtype, Q.device) if dK is None else dK
-    dV = _make(side, V.shape, Q.dtype, Q.device) if dV is None else dV
+    dQ = torch.empty_like(Q) if dQ is None else dQ
+    dK = torch.empty_like(K) if dK is None else dK
+    dV = torch.empty_like(V) if dV is None else dV
     _check_tensor(dQ, "dQ", Q.shape, Q.dtype)
     _check_tensor(dK, "dK", K.shape, Q.dtype)
     _check_tensor(dV, "dV", V.shape, Q.dtype)
     if workspace is None:
-        workspace = _scratch(side, psattn_bwd_workspace_bytes(meta, Hq, Hkv, d), torch.uint8, Q.device)
+        workspace = torch.empty(psattn_bwd_workspace_bytes(meta, Hq, Hkv, d), dtype=torch.uint8, device=Q.device)
     if not workspace.is_cuda or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous device tensor")
     ws_bytes = workspace.numel() * workspace.element_size()
@@ -488,17 +484,18 @@ class Rope:
 
 def psattn_fwd_rope(meta: Meta, rope: Rope, Q, K, V, scale, O=None, LSE=None, Qr=None, Kr=None, stream=None):
     """O, LSE, Qr, Kr = forward with rotary embedding applied to the unrotated Q, K inside the op."""
+    if stream is not None:
+        return _elsewhere(psattn_fwd_rope, locals())
     torch, lib = _TORCH or _torch(), _LIB or load_library()
     T, Hq, d = Q.shape
     Hkv = K.shape[1]
     _check_tensor(Q, "Q", (meta.total_tokens, Hq, d), None)
     _check_tensor(K, "K", (T, Hkv, d), Q.dtype)
     _check_tensor(V, "V", (T, Hkv, d), Q.dtype)
-    side = _side(stream, Q.device)
-    O = _make(side, Q.shape, Q.dtype, Q.device) if O is None else O
-    LSE = _make(side, (Hq, T), torch.float32, Q.device) if LSE is None else LSE
-    Qr = _make(side, Q.shape, Q.dtype, Q.device) if Qr is None else Qr
-    Kr = _make(side, K.shape, Q.dtype, Q.device) if Kr is None else Kr
+    O = torch.empty_like(Q) if O is None else O
+    LSE = torch.empty((Hq, T), dtype=torch.float32, device=Q.device) if LSE is None else LSE
+    Qr = torch.empty_like(Q) if Qr is None else Qr
+    Kr = torch.empty_like(K) if Kr is None else Kr
     _check_tensor(O, "O", Q.shape, Q.dtype)
     _check_tensor(LSE, "LSE", (Hq, T), torch.float32)
     _check_tensor(Qr, "Qr", Q.shape, Q.dtype)
@@ -513,6 +510,8 @@ def psattn_fwd_rope(meta: Meta, rope: Rope, Q, K, V, scale, O=None, LSE=None, Qr
 def psattn_bwd_rope(meta: Meta, rope: Rope, Qr, Kr, V, O, dO, LSE, scale, dQ=None, dK=None, dV=None, workspace=None,
                     stream=None):
     """dQ, dK, dV (w.r.t. the unrotated Q, K) from the forward's rotated Qr, Kr."""
+    if stream is not None:
+        return _elsewhere(psattn_bwd_rope, locals())
     torch, lib = _TORCH or _torch(), _LIB or load_library()
     T, Hq, d = Qr.shape
     Hkv = Kr.shape[1]
@@ -520,14 +519,13 @@ def psattn_bwd_rope(meta: Meta, rope: Rope, Qr, Kr, V, O, dO, LSE, scale, dQ=Non
     for t, name, shape in ((Kr, "Kr", (T, Hkv, d)), (V, "V", (T, Hkv, d)), (O, "O", Qr.shape), (dO, "dO", Qr.shape)):
         _check_tensor(t, name, shape, Qr.dtype)
     _check_tensor(LSE, "LSE", (Hq, T), torch.float32)
-    side = _side(stream, Qr.device)
-    dQ = _make(side, Qr.shape, Qr.dtype, Qr.device) if dQ is None else dQ
-    dK = _make(side, Kr.shape, Qr.dtype, Qr.device) if dK is None else dK
-    dV = _make(side, V.shape, Qr.dtype, Qr.device) if dV is None else dV
+    dQ = torch.empty_like(Qr) if dQ is None else dQ
+    dK = torch.empty_like(Kr) if dK is None else dK
+    dV = torch.empty_like(V) if dV is None else dV
     for t, name, shape in ((dQ, "dQ", Qr.shape), (dK, "dK", Kr.shape), (dV, "dV", Kr.shape)):
         _check_tensor(t, name, shape, Qr.dtype)
     if workspace is None:
-        workspace = _scratch(side, psattn_bwd_workspace_bytes(meta, Hq, Hkv, d), torch.uint8, Qr.device)
+        workspace = torch.empty(psattn_bwd_workspace_bytes(meta, Hq, Hkv, d), dtype=torch.uint8, device=Qr.device)
     st = lib.psattn_bwd_rope(meta.handle, rope.handle, _dtype_code(Qr), Hq, Hkv, d, float(scale), Qr.data_ptr(),
                              Kr.data_ptr(), V.data_ptr(), O.data_ptr(), dO.data_ptr(), LSE.data_ptr(), dQ.data_ptr(),
                              dK.data_ptr(), dV.data_ptr(), workspace.data_ptr(),
@@ -572,13 +570,14 @@ class LogprobPlan:
 
 def psattn_logprob_fwd(plan: LogprobPlan, logits, token_ids, row_lse=None, resp_logp=None, stream=None):
     """row_lse [T], resp_logp [n_responses] from logits [T, vocab] and token_ids int32 [T]."""
+    if stream is not None:
+        return _elsewhere(psattn_logprob_fwd, locals())
     torch = _TORCH or _torch()
     T, V = logits.shape
     _check_tensor(logits, "logits", (plan.total_tokens, V), None)
     _check_tensor(token_ids, "token_ids", (T,), torch.int32)
-    side = _side(stream, logits.device)
-    row_lse = _make(side, T, torch.float32, logits.device, zero=True) if row_lse is None else row_lse
-    resp_logp = _make(side, plan.n_responses, torch.float32, logits.device) if resp_logp is None else resp_logp
+    row_lse = torch.zeros(T, dtype=torch.float32, device=logits.device) if row_lse is None else row_lse
+    resp_logp = torch.empty(plan.n_responses, dtype=torch.float32, device=logits.device) if resp_logp is None else resp_logp
     _check_tensor(row_lse, "row_lse", (T,), torch.float32)
     _check_tensor(resp_logp, "resp_logp", (plan.n_responses,), torch.float32)
     st = load_library().psattn_logprob_fwd(plan.handle, _dtype_code(logits), V, logits.data_ptr(), token_ids.data_ptr(),
@@ -588,13 +587,15 @@ def psattn_logprob_fwd(plan: LogprobPlan, logits, token_ids, row_lse=None, resp_
 
 
 def psattn_logprob_bwd(plan: LogprobPlan, logits, token_ids, row_lse, d_resp_logp, dlogits=None, stream=None):
+    if stream is not None:
+        return _elsewhere(psattn_logprob_bwd, locals())
     torch = _TORCH or _torch()
     T, V = logits.shape
     _check_tensor(logits, "logits", (plan.total_tokens, V), None)
     _check_tensor(token_ids, "token_ids", (T,), torch.int32)
     _check_tensor(row_lse, "row_lse", (T,), torch.float32)
     _check_tensor(d_resp_logp, "d_resp_logp", (plan.n_responses,), torch.float32)
-    dlogits = _make(_side(stream, logits.device), logits.shape, logits.dtype, logits.device) if dlogits is None else dlogits
+    dlogits = torch.empty_like(logits) if dlogits is None else dlogits
     _check_tensor(dlogits, "dlogits", logits.shape, logits.dtype)
     st = load_library().psattn_logprob_bwd(plan.handle, _dtype_code(logits), V, logits.data_ptr(), token_ids.data_ptr(),
                                            row_lse.data_ptr(), d_resp_logp.data_ptr(), dlogits.data_ptr(),
@@ -605,15 +606,16 @@ def psattn_logprob_bwd(plan: LogprobPlan, logits, token_ids, row_lse, d_resp_log
 
 def psattn_dpo_loss(logp_policy, logp_ref, beta, stream=None):
     """loss [n_pairs], d_logp [2 n_pairs] for responses stored as (chosen, rejected) pairs."""
+    if stream is not None:
+        return _elsewhere(psattn_dpo_loss, locals())
     torch = _TORCH or _torch()
     n = logp_policy.shape[0]
     if n % 2 or tuple(logp_ref.shape) != (n,):
         raise ValueError("log-probabilities must come in (chosen, rejected) pairs")
     _check_tensor(logp_policy, "logp_policy", (n,), torch.float32)
     _check_tensor(logp_ref, "logp_ref", (n,), torch.float32)
-    side = _side(stream, logp_policy.device)
-    loss = _make(side, n // 2, torch.float32, logp_policy.device)
-    d = _make(side, n, torch.float32, logp_policy.device)
+    loss = torch.empty(n // 2, dtype=torch.float32, device=logp_policy.device)
+    d = torch.empty(n, dtype=torch.float32, device=logp_policy.device)
     st = load_library().psattn_dpo_loss(n // 2, float(beta), logp_policy.data_ptr(), logp_ref.data_ptr(), loss.data_ptr(),
                                         d.data_ptr(), _stream_ptr(stream))
     _check(st, "psattn_dpo_loss")
@@ -643,10 +645,10 @@ def _check_all(dev, *tensors):
         raise ValueError("%s is on %s, not on cuda:%d" % (name, t.device, dev))
 
 
-def _workspace(given, need, like, side):
-    """A call's workspace: the caller's, or one of its own."""
+def _workspace(given, need, like):
+    """A call's workspace: the caller's, or one that goes back to torch when the call returns."""
     if given is None:
-        return _scratch(side, need, (_TORCH or _torch()).uint8, like.device)
+        return (_TORCH or _torch()).empty(need, dtype=(_TORCH or _torch()).uint8, device=like.device)
     if not given.is_cuda or not given.is_contiguous() or given.device != like.device:
         raise ValueError("workspace must be a contiguous device tensor on %s" % like.device)
     return given
@@ -654,12 +656,14 @@ def _workspace(given, need, like, side):
 
 def psattn_embed_fwd(token_ids, W, scale=1.0, X=None, stream=None):
     """X [T, hidden] = scale * rows of W [vocab, hidden] by token_ids int32 [T]; ids outside the table give rows of zeros."""
+    if stream is not None:
+        return _elsewhere(psattn_embed_fwd, locals())
     torch, lib = _TORCH or _torch(), _LIB or load_library()
     dev = _check_rows(W, "W")
     (V, h), T = W.shape, token_ids.numel()
     dt = _dtype_code(W)
     _check_all(dev, (token_ids, "token_ids", (T,), torch.int32), (X, "X", (T, h), W.dtype))
-    X = _make(_side(stream, W.device), (T, h), W.dtype, W.device) if X is None else X
+    X = torch.empty((T, h), dtype=W.dtype, device=W.device) if X is None else X
     st = lib.psattn_embed_fwd(dt, T, V, h, float(scale), token_ids.data_ptr(), W.data_ptr(), X.data_ptr(), _stream_ptr(stream))
     _check(st, "psattn_embed_fwd")
     return X
@@ -667,6 +671,8 @@ def psattn_embed_fwd(token_ids, W, scale=1.0, X=None, stream=None):
 
 def psattn_embed_bwd(token_ids, dX, vocab, scale=1.0, dW=None, workspace=None, stream=None):
     """dW [vocab, hidden]: the gradient of psattn_embed_fwd's table."""
+    if stream is not None:
+        return _elsewhere(psattn_embed_bwd, locals())
     torch, lib = _TORCH or _torch(), _LIB or load_library()
     dev = _check_rows(dX, "dX")
     (T, h), vocab = dX.shape, int(vocab)
@@ -674,9 +680,8 @@ def psattn_embed_bwd(token_ids, dX, vocab, scale=1.0, dW=None, workspace=None, s
     if not 0 < vocab < 1 << 31:
         raise ValueError("vocab must be a positive 32-bit number, got %d" % vocab)
     _check_all(dev, (token_ids, "token_ids", (T,), torch.int32), (dW, "dW", (vocab, h), dX.dtype))
-    side = _side(stream, dX.device)
-    dW = _make(side, (vocab, h), dX.dtype, dX.device) if dW is None else dW
-    ws = _workspace(workspace, lib.psattn_embed_bwd_workspace_bytes(dt, T, vocab, h), dX, side)
+    dW = torch.empty((vocab, h), dtype=dX.dtype, device=dX.device) if dW is None else dW
+    ws = _workspace(workspace, lib.psattn_embed_bwd_workspace_bytes(dt, T, vocab, h), dX)
     st = lib.psattn_embed_bwd(dt, T, vocab, h, float(scale), token_ids.data_ptr(), dX.data_ptr(), dW.data_ptr(), ws.data_ptr(),
                               ws.numel() * ws.element_size(), _stream_ptr(stream))
     _check(st, "psattn_embed_bwd")
@@ -685,6 +690,8 @@ def psattn_embed_bwd(token_ids, dX, vocab, scale=1.0, dW=None, workspace=None, s
 
 def psattn_layernorm_fwd(X, weight, bias=None, eps=1e-5, residual=None, S=None, Y=None, mean=None, rstd=None, stream=None):
     """Y, S, mean, rstd = layer norm of the rows of S = X + residual (S is X itself without one)."""
+    if stream is not None:
+        return _elsewhere(psattn_layernorm_fwd, locals())
     torch, lib = _TORCH or _torch(), _LIB or load_library()
     dev = _check_rows(X, "X")
     shape, dt, dtype, f32 = X.shape, _dtype_code(X), X.dtype, torch.float32
@@ -693,12 +700,11 @@ def psattn_layernorm_fwd(X, weight, bias=None, eps=1e-5, residual=None, S=None, 
         raise ValueError("S is an output of the residual sum: without a residual it is X")
     _check_all(dev, (weight, "weight", (h,), dtype), (bias, "bias", (h,), dtype), (residual, "residual", shape, dtype), (S, "S", shape, dtype),
                (Y, "Y", shape, dtype), (mean, "mean", (n,), f32), (rstd, "rstd", (n,), f32))
-    side = _side(stream, X.device)
     if residual is not None and S is None:
-        S = _make(side, shape, dtype, X.device)
-    Y = _make(side, shape, dtype, X.device) if Y is None else Y
-    mean = _make(side, n, f32, X.device) if mean is None else mean
-    rstd = _make(side, n, f32, X.device) if rstd is None else rstd
+        S = torch.empty_like(X)
+    Y = torch.empty_like(X) if Y is None else Y
+    mean = torch.empty(n, dtype=f32, device=X.device) if mean is None else mean
+    rstd = torch.empty(n, dtype=f32, device=X.device) if rstd is None else rstd
     st = lib.psattn_layernorm_fwd(dt, n, h, float(eps), X.data_ptr(), None if residual is None else residual.data_ptr(), weight.data_ptr(),
                                   None if bias is None else bias.data_ptr(), None if residual is None else S.data_ptr(), Y.data_ptr(),
                                   mean.data_ptr(), rstd.data_ptr(), _stream_ptr(stream))
@@ -708,6 +714,8 @@ def psattn_layernorm_fwd(X, weight, bias=None, eps=1e-5, residual=None, S=None, 
 
 def psattn_layernorm_bwd(S, weight, mean, rstd, dY, dS=None, bias=True, dX=None, dweight=None, dbias=None, workspace=None, stream=None):
     """dX, dweight, dbias (None where `bias` is false) from the forward's S, mean and rstd; dX has dS added to it."""
+    if stream is not None:
+        return _elsewhere(psattn_layernorm_bwd, locals())
     torch, lib = _TORCH or _torch(), _LIB or load_library()
     dev = _check_rows(S, "S")
     shape, dt, dtype, f32 = S.shape, _dtype_code(S), S.dtype, torch.float32
@@ -719,12 +727,11 @@ def psattn_layernorm_bwd(S, weight, mean, rstd, dY, dS=None, bias=True, dX=None,
             raise ValueError("%s is missing" % name)
     _check_all(dev, (weight, "weight", (h,), dtype), (mean, "mean", (n,), f32), (rstd, "rstd", (n,), f32), (dY, "dY", shape, dtype),
                (dS, "dS", shape, dtype), (dX, "dX", shape, dtype), (dweight, "dweight", (h,), dtype), (dbias, "dbias", (h,), dtype))
-    side = _side(stream, S.device)
-    dX = _make(side, shape, dtype, S.device) if dX is None else dX
-    dweight = _make(side, h, dtype, S.device) if dweight is None else dweight
+    dX = torch.empty_like(S) if dX is None else dX
+    dweight = torch.empty_like(weight) if dweight is None else dweight
     if bias and dbias is None:
-        dbias = _make(side, h, dtype, S.device)
-    ws = _workspace(workspace, lib.psattn_layernorm_bwd_workspace_bytes(n, h), S, side)
+        dbias = torch.empty_like(weight)
+    ws = _workspace(workspace, lib.psattn_layernorm_bwd_workspace_bytes(n, h), S)
     st = lib.psattn_layernorm_bwd(dt, n, h, S.data_ptr(), weight.data_ptr(), mean.data_ptr(), rstd.data_ptr(), dY.data_ptr(),
                                   None if dS is None else dS.data_ptr(), dX.data_ptr(), dweight.data_ptr(),
                                   dbias.data_ptr() if bias else None, ws.data_ptr(), ws.numel() * ws.element_size(), _stream_ptr(stream))
@@ -744,24 +751,17 @@ def _ffn_shapes(X, Wg, Wu, Wd, act):
     return dev, T, h, n, _dtype_code(X), [(Wg, "Wg", (n, h), dtype), (Wu, "Wu", (n, h), dtype), (Wd, "Wd", (h, n), dtype)]
 
 
-def _off_boundary(*tensors):
-    """Whether one of them starts off a 16-byte boundary."""
-    a = 0
-    for t in tensors:
-        a |= t.data_ptr()
-    return a & 15 != 0
-
-
 def psattn_ffn_fwd(X, Wg, Wu, Wd, act="silu", keep=True, Y=None, kept=None, workspace=None, stream=None):
     """Y, kept = (act(X Wg^T) o (X Wu^T)) Wd^T.  `kept` = (G, U, H), [T, inner] each, G and U float32, is what the backward takes;
     with keep=False G and U are not written and None is returned in its place (`kept` may then give H alone, as (None, None, H))."""
+    if stream is not None:
+        return _elsewhere(psattn_ffn_fwd, locals())
     torch, lib = _TORCH or _torch(), _LIB or load_library()
     dev, T, h, n, dt, tensors = _ffn_shapes(X, Wg, Wu, Wd, act)
     G, U, H = kept if kept is not None else (None, None, None)
-    side = _side(stream, X.device)
     if kept is None:
-        G, U = (_make(side, (T, n), torch.float32, X.device) for _ in range(2)) if keep else (None, None)
-        H = (_make if keep else _scratch)(side, (T, n), X.dtype, X.device)  # without `keep` it ends with this call
+        G, U = (torch.empty((T, n), dtype=torch.float32, device=X.device) for _ in range(2)) if keep else (None, None)
+        H = torch.empty((T, n), dtype=X.dtype, device=X.device)
     elif H is None or (keep and (G is None or U is None)):
         raise ValueError("kept must hold G, U and H, or with keep=False H alone")
     if not keep:
@@ -769,18 +769,20 @@ def psattn_ffn_fwd(X, Wg, Wu, Wd, act="silu", keep=True, Y=None, kept=None, work
     if kept is not None:
         tensors += [(G, "G", (T, n), torch.float32), (U, "U", (T, n), torch.float32), (H, "H", (T, n), X.dtype)]
     _check_all(dev, *tensors, (Y, "Y", X.shape, X.dtype))
-    Y = _make(side, X.shape, X.dtype, X.device) if Y is None else Y
-    need = lib.psattn_ffn_fwd_unaligned_workspace_bytes if _off_boundary(X, Wg, Wu, Wd, H) else lib.psattn_ffn_fwd_workspace_bytes
-    ws = _workspace(workspace, need(dt, T, h, n), X, side)
-    st = lib.psattn_ffn_fwd(dt, _ACTS[act], T, h, n, X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(),
-                            G.data_ptr() if keep else None, U.data_ptr() if keep else None, H.data_ptr(), Y.data_ptr(), ws.data_ptr(),
-                            ws.numel() * ws.element_size(), _stream_ptr(stream))
+    Y = torch.empty_like(X) if Y is None else Y
+    x, g, u, d, k = X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(), H.data_ptr()
+    need = lib.psattn_ffn_fwd_unaligned_workspace_bytes if (x | g | u | d | k) & 15 else lib.psattn_ffn_fwd_workspace_bytes
+    ws = _workspace(workspace, need(dt, T, h, n), X)
+    st = lib.psattn_ffn_fwd(dt, _ACTS[act], T, h, n, x, g, u, d, G.data_ptr() if keep else None, U.data_ptr() if keep else None, k, Y.data_ptr(),
+                            ws.data_ptr(), ws.numel() * ws.element_size(), _stream_ptr(None))
     _check(st, "psattn_ffn_fwd")
     return Y, (G, U, H) if keep else None
 
 
 def psattn_ffn_bwd(X, Wg, Wu, Wd, kept, dY, act="silu", dX=None, dWg=None, dWu=None, dWd=None, workspace=None, stream=None):
     """dX, dWg, dWu, dWd from the forward's kept (G, U, H)."""
+    if stream is not None:
+        return _elsewhere(psattn_ffn_bwd, locals())
     torch, lib = _TORCH or _torch(), _LIB or load_library()
     dev, T, h, n, dt, tensors = _ffn_shapes(X, Wg, Wu, Wd, act)
     G, U, H = kept if kept is not None else (None, None, None)
@@ -788,16 +790,15 @@ def psattn_ffn_bwd(X, Wg, Wu, Wd, kept, dY, act="silu", dX=None, dWg=None, dWu=N
         raise ValueError("kept G, U, H (psattn_ffn_fwd without them has keep=False) and dY are needed")
     _check_all(dev, *tensors, (G, "G", (T, n), torch.float32), (U, "U", (T, n), torch.float32), (H, "H", (T, n), X.dtype), (dY, "dY", X.shape, X.dtype),
                (dX, "dX", X.shape, X.dtype), (dWg, "dWg", (n, h), X.dtype), (dWu, "dWu", (n, h), X.dtype), (dWd, "dWd", (h, n), X.dtype))
-    side = _side(stream, X.device)
-    dX = _make(side, X.shape, X.dtype, X.device) if dX is None else dX
-    dWg = _make(side, (n, h), X.dtype, X.device) if dWg is None else dWg
-    dWu = _make(side, (n, h), X.dtype, X.device) if dWu is None else dWu
-    dWd = _make(side, (h, n), X.dtype, X.device) if dWd is None else dWd
-    need = lib.psattn_ffn_bwd_unaligned_workspace_bytes if _off_boundary(X, Wg, Wu, Wd, H, dY) else lib.psattn_ffn_bwd_workspace_bytes
-    ws = _workspace(workspace, need(dt, T, h, n), X, side)
-    st = lib.psattn_ffn_bwd(dt, _ACTS[act], T, h, n, X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(), G.data_ptr(), U.data_ptr(),
-                            H.data_ptr(), dY.data_ptr(), dX.data_ptr(), dWg.data_ptr(), dWu.data_ptr(), dWd.data_ptr(), ws.data_ptr(),
-                            ws.numel() * ws.element_size(), _stream_ptr(stream))
+    dX = torch.empty_like(X) if dX is None else dX
+    dWg = torch.empty_like(Wg) if dWg is None else dWg
+    dWu = torch.empty_like(Wu) if dWu is None else dWu
+    dWd = torch.empty_like(Wd) if dWd is None else dWd
+    x, g, u, d, k, y = X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(), H.data_ptr(), dY.data_ptr()
+    need = lib.psattn_ffn_bwd_unaligned_workspace_bytes if (x | g | u | d | k | y) & 15 else lib.psattn_ffn_bwd_workspace_bytes
+    ws = _workspace(workspace, need(dt, T, h, n), X)
+    st = lib.psattn_ffn_bwd(dt, _ACTS[act], T, h, n, x, g, u, d, G.data_ptr(), U.data_ptr(), k, y, dX.data_ptr(), dWg.data_ptr(), dWu.data_ptr(), dWd.data_ptr(),
+                            ws.data_ptr(), ws.numel() * ws.element_size(), _stream_ptr(None))
     _check(st, "psattn_ffn_bwd")
     return dX, dWg, dWu, dWd
 

@@ -63,9 +63,12 @@ class Layer:
         B._check_tensor(Wo, "Wo", (self.hidden, self.Hq * self.d), bf)
 
     def forward(self, meta, rope, scale, X, Wq, Wk, Wv, Wo, workspace, Y=None, stream=None):
+        if stream is not None:
+            return B._elsewhere(Layer.forward, locals())
+        torch = B._torch()
         T = meta.total_tokens
         self._check_shapes(T, X, Wq, Wk, Wv, Wo)
-        Y = B._make(B._side(stream, X.device), X.shape, X.dtype, X.device) if Y is None else Y
+        Y = torch.empty_like(X) if Y is None else Y
         B._check_tensor(Y, "Y", X.shape, X.dtype)
         st = load_layer_library().psattn_layer_fwd(self._h, meta.handle, rope.handle, T, float(scale), X.data_ptr(),
                                                    Wq.data_ptr(), Wk.data_ptr(), Wv.data_ptr(), Wo.data_ptr(), Y.data_ptr(),
@@ -75,12 +78,14 @@ class Layer:
         return Y
 
     def backward(self, meta, rope, scale, X, Wq, Wk, Wv, Wo, dY, workspace, grads=None, stream=None):
+        if stream is not None:
+            return B._elsewhere(Layer.backward, locals())
+        torch = B._torch()
         T = meta.total_tokens
         self._check_shapes(T, X, Wq, Wk, Wv, Wo)
         B._check_tensor(dY, "dY", X.shape, X.dtype)
         if grads is None:
-            side = B._side(stream, X.device)
-            grads = tuple(B._make(side, t.shape, t.dtype, t.device) for t in (X, Wq, Wk, Wv, Wo))
+            grads = tuple(torch.empty_like(t) for t in (X, Wq, Wk, Wv, Wo))
         for g, t in zip(grads, (X, Wq, Wk, Wv, Wo)):
             B._check_tensor(g, "gradient", t.shape, t.dtype)
         st = load_layer_library().psattn_layer_bwd(self._h, meta.handle, rope.handle, T, float(scale), X.data_ptr(),
