@@ -52,11 +52,17 @@ enum Move { kWhole, kOdd, kFloat };
 
 // What a product takes, in us, from the rounds of workgroups that its tiles make: which tile size, and k in how many parts.  A step is 128
 // bytes of k.  Measured, hidden 4 096, inner 14 336: 256 x 256, one workgroup to a CU, 1.6 us a step (1.25 where few CUs have one);
-// 128 x 128, two to a CU, 1.05 a step, 0.65 by itself; through registers half as much again; fp32 what its MFMAs take.  A round's start and
-// end take 3 us, or 14 (gate) and 30 (dG, dU) with 256 x 256, whose workgroups have nothing beside them to cover it, 3 and 12 with
+// 128 x 128, two to a CU, 1.05 a step, 0.65 by itself; through registers half as much again; fp32 at 158 TFLOP/s, of which large products reach
+// 139.  A round's start and end take 3 us, or 14 (gate) and 30 (dG, dU) with 256 x 256, whose workgroups have nothing beside them to cover it, 3 and 12 with
 // 128 x 128.  The two sizes, in turn: 8 192 tokens 7.0 and 8.5 ms, 1 024 tokens 1.72 and 1.49, 256 tokens 1.16 and 0.72 (unsplit).
 // Parts have no end but their sums' way to memory, and are joined by another launch; sums that outgrow the 256 MB cache go to HBM and back
 // (dWd of 16 384 tokens, 3.5 rounds of 256 x 256: 1 602 us, in two parts 1 637; dG and dU of 4 096 tokens 556 and 669).
+//   Away from those widths the model tells the two sizes apart better than it tells their times: what a plain product stores is not in it (221
+// tokens, 4 096 / 14 336: dWg and dWu 55 for 124 measured, gate and up 70 for 101).  By the rule / 128 x 128 alone / 256 x 256 alone, forward
+// and backward in us: 221 tokens, 4 096 / 14 336 465 / 478 / 476; 1 000, 8 192 / 28 672 3 970 / 4 660 / 3 970; 1 037, 1 024 / 2 736 142 / 142 /
+// 196; 8 192, 512 / 1 376 217 / 219 / 268; 4 096, 1 024 / 4 096 417 / 399 / 449; 16 384, 1 024 / 4 096 1 465 / 1 557 / 1 425; widths 1 001 / 2 731,
+// 1 037 tokens 182 / 183 / 242.  fp32: 168, 512 / 1 376 125 / 125 / 313; 300, 4 096 / 14 336 3 195 / 3 200 / 3 840; 2 048, 2 048 / 8 192 5 065 /
+// 5 165 / 4 600.
 double cost(Move move, Pass pass, TileSize size, int64_t tiles, int64_t steps, int64_t split, double out_bytes) {
     const bool big = size == k256, parts = split > 1;
     const double per_wg = static_cast<double>(cdiv(steps, split)), odd = move == kOdd ? 1.5 : 1;
