@@ -434,7 +434,7 @@ int psattn_layernorm_bwd(int32_t dt, int32_t n_rows, int32_t hidden, const void*
  * psattn_ffn_bwd: dX, dWg, dWu, dWd from the forward's G, U, H and dY.  The gradients of H with respect to G and U are
  * operands of its products, and like H they are rounded to dt once, from fp32.
  * Workspaces: psattn_ffn_..._workspace_bytes has room for the copies that bf16 calls of 320 tokens and more make of tensors whose
- * width is no multiple of 8.  Where tensors of other widths start off a 16-byte boundary, such calls take up to 1.5 times as long,
+ * width is no multiple of 8.  Where tensors of other widths start off a 16-byte boundary, such calls take up to 1.7 times as long,
  * unless the workspace has psattn_ffn_..._unaligned_workspace_bytes, which is never less: then these are copied too.
  */
 int psattn_ffn_fwd(int32_t dt, int32_t act, int32_t n_tokens, int32_t hidden, int32_t inner, const void* X, const void* Wg,

@@ -7,6 +7,11 @@ import pytest
 from test_kernel_build import _asm, _kernels
 
 
+@pytest.fixture(scope="module")
+def layer_norm(tmp_path_factory):
+    return _asm(tmp_path_factory.mktemp("asm"), "psattn_layernorm.hip")
+
+
 def _nothing_in_memory(kernels):
     for name, _, meta in kernels:
         assert int(meta["vgpr_spill_count"]) == 0 and int(meta["private_segment_fixed_size"]) == 0, name
@@ -17,12 +22,11 @@ def test_products_of_any_alignment_and_of_fp32(tmp_path, src):
     _nothing_in_memory(_kernels(_asm(tmp_path, src), "psattn_ffn_tiles", 26))
 
 
-def test_layer_norm_backward(tmp_path):
-    text = _asm(tmp_path, "psattn_layernorm.hip")
-    _nothing_in_memory(_kernels(text, "psattn_ln_bwd", len(re.findall(r"\.amdhsa_kernel \S*psattn_ln_bwd", text))))
+def test_layer_norm_backward(layer_norm):
+    _nothing_in_memory(_kernels(layer_norm, "psattn_ln_bwd", len(re.findall(r"\.amdhsa_kernel \S*psattn_ln_bwd", layer_norm))))
 
 
-def test_no_kernel_that_no_call_reaches(tmp_path):
+def test_no_kernel_that_no_call_reaches(layer_norm):
     """The layer norm's rows of 513 to 768 groups have a backward of their own where they are whole groups, and no other."""
-    names = [name for name, _, _ in _kernels(_asm(tmp_path, "psattn_layernorm.hip"), "psattn_ln_bwd", 38)]
+    names = [name for name, _, _ in _kernels(layer_norm, "psattn_ln_bwd", 38)]
     assert not any("Li256ELi3ELb0E" in name for name in names) and sum("Li256ELi3ELb1E" in name for name in names) == 2
