@@ -52,3 +52,26 @@ def test_memory_that_the_current_stream_has_freed(as_handle):
         del t, got  # the next turn's calls may have this memory, behind the comparisons above
     torch.cuda.synchronize()
     meta.free()
+
+
+def test_captured_on_a_stream_that_forks_from_the_capture():
+    """Calls on a second stream of a capture, which joins again: every replay as the eager calls, with eager ones between."""
+    d = _data()
+    meta = ps.psattn_build_meta([0], [T - 30], [10], [20], T)
+    _all(d, meta, None)
+    torch.cuda.synchronize()
+    side, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        side.wait_stream(torch.cuda.current_stream())
+        out = _all(d, meta, side)
+        torch.cuda.current_stream().wait_stream(side)
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    for turn in range(3):
+        d["X"].copy_(torch.randn(T, H, generator=gen, device="cuda"))
+        d["dY"].copy_(torch.randn(T, H, generator=gen, device="cuda"))
+        want = [t.clone() for t in _all(d, meta, None)]
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, out)), turn
+    meta.free()
