@@ -78,6 +78,10 @@ typedef enum { PSATTN_F32 = 0, PSATTN_BF16 = 1 } psattn_dtype;
 /* activation of the gated feed-forward block: g / (1 + exp(-g)), or g Phi(g) with the normal distribution's Phi (no tanh form) */
 typedef enum { PSATTN_ACT_SILU = 0, PSATTN_ACT_GELU = 1 } psattn_act;
 
+/* which dimensions of a head a rotary table pairs: (i, i + rotary_dim / 2), or (2 i, 2 i + 1); how its frequencies are scaled */
+typedef enum { PSATTN_ROPE_HALF = 0, PSATTN_ROPE_INTERLEAVED = 1 } psattn_rope_layout;
+typedef enum { PSATTN_ROPE_PLAIN = 0, PSATTN_ROPE_LINEAR = 1, PSATTN_ROPE_BASE = 2, PSATTN_ROPE_PARTS = 3 } psattn_rope_scaling;
+
 /* tile classes of the block mask */
 enum { PSATTN_TILE_SKIPPED = 0, PSATTN_TILE_PARTIAL = 1, PSATTN_TILE_FULL = 2 };
 
@@ -341,6 +345,35 @@ int psattn_bwd_rope(const psattn_meta* meta, const psattn_rope* rope, int32_t dt
 int psattn_meta_copy_positions(const psattn_meta* meta, int32_t* pos /* host [T] */, int32_t* n_positions);
 
 /*
+ * Rotary positions of any layout, of part of the head, with frequencies scaled for long contexts, on Q and K in memory.
+ *
+ * psattn_rope_frequencies (host only): inv_freq[i], i < rotary_dim / 2, of the angle position * inv_freq[i].  PLAIN: theta^(-2i /
+ * rotary_dim).  LINEAR: that divided by factor (positions interpolated).  BASE: with theta * factor^(rotary_dim / (rotary_dim - 2)) in
+ * theta's place, which divides the lowest frequency by factor and leaves the highest.  PARTS: f -> k f + (1 - k) f / factor, k = (r - low) /
+ * (high - low) clamped to [0, 1], r = f * original_positions / 2 pi: what turns `high` times and more over the original context stays,
+ * what turns `low` times and less is interpolated.  What a scaling does not name is not looked at.
+ * psattn_rope_create_layout: a table as by psattn_rope_create for the first rotary_dim (even) of head_dim dimensions, at most 512, with
+ * frequencies from the caller (host) and cosines and sines times `amplitude`.  One with the half layout, head_dim = rotary_dim = 128,
+ * may be given to every call that takes a psattn_rope; others to psattn_rope_apply alone (PSATTN_EUNSUPPORTED).
+ *
+ * psattn_rope_apply: Qr = Q and Kr = K, each head's pairs turned by the angles of its token's position, dimensions from
+ * rotary_dim on as they are; transposed != 0: the transposed turn, which gives dQ, dK from dQr, dKr.  Token t's heads are the n_heads *
+ * head_dim elements from Q + t * q_stride on (strides in elements, at least that many: slices of what one projection has
+ * written need no copy); either of Q and K may have no heads.  Any alignment and any even rotary_dim; 16-byte boundaries with
+ * rotary_dim / 2 and what is not turned in multiples of 16 bytes are fastest.  Results are rounded once, from fp32.  Positions: device
+ * int32 [n_tokens], or NULL and those of a block mask of n_tokens tokens (psattn_meta_copy_positions; padding: 0).  A position outside
+ * [0, max_positions) (padding) gives zeros.  Qr may be Q, and Kr K, with the same stride; no other overlap, Q and K of one buffer aside.
+ * PSATTN_EUNSUPPORTED: more than 2^20 heads, or sizes whose grids would have 2^31 threads.  Never allocates or blocks.
+ */
+int psattn_rope_frequencies(int32_t rotary_dim, double theta, int32_t scaling, double factor, double original_positions, double low,
+                            double high, double* inv_freq);
+int psattn_rope_create_layout(int32_t head_dim, int32_t rotary_dim, int32_t layout, const double* inv_freq, double amplitude,
+                              int32_t max_positions, void* hip_stream, psattn_rope** out);
+int psattn_rope_apply(const psattn_rope* rope, int32_t dt, int32_t transposed, int32_t n_tokens, const int32_t* positions,
+                      const psattn_meta* meta, int32_t n_q_heads, const void* Q, int64_t q_stride, void* Qr, int64_t qr_stride,
+                      int32_t n_kv_heads, const void* K, int64_t k_stride, void* Kr, int64_t kr_stride, void* hip_stream);
+
+/*
  * Per-response log-probabilities and the DPO loss (Section 2.1, Eq. 1: the loss needs
  * log pi(y | x), the total log-probability of each completion).  In the prefix-shared
  * sequence the logits row of a token predicts the next token of the token's own branch:
@@ -425,6 +458,26 @@ size_t psattn_layernorm_bwd_workspace_bytes(int32_t n_rows, int32_t hidden);
 int psattn_layernorm_bwd(int32_t dt, int32_t n_rows, int32_t hidden, const void* S, const void* weight, const float* mean,
                          const float* rstd, const void* dY, const void* dS, void* dX, void* dweight, void* dbias,
                          void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * RMS norms before and after a part of a block, with its gate and the residual stream's scale, as one pass:
+ * psattn_gatednorm_fwd: N = B * rstd_b * w_post (N = B without w_post), S = res_scale * X + gate o N rounded to dt, Y = S * rstd_s * w_pre;
+ * rstd = 1 / sqrt(mean square + eps) of a row of B, of S.  B is what a part of the block gives, S the residual stream behind it, Y what
+ * the next part takes.  gate: NULL (gate_rows = 0), one row for all (gate_rows = 1) or n_rows rows.  B = S = NULL (with neither w_post
+ * nor gate, res_scale not looked at): Y is the norm of X alone.  w_post, w_pre: [hidden] of dt, w_post may be NULL.  rstd_b (with
+ * w_post), rstd_s: device float [n_rows], for the backward.
+ * psattn_gatednorm_bwd: from the forward's B, S (X where there was no B), rstd_b and rstd_s, from dY and, where it is not NULL, dS (what reaches S by
+ * the residual stream): dX, dB (NULL where there was no B), dw_post (with w_post), dgate [gate_rows, hidden] (with a gate), dw_pre.  Gradients
+ * of what has one row for all are sums over the rows.  PSATTN_EUNSUPPORTED: 2^21 rows and more, or hidden over 2^24.
+ */
+int psattn_gatednorm_fwd(int32_t dt, int32_t n_rows, int32_t hidden, float eps, float res_scale, const void* X, const void* B,
+                         const void* w_post, const void* gate, int32_t gate_rows, const void* w_pre, void* S, void* Y, float* rstd_b,
+                         float* rstd_s, void* hip_stream);
+size_t psattn_gatednorm_bwd_workspace_bytes(int32_t n_rows, int32_t hidden);
+int psattn_gatednorm_bwd(int32_t dt, int32_t n_rows, int32_t hidden, float res_scale, const void* B, const void* w_post, const void* gate,
+                         int32_t gate_rows, const void* w_pre, const void* S, const float* rstd_b, const float* rstd_s, const void* dY,
+                         const void* dS, void* dX, void* dB, void* dw_post, void* dgate, void* dw_pre, void* workspace,
+                         size_t workspace_bytes, void* hip_stream);
 
 /*
  * psattn_ffn_fwd: G = X Wg^T, U = X Wu^T, H = act(G) o U, Y = H Wd^T.  X, Y [n_tokens, hidden]; Wg, Wu [inner, hidden] and Wd

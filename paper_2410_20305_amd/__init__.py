@@ -12,4 +12,6 @@ from .binding import (  # noqa: F401
     psattn_bwd_static, psattn_bwd_static_max_rows, psattn_probe_dq_atomics, psattn_pack_ffd, psattn_build_meta_multi, Rope, psattn_fwd_rope, psattn_bwd_rope,
     LogprobPlan, psattn_logprob_fwd, psattn_logprob_bwd, psattn_dpo_loss, ACT_SILU, ACT_GELU,
     psattn_embed_fwd, psattn_embed_bwd, psattn_layernorm_fwd, psattn_layernorm_bwd, psattn_ffn_fwd, psattn_ffn_bwd,
+    psattn_rope_frequencies, psattn_rope_apply, psattn_rope_apply_bwd, psattn_head_logprob_fwd, psattn_head_logprob_bwd,
+    psattn_gatednorm_fwd, psattn_gatednorm_bwd,
 )

@@ -29,10 +29,16 @@ EXPORTS = [
     "psattn_layernorm_fwd", "psattn_layernorm_bwd", "psattn_layernorm_bwd_workspace_bytes",
     "psattn_ffn_fwd", "psattn_ffn_bwd", "psattn_ffn_fwd_workspace_bytes", "psattn_ffn_bwd_workspace_bytes",
     "psattn_ffn_fwd_unaligned_workspace_bytes", "psattn_ffn_bwd_unaligned_workspace_bytes",
+    "psattn_rope_frequencies", "psattn_rope_create_layout", "psattn_rope_apply",
+    "psattn_head_logprob_fwd", "psattn_head_logprob_bwd", "psattn_head_logprob_fwd_workspace_bytes",
+    "psattn_head_logprob_bwd_workspace_bytes",
+    "psattn_gatednorm_fwd", "psattn_gatednorm_bwd", "psattn_gatednorm_bwd_workspace_bytes",
 ]
 
 ACT_SILU, ACT_GELU = 0, 1
 _ACTS = {"silu": ACT_SILU, "gelu": ACT_GELU}
+_ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+_ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "parts": 3}
 
 
 class PsattnError(RuntimeError):
@@ -75,6 +81,19 @@ def load_library():
     lib.psattn_logprob_fwd.argtypes = [vp, i32, i32, vp, vp, vp, vp, vp]
     lib.psattn_logprob_bwd.argtypes = [vp, i32, i32, vp, vp, vp, vp, vp, vp]
     lib.psattn_dpo_loss.argtypes = [i32, f32, vp, vp, vp, vp, vp]
+    f64 = C.c_double
+    lib.psattn_rope_frequencies.argtypes = [i32, f64, i32, f64, f64, f64, f64, vp]
+    lib.psattn_rope_create_layout.argtypes = [i32, i32, i32, vp, f64, i32, vp, C.POINTER(vp)]
+    lib.psattn_rope_apply.argtypes = [vp, i32, i32, i32, vp, vp, i32, vp, i64, vp, i64, i32, vp, i64, vp, i64, vp]
+    lib.psattn_head_logprob_fwd.argtypes = [vp, i32, i32, i32] + [vp] * 6 + [C.c_size_t, vp]
+    lib.psattn_head_logprob_bwd.argtypes = [vp, i32, i32, i32] + [vp] * 8 + [C.c_size_t, vp]
+    lib.psattn_gatednorm_fwd.argtypes = [i32, i32, i32, f32, f32, vp, vp, vp, vp, i32] + [vp] * 6
+    lib.psattn_gatednorm_bwd.argtypes = [i32, i32, i32, f32, vp, vp, vp, i32] + [vp] * 12 + [C.c_size_t, vp]
+    lib.psattn_gatednorm_bwd_workspace_bytes.argtypes = [i32, i32]
+    lib.psattn_gatednorm_bwd_workspace_bytes.restype = C.c_size_t
+    for name in ("psattn_head_logprob_fwd_workspace_bytes", "psattn_head_logprob_bwd_workspace_bytes"):
+        getattr(lib, name).argtypes = [vp, i32, i32, i32]
+        getattr(lib, name).restype = C.c_size_t
     lib.psattn_embed_fwd.argtypes = [i32, i32, i32, i32, f32, vp, vp, vp, vp]
     lib.psattn_embed_bwd.argtypes = [i32, i32, i32, i32, f32, vp, vp, vp, vp, C.c_size_t, vp]
     lib.psattn_embed_bwd_workspace_bytes.argtypes = [i32, i32, i32, i32]
@@ -454,14 +473,42 @@ def psattn_bwd_static_max_rows() -> int:
     return int(load_library().psattn_bwd_static_max_rows())
 
 
-class Rope:
-    """Owner of a psattn_rope handle (cos/sin table on the current device)."""
+def psattn_rope_frequencies(rotary_dim, theta, scaling="none", factor=1.0, original_positions=0, low=1.0, high=32.0):
+    """Angle per position of each pair of the first `rotary_dim` dimensions, float64 [rotary_dim / 2] (host only)."""
+    if scaling not in _ROPE_SCALINGS:
+        raise ValueError("scaling must be one of %s, got %r" % (sorted(_ROPE_SCALINGS), scaling))
+    out = np.zeros(max(1, int(rotary_dim) // 2), dtype=np.float64)
+    st = load_library().psattn_rope_frequencies(int(rotary_dim), float(theta), _ROPE_SCALINGS[scaling], float(factor), float(original_positions),
+                                                float(low), float(high), _addr(out))
+    _check(st, "psattn_rope_frequencies")
+    return out
 
-    def __init__(self, head_dim, theta, max_positions, stream=None):
+
+class Rope:
+    """Owner of a psattn_rope handle (cos/sin table on the current device).
+
+    With any of the keywords it is a table for psattn_rope_apply: the first `rotary_dim` dimensions of a head, "half" or "interleaved"
+    pairs, `frequencies` as by psattn_rope_frequencies (default: theta's), cosines and sines times `amplitude`."""
+
+    def __init__(self, head_dim, theta, max_positions, stream=None, *, rotary_dim=None, layout=None, frequencies=None, amplitude=None):
         lib = load_library()
         h = C.c_void_p()
-        _check(lib.psattn_rope_create(int(head_dim), float(theta), int(max_positions), _stream_ptr(stream), C.byref(h)),
-               "psattn_rope_create")
+        self._h = None
+        self.head_dim, self.max_positions = int(head_dim), int(max_positions)
+        self.rotary_dim = self.head_dim if rotary_dim is None else int(rotary_dim)
+        self.layout = "half" if layout is None else layout
+        if rotary_dim is None and layout is None and frequencies is None and amplitude is None:
+            _check(lib.psattn_rope_create(int(head_dim), float(theta), int(max_positions), _stream_ptr(stream), C.byref(h)),
+                   "psattn_rope_create")
+        else:
+            if self.layout not in _ROPE_LAYOUTS:
+                raise ValueError("layout must be one of %s, got %r" % (sorted(_ROPE_LAYOUTS), layout))
+            f = psattn_rope_frequencies(self.rotary_dim, theta) if frequencies is None else np.ascontiguousarray(frequencies, dtype=np.float64)
+            if f.shape != (self.rotary_dim // 2,):
+                raise ValueError("frequencies has shape %s, expected %s" % (f.shape, (self.rotary_dim // 2,)))
+            _check(lib.psattn_rope_create_layout(self.head_dim, self.rotary_dim, _ROPE_LAYOUTS[self.layout], _addr(f),
+                                                 1.0 if amplitude is None else float(amplitude), self.max_positions, _stream_ptr(stream),
+                                                 C.byref(h)), "psattn_rope_create_layout")
         self._h = h
 
     @property
@@ -534,6 +581,70 @@ def psattn_bwd_rope(meta: Meta, rope: Rope, Qr, Kr, V, O, dO, LSE, scale, dQ=Non
     return dQ, dK, dV
 
 
+def _check_heads(dev, t, name, shape, dtype):
+    """Token stride of Q or K: heads and dimensions contiguous, tokens any distance apart."""
+    if not t.is_cuda:
+        raise ValueError("%s must be a device tensor" % name)
+    if t.get_device() != dev:
+        raise ValueError("%s is on %s, not on cuda:%d" % (name, t.device, dev))
+    if t.shape != shape:
+        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
+    if t.dtype != dtype:
+        raise TypeError("%s has dtype %s, expected %s" % (name, t.dtype, dtype))
+    T, H, d = shape
+    s = t.stride()
+    if (d > 1 and s[2] != 1) or (H > 1 and s[1] != d) or (T > 1 and s[0] < H * d):
+        raise ValueError("the heads of a token of %s must be contiguous" % name)
+    return s[0] if T > 1 else H * d
+
+
+def _rope_apply(what, transposed, rope, Q, K, positions, meta, Qr, Kr):
+    torch, lib = _TORCH or _torch(), _LIB or load_library()
+    if Q.dim() != 3 or (K is not None and K.dim() != 3):
+        raise ValueError("Q and K have three dimensions: tokens, heads, head_dim")
+    if (positions is None) == (meta is None):
+        raise ValueError("positions or meta say where the tokens are: one of them")
+    (T, Hq, d), Hk = Q.shape, 0 if K is None else K.shape[1]
+    if max(Q.shape) >= 1 << 31:
+        raise ValueError("Q has shape %s: sizes are 32-bit" % (tuple(Q.shape),))
+    if d != rope.head_dim:
+        raise ValueError("Q has heads of %d, the rotary table of %d" % (d, rope.head_dim))
+    dev, dt = Q.get_device(), _dtype_code(Q)
+    q = _check_heads(dev, Q, "Q", Q.shape, Q.dtype)
+    if dev != torch._C._cuda_getDevice():
+        raise ValueError("Q is on %s, which is not the current device" % Q.device)
+    k = 0 if K is None else _check_heads(dev, K, "K", (T, Hk, d), Q.dtype)
+    if positions is not None:
+        _check_all(dev, (positions, "positions", (T,), torch.int32))
+    if K is None and Kr is not None:
+        raise ValueError("an output for K is given, but no K")
+    Qr = torch.empty((T, Hq, d), dtype=Q.dtype, device=Q.device) if Qr is None else Qr
+    if K is not None and Kr is None:
+        Kr = torch.empty((T, Hk, d), dtype=Q.dtype, device=Q.device)
+    qr = _check_heads(dev, Qr, "the output for Q", Q.shape, Q.dtype)
+    kr = 0 if K is None else _check_heads(dev, Kr, "the output for K", K.shape, Q.dtype)
+    st = lib.psattn_rope_apply(rope.handle, dt, transposed, T, None if positions is None else positions.data_ptr(), None if meta is None else meta.handle,
+                               Hq, Q.data_ptr(), q, Qr.data_ptr(), qr, Hk, None if K is None else K.data_ptr(), k, None if K is None else Kr.data_ptr(), kr,
+                               _stream_ptr(None))
+    _check(st, what)
+    return Qr, Kr
+
+
+def psattn_rope_apply(rope: Rope, Q, K=None, positions=None, meta=None, Qr=None, Kr=None, stream=None):
+    """Qr, Kr = Q [T, Hq, d] and K [T, Hkv, d] (or None) turned by their tokens' positions: int32 [T], or those of a Meta.  Tokens
+    may be any distance apart (slices of one buffer); Qr may be Q and Kr K."""
+    if stream is not None:
+        return _elsewhere(psattn_rope_apply, locals())
+    return _rope_apply("psattn_rope_apply", 0, rope, Q, K, positions, meta, Qr, Kr)
+
+
+def psattn_rope_apply_bwd(rope: Rope, dQr, dKr=None, positions=None, meta=None, dQ=None, dK=None, stream=None):
+    """dQ, dK = gradients of psattn_rope_apply's Q and K from those of Qr and Kr (the transposed turn)."""
+    if stream is not None:
+        return _elsewhere(psattn_rope_apply_bwd, locals())
+    return _rope_apply("psattn_rope_apply_bwd", 1, rope, dQr, dKr, positions, meta, dQ, dK)
+
+
 class LogprobPlan:
     """Owner of a psattn_lp_plan handle."""
 
@@ -602,6 +713,53 @@ def psattn_logprob_bwd(plan: LogprobPlan, logits, token_ids, row_lse, d_resp_log
                                            _stream_ptr(stream))
     _check(st, "psattn_logprob_bwd")
     return dlogits
+
+
+def _head_shapes(plan, X, W, token_ids):
+    dev = _check_rows(X, "X")
+    _check_rows(W, "W")
+    (T, h), V = X.shape, W.shape[0]
+    if T != plan.total_tokens:
+        raise ValueError("X has shape %s, expected %s" % ((T, h), (plan.total_tokens, h)))
+    _check_all(dev, (W, "W", (V, h), X.dtype), (token_ids, "token_ids", (T,), (_TORCH or _torch()).int32))
+    return dev, T, h, V, _dtype_code(X)
+
+
+def psattn_head_logprob_fwd(plan: LogprobPlan, X, W, token_ids, row_lse=None, resp_logp=None, workspace=None, stream=None):
+    """row_lse [T], resp_logp [n_responses] from hidden rows X [T, hidden], W [vocab, hidden] and token_ids int32 [T]; the logits X W^T
+    are never in memory."""
+    if stream is not None:
+        return _elsewhere(psattn_head_logprob_fwd, locals())
+    torch, lib = _TORCH or _torch(), _LIB or load_library()
+    dev, T, h, V, dt = _head_shapes(plan, X, W, token_ids)
+    _check_all(dev, (row_lse, "row_lse", (T,), torch.float32), (resp_logp, "resp_logp", (plan.n_responses,), torch.float32))
+    row_lse = torch.zeros(T, dtype=torch.float32, device=X.device) if row_lse is None else row_lse
+    resp_logp = torch.empty(plan.n_responses, dtype=torch.float32, device=X.device) if resp_logp is None else resp_logp
+    ws = _workspace(workspace, lib.psattn_head_logprob_fwd_workspace_bytes(plan.handle, dt, V, h), X)
+    st = lib.psattn_head_logprob_fwd(plan.handle, dt, V, h, X.data_ptr(), W.data_ptr(), token_ids.data_ptr(), row_lse.data_ptr(), resp_logp.data_ptr(),
+                                     ws.data_ptr(), ws.numel() * ws.element_size(), _stream_ptr(None))
+    _check(st, "psattn_head_logprob_fwd")
+    return row_lse, resp_logp
+
+
+def psattn_head_logprob_bwd(plan: LogprobPlan, X, W, token_ids, row_lse, d_resp_logp, dX=None, dW=None, workspace=None, stream=None):
+    """dX [T, hidden], dW [vocab, hidden] of sum_j d_resp_logp[j] * resp_logp[j], from the forward's row_lse."""
+    if stream is not None:
+        return _elsewhere(psattn_head_logprob_bwd, locals())
+    torch, lib = _TORCH or _torch(), _LIB or load_library()
+    dev, T, h, V, dt = _head_shapes(plan, X, W, token_ids)
+    for t, name in ((row_lse, "row_lse"), (d_resp_logp, "d_resp_logp")):
+        if t is None:
+            raise ValueError("%s is missing" % name)
+    _check_all(dev, (row_lse, "row_lse", (T,), torch.float32), (d_resp_logp, "d_resp_logp", (plan.n_responses,), torch.float32),
+               (dX, "dX", X.shape, X.dtype), (dW, "dW", W.shape, X.dtype))
+    dX = torch.empty_like(X) if dX is None else dX
+    dW = torch.empty_like(W) if dW is None else dW
+    ws = _workspace(workspace, lib.psattn_head_logprob_bwd_workspace_bytes(plan.handle, dt, V, h), X)
+    st = lib.psattn_head_logprob_bwd(plan.handle, dt, V, h, X.data_ptr(), W.data_ptr(), token_ids.data_ptr(), row_lse.data_ptr(), d_resp_logp.data_ptr(),
+                                     dX.data_ptr(), dW.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size(), _stream_ptr(None))
+    _check(st, "psattn_head_logprob_bwd")
+    return dX, dW
 
 
 def psattn_dpo_loss(logp_policy, logp_ref, beta, stream=None):
@@ -737,6 +895,85 @@ def psattn_layernorm_bwd(S, weight, mean, rstd, dY, dS=None, bias=True, dX=None,
                                   dbias.data_ptr() if bias else None, ws.data_ptr(), ws.numel() * ws.element_size(), _stream_ptr(stream))
     _check(st, "psattn_layernorm_bwd")
     return dX, dweight, dbias
+
+
+def _gate_rows(gate, n, h, dtype):
+    """How many rows a gate has, and its check: [hidden], [1, hidden] or [n, hidden]."""
+    if gate is None:
+        return 0, (None, "gate", (h,), dtype)
+    if gate.dim() == 2:
+        return gate.shape[0], (gate, "gate", (1 if gate.shape[0] == 1 else n, h), dtype)
+    return 1, (gate, "gate", (h,), dtype)
+
+
+def psattn_gatednorm_fwd(X, B, w_pre, w_post=None, gate=None, res_scale=1.0, eps=1e-6, S=None, Y=None, rstd_b=None, rstd_s=None, stream=None):
+    """Y, S, rstd_b, rstd_s: S = res_scale * X + gate o (B * rstd_b * w_post), Y = S * rstd_s * w_pre, RMS norms both.  gate: [hidden], [n, hidden]
+    or None; without w_post B itself joins X (rstd_b is None).  B = None: Y is the norm of X, which is S."""
+    if stream is not None:
+        return _elsewhere(psattn_gatednorm_fwd, locals())
+    torch, lib = _TORCH or _torch(), _LIB or load_library()
+    dev = _check_rows(X, "X")
+    shape, dt, dtype, f32 = X.shape, _dtype_code(X), X.dtype, torch.float32
+    n, h = shape
+    if w_pre is None:
+        raise ValueError("w_pre is missing")
+    if B is None and (w_post is not None or gate is not None or S is not None):
+        raise ValueError("w_post, gate and S belong to B, which is None")
+    if w_post is None and rstd_b is not None:
+        raise ValueError("rstd_b is given, but there is no w_post")
+    rows, gate_check = _gate_rows(gate, n, h, dtype)
+    _check_all(dev, (B, "B", shape, dtype), (w_pre, "w_pre", (h,), dtype), (w_post, "w_post", (h,), dtype), gate_check, (S, "S", shape, dtype),
+               (Y, "Y", shape, dtype), (rstd_b, "rstd_b", (n,), f32), (rstd_s, "rstd_s", (n,), f32))
+    if B is not None and S is None:
+        S = torch.empty_like(X)
+    Y = torch.empty_like(X) if Y is None else Y
+    if w_post is not None and rstd_b is None:
+        rstd_b = torch.empty(n, dtype=f32, device=X.device)
+    rstd_s = torch.empty(n, dtype=f32, device=X.device) if rstd_s is None else rstd_s
+    ptr = lambda t: None if t is None else t.data_ptr()
+    st = lib.psattn_gatednorm_fwd(dt, n, h, float(eps), float(res_scale), X.data_ptr(), ptr(B), ptr(w_post), ptr(gate), rows, w_pre.data_ptr(), ptr(S), Y.data_ptr(),
+                                  ptr(rstd_b), rstd_s.data_ptr(), _stream_ptr(None))
+    _check(st, "psattn_gatednorm_fwd")
+    return Y, X if B is None else S, rstd_b, rstd_s
+
+
+def psattn_gatednorm_bwd(B, S, w_pre, rstd_b, rstd_s, dY, dS=None, w_post=None, gate=None, res_scale=1.0, dX=None, dB=None, dw_pre=None, dw_post=None, dgate=None,
+                         workspace=None, stream=None):
+    """dX, dB, dw_pre, dw_post, dgate (None for what there was not) from the forward's B, S, rstd_b and rstd_s."""
+    if stream is not None:
+        return _elsewhere(psattn_gatednorm_bwd, locals())
+    torch, lib = _TORCH or _torch(), _LIB or load_library()
+    dev = _check_rows(S, "S")
+    shape, dt, dtype, f32 = S.shape, _dtype_code(S), S.dtype, torch.float32
+    n, h = shape
+    for t, name in ((w_pre, "w_pre"), (rstd_s, "rstd_s"), (dY, "dY")):
+        if t is None:
+            raise ValueError("%s is missing" % name)
+    if B is None and (w_post is not None or gate is not None or dB is not None):
+        raise ValueError("w_post, gate and dB belong to B, which is None")
+    if (w_post is None) != (rstd_b is None):
+        raise ValueError("rstd_b is the forward's where it had w_post, and None elsewhere")
+    if (w_post is None and dw_post is not None) or (gate is None and dgate is not None):
+        raise ValueError("dw_post or dgate is given, but not w_post or gate")
+    rows, gate_check = _gate_rows(gate, n, h, dtype)
+    _check_all(dev, (B, "B", shape, dtype), (w_pre, "w_pre", (h,), dtype), (rstd_b, "rstd_b", (n,), f32), (rstd_s, "rstd_s", (n,), f32), (dY, "dY", shape, dtype),
+               (dS, "dS", shape, dtype), (w_post, "w_post", (h,), dtype), gate_check, (dX, "dX", shape, dtype), (dB, "dB", shape, dtype), (dw_pre, "dw_pre", (h,), dtype),
+               (dw_post, "dw_post", (h,), dtype), (dgate, "dgate", None if gate is None else gate.shape, dtype))
+    dX = torch.empty_like(S) if dX is None else dX
+    dw_pre = torch.empty_like(w_pre) if dw_pre is None else dw_pre
+    if B is not None and dB is None:
+        dB = torch.empty_like(B)
+    if w_post is not None and dw_post is None:
+        dw_post = torch.empty_like(w_post)
+    if gate is not None and dgate is None:
+        dgate = torch.empty_like(gate)
+    ws = _workspace(workspace, lib.psattn_gatednorm_bwd_workspace_bytes(n, h), S)
+    ptr = lambda t: None if t is None else t.data_ptr()
+    st = lib.psattn_gatednorm_bwd(dt, n, h, float(res_scale), ptr(B), ptr(w_post), ptr(gate), rows, w_pre.data_ptr(), S.data_ptr(), ptr(rstd_b), rstd_s.data_ptr(),
+                                  dY.data_ptr(), ptr(dS), dX.data_ptr(), ptr(dB), ptr(dw_post), ptr(dgate), dw_pre.data_ptr(), ws.data_ptr(),
+                                  ws.numel() * ws.element_size(), _stream_ptr(None))
+    _check(st, "psattn_gatednorm_bwd")
+    return dX, dB, dw_pre, dw_post, dgate
 
 
 def _ffn_shapes(X, Wg, Wu, Wd, act):

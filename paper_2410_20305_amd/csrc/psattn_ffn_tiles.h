@@ -1,5 +1,6 @@
 // The kernel of the feed-forward block's products (psattn_gemm.h has its tiles and operands), built for bf16 with asynchronous
-// copies (psattn_ffn_bf16.hip), for bf16 of any alignment (psattn_ffn_bf16_any.hip) and for fp32 (psattn_ffn_f32.hip).
+// copies (psattn_ffn_bf16.hip), for bf16 of any alignment (psattn_ffn_bf16_any.hip) and for fp32 (psattn_ffn_f32.hip); with other
+// epilogues also of the vocabulary head's (psattn_head_tiles.h).
 //
 // k goes through LDS buffers, 128 bytes of it (64 bf16, 32 fp32) at a time.  The operands of a step (16 bf16, 8 fp32) are
 // read while the step before is multiplied.  Ahead of a tile's last step every wave has read its last operands of it and the
@@ -454,11 +455,110 @@ __global__ __launch_bounds__(S::kThreads, 2) void psattn_ffn_tiles(Product d, in
         });
         return;
     }
+    if constexpr (PASS == kLse) {
+        // A lane's sixteen values of a block are of one row, n = 8 (i / 4) + 4 (l / 32) + i % 4; the half-waves' are joined by an exchange, the
+        // waves' through LDS, which the products are done with
+        __syncthreads();
+        float2* const red = reinterpret_cast<float2*>(lds);  // [WN][BM]
+        const int nw = n0 + wn * NB * 32;                    // the wave's first column
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+            const int row = (wm * MB + mb) * 32 + (le & 31), m = m0 + row;
+            if (nw + NB * 32 > d.N) {
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (nw + nb * 32 + 8 * (i >> 2) + 4 * (le >> 5) + (i & 3) >= d.N) acc[nb][mb][i] = -INFINITY;
+            }
+            float mx = acc[0][mb][0];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) mx = fmaxf(mx, acc[nb][mb][i]);
+            mx = fmaxf(mx, __shfl_xor(mx, 32));
+            const float ref = mx == -INFINITY ? 0.f : mx;
+            float s = 0.f;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {  // in pairs: a sum of 1 and little else would lose as much at each of many additions
+                float e[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) e[i] = exp_of<E>(acc[nb][mb][i] - ref);
+#pragma unroll
+                for (int n = 8; n > 0; n >>= 1)
+#pragma unroll
+                    for (int i = 0; i < n; ++i) e[i] += e[i + n];
+                s += e[0];
+            }
+            s += __shfl_xor(s, 32);
+            if (le < 32) red[wn * S::BM + row] = make_float2(mx, s);
+            const int t = m < d.M ? static_cast<const int32_t*>(d.H)[m] - d.n_load - nw - 4 * (le >> 5) : -1;
+            if (t >= 0 && t < NB * 32 && (t & 4) == 0 && nw + t + 4 * (le >> 5) < d.N) {
+                float hit = 0.f;
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (nb * 32 + 8 * (i >> 2) + (i & 3) == t) hit = acc[nb][mb][i];
+                d.U[m] = hit;
+            }
+        }
+        __syncthreads();
+        for (int row = te; row < S::BM && m0 + row < d.M; row += S::kThreads) {
+            float mx = red[row].x;
+#pragma unroll
+            for (int i = 1; i < S::WN; ++i) mx = fmaxf(mx, red[i * S::BM + row].x);
+            const float ref = mx == -INFINITY ? 0.f : mx;
+            float s = 0.f;
+#pragma unroll
+            for (int i = 0; i < S::WN; ++i) s += red[i * S::BM + row].y * exp_of<E>(red[i * S::BM + row].x - ref);
+            reinterpret_cast<float2*>(d.G)[static_cast<int64_t>(tn) * d.M + m0 + row] = make_float2(mx, s);
+        }
+        return;
+    }
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
         const int m = m0 + (wm * MB + mb) * 32, rows = d.M - m;
         if (rows <= 0) break;
         __builtin_amdgcn_sched_barrier(0);  // one block at a time: beside 128 accumulators there is no room for more
+        if constexpr (PASS == kDlogit) {
+            const int at = m + min(le & 31, rows - 1);
+            const float lse = d.G[at], weight = d.U[at];
+            const int t = static_cast<const int32_t*>(d.H)[at] - d.n_load - 4 * (le >> 5);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                const int n = n0 + (wn * NB + nb) * 32, cols = d.N - n;
+                if (cols <= 0) break;
+                f32x16 x;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float p = exp_of<E>(acc[nb][mb][i] - lse);
+                    x[i] = weight == 0.f ? 0.f : weight * (t - n == 8 * (i >> 2) + (i & 3) ? 1.f - p : -p);
+                }
+                store_out<ASYNC>(static_cast<E*>(d.out[0]) + m * d.ldo + n, d.ldo, rows, cols, chunks(x), le, d.odd);
+            }
+            continue;
+        } else if constexpr (PASS == kSums) {
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                const int n = n0 + (wn * NB + nb) * 32, cols = d.N - n, row = le & 31, col = 8 * (le >> 5);
+                if (cols <= 0) break;
+                Chunks x = chunks(acc[nb][mb]);
+                float* const to = d.parts + (static_cast<int64_t>(part) * d.M + m) * d.ld_part + n;
+                if (d.add && row < rows) {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        if (cols - 16 * k - col <= 0) continue;
+                        Group old;
+                        old.get(to + row * d.ld_part + 16 * k + col, cols - 16 * k - col);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) x.c[k][j] += old.w[j];
+                    }
+                }
+                store_chunks<true>(to, d.ld_part, rows, cols, x, le);
+            }
+            continue;
+        }
         if (d.n_split > 1) {  // this part's sums, as they are: kGate [part][gate, up], else [part][product] of M x ld_part
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {

@@ -1,0 +1,611 @@
+// RMS norms before and after a part of a block, fused with its gate and residual scale, forward and backward.
+//   N = B rb w_post, rb = 1 / sqrt(mean(B^2) + eps)                (N = B without w_post)
+//   S = res X + g o N, rounded to the element type (the residual stream is held in it, and the backward reads it; S = X without B)
+//   Y = S rs w_pre, rs = 1 / sqrt(mean(S^2) + eps)
+// Backward, with bh = B rb, sh = S rs, q = dY w_pre, gw = g w_post:
+//   t = dS + rs q,  m = mean(q sh),  ds = t - rs m sh;  dX = res ds;  dB = rb (ds gw - bh mean(ds gw bh))
+//   dw_pre = sum_rows dY sh;  with C = sum_rows ds bh (of gates for all rows):  dw_post = g C, dg = w_post C
+//                             with gates for each row:  dw_post = sum_rows g ds bh, dg = w_post ds bh
+// mean(ds gw bh) = mean(t gw bh) - rs m mean(sh gw bh): the three sums of a row are taken together, in one pass over it.
+//
+// Bound by HBM: each row is read once and stays in registers (16 bytes to a lane and load) between its sums and its result, in fp32.
+// The sums run over the lanes in a tree of a fixed shape: a row's bits do not depend on the other rows.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "psattn.h"
+#include "psattn_rows.h"
+
+namespace {
+
+using namespace psattn::rows;
+
+template <typename E>
+struct Args {
+    int32_t n_rows, hidden;
+    float eps, res;
+    const E *X, *B, *w_post, *gate, *w_pre;
+    int32_t gate_step;  // elements from one row's gate to the next: hidden, or 0
+    E *S, *Y;
+    float *rstd_b, *rstd_s;
+    // backward
+    const E *dY, *dS;
+    E *dX, *dB, *dgate;  // dgate: of gates for each row
+    float *part, *row_m;
+};
+
+template <typename E, int LANES, int PER, bool WHOLE>
+__global__ __launch_bounds__(kThreads<LANES>) void psattn_gn_fwd(Args<E> a) {
+    constexpr int V = kVec<E>, kAt = kThreads<LANES> / LANES;
+    __shared__ float sm[2][16];
+    const int row = blockIdx.x * kAt + threadIdx.x / LANES, lane = threadIdx.x % LANES, hidden = a.hidden;
+    if (row >= a.n_rows) return;
+    const size_t at = static_cast<size_t>(row) * hidden;
+    const int from = lane * V - (WHOLE ? 0 : misalignment(a.X + at));  // this lane's first column
+    u32x4 xr[PER], br[PER], gr[PER], wr[PER];
+    Place pl[PER];
+    const E* const gate = a.gate ? a.gate + static_cast<size_t>(row) * a.gate_step : nullptr;
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+        pl[p] = place<WHOLE, E>(from + p * LANES * V, hidden);
+        xr[p] = raw<WHOLE>(a.X + at, pl[p], hidden);
+        if (a.B) br[p] = raw<WHOLE>(a.B + at, pl[p], hidden);
+        if (gate) gr[p] = raw<WHOLE>(gate, pl[p], hidden);
+        if (a.w_post) wr[p] = raw<WHOLE>(a.w_post, pl[p], hidden);
+    }
+    float rb = 1.f;
+    if (a.w_post) {
+        float sq[1] = {0.f};
+#pragma unroll
+        for (int p = 0; p < PER; ++p) {
+            float b[V];
+            unpack(settled<WHOLE>(br[p], pl[p].down), b);
+#pragma unroll
+            for (int j = 0; j < V; ++j) sq[0] += b[j] * b[j];
+        }
+        group_sum<LANES>(sq, sm[0]);
+        rb = 1.f / sqrtf(sq[0] / hidden + a.eps);
+    }
+    float x[PER][V], sq[1] = {0.f};
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+        unpack(settled<WHOLE>(xr[p], pl[p].down), x[p]);
+        if (a.B) {
+            float b[V], f[V];
+            unpack(settled<WHOLE>(br[p], pl[p].down), b);
+            if (a.w_post) {
+                unpack(settled<WHOLE>(wr[p], pl[p].down), f);
+#pragma unroll
+                for (int j = 0; j < V; ++j) b[j] *= rb * f[j];
+            }
+            if (gate) {
+                unpack(settled<WHOLE>(gr[p], pl[p].down), f);
+#pragma unroll
+                for (int j = 0; j < V; ++j) b[j] *= f[j];
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j) x[p][j] = hold(fmaf(a.res, x[p][j], b[j]), a.X);
+            store<WHOLE>(a.S + at, from + p * LANES * V, hidden, x[p]);
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) sq[0] += x[p][j] * x[p][j];
+    }
+    group_sum<LANES>(sq, sm[1]);
+    const float rs = 1.f / sqrtf(sq[0] / hidden + a.eps);
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+        float w[V];
+        unpack(settled<WHOLE>(raw<WHOLE>(a.w_pre, pl[p], hidden), pl[p].down), w);
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[p][j] *= rs * w[j];
+        store<WHOLE>(a.Y + at, from + p * LANES * V, hidden, x[p]);
+    }
+    if (lane == 0) {
+        if (a.w_post) a.rstd_b[row] = rb;
+        a.rstd_s[row] = rs;
+    }
+}
+
+// A lane's values of one group of a row, and what comes of them
+template <int V>
+struct Group {
+    float s[V], b[V], dy[V], t[V], g[V], wp[V];  // t: dS, then dS + rs q; g: gate; wp: w_post
+};
+
+// Backward.  A workgroup takes the rows from blockIdx.x on, gridDim.x apart, and keeps its lanes' columns of dw_pre and C in registers;
+// they go to part[workgroup] at its end and are joined by psattn_gn_weights (rows that share a workgroup add up in LDS first).
+// Rows stay in the registers as they came and are unpacked twice, with room for the next row's loads while one is summed.
+//   Without SUMS a workgroup has one row, whose rs m it keeps, and the columns are left to psattn_gn_columns.
+template <typename E, int LANES, int PER, bool WHOLE, bool SUMS>
+__global__ __launch_bounds__(kThreads<LANES>) void psattn_gn_bwd(Args<E> a) {
+    constexpr int V = kVec<E>, kAt = kThreads<LANES> / LANES;  // rows at a time
+    __shared__ float sm[2][48];
+    __shared__ float add[kAt > 1 ? kAt * LANES * PER * V : 1];
+    static_assert(SUMS || kAt == 1, "short rows' columns are summed here");
+    const int lane = threadIdx.x % LANES, own = threadIdx.x / LANES, hidden = a.hidden, n_rows = a.n_rows;
+    float dw[PER][V] = {}, dc[PER][V] = {};
+    constexpr bool kAhead = SUMS;
+    const int step = gridDim.x * kAt;
+    int row = blockIdx.x * kAt + own;
+    // this lane's first column: the same for all its rows, whose misalignment has to be
+    const int from = lane * V - (WHOLE || (step % V != 0 && hidden % V != 0) || row >= n_rows ? 0 : misalignment(a.S + static_cast<size_t>(row) * hidden));
+    Place pl[PER];
+    u32x4 w_pre[PER], w_post[PER];
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+        pl[p] = place<WHOLE, E>(from + p * LANES * V, hidden);
+        w_pre[p] = settled<WHOLE>(raw<WHOLE>(a.w_pre, pl[p], hidden), pl[p].down);
+        if (a.w_post) w_post[p] = settled<WHOLE>(raw<WHOLE>(a.w_post, pl[p], hidden), pl[p].down);
+    }
+    struct Row {
+        u32x4 s[PER], b[PER], dy[PER], ds[PER], g[PER];
+        float rs, rb;
+    } now, next;
+    auto fetch = [&](int r, Row& x) {
+        const size_t at = static_cast<size_t>(r) * hidden;
+        x.rs = a.rstd_s[r];
+        x.rb = a.w_post ? a.rstd_b[r] : 1.f;
+#pragma unroll
+        for (int p = 0; p < PER; ++p) {
+            x.s[p] = raw<WHOLE>(a.S + at, pl[p], hidden);
+            x.dy[p] = raw<WHOLE>(a.dY + at, pl[p], hidden);
+            if (a.B) x.b[p] = raw<WHOLE>(a.B + at, pl[p], hidden);
+            if (a.dS) x.ds[p] = raw<WHOLE>(a.dS + at, pl[p], hidden);
+            if (a.gate) x.g[p] = raw<WHOLE>(a.gate + static_cast<size_t>(r) * a.gate_step, pl[p], hidden);
+        }
+    };
+    if (kAhead && row < n_rows) fetch(row, now);
+    for (int turn = 0; row < n_rows; row += step, turn ^= 1) {
+        if constexpr (!kAhead) fetch(row, now);
+        else if (row + step < n_rows) fetch(row + step, next);
+        // outside of the row s, dy and the weights are zeros
+        auto unpacked = [&](int p, Group<V>& x) {
+            float wv[V];
+            unpack(settled<WHOLE>(now.s[p], pl[p].down), x.s);
+            unpack(settled<WHOLE>(now.dy[p], pl[p].down), x.dy);
+            unpack(w_pre[p], wv);
+#pragma unroll
+            for (int j = 0; j < V; ++j) x.s[j] *= now.rs;
+            if (a.dS) unpack(settled<WHOLE>(now.ds[p], pl[p].down), x.t);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                x.t[j] = fmaf(now.rs, x.dy[j] * wv[j], a.dS ? x.t[j] : 0.f);
+                wv[j] *= x.dy[j];
+            }
+            if (a.B) {
+                unpack(settled<WHOLE>(now.b[p], pl[p].down), x.b);
+#pragma unroll
+                for (int j = 0; j < V; ++j) x.b[j] *= now.rb;
+            }
+            if (a.gate) unpack(settled<WHOLE>(now.g[p], pl[p].down), x.g);
+            if (a.w_post) unpack(w_post[p], x.wp);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                if (!a.B) x.b[j] = 0.f;
+                if (!a.gate) x.g[j] = 1.f;
+                if (!a.w_post) x.wp[j] = 1.f;
+            }
+        };
+        float sum[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+        for (int p = 0; p < PER; ++p) {
+            Group<V> x;
+            float wv[V];
+            unpacked(p, x);
+            unpack(w_pre[p], wv);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                if constexpr (SUMS) dw[p][j] += x.dy[j] * x.s[j];
+                const float gwb = x.g[j] * x.wp[j] * x.b[j];
+                sum[0] += x.dy[j] * wv[j] * x.s[j];
+                sum[1] += x.t[j] * gwb;
+                sum[2] += x.s[j] * gwb;
+            }
+        }
+        group_sum<LANES>(sum, sm[turn]);
+        const float m = now.rs * (sum[0] / hidden), mb = (sum[1] - m * sum[2]) / hidden;
+        const size_t at = static_cast<size_t>(row) * hidden;
+#pragma unroll
+        for (int p = 0; p < PER; ++p) {
+            const int c = from + p * LANES * V;
+            Group<V> x;
+            float o[V];
+            unpacked(p, x);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                x.t[j] = fmaf(-m, x.s[j], x.t[j]);
+                o[j] = a.B ? a.res * x.t[j] : x.t[j];
+            }
+            store<WHOLE>(a.dX + at, c, hidden, o);
+            if (a.B) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    if constexpr (SUMS) dc[p][j] += a.gate_step ? x.g[j] * (x.t[j] * x.b[j]) : x.t[j] * x.b[j];
+                    const float d = x.t[j] * (x.g[j] * x.wp[j]);
+                    o[j] = a.w_post ? now.rb * (d - x.b[j] * mb) : d;
+                }
+                store<WHOLE>(a.dB + at, c, hidden, o);
+                if (a.dgate) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) o[j] = x.wp[j] * (x.t[j] * x.b[j]);
+                    store<WHOLE>(a.dgate + at, c, hidden, o);
+                }
+            }
+        }
+        if constexpr (!SUMS) {  // its one row: nothing is kept for another
+            if (threadIdx.x == 0) a.row_m[row] = m;
+            return;
+        }
+        if constexpr (kAhead) now = next;
+    }
+    if constexpr (!SUMS) return;
+    float* const mine = a.part + 2 * static_cast<size_t>(blockIdx.x) * hidden;
+    auto out = [&](float* to, const float (&v)[PER][V]) {
+        float* const at = kAt > 1 ? add + own * LANES * PER * V : to;  // rows that share the workgroup: by column, then added up
+        if constexpr (kAt > 1) __syncthreads();
+#pragma unroll
+        for (int p = 0; p < PER; ++p)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const int c = from + p * LANES * V + j;
+                if (c >= 0 && c < hidden) at[c] = v[p][j];
+            }
+        if constexpr (kAt > 1) {
+            __syncthreads();
+            for (int c = threadIdx.x; c < hidden; c += kThreads<LANES>) {
+                float t = 0.f;
+#pragma unroll
+                for (int o = 0; o < kAt; ++o) t += add[o * LANES * PER * V + c];
+                to[c] = t;
+            }
+        }
+    };
+    out(mine, dw);
+    if (a.B) out(mine + hidden, dc);
+}
+
+// The weights' gradients from the workgroups' parts: 64 columns to a workgroup, sixteen lanes to a column; the first `hidden` are dw_pre,
+// the others C
+template <typename E>
+__global__ __launch_bounds__(1024) void psattn_gn_weights(int n_parts, int hidden, const float* part, E* dw_pre, E* dw_post, E* dgate, const E* w_post, const E* gate) {
+    __shared__ float sm[16][65];
+    const int c = threadIdx.x & 63, k = threadIdx.x >> 6;
+    const int64_t i = blockIdx.x * 64 + c, width = 2 * static_cast<int64_t>(hidden);
+    const bool there = i < (dw_post || dgate ? width : hidden);
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    if (there) {
+        int p = k;
+        for (; p + 48 < n_parts; p += 64)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] += part[(p + 16 * u) * width + i];
+        for (; p < n_parts; p += 16) v[0] += part[p * width + i];
+    }
+    sm[k][c] = (v[0] + v[1]) + (v[2] + v[3]);
+    __syncthreads();
+    if (k > 0 || !there) return;
+    float t = 0.f;
+#pragma unroll
+    for (int o = 0; o < 16; ++o) t += sm[o][c];
+    if (i < hidden) {
+        store1(dw_pre + i, t);
+    } else {
+        const int64_t at = i - hidden;
+        if (dw_post) store1(dw_post + at, gate ? to_f32(gate[at]) * t : t);
+        if (dgate) store1(dgate + at, w_post ? to_f32(w_post[at]) * t : t);
+    }
+}
+
+// ---- rows too wide for registers: read again for each step
+template <typename E>
+__global__ __launch_bounds__(1024) void psattn_gn_fwd_wide(Args<E> a) {
+    constexpr int V = kVec<E>, kStep = 1024 * V;
+    __shared__ float sm[2][16];
+    const int hidden = a.hidden;
+    const size_t at = static_cast<size_t>(blockIdx.x) * hidden;
+    const E* const gate = a.gate ? a.gate + static_cast<size_t>(blockIdx.x) * a.gate_step : nullptr;
+    const E* x = a.X + at;
+    float rb = 1.f, sq[1] = {0.f};
+    if (a.w_post) {
+        for (int c = threadIdx.x * V; c < hidden; c += kStep) {
+            float b[V];
+            load<false>(a.B + at, c, hidden, b);
+#pragma unroll
+            for (int j = 0; j < V; ++j) sq[0] += b[j] * b[j];
+        }
+        group_sum<1024>(sq, sm[0]);
+        rb = 1.f / sqrtf(sq[0] / hidden + a.eps);
+        sq[0] = 0.f;
+    }
+    for (int c = threadIdx.x * V; c < hidden; c += kStep) {
+        float v[V];
+        load<false>(x, c, hidden, v);
+        if (a.B) {
+            float b[V], f[V];
+            load<false>(a.B + at, c, hidden, b);
+            if (a.w_post) {
+                load<false>(a.w_post, c, hidden, f);
+#pragma unroll
+                for (int j = 0; j < V; ++j) b[j] *= rb * f[j];
+            }
+            if (gate) {
+                load<false>(gate, c, hidden, f);
+#pragma unroll
+                for (int j = 0; j < V; ++j) b[j] *= f[j];
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[j] = hold(fmaf(a.res, v[j], b[j]), x);
+            store<false>(a.S + at, c, hidden, v);
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) sq[0] += v[j] * v[j];
+    }
+    if (a.B) x = a.S + at;  // each lane reads back what it wrote
+    group_sum<1024>(sq, sm[1]);
+    const float rs = 1.f / sqrtf(sq[0] / hidden + a.eps);
+    for (int c = threadIdx.x * V; c < hidden; c += kStep) {
+        float v[V], w[V];
+        load<false>(x, c, hidden, v);
+        load<false>(a.w_pre, c, hidden, w);
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] *= rs * w[j];
+        store<false>(a.Y + at, c, hidden, v);
+    }
+    if (threadIdx.x == 0) {
+        if (a.w_post) a.rstd_b[blockIdx.x] = rb;
+        a.rstd_s[blockIdx.x] = rs;
+    }
+}
+
+// what the backward of one row reads at columns c ..
+template <typename E>
+__device__ __forceinline__ void group_at(const Args<E>& a, int row, float rs, float rb, int c, Group<kVec<E>>& x, float (&q)[kVec<E>]) {
+    constexpr int V = kVec<E>;
+    const size_t at = static_cast<size_t>(row) * a.hidden;
+    load<false>(a.S + at, c, a.hidden, x.s);
+    load<false>(a.dY + at, c, a.hidden, x.dy);
+    load<false>(a.w_pre, c, a.hidden, q);
+    if (a.dS) load<false>(a.dS + at, c, a.hidden, x.t);
+    if (a.B) load<false>(a.B + at, c, a.hidden, x.b);
+    if (a.gate) load<false>(a.gate + static_cast<size_t>(row) * a.gate_step, c, a.hidden, x.g);
+    if (a.w_post) load<false>(a.w_post, c, a.hidden, x.wp);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        q[j] *= x.dy[j];
+        x.s[j] *= rs;
+        x.t[j] = fmaf(rs, q[j], a.dS ? x.t[j] : 0.f);
+        x.b[j] = a.B ? x.b[j] * rb : 0.f;
+        if (!a.gate) x.g[j] = 1.f;
+        if (!a.w_post) x.wp[j] = 1.f;
+    }
+}
+
+template <typename E>
+__global__ __launch_bounds__(1024) void psattn_gn_bwd_wide(Args<E> a) {
+    constexpr int V = kVec<E>, kStep = 1024 * V;
+    __shared__ float sm[48];
+    const int row = blockIdx.x, hidden = a.hidden;
+    const size_t at = static_cast<size_t>(row) * hidden;
+    const float rs = a.rstd_s[row], rb = a.w_post ? a.rstd_b[row] : 1.f;
+    float sum[3] = {0.f, 0.f, 0.f};
+    Group<V> x;
+    float q[V];
+    for (int c = threadIdx.x * V; c < hidden; c += kStep) {
+        group_at(a, row, rs, rb, c, x, q);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const float gwb = x.g[j] * x.wp[j] * x.b[j];
+            sum[0] += q[j] * x.s[j];
+            sum[1] += x.t[j] * gwb;
+            sum[2] += x.s[j] * gwb;
+        }
+    }
+    group_sum<1024>(sum, sm);
+    const float m = rs * (sum[0] / hidden), mb = (sum[1] - m * sum[2]) / hidden;
+    for (int c = threadIdx.x * V; c < hidden; c += kStep) {
+        float o[V];
+        group_at(a, row, rs, rb, c, x, q);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            x.t[j] = fmaf(-m, x.s[j], x.t[j]);
+            o[j] = a.B ? a.res * x.t[j] : x.t[j];
+        }
+        store<false>(a.dX + at, c, hidden, o);
+        if (!a.B) continue;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const float d = x.t[j] * (x.g[j] * x.wp[j]);
+            o[j] = a.w_post ? rb * (d - x.b[j] * mb) : d;
+        }
+        store<false>(a.dB + at, c, hidden, o);
+        if (!a.dgate) continue;
+#pragma unroll
+        for (int j = 0; j < V; ++j) o[j] = x.wp[j] * (x.t[j] * x.b[j]);
+        store<false>(a.dgate + at, c, hidden, o);
+    }
+    if (threadIdx.x == 0) a.row_m[row] = m;
+}
+
+// part[y]: sums of kVec columns to a lane over rows y, y + gridDim.y, ...
+template <typename E>
+__global__ __launch_bounds__(256) void psattn_gn_columns(Args<E> a) {
+    constexpr int V = kVec<E>;
+    const int step = gridDim.y, hidden = a.hidden;
+    const bool same = step % V == 0 || hidden % V == 0;  // all rows of this workgroup start alike
+    const int c = (blockIdx.x * 256 + threadIdx.x) * V - (same ? misalignment(a.S + static_cast<size_t>(blockIdx.y) * hidden) : 0);
+    if (c >= hidden) return;
+    float w[V] = {}, k[V] = {};
+    for (int r = blockIdx.y; r < a.n_rows; r += step) {
+        Group<V> x;
+        float q[V];
+        const float m = a.row_m[r];
+        group_at(a, r, a.rstd_s[r], a.w_post ? a.rstd_b[r] : 1.f, c, x, q);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            w[j] += x.dy[j] * x.s[j];
+            const float t = fmaf(-m, x.s[j], x.t[j]) * x.b[j];
+            k[j] += a.gate_step ? x.g[j] * t : t;
+        }
+    }
+    float* const mine = a.part + 2 * static_cast<size_t>(blockIdx.y) * hidden;
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+        if (c + j >= 0 && c + j < hidden) {
+            mine[c + j] = w[j];
+            mine[hidden + c + j] = k[j];
+        }
+}
+
+// ---- which kernel: rows of up to 32 groups of 16 bytes are sixteen lanes', of up to 128 a wave's, wider ones a workgroup's
+template <typename E, bool BWD, typename F>
+bool sized(int hidden, bool all, F&& f) {
+    using std::integral_constant;
+    auto go = [&](auto lanes, auto per) { return f(lanes, per), true; };
+    const int64_t g = (static_cast<int64_t>(hidden) + kVec<E> - 1) / kVec<E> + (all ? 0 : 1);  // rows that start off a boundary reach into one more
+    constexpr int kWidest = 4 * 8 / kVec<E>;  // groups of a lane: 32 columns
+    using One = integral_constant<int, 1>;
+    using Two = integral_constant<int, 2>;
+    if (g <= 16) return go(integral_constant<int, 16>{}, One{});
+    if (g <= 32) return go(integral_constant<int, 16>{}, Two{});
+    if (g <= 64) return go(integral_constant<int, 64>{}, One{});
+    if (g <= 128) return go(integral_constant<int, 64>{}, Two{});
+    if (g <= 256) return go(integral_constant<int, 256>{}, One{});
+    if (g <= 512) return go(integral_constant<int, 256>{}, Two{});
+    if (g <= 1024) return go(integral_constant<int, 512>{}, Two{});
+    if constexpr (BWD) {
+        if (g <= 2048) return go(integral_constant<int, 512>{}, integral_constant<int, 4>{});
+        if (g <= 512 * kWidest) return go(integral_constant<int, 512>{}, integral_constant<int, kWidest>{});
+    } else {
+        if (g <= 2048) return go(integral_constant<int, 1024>{}, Two{});
+        if (g <= 512 * kWidest) return go(integral_constant<int, 1024>{}, integral_constant<int, kWidest / 2>{});
+    }
+    return false;
+}
+
+// workgroups of the backward, each with a part of the columns' sums.  A part is written and read in fp32, and costs as much memory time
+// as a few rows: one for 26 rows, but 256 of them (one to a CU) at least and 1 024 at most
+int n_parts(int32_t n_rows) { return std::max(1, std::min({n_rows, 1024, std::max(256, n_rows / 26)})); }
+
+bool bad_shape(int32_t dt, int32_t n_rows, int32_t hidden) { return (dt != PSATTN_F32 && dt != PSATTN_BF16) || n_rows < 0 || hidden <= 0; }
+
+template <typename E>
+void fwd(const Args<E>& a, hipStream_t s) {
+    const bool all = whole<E>(a.hidden, {a.X, a.B, a.w_post, a.gate, a.w_pre, a.S, a.Y});
+    const bool done = sized<E, false>(a.hidden, all, [&](auto lanes, auto per) {
+        constexpr int L = decltype(lanes)::value, PER = decltype(per)::value, kAt = kThreads<L> / L;
+        auto go = [&](auto kernel) { kernel<<<(a.n_rows + kAt - 1) / kAt, kThreads<L>, 0, s>>>(a); };
+        all ? go(psattn_gn_fwd<E, L, PER, true>) : go(psattn_gn_fwd<E, L, PER, false>);
+    });
+    if (!done) psattn_gn_fwd_wide<E><<<a.n_rows, 1024, 0, s>>>(a);
+}
+
+template <typename E>
+void bwd(Args<E> a, bool vector_gate, void* dw_pre, void* dw_post, void* dgate, hipStream_t s) {
+    int np = a.n_rows > 0 ? n_parts(a.n_rows) : 0;
+    if (a.n_rows > 0) {
+        const bool all = whole<E>(a.hidden, {a.S, a.B, a.w_post, a.gate, a.w_pre, a.dY, a.dS, a.dX, a.dB, a.dgate});
+        bool sums = false;
+        const bool done = sized<E, true>(a.hidden, all, [&](auto lanes, auto per) {
+            constexpr int L = decltype(lanes)::value, PER = decltype(per)::value, kAt = kThreads<L> / L;
+            constexpr bool SUMS = PER * kVec<E> < 32;  // up to 1 024 groups of bf16, 2 048 of fp32
+            if (SUMS) np = std::min(np, (a.n_rows + kAt - 1) / kAt);
+            if (np > 8) np -= np % 8;  // a workgroup's rows start alike
+            sums = SUMS;
+            auto go = [&](auto kernel) { kernel<<<SUMS ? np : a.n_rows, kThreads<L>, 0, s>>>(a); };
+            all ? go(psattn_gn_bwd<E, L, PER, true, SUMS>) : go(psattn_gn_bwd<E, L, PER, false, SUMS>);
+        });
+        if (!done) psattn_gn_bwd_wide<E><<<a.n_rows, 1024, 0, s>>>(a);
+        if (!sums) {
+            const int cols = (a.hidden + kVec<E> - 1 + 256 * kVec<E> - 1) / (256 * kVec<E>);
+            np = std::min(np, std::max(8, 2048 / cols / 8 * 8));  // eight workgroups to a CU
+            psattn_gn_columns<E><<<dim3(cols, np), 256, 0, s>>>(a);
+        }
+    }
+    E* const to_gate = vector_gate ? static_cast<E*>(dgate) : nullptr;
+    psattn_gn_weights<E><<<((dw_post || to_gate ? 2 : 1) * a.hidden + 63) / 64, 1024, 0, s>>>(np, a.hidden, a.part, static_cast<E*>(dw_pre), static_cast<E*>(dw_post), to_gate,
+                                                                                                np ? a.w_post : nullptr, np && vector_gate ? a.gate : nullptr);
+}
+
+// grids of at most 2^31 threads: a row to 1 024 of them, or 64 columns of the sums
+constexpr int32_t kMostRows = (1 << 21) - 1, kMostHidden = 1 << 24;
+
+template <typename E>
+Args<E> make(int32_t n_rows, int32_t hidden, const void* B, const void* w_post, const void* gate, int32_t gate_rows, const void* w_pre, float* rstd_b, float* rstd_s) {
+    Args<E> a{};
+    a.n_rows = n_rows;
+    a.hidden = hidden;
+    a.B = static_cast<const E*>(B);
+    a.w_post = static_cast<const E*>(w_post);
+    a.gate = static_cast<const E*>(gate);
+    a.gate_step = gate && gate_rows > 1 ? hidden : 0;
+    a.w_pre = static_cast<const E*>(w_pre);
+    a.rstd_b = rstd_b;
+    a.rstd_s = rstd_s;
+    return a;
+}
+
+// gates: none, one row for all, or as many rows as there are
+bool bad_gate(const void* gate, int32_t gate_rows, int32_t n_rows) { return gate ? gate_rows != 1 && gate_rows != n_rows : gate_rows != 0; }
+
+}  // namespace
+
+extern "C" {
+
+int psattn_gatednorm_fwd(int32_t dt, int32_t n_rows, int32_t hidden, float eps, float res_scale, const void* X, const void* B, const void* w_post, const void* gate,
+                         int32_t gate_rows, const void* w_pre, void* S, void* Y, float* rstd_b, float* rstd_s, void* hip_stream) {
+    if (bad_shape(dt, n_rows, hidden) || !(eps >= 0.f) || std::isinf(eps) || !std::isfinite(res_scale)) return PSATTN_EINVAL;
+    if (n_rows == 0) return PSATTN_OK;
+    if (!X || !w_pre || !Y || !rstd_s || bad_gate(gate, gate_rows, n_rows)) return PSATTN_EINVAL;
+    if ((!B) != (!S) || (!B && (w_post || gate)) || (w_post && !rstd_b)) return PSATTN_EINVAL;
+    if (n_rows > kMostRows || hidden > kMostHidden) return PSATTN_EUNSUPPORTED;
+    auto go = [&](auto elem) {
+        using E = decltype(elem);
+        Args<E> a = make<E>(n_rows, hidden, B, w_post, gate, gate_rows, w_pre, rstd_b, rstd_s);
+        a.eps = eps;
+        a.res = res_scale;
+        a.X = static_cast<const E*>(X);
+        a.S = static_cast<E*>(S);
+        a.Y = static_cast<E*>(Y);
+        fwd(a, static_cast<hipStream_t>(hip_stream));
+    };
+    if (dt == PSATTN_BF16) go(uint16_t{});
+    else go(float{});
+    return hipGetLastError() == hipSuccess ? PSATTN_OK : PSATTN_EHIP;
+}
+
+size_t psattn_gatednorm_bwd_workspace_bytes(int32_t n_rows, int32_t hidden) {
+    if (n_rows < 0 || hidden <= 0) return 0;
+    return align_up(2 * sizeof(float) * static_cast<size_t>(n_parts(n_rows)) * hidden, 256) + align_up(sizeof(float) * static_cast<size_t>(n_rows), 256) + 256;
+}
+
+int psattn_gatednorm_bwd(int32_t dt, int32_t n_rows, int32_t hidden, float res_scale, const void* B, const void* w_post, const void* gate, int32_t gate_rows,
+                         const void* w_pre, const void* S, const float* rstd_b, const float* rstd_s, const void* dY, const void* dS, void* dX, void* dB, void* dw_post,
+                         void* dgate, void* dw_pre, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    if (bad_shape(dt, n_rows, hidden) || !std::isfinite(res_scale) || !dw_pre) return PSATTN_EINVAL;
+    if (n_rows > 0 && (!S || !w_pre || !rstd_s || !dY || !dX || !workspace || bad_gate(gate, gate_rows, n_rows))) return PSATTN_EINVAL;
+    if (n_rows > 0 && ((!B) != (!dB) || (!B && (w_post || gate)) || (w_post && !rstd_b) || (!w_post) != (!dw_post) || (!gate) != (!dgate))) return PSATTN_EINVAL;
+    if (n_rows > 0 && workspace_bytes < psattn_gatednorm_bwd_workspace_bytes(n_rows, hidden)) return PSATTN_EINVAL;
+    if (n_rows > kMostRows || hidden > kMostHidden) return PSATTN_EUNSUPPORTED;
+    auto go = [&](auto elem) {
+        using E = decltype(elem);
+        Args<E> a = make<E>(n_rows, hidden, B, w_post, gate, gate_rows, w_pre, const_cast<float*>(rstd_b), const_cast<float*>(rstd_s));
+        a.res = res_scale;
+        a.S = static_cast<E*>(const_cast<void*>(S));
+        a.dY = static_cast<const E*>(dY);
+        a.dS = static_cast<const E*>(dS);
+        a.dX = static_cast<E*>(dX);
+        a.dB = static_cast<E*>(dB);
+        const bool vector_gate = dgate && (n_rows == 0 ? gate_rows == 1 : a.gate_step == 0);
+        a.dgate = vector_gate ? nullptr : static_cast<E*>(dgate);
+        a.part = reinterpret_cast<float*>(align_up(reinterpret_cast<uintptr_t>(workspace), 256));
+        a.row_m = a.part + align_up(2 * sizeof(float) * static_cast<size_t>(n_parts(n_rows)) * hidden, 256) / sizeof(float);
+        bwd(a, vector_gate, dw_pre, dw_post, dgate, static_cast<hipStream_t>(hip_stream));
+    };
+    if (dt == PSATTN_BF16) go(uint16_t{});
+    else go(float{});
+    return hipGetLastError() == hipSuccess ? PSATTN_OK : PSATTN_EHIP;
+}
+
+}  // extern "C"

@@ -27,21 +27,26 @@ enum Pass {
     kPlain,  // out = acc
     kGate,   // Q is two matrices (gate, up): G, U, H = act(G) o U
     kDact,   // acc = dH: dG, dU from the kept G, U
+    // of the vocabulary head, m an item (a row that predicts a token), n a token of the vocabulary
+    kLse,     // acc = logits: maximum and sum of exponentials of each tile's part of a row, the logit of the row's token
+    kDlogit,  // acc = logits: out = weight (1[n = token] - exp(acc - lse))
+    kSums,    // parts = acc in fp32, or what is there and acc
 };
 
 struct Product {
     const void *p[2], *q[2];  // of the segments along k (n_seg), or of two products of one shape (n_prod, p and out only); kGate: q of gate and up
     void* out[2];             // kPlain: out[product]; kDact: dG, dU
-    float *G, *U;             // kGate: written (may be null); kDact: read
-    void* H;                  // kGate: written
+    float *G, *U;             // kGate: written (may be null); kDact: read; kLse: pairs [tile of n][M], logits [M], written; kDlogit: lse, weights [M]
+    void* H;                  // kGate: written; kLse, kDlogit: tokens [M], int32
     int64_t ldp, ldq, ldo;    // elements from one row in memory to the next
     int64_t ld_kept;          // kDact: of G and U
     int32_t M, N, K;          // K: of one segment
     int32_t n_seg, n_prod;
-    int32_t m_load, n_load;   // M, N, or what rows in memory have of them and more (rows padded to whole 16-byte groups)
+    int32_t m_load, n_load;   // M, N, or what rows in memory have of them and more (rows padded to whole 16-byte groups); kLse, kDlogit: n_load is the token of column 0
     int32_t odd;              // what is stored in the element type: rows that are not whole groups on 16-byte boundaries
     // k in n_split parts, whose sums go to `parts` in fp32 (rows of ld_part) and are joined by a kernel of their own
     int32_t n_split;
+    int32_t add;              // kSums: parts hold sums already
     float* parts;
     int64_t ld_part;
 };

@@ -1,0 +1,345 @@
+// The vocabulary head without kept logits: log-probabilities of responses from hidden rows X and the vocabulary matrix W, forward and
+// backward (paper Section 2.1, Eq. 1: the loss needs log pi(y | x) of every completion).
+//   items i: a row r_i that predicts token y_i of response j_i;  z_iv = X[r_i] . W[v],  lse_i = log sum_v exp z_iv
+//   forward:   log pi_j = sum over i of j of (z_{i, y_i} - lse_i)
+//   backward:  dz_iv = d_j (1[v = y_i] - exp(z_iv - lse_i));  dX[r] = sum over i of r of dz_i W,  dW = dz^T X
+//
+// Logits of a packed batch are larger than everything else in a step (65 536 rows of 128 000 bf16: 16.8 GB, and their gradient again).  Here they
+// exist as accumulators of the matrix product alone: its epilogue leaves a maximum and a sum of exponentials of every tile's part of a
+// row, and the target's logit.  The backward makes them again, a piece of the vocabulary at a time, and turns them into dz in the
+// epilogue; dz of a piece (in the element type, rounded once, from fp32) is the operand of the two other products: dW's rows of
+// the piece, written at once, and dX's sums over the pieces in fp32.  Only rows that predict something take part: prompts, most of the
+// tokens, do not.  A prompt's last row predicts the first token of every response and takes part once for each.
+//
+// Bound by the matrix cores (four products of 2 items vocab hidden operations in a training step, one of them to make the logits again), for few rows by
+// reading W.  No atomics: every sum has a fixed order.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <initializer_list>
+
+#include "psattn_head.h"
+#include "psattn_logprob.h"
+#include "psattn_rows.h"
+
+namespace {
+
+using namespace psattn::gemm;
+namespace rows = psattn::rows;
+
+constexpr int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+constexpr int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
+size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+size_t elem_bytes(int32_t dt) { return dt == PSATTN_BF16 ? 2 : 4; }
+
+// ---- the items' rows, made whole: one workgroup to a row.  Without a token of the vocabulary an item has no gradient, and its row is zeros there
+template <typename E, bool BWD>
+__global__ __launch_bounds__(256) void psattn_head_rows(const int32_t* item_row, const int32_t* item_tok, const int32_t* item_resp, const int32_t* token_ids,
+                                                        int vocab, int hidden, const E* X, const float* row_lse, const float* d_logp, E* out, int32_t* target,
+                                                        float* lse, float* weight) {
+    constexpr int V = rows::kVec<E>;
+    const int64_t i = blockIdx.x;
+    const int r = item_row[i], row = r < 0 ? ~r : r, id = token_ids[item_tok[i]];
+    const bool known = id >= 0 && id < vocab;
+    if (threadIdx.x == 0) {
+        target[i] = known ? id : -1;
+        if constexpr (BWD) {
+            lse[i] = known ? row_lse[row] : 0.f;
+            weight[i] = known ? d_logp[item_resp[i]] : 0.f;
+        }
+    }
+    const E* const x = X + static_cast<int64_t>(row) * hidden;
+    E* const to = out + i * ((hidden + 7) / 8 * 8);
+    for (int c = threadIdx.x * V; c < (hidden + 7) / 8 * 8; c += 256 * V) {
+        rows::u32x4 u = {0, 0, 0, 0};
+        if ((!BWD || known) && c < hidden) {
+            const auto at = rows::place<false, E>(c, hidden);
+            u = rows::settled<false>(rows::raw<false>(x, at, hidden), at.down);
+        }
+        *reinterpret_cast<rows::u32x4*>(to + c) = u;
+    }
+}
+
+// ---- joins the tiles' parts of an item's row: AT items to a workgroup, 256 / AT lanes to an item.  log pi of the item as (logit - max) - log(sum),
+// which keeps its accuracy where the token is almost certain
+template <int AT>
+__global__ __launch_bounds__(256) void psattn_head_join(int n_items, int n_parts, const float2* part, const int32_t* item_row, const int32_t* target, const float* hit,
+                                                        float* row_lse, float* item_logp) {
+    constexpr int L = 256 / AT, kAtOnce = 4;
+    __shared__ float2 sm[L][AT];
+    const int k = threadIdx.x / AT, o = threadIdx.x % AT, i = blockIdx.x * AT + o;
+    float m = -INFINITY, s = 0.f;
+    auto merge = [&](float m2, float s2) {
+        const float mn = fmaxf(m, m2), ref = mn == -INFINITY ? 0.f : mn;
+        s = s * expf(m - ref) + s2 * expf(m2 - ref);
+        m = mn;
+    };
+    if (i < n_items) {
+        int p = k;
+        for (; p + (kAtOnce - 1) * L < n_parts; p += kAtOnce * L) {
+            float2 x[kAtOnce];
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) x[u] = part[static_cast<int64_t>(p + u * L) * n_items + i];
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) merge(x[u].x, x[u].y);
+        }
+        for (; p < n_parts; p += L) {
+            const float2 x = part[static_cast<int64_t>(p) * n_items + i];
+            merge(x.x, x.y);
+        }
+    }
+    sm[k][o] = make_float2(m, s);
+    __syncthreads();
+#pragma unroll 1
+    for (int n = L / 2; n > 0; n >>= 1) {
+        if (k < n) {
+            merge(sm[k + n][o].x, sm[k + n][o].y);
+            sm[k][o] = make_float2(m, s);
+        }
+        __syncthreads();
+    }
+    if (k > 0 || i >= n_items) return;
+    const float ls = logf(s);
+    if (const int r = item_row[i]; r >= 0) row_lse[r] = m + ls;
+    item_logp[i] = target[i] >= 0 ? (hit[i] - m) - ls : 0.f;
+}
+
+__global__ __launch_bounds__(256) void psattn_head_responses(int first, const int32_t* item_ptr, const float* item_logp, float* resp_logp) {
+    __shared__ float sm[4];
+    const int j = first + static_cast<int>(blockIdx.x), end = item_ptr[j + 1];
+    float v = 0.f;
+    for (int i = item_ptr[j] + static_cast<int>(threadIdx.x); i < end; i += 256) v += item_logp[i];
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
+    if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = v;
+    __syncthreads();
+    if (threadIdx.x == 0) resp_logp[j] = (sm[0] + sm[1]) + (sm[2] + sm[3]);
+}
+
+// ---- dX of token t: the sums of its items, of all parts of each
+template <typename E>
+__global__ __launch_bounds__(256) void psattn_head_dx(int first, int hidden, int n_items, int n_parts, int64_t ld, const float* parts, const int32_t* row_desc,
+                                                      const int32_t* resp_first, const int32_t* resp_len, const int32_t* resp_prev, const int32_t* samp_ptr,
+                                                      const int32_t* item_ptr, E* dX) {
+    constexpr int V = 4;
+    const int row = first + static_cast<int>(blockIdx.x), desc = row_desc[row];
+    E* const to = dX + static_cast<int64_t>(row) * hidden;
+    int r0 = 0, r1 = 0;  // responses with an item of this row
+    if (desc >= 0) r0 = desc, r1 = desc + 1;
+    else if (desc < -1) r0 = samp_ptr[-2 - desc], r1 = samp_ptr[-1 - desc];
+    for (int c = threadIdx.x * V; c < hidden; c += 256 * V) {
+        float x[V] = {};
+        for (int j = r0; j < r1; ++j) {
+            if (resp_len[j] == 0) continue;
+            const int i = item_ptr[j] + (desc >= 0 ? row - resp_first[j] + (resp_prev[j] >= 0 ? 1 : 0) : 0);
+            for (int p = 0; p < n_parts; ++p) {
+                const float4 u = *reinterpret_cast<const float4*>(parts + (static_cast<int64_t>(p) * n_items + i) * ld + c);
+                x[0] += u.x, x[1] += u.y, x[2] += u.z, x[3] += u.w;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            if (c + k < hidden) rows::store1(to + c + k, x[k]);
+    }
+}
+
+// zeros without a memset, which a captured graph would not replay faithfully
+__global__ void psattn_head_zero(uint16_t* p, size_t n) {
+    for (size_t i = blockIdx.x * static_cast<size_t>(blockDim.x) + threadIdx.x; i < n; i += static_cast<size_t>(gridDim.x) * blockDim.x) p[i] = 0;
+}
+
+// n workgroups in grids of at most 2^31 threads
+template <typename F>
+void in_grids(int64_t n, F launch) {
+    constexpr int64_t most = (int64_t{1} << 31) / 256;
+    for (int64_t at = 0; at < n; at += most) launch(at, static_cast<uint32_t>(std::min<int64_t>(n - at, most)));
+}
+
+// ---- products
+bool at16(std::initializer_list<const void*> p) {
+    uintptr_t a = 0;
+    for (const void* x : p) a |= reinterpret_cast<uintptr_t>(x);
+    return a % 16 == 0;
+}
+
+// Which tile: few rows take tiles of 32 and 64 rows, whose workgroups share a CU; else that of the fewer rounds of workgroups, a step of k costing 1.05
+// with 128 x 128 (two to a CU) and 1.6 with 256 x 256
+TileSize tile_size(int64_t M, int64_t N) {
+    if (M <= 32) return k32;
+    if (M <= 64) return k64;
+    const int64_t small = cdiv(M, 128) * cdiv(N, 128), big = cdiv(M, 256) * cdiv(N, 256);
+    return 1.05 * cdiv(small, 512) < 1.6 * cdiv(big, 256) ? k128 : k256;
+}
+
+int head_product(int32_t dt, Pass pass, Product d, hipStream_t s) {
+    const TileSize size = tile_size(d.M, d.N);
+    d.odd = pass == kDlogit && !(at16({d.out[0]}) && d.ldo % 8 == 0 && d.N % 8 == 0);
+    const bool whole = at16({d.p[0], d.q[0]}) && d.ldp % 8 == 0 && d.ldq % 8 == 0 && (pass != kSums || d.n_load % 8 == 0);
+    return (dt != PSATTN_BF16 ? head_product_f32 : whole ? head_product_bf16 : head_product_bf16_any)(pass, size, d, s);
+}
+
+// dz of a piece of the vocabulary has this much room at most
+constexpr int64_t kPieceBytes = int64_t{512} << 20;
+int64_t piece_rows(int32_t dt, int64_t n_items, int64_t vocab) {
+    const int64_t most = kPieceBytes / static_cast<int64_t>(elem_bytes(dt)) / std::max<int64_t>(n_items, 1) / 256 * 256;
+    if (most >= vocab) return vocab;
+    const int64_t n = cdiv(vocab, std::max<int64_t>(most, 256));
+    return cdiv(cdiv(vocab, n), 256) * 256;
+}
+// parts of the vocabulary for dX's sums: workgroups for the whole chip where the rows' tiles are fewer
+int64_t dx_parts(int32_t dt, int64_t n_items, int64_t vocab, int64_t hidden) {
+    const TileSize size = tile_size(n_items, hidden);
+    const int64_t bm = size == k32 ? 32 : size == k64 ? 64 : size == k128 ? 128 : 256, bn = size == k256 ? 256 : 128;
+    const int64_t tiles = std::max<int64_t>(1, cdiv(n_items, bm)) * cdiv(hidden, bn), slots = size == k256 ? 256 : size == k128 ? 512 : size == k64 ? 768 : 1024;
+    const int64_t steps = piece_rows(dt, n_items, vocab) / (dt == PSATTN_BF16 ? 64 : 32);
+    return std::max<int64_t>(1, std::min({slots / tiles, steps / 4, int64_t{64}}));
+}
+
+struct Room {
+    char* p;
+    explicit Room(void* base) : p(reinterpret_cast<char*>(align_up(reinterpret_cast<uintptr_t>(base), 256))) {}
+    template <typename T>
+    T* take(size_t n) {
+        T* const r = reinterpret_cast<T*>(p);
+        p += align_up(n * sizeof(T), 256);
+        return r;
+    }
+};
+
+bool bad_shape(const psattn_lp_plan* plan, int32_t dt, int32_t vocab, int32_t hidden) {
+    return !plan || (dt != PSATTN_F32 && dt != PSATTN_BF16) || vocab <= 0 || hidden <= 0;
+}
+// a tile's copies have 32-bit offsets, and grids stay below 2^31 threads
+bool too_large(const psattn_lp_plan* plan, int32_t dt, int64_t vocab, int64_t hidden, bool bwd) {
+    const int64_t n = plan->n_items;
+    if (hidden * static_cast<int64_t>(elem_bytes(dt)) * 256 >= (int64_t{1} << 31) || n >= (int64_t{1} << 23) || vocab > INT32_MAX - 512) return true;
+    auto fits = [](int64_t M, int64_t N, TileSize t) {
+        static constexpr int bm[] = {32, 64, 128, 256}, bn[] = {128, 128, 128, 256}, threads[] = {128, 128, 256, 512};
+        return cdiv(M, bm[t]) * cdiv(N, bn[t]) < (int64_t{1} << 31) / threads[t];
+    };
+    if (!bwd) return !fits(n, vocab, tile_size(n, vocab));
+    const int64_t piece = piece_rows(dt, n, vocab);
+    return !fits(n, piece, tile_size(n, piece)) || !fits(n, hidden, tile_size(n, hidden)) || !fits(piece, hidden, k128);
+}
+
+size_t fwd_bytes(const psattn_lp_plan* plan, int32_t dt, int32_t vocab, int32_t hidden) {
+    if (bad_shape(plan, dt, vocab, hidden)) return 0;
+    const size_t n = static_cast<size_t>(plan->n_items);
+    return align_up(n * up8(hidden) * elem_bytes(dt), 256) + align_up(n * cdiv(vocab, 128) * sizeof(float2), 256) + 3 * align_up(n * 4, 256) + 256;
+}
+size_t bwd_bytes(const psattn_lp_plan* plan, int32_t dt, int32_t vocab, int32_t hidden) {
+    if (bad_shape(plan, dt, vocab, hidden)) return 0;
+    const size_t n = static_cast<size_t>(plan->n_items);
+    return align_up(n * up8(hidden) * elem_bytes(dt), 256) + align_up(n * up8(piece_rows(dt, n, vocab)) * elem_bytes(dt), 256) +
+           align_up(n * up8(hidden) * dx_parts(dt, n, vocab, hidden) * sizeof(float), 256) + 3 * align_up(n * 4, 256) + 256;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t psattn_head_logprob_fwd_workspace_bytes(const psattn_lp_plan* plan, int32_t dt, int32_t vocab, int32_t hidden) { return fwd_bytes(plan, dt, vocab, hidden); }
+
+size_t psattn_head_logprob_bwd_workspace_bytes(const psattn_lp_plan* plan, int32_t dt, int32_t vocab, int32_t hidden) { return bwd_bytes(plan, dt, vocab, hidden); }
+
+int psattn_head_logprob_fwd(const psattn_lp_plan* plan, int32_t dt, int32_t vocab, int32_t hidden, const void* X, const void* W, const int32_t* token_ids, float* row_lse,
+                            float* resp_logp, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    if (bad_shape(plan, dt, vocab, hidden)) return PSATTN_EINVAL;
+    if (plan->n_resp == 0) return PSATTN_OK;
+    if (!X || !W || !token_ids || !row_lse || !resp_logp || !workspace || workspace_bytes < fwd_bytes(plan, dt, vocab, hidden)) return PSATTN_EINVAL;
+    if (too_large(plan, dt, vocab, hidden, false)) return PSATTN_EUNSUPPORTED;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    const int n = static_cast<int>(plan->n_items);
+    Room room(workspace);
+    char* const x = room.take<char>(static_cast<size_t>(n) * up8(hidden) * elem_bytes(dt));
+    float2* const part = room.take<float2>(static_cast<size_t>(n) * cdiv(vocab, 128));
+    int32_t* const target = room.take<int32_t>(n);
+    float *const hit = room.take<float>(n), *const logp = room.take<float>(n);
+    if (n > 0) {
+        auto gather = [&](auto* to) {
+            using E = std::remove_pointer_t<decltype(to)>;
+            psattn_head_rows<E, false><<<n, 256, 0, s>>>(plan->item_row, plan->item_tok, plan->item_resp, token_ids, vocab, hidden, static_cast<const E*>(X), nullptr,
+                                                         nullptr, to, target, nullptr, nullptr);
+        };
+        if (dt == PSATTN_BF16) gather(reinterpret_cast<uint16_t*>(x));
+        else gather(reinterpret_cast<float*>(x));
+        Product z{};
+        z.p[0] = x; z.q[0] = W; z.G = reinterpret_cast<float*>(part); z.U = hit; z.H = target;
+        z.ldp = up8(hidden); z.ldq = hidden;
+        z.M = n; z.N = vocab; z.K = hidden; z.n_seg = z.n_prod = z.n_split = 1;
+        const int rc = head_product(dt, kLse, z, s);
+        if (rc != PSATTN_OK) return rc;
+        const int parts = static_cast<int>(cdiv(vocab, tile_size(n, vocab) == k256 ? 256 : 128));
+        if (n <= 256) psattn_head_join<1><<<n, 256, 0, s>>>(n, parts, part, plan->item_row, target, hit, row_lse, logp);
+        else psattn_head_join<16><<<static_cast<uint32_t>(cdiv(n, 16)), 256, 0, s>>>(n, parts, part, plan->item_row, target, hit, row_lse, logp);
+    }
+    in_grids(plan->n_resp, [&](int64_t at, uint32_t grid) { psattn_head_responses<<<grid, 256, 0, s>>>(static_cast<int>(at), plan->item_ptr, logp, resp_logp); });
+    return hipGetLastError() == hipSuccess ? PSATTN_OK : PSATTN_EHIP;
+}
+
+int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t vocab, int32_t hidden, const void* X, const void* W, const int32_t* token_ids,
+                            const float* row_lse, const float* d_resp_logp, void* dX, void* dW, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    if (bad_shape(plan, dt, vocab, hidden) || !dW) return PSATTN_EINVAL;
+    if (plan->T > 0 && !dX) return PSATTN_EINVAL;
+    const int n = static_cast<int>(plan->n_items);
+    if (n > 0 && (!X || !W || !token_ids || !row_lse || !d_resp_logp || !workspace || workspace_bytes < bwd_bytes(plan, dt, vocab, hidden))) return PSATTN_EINVAL;
+    if (too_large(plan, dt, vocab, hidden, true)) return PSATTN_EUNSUPPORTED;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    const size_t e = elem_bytes(dt);
+    Room room(workspace);
+    const int parts = static_cast<int>(dx_parts(dt, n, vocab, hidden));
+    const int64_t ld = up8(hidden), piece = piece_rows(dt, n, vocab), ldz = up8(piece);
+    float* sums = nullptr;
+    if (n == 0) {  // nothing is predicted: sums over nothing
+        psattn_head_zero<<<1024, 256, 0, s>>>(static_cast<uint16_t*>(dW), static_cast<size_t>(vocab) * hidden * e / 2);
+    } else {
+        char* const x = room.take<char>(static_cast<size_t>(n) * ld * e);
+        char* const dz = room.take<char>(static_cast<size_t>(n) * ldz * e);
+        sums = room.take<float>(static_cast<size_t>(n) * ld * parts);
+        int32_t* const target = room.take<int32_t>(n);
+        float *const lse = room.take<float>(n), *const weight = room.take<float>(n);
+        auto gather = [&](auto* to) {
+            using E = std::remove_pointer_t<decltype(to)>;
+            psattn_head_rows<E, true><<<n, 256, 0, s>>>(plan->item_row, plan->item_tok, plan->item_resp, token_ids, vocab, hidden, static_cast<const E*>(X), row_lse,
+                                                        d_resp_logp, to, target, lse, weight);
+        };
+        if (dt == PSATTN_BF16) gather(reinterpret_cast<uint16_t*>(x));
+        else gather(reinterpret_cast<float*>(x));
+        for (int64_t at = 0; at < vocab; at += piece) {
+            const int32_t cols = static_cast<int32_t>(std::min<int64_t>(piece, vocab - at));
+            const char* const w = static_cast<const char*>(W) + at * hidden * e;
+            int rc;
+            Product z{};  // dz
+            z.p[0] = x; z.q[0] = w; z.G = lse; z.U = weight; z.H = target; z.out[0] = dz;
+            z.ldp = ld; z.ldq = hidden; z.ldo = ldz;
+            z.M = n; z.N = cols; z.K = hidden; z.n_seg = z.n_prod = z.n_split = 1;
+            z.n_load = static_cast<int32_t>(at);
+            if ((rc = head_product(dt, kDlogit, z, s)) != PSATTN_OK) return rc;
+            Product a{};  // dX += dz W
+            a.p[0] = dz; a.q[0] = w; a.parts = sums; a.ld_part = ld; a.add = at > 0;
+            a.ldp = ldz; a.ldq = hidden;
+            a.M = n; a.N = a.n_load = hidden; a.K = cols; a.n_seg = a.n_prod = 1; a.n_split = parts;
+            if ((rc = head_product(dt, kSums, a, s)) != PSATTN_OK) return rc;
+            Product g{};  // dW = dz^T X
+            g.p[0] = dz; g.q[0] = x; g.out[0] = static_cast<char*>(dW) + at * hidden * e;
+            g.ldp = ldz; g.ldq = ld; g.ldo = hidden;
+            g.M = cols; g.m_load = static_cast<int32_t>(up8(cols)); g.N = hidden; g.n_load = static_cast<int32_t>(ld); g.K = n; g.n_seg = g.n_prod = g.n_split = 1;
+            g.odd = !(at16({g.out[0]}) && hidden % 8 == 0);
+            const int64_t small = cdiv(cols, 128) * cdiv(hidden, 128), big = cdiv(cols, 256) * cdiv(hidden, 256);
+            const TileSize size = 1.05 * cdiv(small, 512) < 1.6 * cdiv(big, 256) ? k128 : k256;
+            if ((rc = (dt == PSATTN_BF16 ? product_bf16 : product_f32)(kPlain, 0, false, false, size, g, s)) != PSATTN_OK) return rc;
+        }
+    }
+    in_grids(plan->T, [&](int64_t at, uint32_t grid) {
+        auto go = [&](auto* to) {
+            using E = std::remove_pointer_t<decltype(to)>;
+            psattn_head_dx<E><<<grid, 256, 0, s>>>(static_cast<int>(at), hidden, n, parts, ld, sums, plan->row_desc, plan->resp_first, plan->resp_len, plan->resp_prev,
+                                                   plan->samp_ptr, plan->item_ptr, to);
+        };
+        if (dt == PSATTN_BF16) go(static_cast<uint16_t*>(dX));
+        else go(static_cast<float*>(dX));
+    });
+    return hipGetLastError() == hipSuccess ? PSATTN_OK : PSATTN_EHIP;
+}
+
+}  // extern "C"

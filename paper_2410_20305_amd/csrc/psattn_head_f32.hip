@@ -1,0 +1,10 @@
+// The vocabulary head's products: see psattn_head_tiles.h.
+#include "psattn_head_tiles.h"
+
+namespace psattn {
+namespace gemm {
+
+int head_product_f32(Pass pass, TileSize size, const Product& d, hipStream_t s) { return launch_head<float, false>(pass, size, d, s); }
+
+}  // namespace gemm
+}  // namespace psattn

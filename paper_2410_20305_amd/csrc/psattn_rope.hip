@@ -16,19 +16,14 @@
 // the block mask, so no position array is stored either.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
+#include <exception>
 #include <new>
 #include <vector>
 
 #include "psattn_mfma_common.h"
-
-struct psattn_rope {
-    int32_t head_dim = 0;
-    int32_t max_positions = 0;
-    float theta = 0.f;
-    int device = -1;
-    float* d_table = nullptr;  // [max_positions][128]: cos[64] | sin[64]
-};
+#include "psattn_rope.h"
 
 namespace psattn {
 namespace {
@@ -57,43 +52,37 @@ __global__ __launch_bounds__(256) void psattn_rope_k_bf16(AttnArgs a, uint16_t* 
 
 int check_rope(const psattn_meta* meta, const psattn_rope* rope, int32_t dt, int32_t head_dim) {
     if (!meta || !rope) return PSATTN_EINVAL;
-    if (dt != PSATTN_BF16 || head_dim != 128 || rope->head_dim != 128) return PSATTN_EUNSUPPORTED;
+    if (dt != PSATTN_BF16 || head_dim != 128 || rope->head_dim != 128 || rope->rotary_dim != 128 || rope->layout != PSATTN_ROPE_HALF) return PSATTN_EUNSUPPORTED;
     if (!meta->on_device) return PSATTN_ENODEVICE;
     if (meta->n_positions > rope->max_positions) return PSATTN_ELIMIT;
     return PSATTN_OK;
 }
 
 }  // namespace
-}  // namespace psattn
 
-extern "C" {
-
-int psattn_rope_create(int32_t head_dim, float theta, int32_t max_positions, void* hip_stream, psattn_rope** out) {
-    if (!out) return PSATTN_EINVAL;
-    *out = nullptr;
-    if (max_positions <= 0 || !(theta > 0.f)) return PSATTN_EINVAL;
-    if (head_dim != 128) return PSATTN_EUNSUPPORTED;
+int make_rope(int32_t head_dim, int32_t rotary_dim, int32_t layout, const double* inv_freq, double amplitude, int32_t max_positions, void* hip_stream,
+              psattn_rope** out) {
     psattn_rope* r = new (std::nothrow) psattn_rope();
     if (!r) return PSATTN_ENOMEM;
     r->head_dim = head_dim;
+    r->rotary_dim = rotary_dim;
+    r->layout = layout;
     r->max_positions = max_positions;
-    r->theta = theta;
-    const size_t n = static_cast<size_t>(max_positions) * 128;
+    const int half = rotary_dim / 2;
+    const size_t n = static_cast<size_t>(max_positions) * rotary_dim;
     std::vector<float> host;
     try {
         host.resize(n);
-    } catch (const std::bad_alloc&) {
+    } catch (const std::exception&) {  // no memory, or more than a vector may hold
         delete r;
         return PSATTN_ENOMEM;
     }
     // angles in double: a float product position * frequency would lose the low bits of long positions
-    double inv_freq[64];
-    for (int i = 0; i < 64; ++i) inv_freq[i] = std::pow(static_cast<double>(theta), -2.0 * i / head_dim);
     for (int32_t p = 0; p < max_positions; ++p)
-        for (int i = 0; i < 64; ++i) {
+        for (int i = 0; i < half; ++i) {
             const double a = static_cast<double>(p) * inv_freq[i];
-            host[static_cast<size_t>(p) * 128 + i] = static_cast<float>(std::cos(a));
-            host[static_cast<size_t>(p) * 128 + 64 + i] = static_cast<float>(std::sin(a));
+            host[static_cast<size_t>(p) * rotary_dim + i] = static_cast<float>(amplitude * std::cos(a));
+            host[static_cast<size_t>(p) * rotary_dim + half + i] = static_cast<float>(amplitude * std::sin(a));
         }
     if (hipGetDevice(&r->device) != hipSuccess || hipMalloc(reinterpret_cast<void**>(&r->d_table), n * sizeof(float)) != hipSuccess) {
         (void)hipGetLastError();
@@ -110,6 +99,55 @@ int psattn_rope_create(int32_t head_dim, float theta, int32_t max_positions, voi
         return PSATTN_EHIP;
     }
     *out = r;
+    return PSATTN_OK;
+}
+
+}  // namespace psattn
+
+extern "C" {
+
+int psattn_rope_create(int32_t head_dim, float theta, int32_t max_positions, void* hip_stream, psattn_rope** out) {
+    if (!out) return PSATTN_EINVAL;
+    *out = nullptr;
+    if (max_positions <= 0 || !(theta > 0.f)) return PSATTN_EINVAL;
+    if (head_dim != 128) return PSATTN_EUNSUPPORTED;
+    double inv_freq[64];
+    for (int i = 0; i < 64; ++i) inv_freq[i] = std::pow(static_cast<double>(theta), -2.0 * i / head_dim);
+    return psattn::make_rope(head_dim, head_dim, PSATTN_ROPE_HALF, inv_freq, 1.0, max_positions, hip_stream, out);
+}
+
+int psattn_rope_create_layout(int32_t head_dim, int32_t rotary_dim, int32_t layout, const double* inv_freq, double amplitude,
+                              int32_t max_positions, void* hip_stream, psattn_rope** out) {
+    if (!out) return PSATTN_EINVAL;
+    *out = nullptr;
+    if (head_dim <= 0 || rotary_dim <= 0 || rotary_dim % 2 != 0 || rotary_dim > head_dim || max_positions <= 0 || !inv_freq) return PSATTN_EINVAL;
+    if (layout != PSATTN_ROPE_HALF && layout != PSATTN_ROPE_INTERLEAVED) return PSATTN_EINVAL;
+    if (!std::isfinite(amplitude)) return PSATTN_EINVAL;
+    if (head_dim > psattn::kRopeMostDims) return PSATTN_EUNSUPPORTED;
+    for (int i = 0; i < rotary_dim / 2; ++i)
+        if (!std::isfinite(inv_freq[i])) return PSATTN_EINVAL;
+    return psattn::make_rope(head_dim, rotary_dim, layout, inv_freq, amplitude, max_positions, hip_stream, out);
+}
+
+int psattn_rope_frequencies(int32_t rotary_dim, double theta, int32_t scaling, double factor, double original_positions, double low, double high,
+                            double* inv_freq) {
+    if (!inv_freq || rotary_dim <= 0 || rotary_dim % 2 != 0 || !(theta > 0.0) || std::isinf(theta)) return PSATTN_EINVAL;
+    if (scaling < PSATTN_ROPE_PLAIN || scaling > PSATTN_ROPE_PARTS) return PSATTN_EINVAL;
+    if (scaling != PSATTN_ROPE_PLAIN && (!(factor > 0.0) || std::isinf(factor))) return PSATTN_EINVAL;
+    if (scaling == PSATTN_ROPE_PARTS && (!(original_positions > 0.0) || std::isinf(original_positions) || !(high > low) || std::isinf(low) || std::isinf(high))) return PSATTN_EINVAL;
+    const int n = rotary_dim;
+    // the lowest frequency is divided by the factor, the highest stays 1: theta^(-(n - 2) / n) falls by factor^(-1)
+    const double base = scaling == PSATTN_ROPE_BASE && n > 2 ? theta * std::pow(factor, static_cast<double>(n) / (n - 2)) : theta;
+    for (int i = 0; i < n / 2; ++i) {
+        double f = std::pow(base, -2.0 * i / n);
+        if (scaling == PSATTN_ROPE_LINEAR) f /= factor;
+        if (scaling == PSATTN_ROPE_PARTS) {
+            const double turns = f * original_positions / 6.283185307179586476925;
+            const double keep = std::min(1.0, std::max(0.0, (turns - low) / (high - low)));
+            f = keep * f + (1.0 - keep) * f / factor;
+        }
+        inv_freq[i] = f;
+    }
     return PSATTN_OK;
 }
 

@@ -1,4 +1,4 @@
-// Rows of fp32 or bf16 in groups of 16 bytes, whatever address they start at (layer norm, embedding).
+// Rows of fp32 or bf16 in groups of 16 bytes, whatever address they start at (norms, embedding).
 #pragma once
 #include <algorithm>
 #include <initializer_list>
@@ -119,6 +119,35 @@ template <typename E>
 __device__ __forceinline__ int misalignment(const E* row) {
     return static_cast<int>(reinterpret_cast<uintptr_t>(row) / sizeof(E) % kVec<E>);
 }
+
+// a value as the element type holds it
+__device__ __forceinline__ float hold(float v, const uint16_t*) { return __uint_as_float(psattn::mma::pack2(v, 0.f) << 16); }
+__device__ __forceinline__ float hold(float v, const float*) { return v; }
+
+// sums over LANES lanes, the same in each; `sm` (more than a wave): 16 N floats, another place for each call in flight
+template <int LANES, int N>
+__device__ __forceinline__ void group_sum(float (&v)[N], float* sm) {
+#pragma unroll
+    for (int off = (LANES < 64 ? LANES : 64) / 2; off > 0; off >>= 1)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], off);
+    if constexpr (LANES > 64) {
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) sm[(threadIdx.x >> 6) * N + i] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            v[i] = sm[i];
+#pragma unroll
+            for (int w = 1; w < LANES / 64; ++w) v[i] += sm[w * N + i];
+        }
+    }
+}
+
+// A row to LANES lanes, PER groups of 16 bytes to each.  Rows of a wave and less share a workgroup of 256.
+template <int LANES>
+constexpr int kThreads = LANES < 256 ? 256 : LANES;
 
 // rows of `hidden` elements that all start on a 16-byte boundary and are whole groups
 template <typename E>
