@@ -418,6 +418,32 @@ int psattn_dpo_loss(int32_t n_pairs, float beta, const float* logp_policy, const
                     float* loss, float* d_logp, void* hip_stream);
 
 /*
+ * The same log-probabilities from the hidden rows X [T, hidden] and the vocabulary matrix W [vocab, hidden] (the convention [out_features,
+ * in_features]; for a tied model the table of psattn_embed_fwd), logits = X W^T, which are never in memory: the forward
+ * takes their maxima and sums where they are made, the backward makes them again, a piece of the vocabulary at a time.
+ * X and W of dt, any width, any alignment of an element (16-byte boundaries and widths that are whole 16-byte groups are faster).
+ *
+ * psattn_head_logprob_fwd: row_lse and resp_logp as by psattn_logprob_fwd; logits are fp32, not rounded to dt.  Rows of X that predict
+ * nothing are not read.
+ * psattn_head_logprob_bwd: dX [T, hidden] and dW [vocab, hidden] of dt, both overwritten as a whole (dX is zero for rows that predict
+ * nothing): the gradients of sum_j d_resp_logp[j] * resp_logp[j], from the forward's row_lse.  The gradient of the logits is an
+ * operand of the matrix cores and is rounded to dt once, from fp32; sums are fp32 in a fixed order.  A response whose d_resp_logp is 0,
+ * and a token id outside [0, vocab), give nothing.
+ * Workspaces: the caller's device memory, of at least the bytes that the call of that name gives for the plan (never 0 for valid
+ * arguments), contents undefined on entry and exit, one for each call in flight.  The backward's holds the rows and one piece (at most
+ * 512 MiB) of the logits' gradient.  No call allocates or blocks, and all may be captured into a graph.
+ * PSATTN_EUNSUPPORTED: rows of 2^23 bytes and more, 2^23 predicted tokens and more, or sizes whose grids would have 2^31 threads.
+ */
+size_t psattn_head_logprob_fwd_workspace_bytes(const psattn_lp_plan* plan, int32_t dt, int32_t vocab, int32_t hidden);
+int psattn_head_logprob_fwd(const psattn_lp_plan* plan, int32_t dt, int32_t vocab, int32_t hidden, const void* X, const void* W,
+                            const int32_t* token_ids, float* row_lse, float* resp_logp, void* workspace, size_t workspace_bytes,
+                            void* hip_stream);
+size_t psattn_head_logprob_bwd_workspace_bytes(const psattn_lp_plan* plan, int32_t dt, int32_t vocab, int32_t hidden);
+int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t vocab, int32_t hidden, const void* X, const void* W,
+                            const int32_t* token_ids, const float* row_lse, const float* d_resp_logp, void* dX, void* dW, void* workspace,
+                            size_t workspace_bytes, void* hip_stream);
+
+/*
  * What stands beside attention and the loss head in a model: the rows that enter it, the norm in front of each part of a
  * block, and the block's feed-forward part.  They act on single tokens, so prefix sharing saves the same share of them as of
  * the projections (Section 4.2 times such parts with the attention).  A packed buffer of T tokens is T rows; padding is
