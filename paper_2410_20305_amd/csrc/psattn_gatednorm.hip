@@ -109,41 +109,62 @@ __global__ __launch_bounds__(kThreads<LANES>) void psattn_gn_fwd(Args<E> a) {
     }
 }
 
-// A lane's values of one group of a row, and what comes of them
-template <int V>
-struct Group {
-    float s[V], b[V], dy[V], t[V], g[V], wp[V];  // t: dS, then dS + rs q; g: gate; wp: w_post
-};
-
 // Backward.  A workgroup takes the rows from blockIdx.x on, gridDim.x apart, and keeps its lanes' columns of dw_pre and C in registers;
 // they go to part[workgroup] at its end and are joined by psattn_gn_weights (rows that share a workgroup add up in LDS first).
-// Rows stay in the registers as they came and are unpacked twice, with room for the next row's loads while one is summed.
+// Rows stay in the registers as they came and are unpacked twice, with room for the next row's loads while one is summed.  ALL: a gate
+// for each row; else w_post and gate are one factor for all rows.  What there is not stands there as zeros or ones, without branches.
 //   Without SUMS a workgroup has one row, whose rs m it keeps, and the columns are left to psattn_gn_columns.
-template <typename E, int LANES, int PER, bool WHOLE, bool SUMS>
+template <typename E, int LANES, int PER, bool WHOLE, bool SUMS, bool ALL>
 __global__ __launch_bounds__(kThreads<LANES>) void psattn_gn_bwd(Args<E> a) {
     constexpr int V = kVec<E>, kAt = kThreads<LANES> / LANES;  // rows at a time
     __shared__ float sm[2][48];
     __shared__ float add[kAt > 1 ? kAt * LANES * PER * V : 1];
     static_assert(SUMS || kAt == 1, "short rows' columns are summed here");
-    const int lane = threadIdx.x % LANES, own = threadIdx.x / LANES, hidden = a.hidden, n_rows = a.n_rows;
+    const int lane = threadIdx.x % LANES, hidden = a.hidden, n_rows = a.n_rows;
+    // rows of a wave and more are known to be: their addresses are scalar
+    const int own = kAt == 1 ? 0 : LANES == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : static_cast<int>(threadIdx.x) / LANES;
     float dw[PER][V] = {}, dc[PER][V] = {};
-    constexpr bool kAhead = SUMS;
+    constexpr bool kAhead = SUMS && PER <= 2 && (WHOLE || !ALL || PER * V < 16 || LANES < 512);  // the next row's loads, where there are registers for them
     const int step = gridDim.x * kAt;
     int row = blockIdx.x * kAt + own;
     // this lane's first column: the same for all its rows, whose misalignment has to be
     const int from = lane * V - (WHOLE || (step % V != 0 && hidden % V != 0) || row >= n_rows ? 0 : misalignment(a.S + static_cast<size_t>(row) * hidden));
+    // The weights' groups stay in registers, and with one factor for all rows so does its product of w_post and gate, in fp32.  Of rows of four
+    // groups to a lane they are asked for again each time
+    constexpr bool kKeep = PER <= 2;
     Place pl[PER];
-    u32x4 w_pre[PER], w_post[PER];
+    u32x4 w_pre[kKeep ? PER : 1], w_post[kKeep ? PER : 1];
+    float both[kKeep && !ALL ? PER : 1][V];
+    auto weight = [&](const E* w, int p) { return settled<WHOLE>(raw<WHOLE>(w, pl[p], hidden), pl[p].down); };
+    auto post = [&](int p) {
+        float one[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) one[j] = 1.f;
+        return a.w_post ? weight(a.w_post, p) : pack<E>(one);
+    };
+    auto times_gate = [&](int p, float (&f)[V]) {
+        if (!a.gate) return;
+        float g[V];
+        unpack(weight(a.gate, p), g);
+#pragma unroll
+        for (int j = 0; j < V; ++j) f[j] *= g[j];
+    };
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
         pl[p] = place<WHOLE, E>(from + p * LANES * V, hidden);
-        w_pre[p] = settled<WHOLE>(raw<WHOLE>(a.w_pre, pl[p], hidden), pl[p].down);
-        if (a.w_post) w_post[p] = settled<WHOLE>(raw<WHOLE>(a.w_post, pl[p], hidden), pl[p].down);
+        if constexpr (kKeep) {
+            w_pre[p] = weight(a.w_pre, p);
+            w_post[p] = post(p);
+            if constexpr (!ALL) {
+                unpack(w_post[p], both[p]);
+                times_gate(p, both[p]);
+            }
+        }
     }
     struct Row {
-        u32x4 s[PER], b[PER], dy[PER], ds[PER], g[PER];
+        u32x4 s[PER], b[PER], dy[PER], ds[PER], g[ALL ? PER : 1];
         float rs, rb;
-    } now, next;
+    } now = {}, next = {};
     auto fetch = [&](int r, Row& x) {
         const size_t at = static_cast<size_t>(r) * hidden;
         x.rs = a.rstd_s[r];
@@ -154,86 +175,88 @@ __global__ __launch_bounds__(kThreads<LANES>) void psattn_gn_bwd(Args<E> a) {
             x.dy[p] = raw<WHOLE>(a.dY + at, pl[p], hidden);
             if (a.B) x.b[p] = raw<WHOLE>(a.B + at, pl[p], hidden);
             if (a.dS) x.ds[p] = raw<WHOLE>(a.dS + at, pl[p], hidden);
-            if (a.gate) x.g[p] = raw<WHOLE>(a.gate + static_cast<size_t>(r) * a.gate_step, pl[p], hidden);
+            if constexpr (ALL) x.g[p] = raw<WHOLE>(a.gate + at, pl[p], hidden);
         }
     };
     if (kAhead && row < n_rows) fetch(row, now);
     for (int turn = 0; row < n_rows; row += step, turn ^= 1) {
         if constexpr (!kAhead) fetch(row, now);
         else if (row + step < n_rows) fetch(row + step, next);
-        // outside of the row s, dy and the weights are zeros
-        auto unpacked = [&](int p, Group<V>& x) {
-            float wv[V];
-            unpack(settled<WHOLE>(now.s[p], pl[p].down), x.s);
-            unpack(settled<WHOLE>(now.dy[p], pl[p].down), x.dy);
-            unpack(w_pre[p], wv);
-#pragma unroll
-            for (int j = 0; j < V; ++j) x.s[j] *= now.rs;
-            if (a.dS) unpack(settled<WHOLE>(now.ds[p], pl[p].down), x.t);
+        // a lane's values of one group; outside of the row s, b, dy and t are zeros
+        float s[V], b[V], dy[V], t[V], g[V], f[V];
+        auto unpacked = [&](int p, float (&q)[V]) {
+            unpack(settled<WHOLE>(now.s[p], pl[p].down), s);
+            unpack(settled<WHOLE>(now.b[p], pl[p].down), b);
+            unpack(settled<WHOLE>(now.dy[p], pl[p].down), dy);
+            unpack(settled<WHOLE>(now.ds[p], pl[p].down), t);
+            if constexpr (ALL) unpack(settled<WHOLE>(now.g[p], pl[p].down), g);
+            if constexpr (kKeep) {
+                unpack(w_pre[p], q);
+                if constexpr (ALL) unpack(w_post[p], f);
+            } else {
+                unpack(weight(a.w_pre, p), q);
+                unpack(post(p), f);
+                if constexpr (!ALL) times_gate(p, f);
+            }
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                x.t[j] = fmaf(now.rs, x.dy[j] * wv[j], a.dS ? x.t[j] : 0.f);
-                wv[j] *= x.dy[j];
-            }
-            if (a.B) {
-                unpack(settled<WHOLE>(now.b[p], pl[p].down), x.b);
-#pragma unroll
-                for (int j = 0; j < V; ++j) x.b[j] *= now.rb;
-            }
-            if (a.gate) unpack(settled<WHOLE>(now.g[p], pl[p].down), x.g);
-            if (a.w_post) unpack(w_post[p], x.wp);
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                if (!a.B) x.b[j] = 0.f;
-                if (!a.gate) x.g[j] = 1.f;
-                if (!a.w_post) x.wp[j] = 1.f;
+                if constexpr (kKeep && !ALL) f[j] = both[p][j];
+                q[j] *= dy[j];
+                s[j] *= now.rs;
+                b[j] *= now.rb;
+                t[j] = fmaf(now.rs, q[j], t[j]);
             }
         };
         float sum[3] = {0.f, 0.f, 0.f};
 #pragma unroll
         for (int p = 0; p < PER; ++p) {
-            Group<V> x;
-            float wv[V];
-            unpacked(p, x);
-            unpack(w_pre[p], wv);
+            float q[V];
+            unpacked(p, q);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                if constexpr (SUMS) dw[p][j] += x.dy[j] * x.s[j];
-                const float gwb = x.g[j] * x.wp[j] * x.b[j];
-                sum[0] += x.dy[j] * wv[j] * x.s[j];
-                sum[1] += x.t[j] * gwb;
-                sum[2] += x.s[j] * gwb;
+                if constexpr (SUMS) dw[p][j] += dy[j] * s[j];
+                const float fb = (ALL ? g[j] * f[j] : f[j]) * b[j];
+                sum[0] += q[j] * s[j];
+                sum[1] += t[j] * fb;
+                sum[2] += s[j] * fb;
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
         group_sum<LANES>(sum, sm[turn]);
-        const float m = now.rs * (sum[0] / hidden), mb = (sum[1] - m * sum[2]) / hidden;
+        // what was unpacked for the sums is not kept for the results: the compiler would, and has no registers for it
+#pragma unroll
+        for (int p = 0; p < PER; ++p) asm volatile("" : "+v"(now.s[p]), "+v"(now.b[p]), "+v"(now.dy[p]), "+v"(now.ds[p]));
+        if constexpr (ALL)
+#pragma unroll
+            for (int p = 0; p < PER; ++p) asm volatile("" : "+v"(now.g[p]));
+        if constexpr (kKeep)
+#pragma unroll
+            for (int p = 0; p < PER; ++p) asm volatile("" : "+v"(w_pre[p]), "+v"(w_post[p]));
+        const float m = now.rs * (sum[0] / hidden), mb = a.w_post ? (sum[1] - m * sum[2]) / hidden : 0.f, res = a.B ? a.res : 1.f;
         const size_t at = static_cast<size_t>(row) * hidden;
 #pragma unroll
         for (int p = 0; p < PER; ++p) {
             const int c = from + p * LANES * V;
-            Group<V> x;
             float o[V];
-            unpacked(p, x);
+            unpacked(p, o);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                x.t[j] = fmaf(-m, x.s[j], x.t[j]);
-                o[j] = a.B ? a.res * x.t[j] : x.t[j];
+                t[j] = fmaf(-m, s[j], t[j]);
+                o[j] = res * t[j];
             }
             store<WHOLE>(a.dX + at, c, hidden, o);
             if (a.B) {
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    if constexpr (SUMS) dc[p][j] += a.gate_step ? x.g[j] * (x.t[j] * x.b[j]) : x.t[j] * x.b[j];
-                    const float d = x.t[j] * (x.g[j] * x.wp[j]);
-                    o[j] = a.w_post ? now.rb * (d - x.b[j] * mb) : d;
+                    const float tb = t[j] * b[j];
+                    if constexpr (SUMS) dc[p][j] += ALL ? g[j] * tb : tb;
+                    o[j] = now.rb * (t[j] * (ALL ? g[j] * f[j] : f[j]) - b[j] * mb);
+                    if constexpr (ALL) t[j] = f[j] * tb;
                 }
                 store<WHOLE>(a.dB + at, c, hidden, o);
-                if (a.dgate) {
-#pragma unroll
-                    for (int j = 0; j < V; ++j) o[j] = x.wp[j] * (x.t[j] * x.b[j]);
-                    store<WHOLE>(a.dgate + at, c, hidden, o);
-                }
+                if constexpr (ALL) store<WHOLE>(a.dgate + at, c, hidden, t);
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
         if constexpr (!SUMS) {  // its one row: nothing is kept for another
             if (threadIdx.x == 0) a.row_m[row] = m;
@@ -359,6 +382,12 @@ __global__ __launch_bounds__(1024) void psattn_gn_fwd_wide(Args<E> a) {
     }
 }
 
+// A lane's values of one group of a row, and what comes of them
+template <int V>
+struct Group {
+    float s[V], b[V], dy[V], t[V], g[V], wp[V];  // t: dS, then dS + rs q; g: gate; wp: w_post
+};
+
 // what the backward of one row reads at columns c ..
 template <typename E>
 __device__ __forceinline__ void group_at(const Args<E>& a, int row, float rs, float rb, int c, Group<kVec<E>>& x, float (&q)[kVec<E>]) {
@@ -475,8 +504,7 @@ bool sized(int hidden, bool all, F&& f) {
     if (g <= 512) return go(integral_constant<int, 256>{}, Two{});
     if (g <= 1024) return go(integral_constant<int, 512>{}, Two{});
     if constexpr (BWD) {
-        if (g <= 2048) return go(integral_constant<int, 512>{}, integral_constant<int, 4>{});
-        if (g <= 512 * kWidest) return go(integral_constant<int, 512>{}, integral_constant<int, kWidest>{});
+        if (g <= 2048 && all) return go(integral_constant<int, 512>{}, integral_constant<int, 4>{});  // off a boundary there are no registers for four groups
     } else {
         if (g <= 2048) return go(integral_constant<int, 1024>{}, Two{});
         if (g <= 512 * kWidest) return go(integral_constant<int, 1024>{}, integral_constant<int, kWidest / 2>{});
@@ -514,7 +542,9 @@ void bwd(Args<E> a, bool vector_gate, void* dw_pre, void* dw_post, void* dgate, 
             if (np > 8) np -= np % 8;  // a workgroup's rows start alike
             sums = SUMS;
             auto go = [&](auto kernel) { kernel<<<SUMS ? np : a.n_rows, kThreads<L>, 0, s>>>(a); };
-            all ? go(psattn_gn_bwd<E, L, PER, true, SUMS>) : go(psattn_gn_bwd<E, L, PER, false, SUMS>);
+            if constexpr (PER == 4) a.gate_step ? go(psattn_gn_bwd<E, L, PER, true, SUMS, true>) : go(psattn_gn_bwd<E, L, PER, true, SUMS, false>);  // whole rows alone: `sized`
+            else if (a.gate_step) all ? go(psattn_gn_bwd<E, L, PER, true, SUMS, true>) : go(psattn_gn_bwd<E, L, PER, false, SUMS, true>);
+            else all ? go(psattn_gn_bwd<E, L, PER, true, SUMS, false>) : go(psattn_gn_bwd<E, L, PER, false, SUMS, false>);
         });
         if (!done) psattn_gn_bwd_wide<E><<<a.n_rows, 1024, 0, s>>>(a);
         if (!sums) {

@@ -17,6 +17,7 @@
 
 #include <algorithm>
 #include <initializer_list>
+#include <type_traits>
 
 #include "psattn_head.h"
 #include "psattn_logprob.h"
@@ -132,10 +133,20 @@ __global__ __launch_bounds__(256) void psattn_head_dx(int first, int hidden, int
         for (int j = r0; j < r1; ++j) {
             if (resp_len[j] == 0) continue;
             const int i = item_ptr[j] + (desc >= 0 ? row - resp_first[j] + (resp_prev[j] >= 0 ? 1 : 0) : 0);
-            for (int p = 0; p < n_parts; ++p) {
-                const float4 u = *reinterpret_cast<const float4*>(parts + (static_cast<int64_t>(p) * n_items + i) * ld + c);
-                x[0] += u.x, x[1] += u.y, x[2] += u.z, x[3] += u.w;
-            }
+            const float* from = parts + static_cast<int64_t>(i) * ld + c;
+            const int64_t step = n_items * ld;
+            auto add = [&](auto COUNT) {  // loads together, sums in order
+                constexpr int n = decltype(COUNT)::value;
+                float4 u[n];
+#pragma unroll
+                for (int p = 0; p < n; ++p) u[p] = *reinterpret_cast<const float4*>(from + p * step);
+#pragma unroll
+                for (int p = 0; p < n; ++p) x[0] += u[p].x, x[1] += u[p].y, x[2] += u[p].z, x[3] += u[p].w;
+                from += n * step;
+            };
+            int p = 0;
+            for (; p + 8 <= n_parts; p += 8) add(std::integral_constant<int, 8>{});
+            for (; p < n_parts; ++p) add(std::integral_constant<int, 1>{});
         }
 #pragma unroll
         for (int k = 0; k < V; ++k)
@@ -162,17 +173,36 @@ bool at16(std::initializer_list<const void*> p) {
     return a % 16 == 0;
 }
 
-// Which tile: few rows take tiles of 32 and 64 rows, whose workgroups share a CU; else that of the fewer rounds of workgroups, a step of k costing 1.05
-// with 128 x 128 (two to a CU) and 1.6 with 256 x 256
-TileSize tile_size(int64_t M, int64_t N) {
-    if (M <= 32) return k32;
-    if (M <= 64) return k64;
-    const int64_t small = cdiv(M, 128) * cdiv(N, 128), big = cdiv(M, 256) * cdiv(N, 256);
-    return 1.05 * cdiv(small, 512) < 1.6 * cdiv(big, 256) ? k128 : k256;
+// Which tile: few rows take tiles of 32 and 64 rows, whose workgroups share a CU, others what the products' model says
+struct Tiling {
+    TileSize size;
+    int64_t split;  // parts of k
+};
+Tiling tiling(Move move, int64_t M, int64_t N, int64_t K, bool may_split) {
+    static constexpr int bm[] = {32, 64, 128, 256}, bn[] = {128, 128, 128, 256};
+    const int64_t steps = K / (move == kFloat ? 32 : 64);
+    auto tiles = [&](TileSize t) { return std::max<int64_t>(1, cdiv(M, bm[t]) * cdiv(N, bn[t])); };
+    if (M <= 64) {
+        const TileSize t = M <= 32 ? k32 : k64;
+        return {t, may_split ? std::max<int64_t>(1, std::min((M <= 32 ? 1024 : 768) / tiles(t), steps / 4)) : 1};
+    }
+    Tiling best{k128, 1};
+    double least = 0;
+    for (const TileSize t : {k128, k256})
+        for (const int64_t split : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 24, 32, 48, 64}) {
+            if (split > 1 && (!may_split || steps / split < 4)) break;
+            const double us = product_us(move, kPlain, t, tiles(t), steps, split, sizeof(float) * static_cast<double>(M) * static_cast<double>(N));
+            if ((t == k128 && split == 1) || us < least) {
+                least = us;
+                best = {t, split};
+            }
+        }
+    return best;
 }
+Move moved(int32_t dt) { return dt == PSATTN_BF16 ? kWhole : kFloat; }
+Tiling logits_tiling(int32_t dt, int64_t n_items, int64_t cols, int64_t hidden) { return tiling(moved(dt), n_items, cols, hidden, false); }
 
-int head_product(int32_t dt, Pass pass, Product d, hipStream_t s) {
-    const TileSize size = tile_size(d.M, d.N);
+int head_product(int32_t dt, Pass pass, TileSize size, Product d, hipStream_t s) {
     d.odd = pass == kDlogit && !(at16({d.out[0]}) && d.ldo % 8 == 0 && d.N % 8 == 0);
     const bool whole = at16({d.p[0], d.q[0]}) && d.ldp % 8 == 0 && d.ldq % 8 == 0 && (pass != kSums || d.n_load % 8 == 0);
     return (dt != PSATTN_BF16 ? head_product_f32 : whole ? head_product_bf16 : head_product_bf16_any)(pass, size, d, s);
@@ -186,14 +216,8 @@ int64_t piece_rows(int32_t dt, int64_t n_items, int64_t vocab) {
     const int64_t n = cdiv(vocab, std::max<int64_t>(most, 256));
     return cdiv(cdiv(vocab, n), 256) * 256;
 }
-// parts of the vocabulary for dX's sums: workgroups for the whole chip where the rows' tiles are fewer
-int64_t dx_parts(int32_t dt, int64_t n_items, int64_t vocab, int64_t hidden) {
-    const TileSize size = tile_size(n_items, hidden);
-    const int64_t bm = size == k32 ? 32 : size == k64 ? 64 : size == k128 ? 128 : 256, bn = size == k256 ? 256 : 128;
-    const int64_t tiles = std::max<int64_t>(1, cdiv(n_items, bm)) * cdiv(hidden, bn), slots = size == k256 ? 256 : size == k128 ? 512 : size == k64 ? 768 : 1024;
-    const int64_t steps = piece_rows(dt, n_items, vocab) / (dt == PSATTN_BF16 ? 64 : 32);
-    return std::max<int64_t>(1, std::min({slots / tiles, steps / 4, int64_t{64}}));
-}
+// dX's sums: k is a piece of the vocabulary, in parts where the rows' tiles are few
+Tiling dx_tiling(int32_t dt, int64_t n_items, int64_t vocab, int64_t hidden) { return tiling(moved(dt), n_items, hidden, piece_rows(dt, n_items, vocab), true); }
 
 struct Room {
     char* p;
@@ -217,9 +241,9 @@ bool too_large(const psattn_lp_plan* plan, int32_t dt, int64_t vocab, int64_t hi
         static constexpr int bm[] = {32, 64, 128, 256}, bn[] = {128, 128, 128, 256}, threads[] = {128, 128, 256, 512};
         return cdiv(M, bm[t]) * cdiv(N, bn[t]) < (int64_t{1} << 31) / threads[t];
     };
-    if (!bwd) return !fits(n, vocab, tile_size(n, vocab));
+    if (!bwd) return !fits(n, vocab, logits_tiling(dt, n, vocab, hidden).size);
     const int64_t piece = piece_rows(dt, n, vocab);
-    return !fits(n, piece, tile_size(n, piece)) || !fits(n, hidden, tile_size(n, hidden)) || !fits(piece, hidden, k128);
+    return !fits(n, piece, logits_tiling(dt, n, piece, hidden).size) || !fits(n, hidden, dx_tiling(dt, n, vocab, hidden).size) || !fits(piece, hidden, k128);
 }
 
 size_t fwd_bytes(const psattn_lp_plan* plan, int32_t dt, int32_t vocab, int32_t hidden) {
@@ -231,7 +255,7 @@ size_t bwd_bytes(const psattn_lp_plan* plan, int32_t dt, int32_t vocab, int32_t 
     if (bad_shape(plan, dt, vocab, hidden)) return 0;
     const size_t n = static_cast<size_t>(plan->n_items);
     return align_up(n * up8(hidden) * elem_bytes(dt), 256) + align_up(n * up8(piece_rows(dt, n, vocab)) * elem_bytes(dt), 256) +
-           align_up(n * up8(hidden) * dx_parts(dt, n, vocab, hidden) * sizeof(float), 256) + 3 * align_up(n * 4, 256) + 256;
+           align_up(n * up8(hidden) * dx_tiling(dt, n, vocab, hidden).split * sizeof(float), 256) + 3 * align_up(n * 4, 256) + 256;
 }
 
 }  // namespace
@@ -267,9 +291,10 @@ int psattn_head_logprob_fwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
         z.p[0] = x; z.q[0] = W; z.G = reinterpret_cast<float*>(part); z.U = hit; z.H = target;
         z.ldp = up8(hidden); z.ldq = hidden;
         z.M = n; z.N = vocab; z.K = hidden; z.n_seg = z.n_prod = z.n_split = 1;
-        const int rc = head_product(dt, kLse, z, s);
+        const TileSize size = logits_tiling(dt, n, vocab, hidden).size;
+        const int rc = head_product(dt, kLse, size, z, s);
         if (rc != PSATTN_OK) return rc;
-        const int parts = static_cast<int>(cdiv(vocab, tile_size(n, vocab) == k256 ? 256 : 128));
+        const int parts = static_cast<int>(cdiv(vocab, size == k256 ? 256 : 128));
         if (n <= 256) psattn_head_join<1><<<n, 256, 0, s>>>(n, parts, part, plan->item_row, target, hit, row_lse, logp);
         else psattn_head_join<16><<<static_cast<uint32_t>(cdiv(n, 16)), 256, 0, s>>>(n, parts, part, plan->item_row, target, hit, row_lse, logp);
     }
@@ -287,7 +312,8 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     const size_t e = elem_bytes(dt);
     Room room(workspace);
-    const int parts = static_cast<int>(dx_parts(dt, n, vocab, hidden));
+    const Tiling dx = dx_tiling(dt, n, vocab, hidden);
+    const int parts = static_cast<int>(dx.split);
     const int64_t ld = up8(hidden), piece = piece_rows(dt, n, vocab), ldz = up8(piece);
     float* sums = nullptr;
     if (n == 0) {  // nothing is predicted: sums over nothing
@@ -314,19 +340,20 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
             z.ldp = ld; z.ldq = hidden; z.ldo = ldz;
             z.M = n; z.N = cols; z.K = hidden; z.n_seg = z.n_prod = z.n_split = 1;
             z.n_load = static_cast<int32_t>(at);
-            if ((rc = head_product(dt, kDlogit, z, s)) != PSATTN_OK) return rc;
+            if ((rc = head_product(dt, kDlogit, logits_tiling(dt, n, cols, hidden).size, z, s)) != PSATTN_OK) return rc;
             Product a{};  // dX += dz W
             a.p[0] = dz; a.q[0] = w; a.parts = sums; a.ld_part = ld; a.add = at > 0;
             a.ldp = ldz; a.ldq = hidden;
             a.M = n; a.N = a.n_load = hidden; a.K = cols; a.n_seg = a.n_prod = 1; a.n_split = parts;
-            if ((rc = head_product(dt, kSums, a, s)) != PSATTN_OK) return rc;
+            if ((rc = head_product(dt, kSums, dx.size, a, s)) != PSATTN_OK) return rc;
             Product g{};  // dW = dz^T X
             g.p[0] = dz; g.q[0] = x; g.out[0] = static_cast<char*>(dW) + at * hidden * e;
             g.ldp = ldz; g.ldq = ld; g.ldo = hidden;
             g.M = cols; g.m_load = static_cast<int32_t>(up8(cols)); g.N = hidden; g.n_load = static_cast<int32_t>(ld); g.K = n; g.n_seg = g.n_prod = g.n_split = 1;
             g.odd = !(at16({g.out[0]}) && hidden % 8 == 0);
-            const int64_t small = cdiv(cols, 128) * cdiv(hidden, 128), big = cdiv(cols, 256) * cdiv(hidden, 256);
-            const TileSize size = 1.05 * cdiv(small, 512) < 1.6 * cdiv(big, 256) ? k128 : k256;
+            const int64_t steps = n / (dt == PSATTN_BF16 ? 64 : 32);
+            auto us = [&](TileSize t, int64_t side) { return product_us(moved(dt), kPlain, t, cdiv(cols, side) * cdiv(hidden, side), steps, 1, 0); };
+            const TileSize size = us(k256, 256) < us(k128, 128) ? k256 : k128;
             if ((rc = (dt == PSATTN_BF16 ? product_bf16 : product_f32)(kPlain, 0, false, false, size, g, s)) != PSATTN_OK) return rc;
         }
     }
