@@ -207,10 +207,14 @@ template <int BM_, int BN_, int WM_, int WN_, int NBQ_>
 struct Shape {  // tile, waves, LDS buffers of Q (of P: two)
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NBQ = NBQ_, kWaves = WM * WN, kThreads = 64 * kWaves;
     static constexpr int MB = BM / WM / 32, NB = BN / WN / 32;  // blocks of a wave
+    static constexpr int kWavesToSimd = kWaves == 2 && NBQ == 3 ? 1 : 2;  // that LDS has room for
 };
 
+// A workgroup's part of a product: block bx of its tiles, by its product and part of k.  lds: kLds<S> bytes on a boundary of 1 024
+template <typename S>
+constexpr int kLds = 128 * (2 * S::BM + S::NBQ * S::BN);
 template <typename E, bool ASYNC, bool PKC, bool QKC, Pass PASS, int ACT, typename S>
-__global__ __launch_bounds__(S::kThreads, 2) void psattn_ffn_tiles(Product d, int tiles_m, int tiles_n) {
+__device__ __forceinline__ void product_tile(char* lds, const Product& d, int tiles_m, int tiles_n, int bx, int by) {
     constexpr int MB = S::MB, NB = S::NB, kPB = S::BM * 128, kQB = S::BN * 128, kBk = kBK<E>;
     constexpr int kCols = PASS == kGate ? S::BN / 2 : S::BN;  // n of a tile: gate and up share it
     static_assert(PASS != kGate || NB == 2, "a wave holds a block of the gate and the same of up");
@@ -218,12 +222,11 @@ __global__ __launch_bounds__(S::kThreads, 2) void psattn_ffn_tiles(Product d, in
     static_assert(QKC || S::BN % (256 / sizeof(E)) == 0, "whole sub-tiles");
     constexpr int NBQ = S::NBQ;
     static_assert(ASYNC || NBQ == 2, "what goes through registers is one tile ahead");
-    __shared__ __attribute__((aligned(1024))) char lds[2 * kPB + NBQ * kQB];
     char *const ptile = lds, *const qtile = lds + 2 * kPB;
     const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = w / S::WN, wn = w % S::WN;
-    const int z = blockIdx.y / d.n_split, part = blockIdx.y % d.n_split;  // product, part of its k
+    const int z = by / d.n_split, part = by % d.n_split;  // product, part of its k
     int tm, tn;
-    tile_of(blockIdx.x, tiles_m, tiles_n, tm, tn);
+    tile_of(bx, tiles_m, tiles_n, tm, tn);
     const int m0 = tm * S::BM, n0 = tn * kCols;
     Copy<E, PKC, S::BM, S::kWaves, false, ASYNC> cp;
     Copy<E, QKC, S::BN, S::kWaves, PASS == kGate, ASYNC> cq;
@@ -380,7 +383,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void psattn_ffn_tiles(Product d, in
         if (ahead == 0) tile(std::integral_constant<int, 0>{}, 0, NBQ == 2 ? 0 : q0, NBQ == 2 ? 1 : q1, NBQ == 2 ? 0 : q2);
     }
     // With both operands k-major and through registers the lane is asked for again: kept over the loop, it and what is made of it would spill
-    constexpr bool kAskAgain = !ASYNC && !PKC && sizeof(E) == 2;
+    constexpr bool kAskAgain = !ASYNC && !PKC;
     int le = l, te = threadIdx.x;
     if constexpr (kAskAgain) {
         le = static_cast<int>(__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0)));
@@ -586,6 +589,12 @@ __global__ __launch_bounds__(S::kThreads, 2) void psattn_ffn_tiles(Product d, in
             }
         }
     }
+}
+
+template <typename E, bool ASYNC, bool PKC, bool QKC, Pass PASS, int ACT, typename S>
+__global__ __launch_bounds__(S::kThreads, S::kWavesToSimd) void psattn_ffn_tiles(Product d, int tiles_m, int tiles_n) {
+    __shared__ __attribute__((aligned(1024))) char lds[kLds<S>];
+    product_tile<E, ASYNC, PKC, QKC, PASS, ACT, S>(lds, d, tiles_m, tiles_n, blockIdx.x, blockIdx.y);
 }
 
 template <typename E, bool ASYNC, bool PKC, bool QKC, Pass PASS, int ACT, typename S>

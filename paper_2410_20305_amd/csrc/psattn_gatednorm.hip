@@ -512,9 +512,11 @@ bool sized(int hidden, bool all, F&& f) {
     return false;
 }
 
-// workgroups of the backward, each with a part of the columns' sums.  A part is written and read in fp32, and costs as much memory time
-// as a few rows: one for 26 rows, but 256 of them (one to a CU) at least and 1 024 at most
-int n_parts(int32_t n_rows) { return std::max(1, std::min({n_rows, 1024, std::max(256, n_rows / 26)})); }
+// Workgroups of the backward, each with a part of the columns' sums: as many as the chip has room for at once, 512 of 256 threads or 256 of
+// 512, and 1 024 where rows are many.  A few more than fit wait for a second turn (8 334 rows of 4 096 bf16, forward and backward: 256
+// workgroups 158 us, 320 the same, 512 147, 520 180, 1 024 159; 3 000 rows of 8 192: 256 106, 512 118, 1 024 151)
+constexpr int kManyRows = 26 * 1024;
+int n_parts(int32_t n_rows, int lanes) { return std::max(1, std::min(n_rows, n_rows >= kManyRows ? 1024 : lanes >= 512 ? 256 : 512)); }
 
 bool bad_shape(int32_t dt, int32_t n_rows, int32_t hidden) { return (dt != PSATTN_F32 && dt != PSATTN_BF16) || n_rows < 0 || hidden <= 0; }
 
@@ -531,14 +533,14 @@ void fwd(const Args<E>& a, hipStream_t s) {
 
 template <typename E>
 void bwd(Args<E> a, bool vector_gate, void* dw_pre, void* dw_post, void* dgate, hipStream_t s) {
-    int np = a.n_rows > 0 ? n_parts(a.n_rows) : 0;
+    int np = a.n_rows > 0 ? n_parts(a.n_rows, 256) : 0;
     if (a.n_rows > 0) {
         const bool all = whole<E>(a.hidden, {a.S, a.B, a.w_post, a.gate, a.w_pre, a.dY, a.dS, a.dX, a.dB, a.dgate});
         bool sums = false;
         const bool done = sized<E, true>(a.hidden, all, [&](auto lanes, auto per) {
             constexpr int L = decltype(lanes)::value, PER = decltype(per)::value, kAt = kThreads<L> / L;
             constexpr bool SUMS = PER * kVec<E> < 32;  // up to 1 024 groups of bf16, 2 048 of fp32
-            if (SUMS) np = std::min(np, (a.n_rows + kAt - 1) / kAt);
+            np = std::min(n_parts(a.n_rows, L), (a.n_rows + kAt - 1) / kAt);
             if (np > 8) np -= np % 8;  // a workgroup's rows start alike
             sums = SUMS;
             auto go = [&](auto kernel) { kernel<<<SUMS ? np : a.n_rows, kThreads<L>, 0, s>>>(a); };
@@ -607,7 +609,7 @@ int psattn_gatednorm_fwd(int32_t dt, int32_t n_rows, int32_t hidden, float eps, 
 
 size_t psattn_gatednorm_bwd_workspace_bytes(int32_t n_rows, int32_t hidden) {
     if (n_rows < 0 || hidden <= 0) return 0;
-    return align_up(2 * sizeof(float) * static_cast<size_t>(n_parts(n_rows)) * hidden, 256) + align_up(sizeof(float) * static_cast<size_t>(n_rows), 256) + 256;
+    return align_up(2 * sizeof(float) * static_cast<size_t>(n_parts(n_rows, 256)) * hidden, 256) + align_up(sizeof(float) * static_cast<size_t>(n_rows), 256) + 256;
 }
 
 int psattn_gatednorm_bwd(int32_t dt, int32_t n_rows, int32_t hidden, float res_scale, const void* B, const void* w_post, const void* gate, int32_t gate_rows,
@@ -630,7 +632,7 @@ int psattn_gatednorm_bwd(int32_t dt, int32_t n_rows, int32_t hidden, float res_s
         const bool vector_gate = dgate && (n_rows == 0 ? gate_rows == 1 : a.gate_step == 0);
         a.dgate = vector_gate ? nullptr : static_cast<E*>(dgate);
         a.part = reinterpret_cast<float*>(align_up(reinterpret_cast<uintptr_t>(workspace), 256));
-        a.row_m = a.part + align_up(2 * sizeof(float) * static_cast<size_t>(n_parts(n_rows)) * hidden, 256) / sizeof(float);
+        a.row_m = a.part + align_up(2 * sizeof(float) * static_cast<size_t>(n_parts(n_rows, 256)) * hidden, 256) / sizeof(float);
         bwd(a, vector_gate, dw_pre, dw_post, dgate, static_cast<hipStream_t>(hip_stream));
     };
     if (dt == PSATTN_BF16) go(uint16_t{});

@@ -13,5 +13,9 @@ int head_product_bf16(Pass pass, TileSize size, const Product& d, hipStream_t s)
 int head_product_bf16_any(Pass pass, TileSize size, const Product& d, hipStream_t s);
 int head_product_f32(Pass pass, TileSize size, const Product& d, hipStream_t s);
 
+// dX's sums and dW of a piece in one launch, of tiles of 256 x 256, or 128 x 128 of fp32; dz and the rows of X are whole in either
+int head_grads_bf16(const Product& x, const Product& w, hipStream_t s);
+int head_grads_f32(const Product& x, const Product& w, hipStream_t s);
+
 }  // namespace gemm
 }  // namespace psattn

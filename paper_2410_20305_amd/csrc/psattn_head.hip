@@ -30,16 +30,25 @@ namespace rows = psattn::rows;
 
 constexpr int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
+constexpr int64_t up64(int64_t n) { return (n + 63) / 64 * 64; }  // a step of k of bf16, two of fp32
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 size_t elem_bytes(int32_t dt) { return dt == PSATTN_BF16 ? 2 : 4; }
 
-// ---- the items' rows, made whole: one workgroup to a row.  Without a token of the vocabulary an item has no gradient, and its row is zeros there
+// ---- the items' rows, made whole: one workgroup to a row.  Without a token of the vocabulary an item has no gradient, and its row is zeros there.
+// BWD: behind the n_items rows of X and of dz stand rows of zeros, so that dW's k, the items, is whole steps
 template <typename E, bool BWD>
-__global__ __launch_bounds__(256) void psattn_head_rows(const int32_t* item_row, const int32_t* item_tok, const int32_t* item_resp, const int32_t* token_ids,
-                                                        int vocab, int hidden, const E* X, const float* row_lse, const float* d_logp, E* out, int32_t* target,
-                                                        float* lse, float* weight) {
+__global__ __launch_bounds__(256) void psattn_head_rows(int n_items, const int32_t* item_row, const int32_t* item_tok, const int32_t* item_resp,
+                                                        const int32_t* token_ids, int vocab, int hidden, const E* X, const float* row_lse, const float* d_logp, E* out,
+                                                        int32_t* target, float* lse, float* weight, E* dz, int64_t ldz) {
     constexpr int V = rows::kVec<E>;
     const int64_t i = blockIdx.x;
+    if (BWD && i >= n_items) {
+        const rows::u32x4 zero = {0, 0, 0, 0};
+        const int64_t ld = (hidden + 7) / 8 * 8;
+        for (int64_t c = threadIdx.x * V; c < ld; c += 256 * V) *reinterpret_cast<rows::u32x4*>(out + i * ld + c) = zero;
+        for (int64_t c = threadIdx.x * V; c < ldz; c += 256 * V) *reinterpret_cast<rows::u32x4*>(dz + i * ldz + c) = zero;
+        return;
+    }
     const int r = item_row[i], row = r < 0 ? ~r : r, id = token_ids[item_tok[i]];
     const bool known = id >= 0 && id < vocab;
     if (threadIdx.x == 0) {
@@ -61,48 +70,73 @@ __global__ __launch_bounds__(256) void psattn_head_rows(const int32_t* item_row,
     }
 }
 
-// ---- joins the tiles' parts of an item's row: AT items to a workgroup, 256 / AT lanes to an item.  log pi of the item as (logit - max) - log(sum),
-// which keeps its accuracy where the token is almost certain
-template <int AT>
-__global__ __launch_bounds__(256) void psattn_head_join(int n_items, int n_parts, const float2* part, const int32_t* item_row, const int32_t* target, const float* hit,
-                                                        float* row_lse, float* item_logp) {
-    constexpr int L = 256 / AT, kAtOnce = 4;
-    __shared__ float2 sm[L][AT];
-    const int k = threadIdx.x / AT, o = threadIdx.x % AT, i = blockIdx.x * AT + o;
-    float m = -INFINITY, s = 0.f;
-    auto merge = [&](float m2, float s2) {
+// ---- joins the tiles' parts of an item's row, L lanes to an item; the result is lane 0's.  sm: [L][256 / L]
+struct Sum {
+    float m, s;  // maximum, sum of exp(z - m)
+    __device__ __forceinline__ void merge(float m2, float s2) {
         const float mn = fmaxf(m, m2), ref = mn == -INFINITY ? 0.f : mn;
         s = s * expf(m - ref) + s2 * expf(m2 - ref);
         m = mn;
-    };
+    }
+};
+template <int L>
+__device__ __forceinline__ Sum join_item(int n_items, int n_parts, const float2* part, int i, int k, int o, float2* sm) {
+    constexpr int AT = 256 / L, kAtOnce = 4;
+    Sum x{-INFINITY, 0.f};
     if (i < n_items) {
         int p = k;
         for (; p + (kAtOnce - 1) * L < n_parts; p += kAtOnce * L) {
-            float2 x[kAtOnce];
+            float2 y[kAtOnce];
 #pragma unroll
-            for (int u = 0; u < kAtOnce; ++u) x[u] = part[static_cast<int64_t>(p + u * L) * n_items + i];
+            for (int u = 0; u < kAtOnce; ++u) y[u] = part[static_cast<int64_t>(p + u * L) * n_items + i];
 #pragma unroll
-            for (int u = 0; u < kAtOnce; ++u) merge(x[u].x, x[u].y);
+            for (int u = 0; u < kAtOnce; ++u) x.merge(y[u].x, y[u].y);
         }
         for (; p < n_parts; p += L) {
-            const float2 x = part[static_cast<int64_t>(p) * n_items + i];
-            merge(x.x, x.y);
+            const float2 y = part[static_cast<int64_t>(p) * n_items + i];
+            x.merge(y.x, y.y);
         }
     }
-    sm[k][o] = make_float2(m, s);
+    sm[k * AT + o] = make_float2(x.m, x.s);
     __syncthreads();
 #pragma unroll 1
     for (int n = L / 2; n > 0; n >>= 1) {
         if (k < n) {
-            merge(sm[k + n][o].x, sm[k + n][o].y);
-            sm[k][o] = make_float2(m, s);
+            x.merge(sm[(k + n) * AT + o].x, sm[(k + n) * AT + o].y);
+            sm[k * AT + o] = make_float2(x.m, x.s);
         }
         __syncthreads();
     }
+    return x;
+}
+
+// AT items to a workgroup.  log pi of an item as (logit - max) - log(sum), which keeps its accuracy where the token is almost certain
+template <int AT>
+__global__ __launch_bounds__(256) void psattn_head_join(int n_items, int n_parts, const float2* part, const int32_t* item_row, const int32_t* target, const float* hit,
+                                                        float* row_lse, float* item_logp) {
+    __shared__ float2 sm[256];
+    const int k = threadIdx.x / AT, o = threadIdx.x % AT, i = blockIdx.x * AT + o;
+    const Sum x = join_item<256 / AT>(n_items, n_parts, part, i, k, o, sm);
     if (k > 0 || i >= n_items) return;
-    const float ls = logf(s);
-    if (const int r = item_row[i]; r >= 0) row_lse[r] = m + ls;
-    item_logp[i] = target[i] >= 0 ? (hit[i] - m) - ls : 0.f;
+    const float ls = logf(x.s);
+    if (const int r = item_row[i]; r >= 0) row_lse[r] = x.m + ls;
+    item_logp[i] = target[i] >= 0 ? (hit[i] - x.m) - ls : 0.f;
+}
+
+// ... of few items, a response to a workgroup, and their sum: a launch less
+__global__ __launch_bounds__(256) void psattn_head_join_few(int n_items, int n_parts, const float2* part, const int32_t* item_row, const int32_t* item_ptr,
+                                                            const int32_t* target, const float* hit, float* row_lse, float* resp_logp) {
+    __shared__ float2 sm[256];
+    const int j = blockIdx.x, k = threadIdx.x;
+    float logp = 0.f;
+    for (int i = item_ptr[j]; i < item_ptr[j + 1]; ++i) {
+        const Sum x = join_item<256>(n_items, n_parts, part, i, k, 0, sm);
+        const float ls = logf(x.s);
+        if (const int r = item_row[i]; k == 0 && r >= 0) row_lse[r] = x.m + ls;
+        logp += target[i] >= 0 ? (hit[i] - x.m) - ls : 0.f;
+        __syncthreads();
+    }
+    if (k == 0) resp_logp[j] = logp;
 }
 
 __global__ __launch_bounds__(256) void psattn_head_responses(int first, const int32_t* item_ptr, const float* item_logp, float* resp_logp) {
@@ -119,16 +153,17 @@ __global__ __launch_bounds__(256) void psattn_head_responses(int first, const in
 
 // ---- dX of token t: the sums of its items, of all parts of each
 template <typename E>
-__global__ __launch_bounds__(256) void psattn_head_dx(int first, int hidden, int n_items, int n_parts, int64_t ld, const float* parts, const int32_t* row_desc,
+__global__ __launch_bounds__(256) void psattn_head_dx(int64_t first, int col_blocks, int hidden, int n_items, int n_parts, int64_t ld, const float* parts, const int32_t* row_desc,
                                                       const int32_t* resp_first, const int32_t* resp_len, const int32_t* resp_prev, const int32_t* samp_ptr,
                                                       const int32_t* item_ptr, E* dX) {
     constexpr int V = 4;
-    const int row = first + static_cast<int>(blockIdx.x), desc = row_desc[row];
+    const int64_t block = first + blockIdx.x;
+    const int row = static_cast<int>(block / col_blocks), desc = row_desc[row];
     E* const to = dX + static_cast<int64_t>(row) * hidden;
     int r0 = 0, r1 = 0;  // responses with an item of this row
     if (desc >= 0) r0 = desc, r1 = desc + 1;
     else if (desc < -1) r0 = samp_ptr[-2 - desc], r1 = samp_ptr[-1 - desc];
-    for (int c = threadIdx.x * V; c < hidden; c += 256 * V) {
+    for (int c = (static_cast<int>(block - static_cast<int64_t>(row) * col_blocks) * 256 + threadIdx.x) * V; c < hidden; c += col_blocks * 256 * V) {
         float x[V] = {};
         for (int j = r0; j < r1; ++j) {
             if (resp_len[j] == 0) continue;
@@ -216,8 +251,21 @@ int64_t piece_rows(int32_t dt, int64_t n_items, int64_t vocab) {
     const int64_t n = cdiv(vocab, std::max<int64_t>(most, 256));
     return cdiv(cdiv(vocab, n), 256) * 256;
 }
-// dX's sums: k is a piece of the vocabulary, in parts where the rows' tiles are few
-Tiling dx_tiling(int32_t dt, int64_t n_items, int64_t vocab, int64_t hidden) { return tiling(moved(dt), n_items, hidden, piece_rows(dt, n_items, vocab), true); }
+// dX's sums: k is a piece of the vocabulary, in parts where the rows' tiles are few.
+// Both products of dz in one launch, from `both` on: no part longer than half of what a CU has to do
+struct DxTiling : Tiling {
+    bool both;
+};
+DxTiling dx_tiling(int32_t dt, int64_t n_items, int64_t vocab, int64_t hidden) {
+    const int64_t piece = piece_rows(dt, n_items, vocab);
+    if (n_items >= (dt == PSATTN_BF16 ? 1024 : 65) && (dt != PSATTN_BF16 || hidden % 8 == 0)) {
+        const int64_t k = dt == PSATTN_BF16 ? 64 : 32, side = dt == PSATTN_BF16 ? 256 : 128, slots = dt == PSATTN_BF16 ? 256 : 512;
+        const int64_t x_tiles = cdiv(n_items, side) * cdiv(hidden, side), w_tiles = cdiv(piece, side) * cdiv(hidden, side);
+        const int64_t x_steps = piece / k, share = (x_tiles * x_steps + w_tiles * (up64(n_items) / k)) / slots;
+        return {{dt == PSATTN_BF16 ? k256 : k128, std::max<int64_t>(1, std::min<int64_t>(cdiv(2 * x_steps, std::max<int64_t>(share, 1)), x_steps / 8))}, true};
+    }
+    return {tiling(moved(dt), n_items, hidden, piece, true), false};
+}
 
 struct Room {
     char* p;
@@ -254,7 +302,7 @@ size_t fwd_bytes(const psattn_lp_plan* plan, int32_t dt, int32_t vocab, int32_t 
 size_t bwd_bytes(const psattn_lp_plan* plan, int32_t dt, int32_t vocab, int32_t hidden) {
     if (bad_shape(plan, dt, vocab, hidden)) return 0;
     const size_t n = static_cast<size_t>(plan->n_items);
-    return align_up(n * up8(hidden) * elem_bytes(dt), 256) + align_up(n * up8(piece_rows(dt, n, vocab)) * elem_bytes(dt), 256) +
+    return align_up(up64(n) * up8(hidden) * elem_bytes(dt), 256) + align_up(up64(n) * up8(piece_rows(dt, n, vocab)) * elem_bytes(dt), 256) +
            align_up(n * up8(hidden) * dx_tiling(dt, n, vocab, hidden).split * sizeof(float), 256) + 3 * align_up(n * 4, 256) + 256;
 }
 
@@ -279,11 +327,12 @@ int psattn_head_logprob_fwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
     float2* const part = room.take<float2>(static_cast<size_t>(n) * cdiv(vocab, 128));
     int32_t* const target = room.take<int32_t>(n);
     float *const hit = room.take<float>(n), *const logp = room.take<float>(n);
+    constexpr int kFewItems = 4;
     if (n > 0) {
         auto gather = [&](auto* to) {
             using E = std::remove_pointer_t<decltype(to)>;
-            psattn_head_rows<E, false><<<n, 256, 0, s>>>(plan->item_row, plan->item_tok, plan->item_resp, token_ids, vocab, hidden, static_cast<const E*>(X), nullptr,
-                                                         nullptr, to, target, nullptr, nullptr);
+            psattn_head_rows<E, false><<<n, 256, 0, s>>>(n, plan->item_row, plan->item_tok, plan->item_resp, token_ids, vocab, hidden, static_cast<const E*>(X),
+                                                         nullptr, nullptr, to, target, nullptr, nullptr, nullptr, 0);
         };
         if (dt == PSATTN_BF16) gather(reinterpret_cast<uint16_t*>(x));
         else gather(reinterpret_cast<float*>(x));
@@ -295,6 +344,10 @@ int psattn_head_logprob_fwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
         const int rc = head_product(dt, kLse, size, z, s);
         if (rc != PSATTN_OK) return rc;
         const int parts = static_cast<int>(cdiv(vocab, size == k256 ? 256 : 128));
+        if (n <= kFewItems && plan->n_resp <= kFewItems) {
+            psattn_head_join_few<<<plan->n_resp, 256, 0, s>>>(n, parts, part, plan->item_row, plan->item_ptr, target, hit, row_lse, resp_logp);
+            return hipGetLastError() == hipSuccess ? PSATTN_OK : PSATTN_EHIP;
+        }
         if (n <= 256) psattn_head_join<1><<<n, 256, 0, s>>>(n, parts, part, plan->item_row, target, hit, row_lse, logp);
         else psattn_head_join<16><<<static_cast<uint32_t>(cdiv(n, 16)), 256, 0, s>>>(n, parts, part, plan->item_row, target, hit, row_lse, logp);
     }
@@ -312,22 +365,23 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     const size_t e = elem_bytes(dt);
     Room room(workspace);
-    const Tiling dx = dx_tiling(dt, n, vocab, hidden);
+    const DxTiling dx = dx_tiling(dt, n, vocab, hidden);
     const int parts = static_cast<int>(dx.split);
     const int64_t ld = up8(hidden), piece = piece_rows(dt, n, vocab), ldz = up8(piece);
+    const int n_whole = static_cast<int>(up64(n));
     float* sums = nullptr;
     if (n == 0) {  // nothing is predicted: sums over nothing
         psattn_head_zero<<<1024, 256, 0, s>>>(static_cast<uint16_t*>(dW), static_cast<size_t>(vocab) * hidden * e / 2);
     } else {
-        char* const x = room.take<char>(static_cast<size_t>(n) * ld * e);
-        char* const dz = room.take<char>(static_cast<size_t>(n) * ldz * e);
+        char* const x = room.take<char>(static_cast<size_t>(n_whole) * ld * e);
+        char* const dz = room.take<char>(static_cast<size_t>(n_whole) * ldz * e);
         sums = room.take<float>(static_cast<size_t>(n) * ld * parts);
         int32_t* const target = room.take<int32_t>(n);
         float *const lse = room.take<float>(n), *const weight = room.take<float>(n);
         auto gather = [&](auto* to) {
             using E = std::remove_pointer_t<decltype(to)>;
-            psattn_head_rows<E, true><<<n, 256, 0, s>>>(plan->item_row, plan->item_tok, plan->item_resp, token_ids, vocab, hidden, static_cast<const E*>(X), row_lse,
-                                                        d_resp_logp, to, target, lse, weight);
+            psattn_head_rows<E, true><<<n_whole, 256, 0, s>>>(n, plan->item_row, plan->item_tok, plan->item_resp, token_ids, vocab, hidden, static_cast<const E*>(X),
+                                                              row_lse, d_resp_logp, to, target, lse, weight, reinterpret_cast<E*>(dz), ldz);
         };
         if (dt == PSATTN_BF16) gather(reinterpret_cast<uint16_t*>(x));
         else gather(reinterpret_cast<float*>(x));
@@ -345,22 +399,28 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
             a.p[0] = dz; a.q[0] = w; a.parts = sums; a.ld_part = ld; a.add = at > 0;
             a.ldp = ldz; a.ldq = hidden;
             a.M = n; a.N = a.n_load = hidden; a.K = cols; a.n_seg = a.n_prod = 1; a.n_split = parts;
-            if ((rc = head_product(dt, kSums, dx.size, a, s)) != PSATTN_OK) return rc;
             Product g{};  // dW = dz^T X
             g.p[0] = dz; g.q[0] = x; g.out[0] = static_cast<char*>(dW) + at * hidden * e;
             g.ldp = ldz; g.ldq = ld; g.ldo = hidden;
-            g.M = cols; g.m_load = static_cast<int32_t>(up8(cols)); g.N = hidden; g.n_load = static_cast<int32_t>(ld); g.K = n; g.n_seg = g.n_prod = g.n_split = 1;
+            g.M = cols; g.m_load = static_cast<int32_t>(up8(cols)); g.N = hidden; g.n_load = static_cast<int32_t>(ld); g.K = n_whole; g.n_seg = g.n_prod = g.n_split = 1;
             g.odd = !(at16({g.out[0]}) && hidden % 8 == 0);
-            const int64_t steps = n / (dt == PSATTN_BF16 ? 64 : 32);
+            if (dx.both && (dt != PSATTN_BF16 || at16({w}))) {
+                if ((rc = (dt == PSATTN_BF16 ? head_grads_bf16 : head_grads_f32)(a, g, s)) != PSATTN_OK) return rc;
+                continue;
+            }
+            if ((rc = head_product(dt, kSums, dx.size, a, s)) != PSATTN_OK) return rc;
+            const int64_t steps = n_whole / (dt == PSATTN_BF16 ? 64 : 32);
             auto us = [&](TileSize t, int64_t side) { return product_us(moved(dt), kPlain, t, cdiv(cols, side) * cdiv(hidden, side), steps, 1, 0); };
-            const TileSize size = us(k256, 256) < us(k128, 128) ? k256 : k128;
+            const TileSize size = cdiv(cols, 256) * cdiv(hidden, 256) >= 256 || us(k256, 256) < us(k128, 128) ? k256 : k128;
             if ((rc = (dt == PSATTN_BF16 ? product_bf16 : product_f32)(kPlain, 0, false, false, size, g, s)) != PSATTN_OK) return rc;
         }
     }
-    in_grids(plan->T, [&](int64_t at, uint32_t grid) {
+    // a row to a workgroup, or where they are few, 1 024 columns of one
+    const int col_blocks = plan->T < 4096 ? static_cast<int>(cdiv(hidden, 1024)) : 1;
+    in_grids(static_cast<int64_t>(plan->T) * col_blocks, [&](int64_t at, uint32_t grid) {
         auto go = [&](auto* to) {
             using E = std::remove_pointer_t<decltype(to)>;
-            psattn_head_dx<E><<<grid, 256, 0, s>>>(static_cast<int>(at), hidden, n, parts, ld, sums, plan->row_desc, plan->resp_first, plan->resp_len, plan->resp_prev,
+            psattn_head_dx<E><<<grid, 256, 0, s>>>(at, col_blocks, hidden, n, parts, ld, sums, plan->row_desc, plan->resp_first, plan->resp_len, plan->resp_prev,
                                                    plan->samp_ptr, plan->item_ptr, to);
         };
         if (dt == PSATTN_BF16) go(static_cast<uint16_t*>(dX));
