@@ -583,19 +583,21 @@ def psattn_bwd_rope(meta: Meta, rope: Rope, Qr, Kr, V, O, dO, LSE, scale, dQ=Non
 
 def _check_heads(dev, t, name, shape, dtype):
     """Token stride of Q or K: heads and dimensions contiguous, tokens any distance apart."""
-    if not t.is_cuda:
-        raise ValueError("%s must be a device tensor" % name)
-    if t.get_device() != dev:
-        raise ValueError("%s is on %s, not on cuda:%d" % (name, t.device, dev))
-    if t.shape != shape:
-        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
-    if t.dtype != dtype:
+    if t.get_device() != dev or t.shape != shape or t.dtype != dtype:
+        if not t.is_cuda:
+            raise ValueError("%s must be a device tensor" % name)
+        if t.get_device() != dev:
+            raise ValueError("%s is on %s, not on cuda:%d" % (name, t.device, dev))
+        if t.shape != shape:
+            raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
         raise TypeError("%s has dtype %s, expected %s" % (name, t.dtype, dtype))
     T, H, d = shape
-    s = t.stride()
-    if (d > 1 and s[2] != 1) or (H > 1 and s[1] != d) or (T > 1 and s[0] < H * d):
+    at, head, one = t.stride()
+    if T <= 1:
+        at = H * d
+    if (d > 1 and one != 1) or (H > 1 and head != d) or at < H * d:
         raise ValueError("the heads of a token of %s must be contiguous" % name)
-    return s[0] if T > 1 else H * d
+    return at
 
 
 def _rope_apply(what, transposed, rope, Q, K, positions, meta, Qr, Kr):
@@ -604,28 +606,37 @@ def _rope_apply(what, transposed, rope, Q, K, positions, meta, Qr, Kr):
         raise ValueError("Q and K have three dimensions: tokens, heads, head_dim")
     if (positions is None) == (meta is None):
         raise ValueError("positions or meta say where the tokens are: one of them")
-    (T, Hq, d), Hk = Q.shape, 0 if K is None else K.shape[1]
-    if max(Q.shape) >= 1 << 31:
-        raise ValueError("Q has shape %s: sizes are 32-bit" % (tuple(Q.shape),))
+    shape, dtype, dev = Q.shape, Q.dtype, Q.get_device()
+    T, Hq, d = shape
     if d != rope.head_dim:
         raise ValueError("Q has heads of %d, the rotary table of %d" % (d, rope.head_dim))
-    dev, dt = Q.get_device(), _dtype_code(Q)
-    q = _check_heads(dev, Q, "Q", Q.shape, Q.dtype)
+    if not Q.is_cuda:
+        raise ValueError("Q must be a device tensor")
+    if T >= 1 << 31 or Hq >= 1 << 31:
+        raise ValueError("Q has shape %s: sizes are 32-bit" % (tuple(shape),))
     if dev != torch._C._cuda_getDevice():
         raise ValueError("Q is on %s, which is not the current device" % Q.device)
-    k = 0 if K is None else _check_heads(dev, K, "K", (T, Hk, d), Q.dtype)
+    dt, q = _dtype_code(Q), _check_heads(dev, Q, "Q", shape, dtype)
+    if Qr is None:
+        Qr, qr = torch.empty(shape, dtype=dtype, device=Q.device), Hq * d
+    else:
+        qr = _check_heads(dev, Qr, "the output for Q", shape, dtype)
+    Hk = k = kr = 0
+    kp = krp = None
+    if K is not None:
+        Hk = K.shape[1]
+        k = _check_heads(dev, K, "K", (T, Hk, d), dtype)
+        if Kr is None:
+            Kr, kr = torch.empty((T, Hk, d), dtype=dtype, device=Q.device), Hk * d
+        else:
+            kr = _check_heads(dev, Kr, "the output for K", K.shape, dtype)
+        kp, krp = K.data_ptr(), Kr.data_ptr()
+    elif Kr is not None:
+        raise ValueError("an output for K is given, but no K")
     if positions is not None:
         _check_all(dev, (positions, "positions", (T,), torch.int32))
-    if K is None and Kr is not None:
-        raise ValueError("an output for K is given, but no K")
-    Qr = torch.empty((T, Hq, d), dtype=Q.dtype, device=Q.device) if Qr is None else Qr
-    if K is not None and Kr is None:
-        Kr = torch.empty((T, Hk, d), dtype=Q.dtype, device=Q.device)
-    qr = _check_heads(dev, Qr, "the output for Q", Q.shape, Q.dtype)
-    kr = 0 if K is None else _check_heads(dev, Kr, "the output for K", K.shape, Q.dtype)
     st = lib.psattn_rope_apply(rope.handle, dt, transposed, T, None if positions is None else positions.data_ptr(), None if meta is None else meta.handle,
-                               Hq, Q.data_ptr(), q, Qr.data_ptr(), qr, Hk, None if K is None else K.data_ptr(), k, None if K is None else Kr.data_ptr(), kr,
-                               _stream_ptr(None))
+                               Hq, Q.data_ptr(), q, Qr.data_ptr(), qr, Hk, kp, k, krp, kr, _stream_ptr(None))
     _check(st, what)
     return Qr, Kr
 

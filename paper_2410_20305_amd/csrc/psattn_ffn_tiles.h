@@ -235,6 +235,10 @@ __device__ __forceinline__ void product_tile(char* lds, const Product& d, int ti
     const LaneRead<E, PKC> lp(l, wm * MB);
     const LaneRead<E, QKC> lq(l, wn * NB);
     f32x16 acc[NB][MB] = {};
+    // Logits of few rows in chains of 256 bf16 or 128 fp32 of k, joined once each: a single token's log-probability is no more exact than one of
+    // them, where a loss sums over many (one row, hidden 4 096, 8 logits: off by 1.1e-6 instead of 4.0e-6)
+    constexpr bool kChains = (PASS == kLse || PASS == kDlogit) && S::BM <= 64;
+    f32x16 done[kChains ? NB : 1][kChains ? MB : 1] = {};
     Frag<E> fp[2][MB], fq[2][NB];
 
     // whole tiles of k, over both segments; this workgroup's are [first, first + total)
@@ -379,6 +383,17 @@ __device__ __forceinline__ void product_tile(char* lds, const Product& d, int ti
             turn();
             tile(std::integral_constant<int, 1>{}, ahead, NBQ == 2 ? 1 : q0, NBQ == 2 ? 0 : q1, NBQ == 2 ? 1 : q2);
             turn();
+            if constexpr (kChains) {
+                if ((ahead & 2) == 0) {
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                        for (int mb = 0; mb < MB; ++mb) {
+                            done[nb][mb] += acc[nb][mb];
+                            acc[nb][mb] = f32x16{};
+                        }
+                }
+            }
         }
         if (ahead == 0) tile(std::integral_constant<int, 0>{}, 0, NBQ == 2 ? 0 : q0, NBQ == 2 ? 1 : q1, NBQ == 2 ? 0 : q2);
     }
@@ -409,6 +424,12 @@ __device__ __forceinline__ void product_tile(char* lds, const Product& d, int ti
                 });
             });
         }
+    }
+    if constexpr (kChains) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) acc[nb][mb] += done[nb][mb];
     }
     if (PASS == kDact && d.n_split == 1) {
         // G and U of the wave's next block are asked for before this one's results are made.  Rows outside are read from inside and not
@@ -539,6 +560,13 @@ __device__ __forceinline__ void product_tile(char* lds, const Product& d, int ti
                     x[i] = weight == 0.f ? 0.f : weight * (t - n == 8 * (i >> 2) + (i & 3) ? 1.f - p : -p);
                 }
                 store_out<ASYNC>(static_cast<E*>(d.out[0]) + m * d.ldo + n, d.ldo, rows, cols, chunks(x), le, d.odd);
+                if constexpr (sizeof(E) == 2 && S::BM == 32) {  // what the rounding leaves, as rows of their own
+                    if (d.out[1]) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) x[i] -= __uint_as_float(mma::pack2(x[i], 0.f) << 16);
+                        store_out<ASYNC>(static_cast<E*>(d.out[1]) + m * d.ldo + n, d.ldo, rows, cols, chunks(x), le, d.odd);
+                    }
+                }
             }
             continue;
         } else if constexpr (PASS == kSums) {

@@ -35,7 +35,7 @@ enum Pass {
 
 struct Product {
     const void *p[2], *q[2];  // of the segments along k (n_seg), or of two products of one shape (n_prod, p and out only); kGate: q of gate and up
-    void* out[2];             // kPlain: out[product]; kDact: dG, dU
+    void* out[2];             // kPlain: out[product]; kDact: dG, dU; kDlogit: dz and, of bf16 and 32 rows at most, what its rounding leaves (may be null)
     float *G, *U;             // kGate: written (may be null); kDact: read; kLse: pairs [tile of n][M], logits [M], written; kDlogit: lse, weights [M]
     void* H;                  // kGate: written; kLse, kDlogit: tokens [M], int32
     int64_t ldp, ldq, ldo;    // elements from one row in memory to the next

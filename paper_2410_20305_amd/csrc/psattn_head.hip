@@ -35,23 +35,24 @@ size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 size_t elem_bytes(int32_t dt) { return dt == PSATTN_BF16 ? 2 : 4; }
 
 // ---- the items' rows, made whole: one workgroup to a row.  Without a token of the vocabulary an item has no gradient, and its row is zeros there.
-// BWD: behind the n_items rows of X and of dz stand rows of zeros, so that dW's k, the items, is whole steps
+// BWD: up to `again` the rows stand there once more (for the second part of dz), and behind them, in dz too, rows of zeros, so that dW's
+// k is whole steps
 template <typename E, bool BWD>
-__global__ __launch_bounds__(256) void psattn_head_rows(int n_items, const int32_t* item_row, const int32_t* item_tok, const int32_t* item_resp,
+__global__ __launch_bounds__(256) void psattn_head_rows(int n_items, int again, const int32_t* item_row, const int32_t* item_tok, const int32_t* item_resp,
                                                         const int32_t* token_ids, int vocab, int hidden, const E* X, const float* row_lse, const float* d_logp, E* out,
                                                         int32_t* target, float* lse, float* weight, E* dz, int64_t ldz) {
     constexpr int V = rows::kVec<E>;
-    const int64_t i = blockIdx.x;
-    if (BWD && i >= n_items) {
+    const int64_t at = blockIdx.x, ld = (hidden + 7) / 8 * 8;
+    if (BWD && at >= again) {
         const rows::u32x4 zero = {0, 0, 0, 0};
-        const int64_t ld = (hidden + 7) / 8 * 8;
-        for (int64_t c = threadIdx.x * V; c < ld; c += 256 * V) *reinterpret_cast<rows::u32x4*>(out + i * ld + c) = zero;
-        for (int64_t c = threadIdx.x * V; c < ldz; c += 256 * V) *reinterpret_cast<rows::u32x4*>(dz + i * ldz + c) = zero;
+        for (int64_t c = threadIdx.x * V; c < ld; c += 256 * V) *reinterpret_cast<rows::u32x4*>(out + at * ld + c) = zero;
+        for (int64_t c = threadIdx.x * V; c < ldz; c += 256 * V) *reinterpret_cast<rows::u32x4*>(dz + at * ldz + c) = zero;
         return;
     }
+    const int64_t i = at < n_items ? at : at - n_items;
     const int r = item_row[i], row = r < 0 ? ~r : r, id = token_ids[item_tok[i]];
     const bool known = id >= 0 && id < vocab;
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == 0 && at < n_items) {
         target[i] = known ? id : -1;
         if constexpr (BWD) {
             lse[i] = known ? row_lse[row] : 0.f;
@@ -59,14 +60,87 @@ __global__ __launch_bounds__(256) void psattn_head_rows(int n_items, const int32
         }
     }
     const E* const x = X + static_cast<int64_t>(row) * hidden;
-    E* const to = out + i * ((hidden + 7) / 8 * 8);
-    for (int c = threadIdx.x * V; c < (hidden + 7) / 8 * 8; c += 256 * V) {
+    for (int c = threadIdx.x * V; c < ld; c += 256 * V) {
         rows::u32x4 u = {0, 0, 0, 0};
         if ((!BWD || known) && c < hidden) {
-            const auto at = rows::place<false, E>(c, hidden);
-            u = rows::settled<false>(rows::raw<false>(x, at, hidden), at.down);
+            const auto p = rows::place<false, E>(c, hidden);
+            u = rows::settled<false>(rows::raw<false>(x, p, hidden), p.down);
         }
-        *reinterpret_cast<rows::u32x4*>(to + c) = u;
+        *reinterpret_cast<rows::u32x4*>(out + at * ld + c) = u;
+    }
+}
+
+// ---- logits whose tiles are too few for the chip: their products' parts of k, [part][item][ld], joined here
+// four logits from column c on; what is behind the last is -inf
+__device__ __forceinline__ void joined(const float* parts, int64_t step, int n_parts, int c, int cols, float (&z)[4]) {
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    int p = 0;
+    auto add = [&](auto COUNT) {  // loads together, sums in order
+        constexpr int n = decltype(COUNT)::value;
+        float4 u[n];
+#pragma unroll
+        for (int k = 0; k < n; ++k) u[k] = *reinterpret_cast<const float4*>(parts + (p + k) * step + c);
+#pragma unroll
+        for (int k = 0; k < n; ++k) sum.x += u[k].x, sum.y += u[k].y, sum.z += u[k].z, sum.w += u[k].w;
+        p += n;
+    };
+    while (p + 8 <= n_parts) add(std::integral_constant<int, 8>{});
+    while (p < n_parts) add(std::integral_constant<int, 1>{});
+    z[0] = sum.x;
+    z[1] = c + 1 < cols ? sum.y : -INFINITY;
+    z[2] = c + 2 < cols ? sum.z : -INFINITY;
+    z[3] = c + 3 < cols ? sum.w : -INFINITY;
+}
+
+// an item to a workgroup: its log-sum-exp and its token's log-probability
+__global__ __launch_bounds__(1024) void psattn_head_parts_lse(int n_items, int n_parts, int cols, int64_t ld, const float* parts, const int32_t* item_row, const int32_t* target,
+                                                              float* row_lse, float* item_logp) {
+    __shared__ float2 sm[16];
+    __shared__ float hit;
+    const int i = blockIdx.x, t = target[i];
+    const float* const z0 = parts + static_cast<int64_t>(i) * ld;
+    float m = -INFINITY, s = 0.f;
+    auto merge = [&](float m2, float s2) {
+        const float mn = fmaxf(m, m2), ref = mn == -INFINITY ? 0.f : mn;
+        s = s * expf(m - ref) + s2 * expf(m2 - ref);
+        m = mn;
+    };
+    for (int c = threadIdx.x * 4; c < cols; c += 4096) {
+        float z[4];
+        joined(z0, n_items * ld, n_parts, c, cols, z);
+        const float mx = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), ref = mx == -INFINITY ? 0.f : mx;
+        merge(mx, (expf(z[0] - ref) + expf(z[1] - ref)) + (expf(z[2] - ref) + expf(z[3] - ref)));
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (c + k == t) hit = z[k];
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) merge(__shfl_xor(m, off), __shfl_xor(s, off));
+    if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = make_float2(m, s);
+    __syncthreads();
+    if (threadIdx.x > 0) return;
+    for (int w = 1; w < 16; ++w) merge(sm[w].x, sm[w].y);
+    const float ls = logf(s);
+    if (const int r = item_row[i]; r >= 0) row_lse[r] = m + ls;
+    item_logp[i] = t >= 0 ? (hit - m) - ls : 0.f;
+}
+
+// dz of an item, and of bf16 what its rounding leaves where that is asked for: 1 024 columns to a workgroup
+template <typename E>
+__global__ __launch_bounds__(256) void psattn_head_parts_dz(int n_items, int n_parts, int first, int cols, int64_t ld, const float* parts, const int32_t* target, const float* lse,
+                                                            const float* weight, E* dz, E* rest, int64_t ldz) {
+    const int64_t i = blockIdx.y;
+    const int c = (blockIdx.x * 256 + threadIdx.x) * 4, t = target[i] - first;
+    if (c >= cols) return;
+    const float l = lse[i], w = weight[i];
+    float z[4];
+    joined(parts + i * ld, n_items * ld, n_parts, c, cols, z);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (c + k >= cols) break;
+        const float p = expf(z[k] - l), x = w == 0.f ? 0.f : w * (c + k == t ? 1.f - p : -p);
+        rows::store1(dz + i * ldz + c + k, x);
+        if (rest) rows::store1(rest + i * ldz + c + k, x - rows::hold(x, dz));
     }
 }
 
@@ -151,9 +225,9 @@ __global__ __launch_bounds__(256) void psattn_head_responses(int first, const in
     if (threadIdx.x == 0) resp_logp[j] = (sm[0] + sm[1]) + (sm[2] + sm[3]);
 }
 
-// ---- dX of token t: the sums of its items, of all parts of each
+// ---- dX of token t: the sums of its items, of all parts of each; `again` rows to a part
 template <typename E>
-__global__ __launch_bounds__(256) void psattn_head_dx(int64_t first, int col_blocks, int hidden, int n_items, int n_parts, int64_t ld, const float* parts, const int32_t* row_desc,
+__global__ __launch_bounds__(256) void psattn_head_dx(int64_t first, int col_blocks, int hidden, int n_items, int again, int n_parts, int64_t ld, const float* parts, const int32_t* row_desc,
                                                       const int32_t* resp_first, const int32_t* resp_len, const int32_t* resp_prev, const int32_t* samp_ptr,
                                                       const int32_t* item_ptr, E* dX) {
     constexpr int V = 4;
@@ -168,20 +242,22 @@ __global__ __launch_bounds__(256) void psattn_head_dx(int64_t first, int col_blo
         for (int j = r0; j < r1; ++j) {
             if (resp_len[j] == 0) continue;
             const int i = item_ptr[j] + (desc >= 0 ? row - resp_first[j] + (resp_prev[j] >= 0 ? 1 : 0) : 0);
-            const float* from = parts + static_cast<int64_t>(i) * ld + c;
-            const int64_t step = n_items * ld;
-            auto add = [&](auto COUNT) {  // loads together, sums in order
-                constexpr int n = decltype(COUNT)::value;
-                float4 u[n];
+            const int64_t step = again * ld;
+            for (int64_t row_of = i; row_of < again; row_of += n_items) {  // and its second part's
+                const float* from = parts + row_of * ld + c;
+                auto add = [&](auto COUNT) {  // loads together, sums in order
+                    constexpr int n = decltype(COUNT)::value;
+                    float4 u[n];
 #pragma unroll
-                for (int p = 0; p < n; ++p) u[p] = *reinterpret_cast<const float4*>(from + p * step);
+                    for (int p = 0; p < n; ++p) u[p] = *reinterpret_cast<const float4*>(from + p * step);
 #pragma unroll
-                for (int p = 0; p < n; ++p) x[0] += u[p].x, x[1] += u[p].y, x[2] += u[p].z, x[3] += u[p].w;
-                from += n * step;
-            };
-            int p = 0;
-            for (; p + 8 <= n_parts; p += 8) add(std::integral_constant<int, 8>{});
-            for (; p < n_parts; ++p) add(std::integral_constant<int, 1>{});
+                    for (int p = 0; p < n; ++p) x[0] += u[p].x, x[1] += u[p].y, x[2] += u[p].z, x[3] += u[p].w;
+                    from += n * step;
+                };
+                int p = 0;
+                for (; p + 8 <= n_parts; p += 8) add(std::integral_constant<int, 8>{});
+                for (; p < n_parts; ++p) add(std::integral_constant<int, 1>{});
+            }
         }
 #pragma unroll
         for (int k = 0; k < V; ++k)
@@ -207,6 +283,8 @@ bool at16(std::initializer_list<const void*> p) {
     for (const void* x : p) a |= reinterpret_cast<uintptr_t>(x);
     return a % 16 == 0;
 }
+
+constexpr int64_t kPartBytes = 64 << 20, kPartItems = 4096;  // of logits in parts, at most
 
 // Which tile: few rows take tiles of 32 and 64 rows, whose workgroups share a CU, others what the products' model says
 struct Tiling {
@@ -235,12 +313,24 @@ Tiling tiling(Move move, int64_t M, int64_t N, int64_t K, bool may_split) {
     return best;
 }
 Move moved(int32_t dt) { return dt == PSATTN_BF16 ? kWhole : kFloat; }
-Tiling logits_tiling(int32_t dt, int64_t n_items, int64_t cols, int64_t hidden) { return tiling(moved(dt), n_items, cols, hidden, false); }
+// Logits: their parts of k, where one workgroup to a tile would leave most of the chip idle, are small beside W
+Tiling logits_tiling(int32_t dt, int64_t n_items, int64_t cols, int64_t hidden) {
+    const int64_t steps = hidden / (dt == PSATTN_BF16 ? 64 : 32), bytes = 4 * n_items * up8(cols);
+    const bool may_split = n_items <= kPartItems && bytes <= kPartBytes;
+    Tiling t = tiling(moved(dt), n_items, cols, hidden, may_split);
+    if (n_items <= 64) {
+        const int64_t tiles = cdiv(cols, 128);
+        t.split = tiles >= 200 ? 1 : std::max<int64_t>(1, std::min(512 / tiles, steps / 4));
+    }
+    t.split = may_split ? std::max<int64_t>(1, std::min(t.split, kPartBytes / std::max<int64_t>(bytes, 1))) : 1;
+    return t;
+}
+size_t part_bytes(const Tiling& t, int64_t n_items, int64_t cols) { return t.split > 1 ? sizeof(float) * t.split * n_items * up8(cols) : 0; }
 
-int head_product(int32_t dt, Pass pass, TileSize size, Product d, hipStream_t s) {
+int head_product(int32_t dt, Pass pass, bool qkc, TileSize size, Product d, hipStream_t s) {
     d.odd = pass == kDlogit && !(at16({d.out[0]}) && d.ldo % 8 == 0 && d.N % 8 == 0);
-    const bool whole = at16({d.p[0], d.q[0]}) && d.ldp % 8 == 0 && d.ldq % 8 == 0 && (pass != kSums || d.n_load % 8 == 0);
-    return (dt != PSATTN_BF16 ? head_product_f32 : whole ? head_product_bf16 : head_product_bf16_any)(pass, size, d, s);
+    const bool whole = at16({d.p[0], d.q[0]}) && d.ldp % 8 == 0 && d.ldq % 8 == 0 && (qkc || d.n_load % 8 == 0);
+    return (dt != PSATTN_BF16 ? head_product_f32 : whole ? head_product_bf16 : head_product_bf16_any)(pass, qkc, size, d, s);
 }
 
 // dz of a piece of the vocabulary has this much room at most
@@ -251,6 +341,10 @@ int64_t piece_rows(int32_t dt, int64_t n_items, int64_t vocab) {
     const int64_t n = cdiv(vocab, std::max<int64_t>(most, 256));
     return cdiv(cdiv(vocab, n), 256) * 256;
 }
+// Few items of bf16: dz as two numbers each, the second what the first one's rounding leaves, as items of their own.  The gradients are as
+// exact as their own rounding then; of more items the errors of dz are beside each other (a token's row of dW off by 2^-9 of itself at most)
+constexpr int64_t kTwice = 32;
+int64_t dz_rows(int32_t dt, int64_t n_items) { return dt == PSATTN_BF16 && n_items <= kTwice ? 2 * n_items : n_items; }
 // dX's sums: k is a piece of the vocabulary, in parts where the rows' tiles are few.
 // Both products of dz in one launch, from `both` on: no part longer than half of what a CU has to do
 struct DxTiling : Tiling {
@@ -264,7 +358,7 @@ DxTiling dx_tiling(int32_t dt, int64_t n_items, int64_t vocab, int64_t hidden) {
         const int64_t x_steps = piece / k, share = (x_tiles * x_steps + w_tiles * (up64(n_items) / k)) / slots;
         return {{dt == PSATTN_BF16 ? k256 : k128, std::max<int64_t>(1, std::min<int64_t>(cdiv(2 * x_steps, std::max<int64_t>(share, 1)), x_steps / 8))}, true};
     }
-    return {tiling(moved(dt), n_items, hidden, piece, true), false};
+    return {tiling(moved(dt), dz_rows(dt, n_items), hidden, piece, true), false};
 }
 
 struct Room {
@@ -297,13 +391,21 @@ bool too_large(const psattn_lp_plan* plan, int32_t dt, int64_t vocab, int64_t hi
 size_t fwd_bytes(const psattn_lp_plan* plan, int32_t dt, int32_t vocab, int32_t hidden) {
     if (bad_shape(plan, dt, vocab, hidden)) return 0;
     const size_t n = static_cast<size_t>(plan->n_items);
-    return align_up(n * up8(hidden) * elem_bytes(dt), 256) + align_up(n * cdiv(vocab, 128) * sizeof(float2), 256) + 3 * align_up(n * 4, 256) + 256;
+    const size_t parts = std::max(part_bytes(logits_tiling(dt, n, vocab, hidden), n, vocab), n * cdiv(vocab, 128) * sizeof(float2));
+    return align_up(n * up8(hidden) * elem_bytes(dt), 256) + align_up(parts, 256) + 3 * align_up(n * 4, 256) + 256;
+}
+// parts of the logits of a piece, or of the last one, which is smaller
+size_t logits_bytes(int32_t dt, int64_t n, int64_t vocab, int64_t piece, int64_t hidden) {
+    const int64_t last = vocab - (vocab - 1) / piece * piece;
+    return std::max(part_bytes(logits_tiling(dt, n, piece, hidden), n, piece), part_bytes(logits_tiling(dt, n, last, hidden), n, last));
 }
 size_t bwd_bytes(const psattn_lp_plan* plan, int32_t dt, int32_t vocab, int32_t hidden) {
     if (bad_shape(plan, dt, vocab, hidden)) return 0;
     const size_t n = static_cast<size_t>(plan->n_items);
-    return align_up(up64(n) * up8(hidden) * elem_bytes(dt), 256) + align_up(up64(n) * up8(piece_rows(dt, n, vocab)) * elem_bytes(dt), 256) +
-           align_up(n * up8(hidden) * dx_tiling(dt, n, vocab, hidden).split * sizeof(float), 256) + 3 * align_up(n * 4, 256) + 256;
+    const int64_t m = dz_rows(dt, n), piece = piece_rows(dt, n, vocab);
+    const size_t sums = m * up8(hidden) * dx_tiling(dt, n, vocab, hidden).split * sizeof(float), parts = logits_bytes(dt, n, vocab, piece, hidden);
+    return align_up(up64(m) * up8(hidden) * elem_bytes(dt), 256) + align_up(up64(m) * up8(piece) * elem_bytes(dt), 256) + align_up(sums, 256) + align_up(parts, 256) +
+           3 * align_up(n * 4, 256) + 256;
 }
 
 }  // namespace
@@ -324,14 +426,15 @@ int psattn_head_logprob_fwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
     const int n = static_cast<int>(plan->n_items);
     Room room(workspace);
     char* const x = room.take<char>(static_cast<size_t>(n) * up8(hidden) * elem_bytes(dt));
-    float2* const part = room.take<float2>(static_cast<size_t>(n) * cdiv(vocab, 128));
+    const Tiling tiling = logits_tiling(dt, n, vocab, hidden);
+    float2* const part = reinterpret_cast<float2*>(room.take<char>(std::max(part_bytes(tiling, n, vocab), n * cdiv(vocab, 128) * sizeof(float2))));
     int32_t* const target = room.take<int32_t>(n);
     float *const hit = room.take<float>(n), *const logp = room.take<float>(n);
     constexpr int kFewItems = 4;
     if (n > 0) {
         auto gather = [&](auto* to) {
             using E = std::remove_pointer_t<decltype(to)>;
-            psattn_head_rows<E, false><<<n, 256, 0, s>>>(n, plan->item_row, plan->item_tok, plan->item_resp, token_ids, vocab, hidden, static_cast<const E*>(X),
+            psattn_head_rows<E, false><<<n, 256, 0, s>>>(n, n, plan->item_row, plan->item_tok, plan->item_resp, token_ids, vocab, hidden, static_cast<const E*>(X),
                                                          nullptr, nullptr, to, target, nullptr, nullptr, nullptr, 0);
         };
         if (dt == PSATTN_BF16) gather(reinterpret_cast<uint16_t*>(x));
@@ -340,16 +443,21 @@ int psattn_head_logprob_fwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
         z.p[0] = x; z.q[0] = W; z.G = reinterpret_cast<float*>(part); z.U = hit; z.H = target;
         z.ldp = up8(hidden); z.ldq = hidden;
         z.M = n; z.N = vocab; z.K = hidden; z.n_seg = z.n_prod = z.n_split = 1;
-        const TileSize size = logits_tiling(dt, n, vocab, hidden).size;
-        const int rc = head_product(dt, kLse, size, z, s);
-        if (rc != PSATTN_OK) return rc;
-        const int parts = static_cast<int>(cdiv(vocab, size == k256 ? 256 : 128));
-        if (n <= kFewItems && plan->n_resp <= kFewItems) {
-            psattn_head_join_few<<<plan->n_resp, 256, 0, s>>>(n, parts, part, plan->item_row, plan->item_ptr, target, hit, row_lse, resp_logp);
-            return hipGetLastError() == hipSuccess ? PSATTN_OK : PSATTN_EHIP;
+        int rc;
+        if (tiling.split > 1) {
+            z.parts = reinterpret_cast<float*>(part); z.ld_part = up8(vocab); z.n_split = static_cast<int32_t>(tiling.split);
+            if ((rc = head_product(dt, kSums, true, tiling.size, z, s)) != PSATTN_OK) return rc;
+            psattn_head_parts_lse<<<n, 1024, 0, s>>>(n, z.n_split, vocab, z.ld_part, z.parts, plan->item_row, target, row_lse, logp);
+        } else {
+            if ((rc = head_product(dt, kLse, true, tiling.size, z, s)) != PSATTN_OK) return rc;
+            const int parts = static_cast<int>(cdiv(vocab, tiling.size == k256 ? 256 : 128));
+            if (n <= kFewItems && plan->n_resp <= kFewItems) {
+                psattn_head_join_few<<<plan->n_resp, 256, 0, s>>>(n, parts, part, plan->item_row, plan->item_ptr, target, hit, row_lse, resp_logp);
+                return hipGetLastError() == hipSuccess ? PSATTN_OK : PSATTN_EHIP;
+            }
+            if (n <= 256) psattn_head_join<1><<<n, 256, 0, s>>>(n, parts, part, plan->item_row, target, hit, row_lse, logp);
+            else psattn_head_join<16><<<static_cast<uint32_t>(cdiv(n, 16)), 256, 0, s>>>(n, parts, part, plan->item_row, target, hit, row_lse, logp);
         }
-        if (n <= 256) psattn_head_join<1><<<n, 256, 0, s>>>(n, parts, part, plan->item_row, target, hit, row_lse, logp);
-        else psattn_head_join<16><<<static_cast<uint32_t>(cdiv(n, 16)), 256, 0, s>>>(n, parts, part, plan->item_row, target, hit, row_lse, logp);
     }
     in_grids(plan->n_resp, [&](int64_t at, uint32_t grid) { psattn_head_responses<<<grid, 256, 0, s>>>(static_cast<int>(at), plan->item_ptr, logp, resp_logp); });
     return hipGetLastError() == hipSuccess ? PSATTN_OK : PSATTN_EHIP;
@@ -368,19 +476,21 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
     const DxTiling dx = dx_tiling(dt, n, vocab, hidden);
     const int parts = static_cast<int>(dx.split);
     const int64_t ld = up8(hidden), piece = piece_rows(dt, n, vocab), ldz = up8(piece);
-    const int n_whole = static_cast<int>(up64(n));
+    const int again = static_cast<int>(dz_rows(dt, n)), n_whole = static_cast<int>(up64(again));
     float* sums = nullptr;
     if (n == 0) {  // nothing is predicted: sums over nothing
         psattn_head_zero<<<1024, 256, 0, s>>>(static_cast<uint16_t*>(dW), static_cast<size_t>(vocab) * hidden * e / 2);
     } else {
         char* const x = room.take<char>(static_cast<size_t>(n_whole) * ld * e);
         char* const dz = room.take<char>(static_cast<size_t>(n_whole) * ldz * e);
-        sums = room.take<float>(static_cast<size_t>(n) * ld * parts);
+        sums = room.take<float>(static_cast<size_t>(again) * ld * parts);
+        float* const z_parts = reinterpret_cast<float*>(room.take<char>(logits_bytes(dt, n, vocab, piece, hidden)));
+        char* const rest = again > n ? dz + n * ldz * e : nullptr;
         int32_t* const target = room.take<int32_t>(n);
         float *const lse = room.take<float>(n), *const weight = room.take<float>(n);
         auto gather = [&](auto* to) {
             using E = std::remove_pointer_t<decltype(to)>;
-            psattn_head_rows<E, true><<<n_whole, 256, 0, s>>>(n, plan->item_row, plan->item_tok, plan->item_resp, token_ids, vocab, hidden, static_cast<const E*>(X),
+            psattn_head_rows<E, true><<<n_whole, 256, 0, s>>>(n, again, plan->item_row, plan->item_tok, plan->item_resp, token_ids, vocab, hidden, static_cast<const E*>(X),
                                                               row_lse, d_resp_logp, to, target, lse, weight, reinterpret_cast<E*>(dz), ldz);
         };
         if (dt == PSATTN_BF16) gather(reinterpret_cast<uint16_t*>(x));
@@ -390,15 +500,28 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
             const char* const w = static_cast<const char*>(W) + at * hidden * e;
             int rc;
             Product z{};  // dz
-            z.p[0] = x; z.q[0] = w; z.G = lse; z.U = weight; z.H = target; z.out[0] = dz;
+            z.p[0] = x; z.q[0] = w; z.G = lse; z.U = weight; z.H = target; z.out[0] = dz; z.out[1] = rest;
             z.ldp = ld; z.ldq = hidden; z.ldo = ldz;
             z.M = n; z.N = cols; z.K = hidden; z.n_seg = z.n_prod = z.n_split = 1;
             z.n_load = static_cast<int32_t>(at);
-            if ((rc = head_product(dt, kDlogit, logits_tiling(dt, n, cols, hidden).size, z, s)) != PSATTN_OK) return rc;
+            const Tiling tiling = logits_tiling(dt, n, cols, hidden);
+            if (tiling.split > 1) {
+                z.parts = z_parts; z.ld_part = up8(cols); z.n_split = static_cast<int32_t>(tiling.split);
+                if ((rc = head_product(dt, kSums, true, tiling.size, z, s)) != PSATTN_OK) return rc;
+                auto go = [&](auto* to) {
+                    using E = std::remove_pointer_t<decltype(to)>;
+                    psattn_head_parts_dz<E><<<dim3(static_cast<uint32_t>(cdiv(cols, 1024)), n), 256, 0, s>>>(n, z.n_split, static_cast<int>(at), cols, z.ld_part, z_parts, target, lse,
+                                                                                                            weight, to, reinterpret_cast<E*>(rest), ldz);
+                };
+                if (dt == PSATTN_BF16) go(reinterpret_cast<uint16_t*>(dz));
+                else go(reinterpret_cast<float*>(dz));
+            } else if ((rc = head_product(dt, kDlogit, true, tiling.size, z, s)) != PSATTN_OK) {
+                return rc;
+            }
             Product a{};  // dX += dz W
             a.p[0] = dz; a.q[0] = w; a.parts = sums; a.ld_part = ld; a.add = at > 0;
             a.ldp = ldz; a.ldq = hidden;
-            a.M = n; a.N = a.n_load = hidden; a.K = cols; a.n_seg = a.n_prod = 1; a.n_split = parts;
+            a.M = again; a.N = a.n_load = hidden; a.K = cols; a.n_seg = a.n_prod = 1; a.n_split = parts;
             Product g{};  // dW = dz^T X
             g.p[0] = dz; g.q[0] = x; g.out[0] = static_cast<char*>(dW) + at * hidden * e;
             g.ldp = ldz; g.ldq = ld; g.ldo = hidden;
@@ -408,7 +531,7 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
                 if ((rc = (dt == PSATTN_BF16 ? head_grads_bf16 : head_grads_f32)(a, g, s)) != PSATTN_OK) return rc;
                 continue;
             }
-            if ((rc = head_product(dt, kSums, dx.size, a, s)) != PSATTN_OK) return rc;
+            if ((rc = head_product(dt, kSums, false, dx.size, a, s)) != PSATTN_OK) return rc;
             const int64_t steps = n_whole / (dt == PSATTN_BF16 ? 64 : 32);
             auto us = [&](TileSize t, int64_t side) { return product_us(moved(dt), kPlain, t, cdiv(cols, side) * cdiv(hidden, side), steps, 1, 0); };
             const TileSize size = cdiv(cols, 256) * cdiv(hidden, 256) >= 256 || us(k256, 256) < us(k128, 128) ? k256 : k128;
@@ -420,7 +543,7 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
     in_grids(static_cast<int64_t>(plan->T) * col_blocks, [&](int64_t at, uint32_t grid) {
         auto go = [&](auto* to) {
             using E = std::remove_pointer_t<decltype(to)>;
-            psattn_head_dx<E><<<grid, 256, 0, s>>>(at, col_blocks, hidden, n, parts, ld, sums, plan->row_desc, plan->resp_first, plan->resp_len, plan->resp_prev,
+            psattn_head_dx<E><<<grid, 256, 0, s>>>(at, col_blocks, hidden, n, again, parts, ld, sums, plan->row_desc, plan->resp_first, plan->resp_len, plan->resp_prev,
                                                    plan->samp_ptr, plan->item_ptr, to);
         };
         if (dt == PSATTN_BF16) go(static_cast<uint16_t*>(dX));

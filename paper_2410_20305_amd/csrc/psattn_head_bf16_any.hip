@@ -4,7 +4,7 @@
 namespace psattn {
 namespace gemm {
 
-int head_product_bf16_any(Pass pass, TileSize size, const Product& d, hipStream_t s) { return launch_head<uint16_t, false>(pass, size, d, s); }
+int head_product_bf16_any(Pass pass, bool qkc, TileSize size, const Product& d, hipStream_t s) { return launch_head<uint16_t, false>(pass, qkc, size, d, s); }
 
 }  // namespace gemm
 }  // namespace psattn

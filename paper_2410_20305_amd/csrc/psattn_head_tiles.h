@@ -16,9 +16,10 @@ int launch_logits(TileSize size, const Product& d, hipStream_t s) {
 }
 
 template <typename E, bool ASYNC>
-int launch_head(Pass pass, TileSize size, const Product& d, hipStream_t s) {
+int launch_head(Pass pass, bool qkc, TileSize size, const Product& d, hipStream_t s) {
     if (pass == kLse) return launch_logits<E, ASYNC, kLse>(size, d, s);
     if (pass == kDlogit) return launch_logits<E, ASYNC, kDlogit>(size, d, s);
+    if (qkc) return launch_logits<E, ASYNC, kSums>(size, d, s);
     return launch_sized<E, ASYNC, true, false, kSums, 0>(size, d, s);
 }
 

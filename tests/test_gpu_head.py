@@ -240,3 +240,27 @@ def test_several_pieces_of_the_vocabulary():
         off = (got.double() - want).abs() - (HALF["bf16"] * want.abs() + (e + 6100 * EPS32) * size)
         assert off.max().item() <= 0, off.max().item()
     assert torch.all(dX[-1] == 0)
+
+
+# logits in parts of k: few columns of wide rows, one row and many, with whole and odd rows
+PARTS = [("one_token", 130, 4096), ("two_responses", 1000, 2056), ("three_samples", 700, 3001), ("sixty_five_items", 513, 2048), ("packed", 260, 4104), ("long", 300, 2050),
+         ("empty_responses_and_prompts", 3, 5000), ("many_responses", 1, 8192)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("table,V,h", PARTS)
+def test_wide_rows_of_a_small_vocabulary(table, V, h, dtype):
+    a = _inputs(table, V, h, dtype)
+    _check(*a, _call(table, *a[:3], a[4], dtype), dtype)
+
+
+def test_few_items_have_gradients_as_exact_as_their_rounding():
+    """bf16: one token.  Its gradients are one number times a row, and of that number two roundings are kept, 2^-17 of it off at most."""
+    X, W, ids, items, d = _inputs("one_token", 400, 256, "bf16", lean=0.0)
+    lse, logp, dX, dW = _call("one_token", X, W, ids, d, "bf16")
+    rX, rW, G = blk.head_grad(X, W, ids, items, d)
+    r = items[0][1]
+    ez = (258 * EPS32 * (np.abs(X[r]) @ np.abs(W.T))).max() + 500 * EPS32  # of a logit and of the log-sum-exp
+    rel = 2 * ez + 2.0 ** -17 + 8 * EPS32
+    close(dW, rW, (HALF["bf16"] + rel) * np.abs(rW) + 2 * EPS32 * np.abs(rW) + abs(d[0]) * ez * np.abs(X[r]) + TINY, "dW")
+    close(dX, rX, HALF["bf16"] * np.abs(rX) + (rel + 500 * EPS32) * (np.abs(G) @ np.abs(W)) + TINY, "dX")
