@@ -12,7 +12,7 @@ LIB = os.path.join(HERE, "libpsattn.so")
 LAYER_LIB = os.path.join(HERE, "libpsattn_layer.so")   # the attention-layer benchmark: libpsattn + rocBLAS
 SOURCES = ["psattn_meta.cpp", "psattn_pack.cpp", "psattn_api.hip", "psattn_upload.hip", "psattn_generic.hip", "psattn_mfma_fwd.hip", "psattn_mfma_fwd64.hip", "psattn_mfma_fwd3.hip", "psattn_mfma_bwd.hip",
            "psattn_mfma_dkdv.hip", "psattn_mfma_dkdv64.hip", "psattn_bwd_static.hip", "psattn_probe.hip", "psattn_rope.hip", "psattn_logprob.hip",
-           "psattn_rope_apply.hip", "psattn_head.hip", "psattn_head_bf16.hip", "psattn_head_bf16_any.hip", "psattn_head_f32.hip",
+           "psattn_rope_apply.hip", "psattn_head.hip", "psattn_head_bf16.hip", "psattn_head_bf16_any.hip", "psattn_head_f32.hip", "psattn_head_f32_whole.hip",
            "psattn_embed.hip", "psattn_layernorm.hip", "psattn_gatednorm.hip", "psattn_ffn.hip", "psattn_ffn_bf16.hip", "psattn_ffn_bf16_any.hip", "psattn_ffn_f32.hip"]
 
 # Packed-fp32 VALU instructions are switched off for all device code (the compiler

@@ -8,14 +8,18 @@ namespace psattn {
 namespace gemm {
 
 // One product (k is the contiguous axis of P, and of Q with kLse, kDlogit, or as kSums is told), enqueued on s.  Returns a psattn_status.
-// bf16 where every row of P, Q and what is stored is whole 16-byte groups on 16-byte boundaries; bf16; fp32
+// bf16 and fp32, where every row of P and Q is whole 16-byte groups on 16-byte boundaries, and of any alignment
 int head_product_bf16(Pass pass, bool qkc, TileSize size, const Product& d, hipStream_t s);
 int head_product_bf16_any(Pass pass, bool qkc, TileSize size, const Product& d, hipStream_t s);
+int head_product_f32_whole(Pass pass, bool qkc, TileSize size, const Product& d, hipStream_t s);
 int head_product_f32(Pass pass, bool qkc, TileSize size, const Product& d, hipStream_t s);
 
 // dX's sums and dW of a piece in one launch, of tiles of 256 x 256, or 128 x 128 of fp32; dz and the rows of X are whole in either
 int head_grads_bf16(const Product& x, const Product& w, hipStream_t s);
 int head_grads_f32(const Product& x, const Product& w, hipStream_t s);
+// dW alone, of few items: k is theirs, and behind them stand rows of zeros up to a multiple of 64
+int head_outer_bf16(const Product& w, hipStream_t s);
+int head_outer_f32(const Product& w, hipStream_t s);
 
 }  // namespace gemm
 }  // namespace psattn

@@ -265,6 +265,51 @@ __global__ __launch_bounds__(256) void psattn_head_dx(int64_t first, int col_blo
     }
 }
 
+// ... where it has many parts: 256 columns to a workgroup, whose sixteen waves share the parts
+template <typename E>
+__global__ __launch_bounds__(1024) void psattn_head_dx_parts(int64_t first, int col_blocks, int hidden, int n_items, int again, int n_parts, int64_t ld, const float* parts,
+                                                             const int32_t* row_desc, const int32_t* resp_first, const int32_t* resp_len, const int32_t* resp_prev,
+                                                             const int32_t* samp_ptr, const int32_t* item_ptr, E* dX) {
+    constexpr int V = 4, kAtOnce = 4;
+    __shared__ float4 sm[16][64];
+    const int64_t block = first + blockIdx.x;
+    const int row = static_cast<int>(block / col_blocks), desc = row_desc[row], w = threadIdx.x >> 6, l = threadIdx.x & 63;
+    const int c = (static_cast<int>(block - static_cast<int64_t>(row) * col_blocks) * 64 + l) * V;
+    int r0 = 0, r1 = 0;
+    if (desc >= 0) r0 = desc, r1 = desc + 1;
+    else if (desc < -1) r0 = samp_ptr[-2 - desc], r1 = samp_ptr[-1 - desc];
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int64_t step = again * ld;
+    auto add = [&](const float4& u) { x.x += u.x, x.y += u.y, x.z += u.z, x.w += u.w; };
+    if (c < hidden)
+        for (int j = r0; j < r1; ++j) {
+            if (resp_len[j] == 0) continue;
+            const int i = item_ptr[j] + (desc >= 0 ? row - resp_first[j] + (resp_prev[j] >= 0 ? 1 : 0) : 0);
+            for (int64_t row_of = i; row_of < again; row_of += n_items) {
+                const float* const from = parts + row_of * ld + c;
+                int p = w;
+                for (; p + 16 * (kAtOnce - 1) < n_parts; p += 16 * kAtOnce) {
+                    float4 u[kAtOnce];
+#pragma unroll
+                    for (int k = 0; k < kAtOnce; ++k) u[k] = *reinterpret_cast<const float4*>(from + (p + 16 * k) * step);
+#pragma unroll
+                    for (int k = 0; k < kAtOnce; ++k) add(u[k]);
+                }
+                for (; p < n_parts; p += 16) add(*reinterpret_cast<const float4*>(from + p * step));
+            }
+        }
+    sm[w][l] = x;
+    __syncthreads();
+    if (w > 0 || c >= hidden) return;
+#pragma unroll
+    for (int k = 1; k < 16; ++k) add(sm[k][l]);
+    E* const to = dX + static_cast<int64_t>(row) * hidden + c;
+    const float v[V] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+        if (c + k < hidden) rows::store1(to + k, v[k]);
+}
+
 // zeros without a memset, which a captured graph would not replay faithfully
 __global__ void psattn_head_zero(uint16_t* p, size_t n) {
     for (size_t i = blockIdx.x * static_cast<size_t>(blockDim.x) + threadIdx.x; i < n; i += static_cast<size_t>(gridDim.x) * blockDim.x) p[i] = 0;
@@ -272,8 +317,8 @@ __global__ void psattn_head_zero(uint16_t* p, size_t n) {
 
 // n workgroups in grids of at most 2^31 threads
 template <typename F>
-void in_grids(int64_t n, F launch) {
-    constexpr int64_t most = (int64_t{1} << 31) / 256;
+void in_grids(int64_t n, int threads, F launch) {
+    const int64_t most = (int64_t{1} << 31) / threads;
     for (int64_t at = 0; at < n; at += most) launch(at, static_cast<uint32_t>(std::min<int64_t>(n - at, most)));
 }
 
@@ -320,7 +365,7 @@ Tiling logits_tiling(int32_t dt, int64_t n_items, int64_t cols, int64_t hidden) 
     Tiling t = tiling(moved(dt), n_items, cols, hidden, may_split);
     if (n_items <= 64) {
         const int64_t tiles = cdiv(cols, 128);
-        t.split = tiles >= 200 ? 1 : std::max<int64_t>(1, std::min(512 / tiles, steps / 4));
+        t.split = tiles >= 128 ? 1 : std::max<int64_t>(1, std::min(512 / tiles, steps / 4));
     }
     t.split = may_split ? std::max<int64_t>(1, std::min(t.split, kPartBytes / std::max<int64_t>(bytes, 1))) : 1;
     return t;
@@ -329,8 +374,10 @@ size_t part_bytes(const Tiling& t, int64_t n_items, int64_t cols) { return t.spl
 
 int head_product(int32_t dt, Pass pass, bool qkc, TileSize size, Product d, hipStream_t s) {
     d.odd = pass == kDlogit && !(at16({d.out[0]}) && d.ldo % 8 == 0 && d.N % 8 == 0);
-    const bool whole = at16({d.p[0], d.q[0]}) && d.ldp % 8 == 0 && d.ldq % 8 == 0 && (qkc || d.n_load % 8 == 0);
-    return (dt != PSATTN_BF16 ? head_product_f32 : whole ? head_product_bf16 : head_product_bf16_any)(pass, qkc, size, d, s);
+    const int group = dt == PSATTN_BF16 ? 8 : 4;
+    const bool whole = at16({d.p[0], d.q[0]}) && d.ldp % group == 0 && d.ldq % group == 0 && (qkc || d.n_load % group == 0);
+    if (dt == PSATTN_BF16) return (whole ? head_product_bf16 : head_product_bf16_any)(pass, qkc, size, d, s);
+    return (whole ? head_product_f32_whole : head_product_f32)(pass, qkc, size, d, s);
 }
 
 // dz of a piece of the vocabulary has this much room at most
@@ -345,6 +392,7 @@ int64_t piece_rows(int32_t dt, int64_t n_items, int64_t vocab) {
 // exact as their own rounding then; of more items the errors of dz are beside each other (a token's row of dW off by 2^-9 of itself at most)
 constexpr int64_t kTwice = 32;
 int64_t dz_rows(int32_t dt, int64_t n_items) { return dt == PSATTN_BF16 && n_items <= kTwice ? 2 * n_items : n_items; }
+constexpr int kManyParts = 16;
 // dX's sums: k is a piece of the vocabulary, in parts where the rows' tiles are few.
 // Both products of dz in one launch, from `both` on: no part longer than half of what a CU has to do
 struct DxTiling : Tiling {
@@ -459,7 +507,7 @@ int psattn_head_logprob_fwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
             else psattn_head_join<16><<<static_cast<uint32_t>(cdiv(n, 16)), 256, 0, s>>>(n, parts, part, plan->item_row, target, hit, row_lse, logp);
         }
     }
-    in_grids(plan->n_resp, [&](int64_t at, uint32_t grid) { psattn_head_responses<<<grid, 256, 0, s>>>(static_cast<int>(at), plan->item_ptr, logp, resp_logp); });
+    in_grids(plan->n_resp, 256, [&](int64_t at, uint32_t grid) { psattn_head_responses<<<grid, 256, 0, s>>>(static_cast<int>(at), plan->item_ptr, logp, resp_logp); });
     return hipGetLastError() == hipSuccess ? PSATTN_OK : PSATTN_EHIP;
 }
 
@@ -526,25 +574,32 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
             g.p[0] = dz; g.q[0] = x; g.out[0] = static_cast<char*>(dW) + at * hidden * e;
             g.ldp = ldz; g.ldq = ld; g.ldo = hidden;
             g.M = cols; g.m_load = static_cast<int32_t>(up8(cols)); g.N = hidden; g.n_load = static_cast<int32_t>(ld); g.K = n_whole; g.n_seg = g.n_prod = g.n_split = 1;
-            g.odd = !(at16({g.out[0]}) && hidden % 8 == 0);
+            g.odd = !(at16({g.out[0]}) && hidden % (dt == PSATTN_BF16 ? 8 : 4) == 0);
             if (dx.both && (dt != PSATTN_BF16 || at16({w}))) {
                 if ((rc = (dt == PSATTN_BF16 ? head_grads_bf16 : head_grads_f32)(a, g, s)) != PSATTN_OK) return rc;
                 continue;
             }
             if ((rc = head_product(dt, kSums, false, dx.size, a, s)) != PSATTN_OK) return rc;
+            if (n_whole <= (dt == PSATTN_BF16 ? 256 : 64)) {
+                g.K = again;
+                if ((rc = (dt == PSATTN_BF16 ? head_outer_bf16 : head_outer_f32)(g, s)) != PSATTN_OK) return rc;
+                continue;
+            }
             const int64_t steps = n_whole / (dt == PSATTN_BF16 ? 64 : 32);
             auto us = [&](TileSize t, int64_t side) { return product_us(moved(dt), kPlain, t, cdiv(cols, side) * cdiv(hidden, side), steps, 1, 0); };
             const TileSize size = cdiv(cols, 256) * cdiv(hidden, 256) >= 256 || us(k256, 256) < us(k128, 128) ? k256 : k128;
             if ((rc = (dt == PSATTN_BF16 ? product_bf16 : product_f32)(kPlain, 0, false, false, size, g, s)) != PSATTN_OK) return rc;
         }
     }
-    // a row to a workgroup, or where they are few, 1 024 columns of one
-    const int col_blocks = plan->T < 4096 ? static_cast<int>(cdiv(hidden, 1024)) : 1;
-    in_grids(static_cast<int64_t>(plan->T) * col_blocks, [&](int64_t at, uint32_t grid) {
+    // a row to a workgroup; where they are few, 1 024 columns of one, or with many parts 256
+    const bool many = n <= 64 && parts * (again / std::max(n, 1)) >= kManyParts && plan->T < 4096;
+    const int col_blocks = many ? static_cast<int>(cdiv(hidden, 256)) : plan->T < 4096 ? static_cast<int>(cdiv(hidden, 1024)) : 1;
+    in_grids(static_cast<int64_t>(plan->T) * col_blocks, many ? 1024 : 256, [&](int64_t at, uint32_t grid) {
         auto go = [&](auto* to) {
             using E = std::remove_pointer_t<decltype(to)>;
-            psattn_head_dx<E><<<grid, 256, 0, s>>>(at, col_blocks, hidden, n, again, parts, ld, sums, plan->row_desc, plan->resp_first, plan->resp_len, plan->resp_prev,
-                                                   plan->samp_ptr, plan->item_ptr, to);
+            auto kernel = many ? psattn_head_dx_parts<E> : psattn_head_dx<E>;
+            kernel<<<grid, many ? 1024 : 256, 0, s>>>(at, col_blocks, hidden, n, again, parts, ld, sums, plan->row_desc, plan->resp_first, plan->resp_len, plan->resp_prev,
+                                                     plan->samp_ptr, plan->item_ptr, to);
         };
         if (dt == PSATTN_BF16) go(static_cast<uint16_t*>(dX));
         else go(static_cast<float*>(dX));
