@@ -363,7 +363,8 @@ int psattn_meta_copy_positions(const psattn_meta* meta, int32_t* pos /* host [T]
  * rotary_dim / 2 and what is not turned in multiples of 16 bytes are fastest.  Results are rounded once, from fp32.  Positions: device
  * int32 [n_tokens], or NULL and those of a block mask of n_tokens tokens (psattn_meta_copy_positions; padding: 0).  A position outside
  * [0, max_positions) (padding) gives zeros.  Qr may be Q, and Kr K, with the same stride; no other overlap, Q and K of one buffer aside.
- * PSATTN_EUNSUPPORTED: more than 2^20 heads, or sizes whose grids would have 2^31 threads.  Never allocates or blocks.
+ * PSATTN_EUNSUPPORTED: more than 2^20 heads, or sizes whose grids would have 2^31 threads.  PSATTN_EINVAL also for a table of
+ * another device than the current one.  Never allocates or blocks.
  */
 int psattn_rope_frequencies(int32_t rotary_dim, double theta, int32_t scaling, double factor, double original_positions, double low,
                             double high, double* inv_freq);
@@ -432,7 +433,8 @@ int psattn_dpo_loss(int32_t n_pairs, float beta, const float* logp_policy, const
  * Workspaces: the caller's device memory, of at least the bytes that the call of that name gives for the plan (never 0 for valid
  * arguments), contents undefined on entry and exit, one for each call in flight.  The backward's holds the rows and one piece (at most
  * 512 MiB) of the logits' gradient.  No call allocates or blocks, and all may be captured into a graph.
- * PSATTN_EUNSUPPORTED: rows of 2^23 bytes and more, 2^23 predicted tokens and more, or sizes whose grids would have 2^31 threads.
+ * PSATTN_EUNSUPPORTED: rows of 2^23 bytes and more, some 2^23 predicted tokens and more, or sizes whose grids would have 2^31
+ * threads.  PSATTN_EINVAL also for a plan of another device than the current one.
  */
 size_t psattn_head_logprob_fwd_workspace_bytes(const psattn_lp_plan* plan, int32_t dt, int32_t vocab, int32_t hidden);
 int psattn_head_logprob_fwd(const psattn_lp_plan* plan, int32_t dt, int32_t vocab, int32_t hidden, const void* X, const void* W,

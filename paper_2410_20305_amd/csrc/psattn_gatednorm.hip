@@ -518,6 +518,12 @@ bool sized(int hidden, bool all, F&& f) {
 constexpr int kManyRows = 26 * 1024;
 int n_parts(int32_t n_rows, int lanes) { return std::max(1, std::min(n_rows, n_rows >= kManyRows ? 1024 : lanes >= 512 ? 256 : 512)); }
 
+// ... that a workspace has room for.  Rows wider than 8 192 have their columns summed apart, in fewer parts the wider they are
+int most_parts(int32_t n_rows, int32_t hidden) {
+    const int cols = (hidden + 2047) / 2048;  // of bf16
+    return hidden <= 8192 ? n_parts(n_rows, 256) : std::min(n_parts(n_rows, 256), std::max(8, 2048 / cols / 8 * 8));
+}
+
 bool bad_shape(int32_t dt, int32_t n_rows, int32_t hidden) { return (dt != PSATTN_F32 && dt != PSATTN_BF16) || n_rows < 0 || hidden <= 0; }
 
 template <typename E>
@@ -609,7 +615,7 @@ int psattn_gatednorm_fwd(int32_t dt, int32_t n_rows, int32_t hidden, float eps, 
 
 size_t psattn_gatednorm_bwd_workspace_bytes(int32_t n_rows, int32_t hidden) {
     if (n_rows < 0 || hidden <= 0) return 0;
-    return align_up(2 * sizeof(float) * static_cast<size_t>(n_parts(n_rows, 256)) * hidden, 256) + align_up(sizeof(float) * static_cast<size_t>(n_rows), 256) + 256;
+    return align_up(2 * sizeof(float) * static_cast<size_t>(most_parts(n_rows, hidden)) * hidden, 256) + align_up(sizeof(float) * static_cast<size_t>(n_rows), 256) + 256;
 }
 
 int psattn_gatednorm_bwd(int32_t dt, int32_t n_rows, int32_t hidden, float res_scale, const void* B, const void* w_post, const void* gate, int32_t gate_rows,
@@ -632,7 +638,7 @@ int psattn_gatednorm_bwd(int32_t dt, int32_t n_rows, int32_t hidden, float res_s
         const bool vector_gate = dgate && (n_rows == 0 ? gate_rows == 1 : a.gate_step == 0);
         a.dgate = vector_gate ? nullptr : static_cast<E*>(dgate);
         a.part = reinterpret_cast<float*>(align_up(reinterpret_cast<uintptr_t>(workspace), 256));
-        a.row_m = a.part + align_up(2 * sizeof(float) * static_cast<size_t>(n_parts(n_rows, 256)) * hidden, 256) / sizeof(float);
+        a.row_m = a.part + align_up(2 * sizeof(float) * static_cast<size_t>(most_parts(n_rows, hidden)) * hidden, 256) / sizeof(float);
         bwd(a, vector_gate, dw_pre, dw_post, dgate, static_cast<hipStream_t>(hip_stream));
     };
     if (dt == PSATTN_BF16) go(uint16_t{});

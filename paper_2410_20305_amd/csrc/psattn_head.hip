@@ -420,13 +420,18 @@ struct Room {
     }
 };
 
+// a plan's tables are on the device that was current when it was made
+bool elsewhere(const psattn_lp_plan* plan) {
+    int device = -1;
+    return hipGetDevice(&device) == hipSuccess && device != plan->device;
+}
 bool bad_shape(const psattn_lp_plan* plan, int32_t dt, int32_t vocab, int32_t hidden) {
     return !plan || (dt != PSATTN_F32 && dt != PSATTN_BF16) || vocab <= 0 || hidden <= 0;
 }
 // a tile's copies have 32-bit offsets, and grids stay below 2^31 threads
 bool too_large(const psattn_lp_plan* plan, int32_t dt, int64_t vocab, int64_t hidden, bool bwd) {
     const int64_t n = plan->n_items;
-    if (hidden * static_cast<int64_t>(elem_bytes(dt)) * 256 >= (int64_t{1} << 31) || n >= (int64_t{1} << 23) || vocab > INT32_MAX - 512) return true;
+    if (hidden * static_cast<int64_t>(elem_bytes(dt)) * 256 >= (int64_t{1} << 31) || n > (int64_t{1} << 23) - 128 || vocab > INT32_MAX - 512) return true;
     auto fits = [](int64_t M, int64_t N, TileSize t) {
         static constexpr int bm[] = {32, 64, 128, 256}, bn[] = {128, 128, 128, 256}, threads[] = {128, 128, 256, 512};
         return cdiv(M, bm[t]) * cdiv(N, bn[t]) < (int64_t{1} << 31) / threads[t];
@@ -470,6 +475,7 @@ int psattn_head_logprob_fwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
     if (plan->n_resp == 0) return PSATTN_OK;
     if (!X || !W || !token_ids || !row_lse || !resp_logp || !workspace || workspace_bytes < fwd_bytes(plan, dt, vocab, hidden)) return PSATTN_EINVAL;
     if (too_large(plan, dt, vocab, hidden, false)) return PSATTN_EUNSUPPORTED;
+    if (elsewhere(plan)) return PSATTN_EINVAL;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     const int n = static_cast<int>(plan->n_items);
     Room room(workspace);
@@ -518,6 +524,7 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
     const int n = static_cast<int>(plan->n_items);
     if (n > 0 && (!X || !W || !token_ids || !row_lse || !d_resp_logp || !workspace || workspace_bytes < bwd_bytes(plan, dt, vocab, hidden))) return PSATTN_EINVAL;
     if (too_large(plan, dt, vocab, hidden, true)) return PSATTN_EUNSUPPORTED;
+    if (plan->T > 0 && elsewhere(plan)) return PSATTN_EINVAL;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     const size_t e = elem_bytes(dt);
     Room room(workspace);
@@ -582,13 +589,12 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
             if ((rc = head_product(dt, kSums, false, dx.size, a, s)) != PSATTN_OK) return rc;
             if (n_whole <= (dt == PSATTN_BF16 ? 256 : 64)) {
                 g.K = again;
-                if ((rc = (dt == PSATTN_BF16 ? head_outer_bf16 : head_outer_f32)(g, s)) != PSATTN_OK) return rc;
-                continue;
+                rc = (dt == PSATTN_BF16 ? head_outer_bf16 : head_outer_f32)(g, s);
+            } else {  // bf16: fp32 takes one way or the other above
+                auto us = [&](TileSize t, int64_t side) { return product_us(kWhole, kPlain, t, cdiv(cols, side) * cdiv(hidden, side), n_whole / 64, 1, 0); };
+                rc = product_bf16(kPlain, 0, false, false, cdiv(cols, 256) * cdiv(hidden, 256) >= 256 || us(k256, 256) < us(k128, 128) ? k256 : k128, g, s);
             }
-            const int64_t steps = n_whole / (dt == PSATTN_BF16 ? 64 : 32);
-            auto us = [&](TileSize t, int64_t side) { return product_us(moved(dt), kPlain, t, cdiv(cols, side) * cdiv(hidden, side), steps, 1, 0); };
-            const TileSize size = cdiv(cols, 256) * cdiv(hidden, 256) >= 256 || us(k256, 256) < us(k128, 128) ? k256 : k128;
-            if ((rc = (dt == PSATTN_BF16 ? product_bf16 : product_f32)(kPlain, 0, false, false, size, g, s)) != PSATTN_OK) return rc;
+            if (rc != PSATTN_OK) return rc;
         }
     }
     // a row to a workgroup; where they are few, 1 024 columns of one, or with many parts 256

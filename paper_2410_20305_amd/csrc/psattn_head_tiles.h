@@ -20,7 +20,12 @@ int launch_head(Pass pass, bool qkc, TileSize size, const Product& d, hipStream_
     if (pass == kLse) return launch_logits<E, ASYNC, kLse>(size, d, s);
     if (pass == kDlogit) return launch_logits<E, ASYNC, kDlogit>(size, d, s);
     if (qkc) return launch_logits<E, ASYNC, kSums>(size, d, s);
-    return launch_sized<E, ASYNC, true, false, kSums, 0>(size, d, s);
+    if constexpr (sizeof(E) == 4) {  // dX of more items comes with dW
+        if (size == k32) return launch_tiles<E, ASYNC, true, false, kSums, 0, Shape<32, 128, 1, 2, 2>>(d, s);
+        return launch_tiles<E, ASYNC, true, false, kSums, 0, Shape<64, 128, 1, 2, 2>>(d, s);
+    } else {
+        return launch_sized<E, ASYNC, true, false, kSums, 0>(size, d, s);
+    }
 }
 
 // A piece's two products of dz in one launch, tiles of 256 x 256, or 128 x 128 of fp32: first dX's, whose k is the piece, then dW's, whose k is the items and
