@@ -9,6 +9,7 @@
 // mean(ds gw bh) = mean(t gw bh) - rs m mean(sh gw bh): the three sums of a row are taken together, in one pass over it.
 //
 // Bound by HBM: each row is read once and stays in registers (16 bytes to a lane and load) between its sums and its result, in fp32.
+// 65 536 rows of 8 192 bf16 with a gate for each: forward 920 us (5.8 TB/s), backward 1 616 (5.3); 8 334 of 4 096 with one for all 52 and 90.
 // The sums run over the lanes in a tree of a fixed shape: a row's bits do not depend on the other rows.
 #include <hip/hip_runtime.h>
 
@@ -112,19 +113,41 @@ __global__ __launch_bounds__(kThreads<LANES>) void psattn_gn_fwd(Args<E> a) {
 // Backward.  A workgroup takes the rows from blockIdx.x on, gridDim.x apart, and keeps its lanes' columns of dw_pre and C in registers;
 // they go to part[workgroup] at its end and are joined by psattn_gn_weights (rows that share a workgroup add up in LDS first).
 // Rows stay in the registers as they came and are unpacked twice, with room for the next row's loads while one is summed.  ALL: a gate
-// for each row; else w_post and gate are one factor for all rows.  What there is not stands there as zeros or ones, without branches.
-//   Without SUMS a workgroup has one row, whose rs m it keeps, and the columns are left to psattn_gn_columns.
-template <typename E, int LANES, int PER, bool WHOLE, bool SUMS, bool ALL>
+// for each row; else w_post and gate are one factor for all rows.  What there is not stands there as zeros or ones, without branches, and
+// what the sums have unpacked is unpacked again for the results: kept, it spilled (65 536 x 8 192, a gate for each row: 3 670 us).
+//   Rows of 32 columns to a lane keep the columns' sums in LDS, each lane its own (20 000 rows of 16 384 bf16, forward and backward: in a second pass
+// over the rows 2 113 us, so 1 528).
+template <typename E, int LANES, int PER, bool WHOLE, bool ALL>
 __global__ __launch_bounds__(kThreads<LANES>) void psattn_gn_bwd(Args<E> a) {
     constexpr int V = kVec<E>, kAt = kThreads<LANES> / LANES;  // rows at a time
+    constexpr bool kInLds = PER * V >= 32;
+    __shared__ float4 columns[kInLds ? 2 * PER * (V / 4) * LANES : 1];  // [dw_pre, C][group][four of V][lane]
     __shared__ float sm[2][48];
     __shared__ float add[kAt > 1 ? kAt * LANES * PER * V : 1];
-    static_assert(SUMS || kAt == 1, "short rows' columns are summed here");
     const int lane = threadIdx.x % LANES, hidden = a.hidden, n_rows = a.n_rows;
     // rows of a wave and more are known to be: their addresses are scalar
     const int own = kAt == 1 ? 0 : LANES == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : static_cast<int>(threadIdx.x) / LANES;
-    float dw[PER][V] = {}, dc[PER][V] = {};
-    constexpr bool kAhead = SUMS && PER <= 2 && (WHOLE || !ALL || PER * V < 16 || LANES < 512);  // the next row's loads, where there are registers for them
+    float sums[2][kInLds ? 1 : PER][V] = {};
+    auto slot = [&](int which, int p, int q) -> float4& { return columns[((which * PER + p) * (V / 4) + q) * LANES + lane]; };
+    if constexpr (kInLds) {
+#pragma unroll
+        for (int i = 0; i < 2 * PER * (V / 4); ++i) columns[i * LANES + lane] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    auto collect = [&](int which, int p, const float (&x)[V]) {  // a lane's own columns
+        if constexpr (kInLds) {
+#pragma unroll
+            for (int q = 0; q < V / 4; ++q) {
+                float4& to = slot(which, p, q);
+                float4 s = to;
+                s.x += x[4 * q], s.y += x[4 * q + 1], s.z += x[4 * q + 2], s.w += x[4 * q + 3];
+                to = s;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) sums[which][p][j] += x[j];
+        }
+    };
+    constexpr bool kAhead = PER <= 2 && (WHOLE || !ALL || PER * V < 16 || LANES < 512);  // the next row's loads, where there are registers for them
     const int step = gridDim.x * kAt;
     int row = blockIdx.x * kAt + own;
     // this lane's first column: the same for all its rows, whose misalignment has to be
@@ -210,16 +233,17 @@ __global__ __launch_bounds__(kThreads<LANES>) void psattn_gn_bwd(Args<E> a) {
         float sum[3] = {0.f, 0.f, 0.f};
 #pragma unroll
         for (int p = 0; p < PER; ++p) {
-            float q[V];
+            float q[V], dw[V];
             unpacked(p, q);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                if constexpr (SUMS) dw[p][j] += dy[j] * s[j];
+                dw[j] = dy[j] * s[j];
                 const float fb = (ALL ? g[j] * f[j] : f[j]) * b[j];
                 sum[0] += q[j] * s[j];
                 sum[1] += t[j] * fb;
                 sum[2] += s[j] * fb;
             }
+            collect(0, p, dw);
             __builtin_amdgcn_sched_barrier(0);
         }
         group_sum<LANES>(sum, sm[turn]);
@@ -246,27 +270,28 @@ __global__ __launch_bounds__(kThreads<LANES>) void psattn_gn_bwd(Args<E> a) {
             }
             store<WHOLE>(a.dX + at, c, hidden, o);
             if (a.B) {
+                float dc[V];
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
                     const float tb = t[j] * b[j];
-                    if constexpr (SUMS) dc[p][j] += ALL ? g[j] * tb : tb;
+                    dc[j] = ALL ? g[j] * tb : tb;
                     o[j] = now.rb * (t[j] * (ALL ? g[j] * f[j] : f[j]) - b[j] * mb);
                     if constexpr (ALL) t[j] = f[j] * tb;
                 }
+                collect(1, p, dc);
                 store<WHOLE>(a.dB + at, c, hidden, o);
                 if constexpr (ALL) store<WHOLE>(a.dgate + at, c, hidden, t);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        if constexpr (!SUMS) {  // its one row: nothing is kept for another
-            if (threadIdx.x == 0) a.row_m[row] = m;
-            return;
-        }
         if constexpr (kAhead) now = next;
     }
-    if constexpr (!SUMS) return;
     float* const mine = a.part + 2 * static_cast<size_t>(blockIdx.x) * hidden;
-    auto out = [&](float* to, const float (&v)[PER][V]) {
+    auto value = [&](int which, int p, int j) {
+        if constexpr (kInLds) return reinterpret_cast<const float*>(&slot(which, p, j / 4))[j % 4];
+        else return sums[which][p][j];
+    };
+    auto out = [&](float* to, int which) {
         float* const at = kAt > 1 ? add + own * LANES * PER * V : to;  // rows that share the workgroup: by column, then added up
         if constexpr (kAt > 1) __syncthreads();
 #pragma unroll
@@ -274,7 +299,7 @@ __global__ __launch_bounds__(kThreads<LANES>) void psattn_gn_bwd(Args<E> a) {
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 const int c = from + p * LANES * V + j;
-                if (c >= 0 && c < hidden) at[c] = v[p][j];
+                if (c >= 0 && c < hidden) at[c] = value(which, p, j);
             }
         if constexpr (kAt > 1) {
             __syncthreads();
@@ -286,8 +311,8 @@ __global__ __launch_bounds__(kThreads<LANES>) void psattn_gn_bwd(Args<E> a) {
             }
         }
     };
-    out(mine, dw);
-    if (a.B) out(mine + hidden, dc);
+    out(mine, 0);
+    if (a.B) out(mine + hidden, 1);
 }
 
 // The weights' gradients from the workgroups' parts: 64 columns to a workgroup, sixteen lanes to a column; the first `hidden` are dw_pre,
@@ -518,10 +543,10 @@ bool sized(int hidden, bool all, F&& f) {
 constexpr int kManyRows = 26 * 1024;
 int n_parts(int32_t n_rows, int lanes) { return std::max(1, std::min(n_rows, n_rows >= kManyRows ? 1024 : lanes >= 512 ? 256 : 512)); }
 
-// ... that a workspace has room for.  Rows wider than 8 192 have their columns summed apart, in fewer parts the wider they are
+// ... that a workspace has room for.  Rows wider than 16 384 have their columns summed apart, in fewer parts the wider they are
 int most_parts(int32_t n_rows, int32_t hidden) {
     const int cols = (hidden + 2047) / 2048;  // of bf16
-    return hidden <= 8192 ? n_parts(n_rows, 256) : std::min(n_parts(n_rows, 256), std::max(8, 2048 / cols / 8 * 8));
+    return hidden <= 16384 ? n_parts(n_rows, 256) : std::min(n_parts(n_rows, 256), std::max(8, 2048 / cols / 8 * 8));
 }
 
 bool bad_shape(int32_t dt, int32_t n_rows, int32_t hidden) { return (dt != PSATTN_F32 && dt != PSATTN_BF16) || n_rows < 0 || hidden <= 0; }
@@ -542,20 +567,17 @@ void bwd(Args<E> a, bool vector_gate, void* dw_pre, void* dw_post, void* dgate, 
     int np = a.n_rows > 0 ? n_parts(a.n_rows, 256) : 0;
     if (a.n_rows > 0) {
         const bool all = whole<E>(a.hidden, {a.S, a.B, a.w_post, a.gate, a.w_pre, a.dY, a.dS, a.dX, a.dB, a.dgate});
-        bool sums = false;
         const bool done = sized<E, true>(a.hidden, all, [&](auto lanes, auto per) {
             constexpr int L = decltype(lanes)::value, PER = decltype(per)::value, kAt = kThreads<L> / L;
-            constexpr bool SUMS = PER * kVec<E> < 32;  // up to 1 024 groups of bf16, 2 048 of fp32
             np = std::min(n_parts(a.n_rows, L), (a.n_rows + kAt - 1) / kAt);
             if (np > 8) np -= np % 8;  // a workgroup's rows start alike
-            sums = SUMS;
-            auto go = [&](auto kernel) { kernel<<<SUMS ? np : a.n_rows, kThreads<L>, 0, s>>>(a); };
-            if constexpr (PER == 4) a.gate_step ? go(psattn_gn_bwd<E, L, PER, true, SUMS, true>) : go(psattn_gn_bwd<E, L, PER, true, SUMS, false>);  // whole rows alone: `sized`
-            else if (a.gate_step) all ? go(psattn_gn_bwd<E, L, PER, true, SUMS, true>) : go(psattn_gn_bwd<E, L, PER, false, SUMS, true>);
-            else all ? go(psattn_gn_bwd<E, L, PER, true, SUMS, false>) : go(psattn_gn_bwd<E, L, PER, false, SUMS, false>);
+            auto go = [&](auto kernel) { kernel<<<np, kThreads<L>, 0, s>>>(a); };
+            if constexpr (PER == 4) a.gate_step ? go(psattn_gn_bwd<E, L, PER, true, true>) : go(psattn_gn_bwd<E, L, PER, true, false>);  // whole rows alone: `sized`
+            else if (a.gate_step) all ? go(psattn_gn_bwd<E, L, PER, true, true>) : go(psattn_gn_bwd<E, L, PER, false, true>);
+            else all ? go(psattn_gn_bwd<E, L, PER, true, false>) : go(psattn_gn_bwd<E, L, PER, false, false>);
         });
-        if (!done) psattn_gn_bwd_wide<E><<<a.n_rows, 1024, 0, s>>>(a);
-        if (!sums) {
+        if (!done) {
+            psattn_gn_bwd_wide<E><<<a.n_rows, 1024, 0, s>>>(a);
             const int cols = (a.hidden + kVec<E> - 1 + 256 * kVec<E> - 1) / (256 * kVec<E>);
             np = std::min(np, std::max(8, 2048 / cols / 8 * 8));  // eight workgroups to a CU
             psattn_gn_columns<E><<<dim3(cols, np), 256, 0, s>>>(a);
