@@ -431,8 +431,8 @@ int psattn_dpo_loss(int32_t n_pairs, float beta, const float* logp_policy, const
  * operand of the matrix cores and is rounded to dt once, from fp32; sums are fp32 in a fixed order.  A response whose d_resp_logp is 0,
  * and a token id outside [0, vocab), give nothing.
  * Workspaces: the caller's device memory, of at least the bytes that the call of that name gives for the plan (never 0 for valid
- * arguments), contents undefined on entry and exit, one for each call in flight.  The backward's holds the rows and one piece (at most
- * 512 MiB) of the logits' gradient.  No call allocates or blocks, and all may be captured into a graph.
+ * arguments), contents undefined on entry and exit, one for each call in flight.  The backward's holds the rows and one piece (some
+ * 512 MiB, 256 tokens of the vocabulary at least) of the logits' gradient.  No call allocates or blocks, and all may be captured into a graph.
  * PSATTN_EUNSUPPORTED: rows of 2^23 bytes and more, some 2^23 predicted tokens and more, or sizes whose grids would have 2^31
  * threads.  PSATTN_EINVAL also for a plan of another device than the current one.
  */

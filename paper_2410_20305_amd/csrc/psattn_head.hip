@@ -358,7 +358,9 @@ Tiling tiling(Move move, int64_t M, int64_t N, int64_t K, bool may_split) {
     return best;
 }
 Move moved(int32_t dt) { return dt == PSATTN_BF16 ? kWhole : kFloat; }
-// Logits: their parts of k, where one workgroup to a tile would leave most of the chip idle, are small beside W
+// Logits: in parts of k where one workgroup to a tile would leave much of the chip idle and the parts are small beside W.  A whole step in us,
+// whole / in parts: 4 items, vocabulary 2 423, hidden 5 632 109 / 65; 2 items, 1 021, 6 592 108 / 54; forward, 3 items, 3 013, 5 321 87 / 27; fp32,
+// 224 items, 2 119, 1 577 129 / 48; but 14 items, 22 005 (172 tiles), 1 472 97 / 119
 Tiling logits_tiling(int32_t dt, int64_t n_items, int64_t cols, int64_t hidden) {
     const int64_t steps = hidden / (dt == PSATTN_BF16 ? 64 : 32), bytes = 4 * n_items * up8(cols);
     const bool may_split = n_items <= kPartItems && bytes <= kPartBytes;
@@ -394,7 +396,9 @@ constexpr int64_t kTwice = 32;
 int64_t dz_rows(int32_t dt, int64_t n_items) { return dt == PSATTN_BF16 && n_items <= kTwice ? 2 * n_items : n_items; }
 constexpr int kManyParts = 16;
 // dX's sums: k is a piece of the vocabulary, in parts where the rows' tiles are few.
-// Both products of dz in one launch, from `both` on: no part longer than half of what a CU has to do
+// `both`: dX and dW of a piece in one launch, no part of k longer than half of what a CU has to do.  A whole step in us, apart / so: bf16, vocabulary
+// 32 000, hidden 4 096, 300 tokens (60 in 100 predicted) 357 / 366, 600 500 / 510, 1 200 825 / 827, 2 400 1 406 / 1 347, 5 000 2 679 / 2 649; 16 384 tokens, 128 000
+// the same (the chip's clock falls with what its matrix cores do); fp32, 20 000, 1 024: 300 tokens 506 / 454, 1 200 1 234 / 1 082, 3 000 2 992 / 2 590
 struct DxTiling : Tiling {
     bool both;
 };
@@ -582,8 +586,9 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
             g.ldp = ldz; g.ldq = ld; g.ldo = hidden;
             g.M = cols; g.m_load = static_cast<int32_t>(up8(cols)); g.N = hidden; g.n_load = static_cast<int32_t>(ld); g.K = n_whole; g.n_seg = g.n_prod = g.n_split = 1;
             g.odd = !(at16({g.out[0]}) && hidden % (dt == PSATTN_BF16 ? 8 : 4) == 0);
-            if (dx.both && (dt != PSATTN_BF16 || at16({w}))) {
-                if ((rc = (dt == PSATTN_BF16 ? head_grads_bf16 : head_grads_f32)(a, g, s)) != PSATTN_OK) return rc;
+            const bool whole = at16({w}) && hidden % (dt == PSATTN_BF16 ? 8 : 4) == 0;
+            if (dx.both && (whole || dt != PSATTN_BF16)) {
+                if ((rc = (dt == PSATTN_BF16 ? head_grads_bf16 : whole ? head_grads_f32_whole : head_grads_f32)(a, g, s)) != PSATTN_OK) return rc;
                 continue;
             }
             if ((rc = head_product(dt, kSums, false, dx.size, a, s)) != PSATTN_OK) return rc;

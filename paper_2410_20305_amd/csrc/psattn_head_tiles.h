@@ -143,7 +143,7 @@ int launch_outer(const Product& d, hipStream_t s) {
 
 template <typename E, bool ASYNC>
 int launch_grads(const Product& x, const Product& w, hipStream_t s) {
-    using S = std::conditional_t<sizeof(E) == 2, Shape<256, 256, 2, 4, 3>, Shape<128, 128, 2, 2, 2>>;
+    using S = std::conditional_t<sizeof(E) == 2, Shape<256, 256, 2, 4, 3>, Shape<128, 128, 2, 2, ASYNC ? 3 : 2>>;
     auto tiles = [](int64_t n) { return (n + S::BM - 1) / S::BM; };
     const int64_t xm = tiles(x.M), xn = tiles(x.N), wm = tiles(w.M), wn = tiles(w.N), n = xm * xn * x.n_split + wm * wn;
     if (n >= (int64_t{1} << 31) / S::kThreads) return PSATTN_EUNSUPPORTED;
