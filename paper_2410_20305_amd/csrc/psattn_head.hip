@@ -40,7 +40,7 @@ size_t elem_bytes(int32_t dt) { return dt == PSATTN_BF16 ? 2 : 4; }
 template <typename E, bool BWD>
 __global__ __launch_bounds__(256) void psattn_head_rows(int n_items, int again, const int32_t* item_row, const int32_t* item_tok, const int32_t* item_resp,
                                                         const int32_t* token_ids, int vocab, int hidden, const E* X, const float* row_lse, const float* d_logp, E* out,
-                                                        int32_t* target, float* lse, float* weight, E* dz, int64_t ldz) {
+                                                        int32_t* target, float* lse, float* weight, float* left, E* dz, int64_t ldz) {
     constexpr int V = rows::kVec<E>;
     const int64_t at = blockIdx.x, ld = (hidden + 7) / 8 * 8;
     if (BWD && at >= again) {
@@ -57,6 +57,7 @@ __global__ __launch_bounds__(256) void psattn_head_rows(int n_items, int again, 
         if constexpr (BWD) {
             lse[i] = known ? row_lse[row] : 0.f;
             weight[i] = known ? d_logp[item_resp[i]] : 0.f;
+            left[i] = 0.f;
         }
     }
     const E* const x = X + static_cast<int64_t>(row) * hidden;
@@ -128,7 +129,7 @@ __global__ __launch_bounds__(1024) void psattn_head_parts_lse(int n_items, int n
 // dz of an item, and of bf16 what its rounding leaves where that is asked for: 1 024 columns to a workgroup
 template <typename E>
 __global__ __launch_bounds__(256) void psattn_head_parts_dz(int n_items, int n_parts, int first, int cols, int64_t ld, const float* parts, const int32_t* target, const float* lse,
-                                                            const float* weight, E* dz, E* rest, int64_t ldz) {
+                                                            const float* weight, E* dz, E* rest, float* left, int64_t ldz) {
     const int64_t i = blockIdx.y;
     const int c = (blockIdx.x * 256 + threadIdx.x) * 4, t = target[i] - first;
     if (c >= cols) return;
@@ -141,6 +142,7 @@ __global__ __launch_bounds__(256) void psattn_head_parts_dz(int n_items, int n_p
         const float p = expf(z[k] - l), x = w == 0.f ? 0.f : w * (c + k == t ? 1.f - p : -p);
         rows::store1(dz + i * ldz + c + k, x);
         if (rest) rows::store1(rest + i * ldz + c + k, x - rows::hold(x, dz));
+        if (left && c + k == t) left[i] = x - rows::hold(x, dz);
     }
 }
 
@@ -225,11 +227,21 @@ __global__ __launch_bounds__(256) void psattn_head_responses(int first, const in
     if (threadIdx.x == 0) resp_logp[j] = (sm[0] + sm[1]) + (sm[2] + sm[3]);
 }
 
+// what the rounding left of dz at an item's token: that token's row of W has all of its gradient's largest term in one number, whose rounding
+// error is that of every column alike (99 items: dX off by 2.5e-3 without, 1.7e-3 with it, the rounding of dX itself)
+template <typename E>
+__device__ __forceinline__ void add_left(float left, const E* w, int c, int hidden, float (&x)[4]) {
+    if (left == 0.f) return;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (c + k < hidden) x[k] = fmaf(left, rows::to_f32(w[c + k]), x[k]);
+}
+
 // ---- dX of token t: the sums of its items, of all parts of each; `again` rows to a part
 template <typename E>
 __global__ __launch_bounds__(256) void psattn_head_dx(int64_t first, int col_blocks, int hidden, int n_items, int again, int n_parts, int64_t ld, const float* parts, const int32_t* row_desc,
                                                       const int32_t* resp_first, const int32_t* resp_len, const int32_t* resp_prev, const int32_t* samp_ptr,
-                                                      const int32_t* item_ptr, E* dX) {
+                                                      const int32_t* item_ptr, const int32_t* target, const float* left, const E* W, E* dX) {
     constexpr int V = 4;
     const int64_t block = first + blockIdx.x;
     const int row = static_cast<int>(block / col_blocks), desc = row_desc[row];
@@ -258,6 +270,7 @@ __global__ __launch_bounds__(256) void psattn_head_dx(int64_t first, int col_blo
                 for (; p + 8 <= n_parts; p += 8) add(std::integral_constant<int, 8>{});
                 for (; p < n_parts; ++p) add(std::integral_constant<int, 1>{});
             }
+            if (left) add_left(left[i], W + static_cast<int64_t>(target[i]) * hidden, c, hidden, x);
         }
 #pragma unroll
         for (int k = 0; k < V; ++k)
@@ -269,7 +282,7 @@ __global__ __launch_bounds__(256) void psattn_head_dx(int64_t first, int col_blo
 template <typename E>
 __global__ __launch_bounds__(1024) void psattn_head_dx_parts(int64_t first, int col_blocks, int hidden, int n_items, int again, int n_parts, int64_t ld, const float* parts,
                                                              const int32_t* row_desc, const int32_t* resp_first, const int32_t* resp_len, const int32_t* resp_prev,
-                                                             const int32_t* samp_ptr, const int32_t* item_ptr, E* dX) {
+                                                             const int32_t* samp_ptr, const int32_t* item_ptr, const int32_t* target, const float* left, const E* W, E* dX) {
     constexpr int V = 4, kAtOnce = 4;
     __shared__ float4 sm[16][64];
     const int64_t block = first + blockIdx.x;
@@ -296,6 +309,11 @@ __global__ __launch_bounds__(1024) void psattn_head_dx_parts(int64_t first, int 
                     for (int k = 0; k < kAtOnce; ++k) add(u[k]);
                 }
                 for (; p < n_parts; p += 16) add(*reinterpret_cast<const float4*>(from + p * step));
+            }
+            if (left && w == 0) {
+                float y[V] = {x.x, x.y, x.z, x.w};
+                add_left(left[i], W + static_cast<int64_t>(target[i]) * hidden, c, hidden, y);
+                x = make_float4(y[0], y[1], y[2], y[3]);
             }
         }
     sm[w][l] = x;
@@ -391,7 +409,7 @@ int64_t piece_rows(int32_t dt, int64_t n_items, int64_t vocab) {
     return cdiv(cdiv(vocab, n), 256) * 256;
 }
 // Few items of bf16: dz as two numbers each, the second what the first one's rounding leaves, as items of their own.  The gradients are as
-// exact as their own rounding then; of more items the errors of dz are beside each other (a token's row of dW off by 2^-9 of itself at most)
+// exact as their own rounding then; of more items a token's row of dW is off by 2^-9 of itself at most besides
 constexpr int64_t kTwice = 32;
 int64_t dz_rows(int32_t dt, int64_t n_items) { return dt == PSATTN_BF16 && n_items <= kTwice ? 2 * n_items : n_items; }
 constexpr int kManyParts = 16;
@@ -462,7 +480,7 @@ size_t bwd_bytes(const psattn_lp_plan* plan, int32_t dt, int32_t vocab, int32_t 
     const int64_t m = dz_rows(dt, n), piece = piece_rows(dt, n, vocab);
     const size_t sums = m * up8(hidden) * dx_tiling(dt, n, vocab, hidden).split * sizeof(float), parts = logits_bytes(dt, n, vocab, piece, hidden);
     return align_up(up64(m) * up8(hidden) * elem_bytes(dt), 256) + align_up(up64(m) * up8(piece) * elem_bytes(dt), 256) + align_up(sums, 256) + align_up(parts, 256) +
-           3 * align_up(n * 4, 256) + 256;
+           4 * align_up(n * 4, 256) + 256;
 }
 
 }  // namespace
@@ -493,7 +511,7 @@ int psattn_head_logprob_fwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
         auto gather = [&](auto* to) {
             using E = std::remove_pointer_t<decltype(to)>;
             psattn_head_rows<E, false><<<n, 256, 0, s>>>(n, n, plan->item_row, plan->item_tok, plan->item_resp, token_ids, vocab, hidden, static_cast<const E*>(X),
-                                                         nullptr, nullptr, to, target, nullptr, nullptr, nullptr, 0);
+                                                         nullptr, nullptr, to, target, nullptr, nullptr, nullptr, nullptr, 0);
         };
         if (dt == PSATTN_BF16) gather(reinterpret_cast<uint16_t*>(x));
         else gather(reinterpret_cast<float*>(x));
@@ -536,7 +554,8 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
     const int parts = static_cast<int>(dx.split);
     const int64_t ld = up8(hidden), piece = piece_rows(dt, n, vocab), ldz = up8(piece);
     const int again = static_cast<int>(dz_rows(dt, n)), n_whole = static_cast<int>(up64(again));
-    float* sums = nullptr;
+    float *sums = nullptr, *left = nullptr;
+    const int32_t* target = nullptr;
     if (n == 0) {  // nothing is predicted: sums over nothing
         psattn_head_zero<<<1024, 256, 0, s>>>(static_cast<uint16_t*>(dW), static_cast<size_t>(vocab) * hidden * e / 2);
     } else {
@@ -545,12 +564,14 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
         sums = room.take<float>(static_cast<size_t>(again) * ld * parts);
         float* const z_parts = reinterpret_cast<float*>(room.take<char>(logits_bytes(dt, n, vocab, piece, hidden)));
         char* const rest = again > n ? dz + n * ldz * e : nullptr;
-        int32_t* const target = room.take<int32_t>(n);
+        int32_t* const targets = room.take<int32_t>(n);
         float *const lse = room.take<float>(n), *const weight = room.take<float>(n);
+        left = room.take<float>(n);
+        target = targets;
         auto gather = [&](auto* to) {
             using E = std::remove_pointer_t<decltype(to)>;
             psattn_head_rows<E, true><<<n_whole, 256, 0, s>>>(n, again, plan->item_row, plan->item_tok, plan->item_resp, token_ids, vocab, hidden, static_cast<const E*>(X),
-                                                              row_lse, d_resp_logp, to, target, lse, weight, reinterpret_cast<E*>(dz), ldz);
+                                                              row_lse, d_resp_logp, to, targets, lse, weight, left, reinterpret_cast<E*>(dz), ldz);
         };
         if (dt == PSATTN_BF16) gather(reinterpret_cast<uint16_t*>(x));
         else gather(reinterpret_cast<float*>(x));
@@ -559,7 +580,7 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
             const char* const w = static_cast<const char*>(W) + at * hidden * e;
             int rc;
             Product z{};  // dz
-            z.p[0] = x; z.q[0] = w; z.G = lse; z.U = weight; z.H = target; z.out[0] = dz; z.out[1] = rest;
+            z.p[0] = x; z.q[0] = w; z.G = lse; z.U = weight; z.H = targets; z.out[0] = dz; z.out[1] = rest; z.parts = rest ? nullptr : left;
             z.ldp = ld; z.ldq = hidden; z.ldo = ldz;
             z.M = n; z.N = cols; z.K = hidden; z.n_seg = z.n_prod = z.n_split = 1;
             z.n_load = static_cast<int32_t>(at);
@@ -569,8 +590,8 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
                 if ((rc = head_product(dt, kSums, true, tiling.size, z, s)) != PSATTN_OK) return rc;
                 auto go = [&](auto* to) {
                     using E = std::remove_pointer_t<decltype(to)>;
-                    psattn_head_parts_dz<E><<<dim3(static_cast<uint32_t>(cdiv(cols, 1024)), n), 256, 0, s>>>(n, z.n_split, static_cast<int>(at), cols, z.ld_part, z_parts, target, lse,
-                                                                                                            weight, to, reinterpret_cast<E*>(rest), ldz);
+                    psattn_head_parts_dz<E><<<dim3(static_cast<uint32_t>(cdiv(cols, 1024)), n), 256, 0, s>>>(n, z.n_split, static_cast<int>(at), cols, z.ld_part, z_parts, targets, lse,
+                                                                                                            weight, to, reinterpret_cast<E*>(rest), rest ? nullptr : left, ldz);
                 };
                 if (dt == PSATTN_BF16) go(reinterpret_cast<uint16_t*>(dz));
                 else go(reinterpret_cast<float*>(dz));
@@ -610,7 +631,7 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
             using E = std::remove_pointer_t<decltype(to)>;
             auto kernel = many ? psattn_head_dx_parts<E> : psattn_head_dx<E>;
             kernel<<<grid, many ? 1024 : 256, 0, s>>>(at, col_blocks, hidden, n, again, parts, ld, sums, plan->row_desc, plan->resp_first, plan->resp_len, plan->resp_prev,
-                                                     plan->samp_ptr, plan->item_ptr, to);
+                                                     plan->samp_ptr, plan->item_ptr, target, again > n || dt != PSATTN_BF16 ? nullptr : left, static_cast<const E*>(W), to);
         };
         if (dt == PSATTN_BF16) go(static_cast<uint16_t*>(dX));
         else go(static_cast<float*>(dX));
