@@ -560,16 +560,19 @@ __device__ __forceinline__ void product_tile(char* lds, const Product& d, int ti
                     const float p = exp_of<E>(acc[nb][mb][i] - lse);
                     x[i] = weight == 0.f ? 0.f : weight * (t - n == 8 * (i >> 2) + (i & 3) ? 1.f - p : -p);
                 }
-                store_out<ASYNC>(static_cast<E*>(d.out[0]) + m * d.ldo + n, d.ldo, rows, cols, chunks(x), le, d.odd);
                 if constexpr (sizeof(E) == 2) {
                     if (d.parts && t - n >= 0 && t - n < 32 && ((t - n) & 4) == 0 && t - n + 4 * (le >> 5) < cols && (le & 31) < rows) {
                         float at_token = 0.f;
 #pragma unroll
                         for (int i = 0; i < 16; ++i)
-                            if (t - n == 8 * (i >> 2) + (i & 3)) at_token = x[i];
-                        d.parts[at] = at_token - __uint_as_float(mma::pack2(at_token, 0.f) << 16);
+                            if (t - n == 8 * (i >> 2) + (i & 3)) {
+                                at_token = x[i];
+                                x[i] = 0.f;
+                            }
+                        d.parts[at] = at_token;
                     }
                 }
+                store_out<ASYNC>(static_cast<E*>(d.out[0]) + m * d.ldo + n, d.ldo, rows, cols, chunks(x), le, d.odd);
                 if constexpr (sizeof(E) == 2 && S::BM == 32) {  // what the rounding leaves, as rows of their own
                     if (d.out[1]) {
 #pragma unroll

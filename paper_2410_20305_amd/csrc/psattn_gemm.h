@@ -47,7 +47,7 @@ struct Product {
     // k in n_split parts, whose sums go to `parts` in fp32 (rows of ld_part) and are joined by a kernel of their own
     int32_t n_split;
     int32_t add;              // kSums: parts hold sums already
-    float* parts;             // kDlogit: [M], what the rounding of bf16 leaves of dz at an item's token (may be null)
+    float* parts;             // kDlogit of bf16: [M], dz at the items' tokens, where out gets 0 then (may be null)
     int64_t ld_part;
 };
 

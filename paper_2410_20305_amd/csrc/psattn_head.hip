@@ -40,7 +40,7 @@ size_t elem_bytes(int32_t dt) { return dt == PSATTN_BF16 ? 2 : 4; }
 template <typename E, bool BWD>
 __global__ __launch_bounds__(256) void psattn_head_rows(int n_items, int again, const int32_t* item_row, const int32_t* item_tok, const int32_t* item_resp,
                                                         const int32_t* token_ids, int vocab, int hidden, const E* X, const float* row_lse, const float* d_logp, E* out,
-                                                        int32_t* target, float* lse, float* weight, float* left, E* dz, int64_t ldz) {
+                                                        int32_t* target, float* lse, float* weight, float* at_token, E* dz, int64_t ldz) {
     constexpr int V = rows::kVec<E>;
     const int64_t at = blockIdx.x, ld = (hidden + 7) / 8 * 8;
     if (BWD && at >= again) {
@@ -57,7 +57,7 @@ __global__ __launch_bounds__(256) void psattn_head_rows(int n_items, int again, 
         if constexpr (BWD) {
             lse[i] = known ? row_lse[row] : 0.f;
             weight[i] = known ? d_logp[item_resp[i]] : 0.f;
-            left[i] = 0.f;
+            at_token[i] = 0.f;
         }
     }
     const E* const x = X + static_cast<int64_t>(row) * hidden;
@@ -126,10 +126,10 @@ __global__ __launch_bounds__(1024) void psattn_head_parts_lse(int n_items, int n
     item_logp[i] = t >= 0 ? (hit - m) - ls : 0.f;
 }
 
-// dz of an item, and of bf16 what its rounding leaves where that is asked for: 1 024 columns to a workgroup
+// dz of an item, 1 024 columns to a workgroup.  bf16: what its rounding leaves, or its value at the item's token apart, where that is asked for
 template <typename E>
 __global__ __launch_bounds__(256) void psattn_head_parts_dz(int n_items, int n_parts, int first, int cols, int64_t ld, const float* parts, const int32_t* target, const float* lse,
-                                                            const float* weight, E* dz, E* rest, float* left, int64_t ldz) {
+                                                            const float* weight, E* dz, E* rest, float* at_token, int64_t ldz) {
     const int64_t i = blockIdx.y;
     const int c = (blockIdx.x * 256 + threadIdx.x) * 4, t = target[i] - first;
     if (c >= cols) return;
@@ -140,9 +140,10 @@ __global__ __launch_bounds__(256) void psattn_head_parts_dz(int n_items, int n_p
     for (int k = 0; k < 4; ++k) {
         if (c + k >= cols) break;
         const float p = expf(z[k] - l), x = w == 0.f ? 0.f : w * (c + k == t ? 1.f - p : -p);
-        rows::store1(dz + i * ldz + c + k, x);
+        const bool apart = at_token && c + k == t;
+        rows::store1(dz + i * ldz + c + k, apart ? 0.f : x);
         if (rest) rows::store1(rest + i * ldz + c + k, x - rows::hold(x, dz));
-        if (left && c + k == t) left[i] = x - rows::hold(x, dz);
+        if (apart) at_token[i] = x;
     }
 }
 
@@ -227,21 +228,96 @@ __global__ __launch_bounds__(256) void psattn_head_responses(int first, const in
     if (threadIdx.x == 0) resp_logp[j] = (sm[0] + sm[1]) + (sm[2] + sm[3]);
 }
 
-// what the rounding left of dz at an item's token: that token's row of W has all of its gradient's largest term in one number, whose rounding
-// error is that of every column alike (99 items: dX off by 2.5e-3 without, 1.7e-3 with it, the rounding of dX itself)
+// ---- bf16: dz at an item's own token.  It is most of its row's weight, and its rounding error would be that of all columns of dX and of the
+// token's row of dW alike: it stays in fp32, out of the products, and joins their results here.  (99 items, gradients against 64 bits: dX 2.4e-3
+// in the products, 1.66e-3 apart, which is its own rounding; dW 2.34e-3 and DD.)
 template <typename E>
-__device__ __forceinline__ void add_left(float left, const E* w, int c, int hidden, float (&x)[4]) {
-    if (left == 0.f) return;
+__device__ __forceinline__ void add_token(float at_token, const E* w, int c, int hidden, float (&x)[4]) {
+    if (at_token == 0.f) return;
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-        if (c + k < hidden) x[k] = fmaf(left, rows::to_f32(w[c + k]), x[k]);
+        if (c + k < hidden) x[k] = fmaf(at_token, rows::to_f32(w[c + k]), x[k]);
+}
+
+// dW[token] += sum of dz X over the items of that token, in their order: the first of them does it, 1 024 columns to a workgroup
+template <typename E>
+__global__ __launch_bounds__(256) void psattn_head_dw_tokens(int first, int col_blocks, int n_items, int hidden, int64_t ld, const int32_t* target, const float* at_token,
+                                                             const E* x, E* dW) {
+    constexpr int V = 4, kAtOnce = 4, kSpan = 1024;  // items looked at together: 4 to a thread
+    __shared__ int found[kSpan], count[4];
+    const int i = first + static_cast<int>(blockIdx.x) / col_blocks, token = target[i], mine = static_cast<int>(threadIdx.x) * 4, l = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (token < 0) return;
+    auto same = [&](int base, int from, int to) {  // which of the thread's four are in [from, to) and of that token
+        if (base + mine >= n_items) return 0u;
+        const int4 t = *reinterpret_cast<const int4*>(target + base + mine);  // the table's last four are its own: it is of whole 256 bytes
+        const int tok[4] = {t.x, t.y, t.z, t.w};
+        uint32_t yes = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) yes |= tok[k] == token && base + mine + k >= from && base + mine + k < to ? 1u << k : 0u;
+        return yes;
+    };
+    const int own = i / kSpan * kSpan;
+    for (int base = own; base >= 0; base -= kSpan)  // the nearest first: frequent tokens end here soon
+        if (__syncthreads_or(same(base, 0, i))) return;
+    const int c = (static_cast<int>(blockIdx.x) % col_blocks * 256 + static_cast<int>(threadIdx.x)) * V;
+    float sum[V] = {};
+    for (int base = own; base < n_items; base += kSpan) {
+        const uint32_t yes = same(base, i, n_items);
+        if (!__syncthreads_or(yes)) continue;
+        int at = 0, n = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint64_t votes = __builtin_amdgcn_ballot_w64(yes >> k & 1);
+            at += __builtin_popcountll(votes & ((uint64_t{1} << l) - 1));
+            n += __builtin_popcountll(votes);
+        }
+        if (l == 0) count[wave] = n;
+        __syncthreads();
+        n = 0;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            at += w < wave ? count[w] : 0;
+            n += count[w];
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (yes >> k & 1) found[at++] = base + mine + k;
+        __syncthreads();
+        if (c >= hidden) continue;
+        auto add = [&](int k, auto COUNT) {  // loads together, sums in order
+            constexpr int m = decltype(COUNT)::value;
+            uint2 u[m];
+            float w[m];
+#pragma unroll
+            for (int q = 0; q < m; ++q) {
+                const int64_t item = found[k + q];
+                u[q] = *reinterpret_cast<const uint2*>(x + item * ld + c);
+                w[q] = at_token[item];
+            }
+#pragma unroll
+            for (int q = 0; q < m; ++q) {
+                if (w[q] == 0.f) continue;
+                sum[0] = fmaf(w[q], __uint_as_float(u[q].x << 16), sum[0]);
+                sum[1] = fmaf(w[q], __uint_as_float(u[q].x & 0xffff0000u), sum[1]);
+                sum[2] = fmaf(w[q], __uint_as_float(u[q].y << 16), sum[2]);
+                sum[3] = fmaf(w[q], __uint_as_float(u[q].y & 0xffff0000u), sum[3]);
+            }
+        };
+        int k = 0;
+        for (; k + kAtOnce <= n; k += kAtOnce) add(k, std::integral_constant<int, kAtOnce>{});
+        for (; k < n; ++k) add(k, std::integral_constant<int, 1>{});
+    }
+    E* const to = dW + static_cast<int64_t>(token) * hidden + c;
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+        if (c + k < hidden) rows::store1(to + k, rows::to_f32(to[k]) + sum[k]);
 }
 
 // ---- dX of token t: the sums of its items, of all parts of each; `again` rows to a part
 template <typename E>
 __global__ __launch_bounds__(256) void psattn_head_dx(int64_t first, int col_blocks, int hidden, int n_items, int again, int n_parts, int64_t ld, const float* parts, const int32_t* row_desc,
                                                       const int32_t* resp_first, const int32_t* resp_len, const int32_t* resp_prev, const int32_t* samp_ptr,
-                                                      const int32_t* item_ptr, const int32_t* target, const float* left, const E* W, E* dX) {
+                                                      const int32_t* item_ptr, const int32_t* target, const float* at_token, const E* W, E* dX) {
     constexpr int V = 4;
     const int64_t block = first + blockIdx.x;
     const int row = static_cast<int>(block / col_blocks), desc = row_desc[row];
@@ -270,7 +346,7 @@ __global__ __launch_bounds__(256) void psattn_head_dx(int64_t first, int col_blo
                 for (; p + 8 <= n_parts; p += 8) add(std::integral_constant<int, 8>{});
                 for (; p < n_parts; ++p) add(std::integral_constant<int, 1>{});
             }
-            if (left) add_left(left[i], W + static_cast<int64_t>(target[i]) * hidden, c, hidden, x);
+            if (at_token) add_token(at_token[i], W + static_cast<int64_t>(target[i]) * hidden, c, hidden, x);
         }
 #pragma unroll
         for (int k = 0; k < V; ++k)
@@ -282,7 +358,7 @@ __global__ __launch_bounds__(256) void psattn_head_dx(int64_t first, int col_blo
 template <typename E>
 __global__ __launch_bounds__(1024) void psattn_head_dx_parts(int64_t first, int col_blocks, int hidden, int n_items, int again, int n_parts, int64_t ld, const float* parts,
                                                              const int32_t* row_desc, const int32_t* resp_first, const int32_t* resp_len, const int32_t* resp_prev,
-                                                             const int32_t* samp_ptr, const int32_t* item_ptr, const int32_t* target, const float* left, const E* W, E* dX) {
+                                                             const int32_t* samp_ptr, const int32_t* item_ptr, const int32_t* target, const float* at_token, const E* W, E* dX) {
     constexpr int V = 4, kAtOnce = 4;
     __shared__ float4 sm[16][64];
     const int64_t block = first + blockIdx.x;
@@ -310,9 +386,9 @@ __global__ __launch_bounds__(1024) void psattn_head_dx_parts(int64_t first, int 
                 }
                 for (; p < n_parts; p += 16) add(*reinterpret_cast<const float4*>(from + p * step));
             }
-            if (left && w == 0) {
+            if (at_token && w == 0) {
                 float y[V] = {x.x, x.y, x.z, x.w};
-                add_left(left[i], W + static_cast<int64_t>(target[i]) * hidden, c, hidden, y);
+                add_token(at_token[i], W + static_cast<int64_t>(target[i]) * hidden, c, hidden, y);
                 x = make_float4(y[0], y[1], y[2], y[3]);
             }
         }
@@ -409,7 +485,7 @@ int64_t piece_rows(int32_t dt, int64_t n_items, int64_t vocab) {
     return cdiv(cdiv(vocab, n), 256) * 256;
 }
 // Few items of bf16: dz as two numbers each, the second what the first one's rounding leaves, as items of their own.  The gradients are as
-// exact as their own rounding then; of more items a token's row of dW is off by 2^-9 of itself at most besides
+// exact as their own rounding then.  Of more items dz at their tokens alone is kept exact (psattn_head_dw_tokens)
 constexpr int64_t kTwice = 32;
 int64_t dz_rows(int32_t dt, int64_t n_items) { return dt == PSATTN_BF16 && n_items <= kTwice ? 2 * n_items : n_items; }
 constexpr int kManyParts = 16;
@@ -554,24 +630,27 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
     const int parts = static_cast<int>(dx.split);
     const int64_t ld = up8(hidden), piece = piece_rows(dt, n, vocab), ldz = up8(piece);
     const int again = static_cast<int>(dz_rows(dt, n)), n_whole = static_cast<int>(up64(again));
-    float *sums = nullptr, *left = nullptr;
+    const bool apart = dt == PSATTN_BF16 && again == n;  // dz at the items' tokens
+    float *sums = nullptr, *at_token = nullptr;
     const int32_t* target = nullptr;
+    const uint16_t* x_rows = nullptr;
     if (n == 0) {  // nothing is predicted: sums over nothing
         psattn_head_zero<<<1024, 256, 0, s>>>(static_cast<uint16_t*>(dW), static_cast<size_t>(vocab) * hidden * e / 2);
     } else {
         char* const x = room.take<char>(static_cast<size_t>(n_whole) * ld * e);
+        x_rows = reinterpret_cast<const uint16_t*>(x);
         char* const dz = room.take<char>(static_cast<size_t>(n_whole) * ldz * e);
         sums = room.take<float>(static_cast<size_t>(again) * ld * parts);
         float* const z_parts = reinterpret_cast<float*>(room.take<char>(logits_bytes(dt, n, vocab, piece, hidden)));
         char* const rest = again > n ? dz + n * ldz * e : nullptr;
         int32_t* const targets = room.take<int32_t>(n);
         float *const lse = room.take<float>(n), *const weight = room.take<float>(n);
-        left = room.take<float>(n);
+        at_token = room.take<float>(n);
         target = targets;
         auto gather = [&](auto* to) {
             using E = std::remove_pointer_t<decltype(to)>;
             psattn_head_rows<E, true><<<n_whole, 256, 0, s>>>(n, again, plan->item_row, plan->item_tok, plan->item_resp, token_ids, vocab, hidden, static_cast<const E*>(X),
-                                                              row_lse, d_resp_logp, to, targets, lse, weight, left, reinterpret_cast<E*>(dz), ldz);
+                                                              row_lse, d_resp_logp, to, targets, lse, weight, at_token, reinterpret_cast<E*>(dz), ldz);
         };
         if (dt == PSATTN_BF16) gather(reinterpret_cast<uint16_t*>(x));
         else gather(reinterpret_cast<float*>(x));
@@ -580,7 +659,7 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
             const char* const w = static_cast<const char*>(W) + at * hidden * e;
             int rc;
             Product z{};  // dz
-            z.p[0] = x; z.q[0] = w; z.G = lse; z.U = weight; z.H = targets; z.out[0] = dz; z.out[1] = rest; z.parts = rest ? nullptr : left;
+            z.p[0] = x; z.q[0] = w; z.G = lse; z.U = weight; z.H = targets; z.out[0] = dz; z.out[1] = rest; z.parts = apart ? at_token : nullptr;
             z.ldp = ld; z.ldq = hidden; z.ldo = ldz;
             z.M = n; z.N = cols; z.K = hidden; z.n_seg = z.n_prod = z.n_split = 1;
             z.n_load = static_cast<int32_t>(at);
@@ -591,7 +670,7 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
                 auto go = [&](auto* to) {
                     using E = std::remove_pointer_t<decltype(to)>;
                     psattn_head_parts_dz<E><<<dim3(static_cast<uint32_t>(cdiv(cols, 1024)), n), 256, 0, s>>>(n, z.n_split, static_cast<int>(at), cols, z.ld_part, z_parts, targets, lse,
-                                                                                                            weight, to, reinterpret_cast<E*>(rest), rest ? nullptr : left, ldz);
+                                                                                                            weight, to, reinterpret_cast<E*>(rest), apart ? at_token : nullptr, ldz);
                 };
                 if (dt == PSATTN_BF16) go(reinterpret_cast<uint16_t*>(dz));
                 else go(reinterpret_cast<float*>(dz));
@@ -623,6 +702,13 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
             if (rc != PSATTN_OK) return rc;
         }
     }
+    if (apart && n > 0) {
+        const int blocks = static_cast<int>(cdiv(hidden, 1024));
+        const int64_t most = ((int64_t{1} << 31) - 1) / 256 / blocks;
+        for (int64_t at = 0; at < n; at += most)
+            psattn_head_dw_tokens<uint16_t><<<static_cast<uint32_t>(std::min<int64_t>(most, n - at) * blocks), 256, 0, s>>>(static_cast<int>(at), blocks, n, hidden, ld, target, at_token,
+                                                                                                                          x_rows, static_cast<uint16_t*>(dW));
+    }
     // a row to a workgroup; where they are few, 1 024 columns of one, or with many parts 256
     const bool many = n <= 64 && parts * (again / std::max(n, 1)) >= kManyParts && plan->T < 4096;
     const int col_blocks = many ? static_cast<int>(cdiv(hidden, 256)) : plan->T < 4096 ? static_cast<int>(cdiv(hidden, 1024)) : 1;
@@ -631,7 +717,7 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
             using E = std::remove_pointer_t<decltype(to)>;
             auto kernel = many ? psattn_head_dx_parts<E> : psattn_head_dx<E>;
             kernel<<<grid, many ? 1024 : 256, 0, s>>>(at, col_blocks, hidden, n, again, parts, ld, sums, plan->row_desc, plan->resp_first, plan->resp_len, plan->resp_prev,
-                                                     plan->samp_ptr, plan->item_ptr, target, again > n || dt != PSATTN_BF16 ? nullptr : left, static_cast<const E*>(W), to);
+                                                     plan->samp_ptr, plan->item_ptr, target, apart ? at_token : nullptr, static_cast<const E*>(W), to);
         };
         if (dt == PSATTN_BF16) go(static_cast<uint16_t*>(dX));
         else go(static_cast<float*>(dX));
