@@ -23,10 +23,14 @@ TABLES = {
     "packed": ([0, 300], [100, 20], [0, 2, 4], [60, 70, 40, 90], 460),
     "long": ([0], [5], [0, 2], [300, 420], 740),
 }
+MORE = {
+    "halfway": ([3 * i for i in range(40)], [1] * 40, list(range(41)), [1] * 40, 120),
+    "again": ([0], [1], [0, 2], [1300, 1300], 2604),
+}
 
 
 def _inputs(table, V, h, dtype, seed=0, lean=4.0):
-    off, P, ptr, rl, T = TABLES[table]
+    off, P, ptr, rl, T = {**TABLES, **MORE}[table]
     rng = np.random.default_rng(V * 31 + h + seed)
     W = rnd(rng, V, h, scale=1.3 * h ** -0.5, dtype=dtype)
     ids = rng.integers(0, V, T)
@@ -40,7 +44,7 @@ def _inputs(table, V, h, dtype, seed=0, lean=4.0):
 
 
 def _call(table, X, W, ids, d, dtype, shift=0):
-    off, P, ptr, rl, T = TABLES[table]
+    off, P, ptr, rl, T = {**TABLES, **MORE}[table]
     plan = ps.LogprobPlan(off, P, ptr, rl, T)
     dev = Guarded(dtype, shift)
     tX, tW = dev.put(X), dev.put(W)
@@ -264,3 +268,49 @@ def test_few_items_have_gradients_as_exact_as_their_rounding():
     rel = 2 * ez + 2.0 ** -17 + 8 * EPS32
     close(dW, rW, (HALF["bf16"] + rel) * np.abs(rW) + 2 * EPS32 * np.abs(rW) + abs(d[0]) * ez * np.abs(X[r]) + TINY, "dW")
     close(dX, rX, HALF["bf16"] * np.abs(rX) + (rel + 500 * EPS32) * (np.abs(G) @ np.abs(W)) + TINY, "dX")
+
+
+@pytest.mark.parametrize("same", [False, True])
+@pytest.mark.parametrize("V,h", [(1500, 512), (700, 1023)])
+def test_dz_at_the_token_is_not_rounded(V, h, same):
+    """More than 32 items of bf16, whose dz at their tokens lie half way between two numbers of the type: rounded, they would put the
+    gradients off by 2^-8 at once.  They are off by their own rounding, e0 of the exact gradient (which moves by no more than its
+    argument does: twice that in all), by what rounds dz elsewhere, of which sum_c a_c W_c has at most |a| sigma(W), and at a token's row
+    by the rounding of the products' part of it."""
+    n, half = 40, HALF["bf16"]
+    rng = np.random.default_rng(V + h)
+    W = rnd(rng, V, h, scale=h ** -0.5, dtype="bf16")
+    ids = np.full(3 * n, 17) if same else np.resize(rng.permutation(V), 3 * n)
+    X = rnd(rng, 3 * n, h, dtype="bf16") * (rng.permuted(np.arange(3 * n * h).reshape(3 * n, h) % h, axis=1) < 16)  # 16 terms to a logit
+    items = orc.prediction_items(*MORE["halfway"][:4])
+    assert len(items) == n
+    ref, _ = blk.head(X, W, ids, items)
+    rows, tok = np.array([r for _, r, _ in items]), np.array([ids[t] for _, _, t in items])
+    P = np.exp(X @ W.T - ref[:, None])
+    d = (1 + 2.0 ** -8) / (1 - P[rows, tok])
+    d = torch.from_numpy(d).float().double().numpy()
+    rX, rW, G = blk.head_grad(X, W, ids, items, d)
+    _, _, dX, dW = _call("halfway", X, W, ids, d, "bf16")
+    G, x = G[rows], X[rows]
+    off = G.copy()
+    off[np.arange(n), tok] = 0
+    norm = np.linalg.norm
+    bf = lambda a: torch.from_numpy(a).bfloat16().double().numpy()
+    ez = (16 + 2) * EPS32 * (np.abs(x) @ np.abs(W.T))
+    e32 = np.abs(G) * (2 * ez.max() + EPS32 * (V / 64 + 140))
+    at_row = np.zeros_like(rW)
+    at_row[tok] = (off.T @ x)[tok]
+    for got, want, move, lost in (
+            (dX, rX, half * norm(off) * norm(W, 2) + norm(e32 @ np.abs(W) + (V + 70) * EPS32 * np.abs(G) @ np.abs(W)), norm(W[tok])),
+            (dW, rW, half * norm(off) * norm(x, 2) + half * norm(at_row) + norm(e32.T @ np.abs(x) + (n + 4) * EPS32 * np.abs(G).T @ np.abs(x)),
+             norm(x.sum(0)) if same else norm(x))):
+        bound = norm(bf(want) - want) + 2 * move
+        assert bound < (norm(bf(want) - want) ** 2 + (0.99 * half * lost) ** 2) ** 0.5, "the bound tells the two apart"
+        assert norm(np64(got) - want) <= bound
+
+
+@pytest.mark.parametrize("V,h", [(5, 64), (400, 130), (20000, 64)])
+def test_tokens_that_come_again(V, h):
+    """Rows of dW that sum over items of several thousands, next to others of a single one"""
+    a = _inputs("again", V, h, "bf16")
+    _check(*a, _call("again", *a[:3], a[4], "bf16"), "bf16")
