@@ -230,7 +230,7 @@ __global__ __launch_bounds__(256) void psattn_head_responses(int first, const in
 
 // ---- bf16: dz at an item's own token.  It is most of its row's weight, and its rounding error would be that of all columns of dX and of the
 // token's row of dW alike: it stays in fp32, out of the products, and joins their results here.  (99 items, gradients against 64 bits: dX 2.4e-3
-// in the products, 1.66e-3 apart, which is its own rounding; dW 2.34e-3 and DD.)
+// in the products, 1.66e-3 apart, which is its own rounding; dW 2.34e-3 and 1.66e-3.)
 template <typename E>
 __device__ __forceinline__ void add_token(float at_token, const E* w, int c, int hidden, float (&x)[4]) {
     if (at_token == 0.f) return;
@@ -239,12 +239,15 @@ __device__ __forceinline__ void add_token(float at_token, const E* w, int c, int
         if (c + k < hidden) x[k] = fmaf(at_token, rows::to_f32(w[c + k]), x[k]);
 }
 
-// dW[token] += sum of dz X over the items of that token, in their order: the first of them does it, 1 024 columns to a workgroup
-template <typename E>
-__global__ __launch_bounds__(256) void psattn_head_dw_tokens(int first, int col_blocks, int n_items, int hidden, int64_t ld, const int32_t* target, const float* at_token,
-                                                             const E* x, E* dW) {
-    constexpr int V = 4, kAtOnce = 4, kSpan = 1024;  // items looked at together: 4 to a thread
+// dW[token] += sum of dz X over the items of that token: the first of them does it, `lanes` * 4 columns to a workgroup, whose 256 / lanes groups
+// take items in turn.  It looks for the others among all items, n V / 1 024 steps at most beside the products' n V hidden: 152 of 33 600 us
+// for 9 727 items of 128 000 x 4 096.  Items of a single token are the worst: 8 000 of 32 000 x 4 096 take 6.4 ms for 5.3.  The row is rounded a
+// second time, from the first one's sum without the token's own part.
+__global__ __launch_bounds__(256) void psattn_head_dw_tokens(int first, int lanes, int col_blocks, int n_items, int hidden, int64_t ld, const int32_t* target, const float* at_token,
+                                                             const uint16_t* x, uint16_t* dW) {
+    constexpr int V = 4, kAtOnce = 8, kSpan = 1024;  // items looked at together: 4 to a thread
     __shared__ int found[kSpan], count[4];
+    __shared__ float4 sums[256];
     const int i = first + static_cast<int>(blockIdx.x) / col_blocks, token = target[i], mine = static_cast<int>(threadIdx.x) * 4, l = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (token < 0) return;
     auto same = [&](int base, int from, int to) {  // which of the thread's four are in [from, to) and of that token
@@ -259,7 +262,8 @@ __global__ __launch_bounds__(256) void psattn_head_dw_tokens(int first, int col_
     const int own = i / kSpan * kSpan;
     for (int base = own; base >= 0; base -= kSpan)  // the nearest first: frequent tokens end here soon
         if (__syncthreads_or(same(base, 0, i))) return;
-    const int c = (static_cast<int>(blockIdx.x) % col_blocks * 256 + static_cast<int>(threadIdx.x)) * V;
+    const int lane = static_cast<int>(threadIdx.x) & (lanes - 1), group = static_cast<int>(threadIdx.x) / lanes, groups = 256 / lanes;
+    const int c = (static_cast<int>(blockIdx.x) % col_blocks * lanes + lane) * V;
     float sum[V] = {};
     for (int base = own; base < n_items; base += kSpan) {
         const uint32_t yes = same(base, i, n_items);
@@ -290,7 +294,7 @@ __global__ __launch_bounds__(256) void psattn_head_dw_tokens(int first, int col_
             float w[m];
 #pragma unroll
             for (int q = 0; q < m; ++q) {
-                const int64_t item = found[k + q];
+                const int64_t item = found[k + q * groups];
                 u[q] = *reinterpret_cast<const uint2*>(x + item * ld + c);
                 w[q] = at_token[item];
             }
@@ -303,11 +307,20 @@ __global__ __launch_bounds__(256) void psattn_head_dw_tokens(int first, int col_
                 sum[3] = fmaf(w[q], __uint_as_float(u[q].y & 0xffff0000u), sum[3]);
             }
         };
-        int k = 0;
-        for (; k + kAtOnce <= n; k += kAtOnce) add(k, std::integral_constant<int, kAtOnce>{});
-        for (; k < n; ++k) add(k, std::integral_constant<int, 1>{});
+        int k = group;
+        for (; k + (kAtOnce - 1) * groups < n; k += kAtOnce * groups) add(k, std::integral_constant<int, kAtOnce>{});
+        for (; k < n; k += groups) add(k, std::integral_constant<int, 1>{});
     }
-    E* const to = dW + static_cast<int64_t>(token) * hidden + c;
+    if (groups > 1) {
+        sums[threadIdx.x] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+        __syncthreads();
+        if (group) return;
+        for (int g = 1; g < groups; ++g) {
+            const float4 x = sums[g * lanes + lane];
+            sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
+        }
+    }
+    uint16_t* const to = dW + static_cast<int64_t>(token) * hidden + c;
 #pragma unroll
     for (int k = 0; k < V; ++k)
         if (c + k < hidden) rows::store1(to + k, rows::to_f32(to[k]) + sum[k]);
@@ -703,10 +716,12 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
         }
     }
     if (apart && n > 0) {
-        const int blocks = static_cast<int>(cdiv(hidden, 1024));
+        int lanes = 4;
+        while (lanes < 256 && lanes * 4 < hidden) lanes *= 2;
+        const int blocks = static_cast<int>(cdiv(hidden, lanes * 4));
         const int64_t most = ((int64_t{1} << 31) - 1) / 256 / blocks;
         for (int64_t at = 0; at < n; at += most)
-            psattn_head_dw_tokens<uint16_t><<<static_cast<uint32_t>(std::min<int64_t>(most, n - at) * blocks), 256, 0, s>>>(static_cast<int>(at), blocks, n, hidden, ld, target, at_token,
+            psattn_head_dw_tokens<<<static_cast<uint32_t>(std::min<int64_t>(most, n - at) * blocks), 256, 0, s>>>(static_cast<int>(at), lanes, blocks, n, hidden, ld, target, at_token,
                                                                                                                           x_rows, static_cast<uint16_t*>(dW));
     }
     // a row to a workgroup; where they are few, 1 024 columns of one, or with many parts 256
