@@ -240,8 +240,8 @@ __device__ __forceinline__ void add_token(float at_token, const E* w, int c, int
 }
 
 // dW[token] += sum of dz X over the items of that token: the first of them does it, `lanes` * 4 columns to a workgroup, whose 256 / lanes groups
-// take items in turn.  It looks for the others among all items, n V / 1 024 steps at most beside the products' n V hidden: 152 of 33 600 us
-// for 9 727 items of 128 000 x 4 096.  Items of a single token are the worst: 8 000 of 32 000 x 4 096 take 6.4 ms for 5.3.  The row is rounded a
+// take items in turn.  It looks for the others among all items, n V / 1 024 steps at most beside the products' n V hidden: 160 of 34 400 us
+// for 9 812 items of 128 000 x 4 096.  Items of a single token are the worst: 8 000 of 32 000 x 4 096 take 6.4 ms for 5.3.  The row is rounded a
 // second time, from the first one's sum without the token's own part.
 __global__ __launch_bounds__(256) void psattn_head_dw_tokens(int first, int lanes, int col_blocks, int n_items, int hidden, int64_t ld, const int32_t* target, const float* at_token,
                                                              const uint16_t* x, uint16_t* dW) {
