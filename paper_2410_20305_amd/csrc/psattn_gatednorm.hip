@@ -38,14 +38,44 @@ struct Args {
     float *part, *row_m;
 };
 
+// Groups p of a row whose lanes take PER each: the first PER / 2 of them lie inside of it (`sized`), but for what lane 0 has before its start,
+// so that only the first and those of the second half have an edge, on one side
+template <bool WHOLE, int PER>
+__device__ __forceinline__ u32x4 settled_at(const u32x4& x, int p, int down) {
+    if (WHOLE || (PER > 1 && p > 0 && p < PER / 2)) return x;
+    if (PER == 1) return settled<WHOLE>(x, down);
+    return settled<WHOLE>(x, p == 0 ? min(down, 0) : max(down, 0));
+}
+template <bool WHOLE, int PER, typename E>
+__device__ __forceinline__ void store_at(E* row, int p, int c, int hidden, const float (&x)[kVec<E>]) {
+    if constexpr (WHOLE || PER == 1) {
+        store<WHOLE>(row, c, hidden, x);
+    } else if (p > 0 && p < PER / 2) {
+        reinterpret_cast<Raw*>(row + c)->u = pack<E>(x);
+    } else if (p == 0 ? c >= 0 : c + kVec<E> <= hidden) {
+        reinterpret_cast<Raw*>(row + c)->u = pack<E>(x);
+    } else {
+#pragma unroll
+        for (int j = 0; j < kVec<E>; ++j)
+            if (p == 0 ? c + j >= 0 : c + j < hidden) store1(row + c + j, x[j]);
+    }
+}
+
+// whether the lanes reach over a row that starts anywhere behind a 16-byte boundary: its groups are taken on such boundaries then.  Where they
+// do not quite, groups off a boundary cost less than twice the lanes (20 000 rows of 4 095 bf16, forward and backward: 512 lanes 677 us, 256 389)
+template <typename E>
+__device__ __forceinline__ bool shifts(int hidden, int lanes, int per) {
+    return hidden + kVec<E> - 1 <= lanes * per * kVec<E>;
+}
+
 template <typename E, int LANES, int PER, bool WHOLE>
-__global__ __launch_bounds__(kThreads<LANES>) void psattn_gn_fwd(Args<E> a) {
+__global__ __launch_bounds__(kThreads<LANES>, LANES * PER == 2048 ? 8 : 1) void psattn_gn_fwd(Args<E> a) {
     constexpr int V = kVec<E>, kAt = kThreads<LANES> / LANES;
     __shared__ float sm[2][16];
     const int row = blockIdx.x * kAt + threadIdx.x / LANES, lane = threadIdx.x % LANES, hidden = a.hidden;
     if (row >= a.n_rows) return;
     const size_t at = static_cast<size_t>(row) * hidden;
-    const int from = lane * V - (WHOLE ? 0 : misalignment(a.X + at));  // this lane's first column
+    const int from = lane * V - (WHOLE || !shifts<E>(hidden, LANES, PER) ? 0 : misalignment(a.X + at));  // this lane's first column
     u32x4 xr[PER], br[PER], gr[PER], wr[PER];
     Place pl[PER];
     const E* const gate = a.gate ? a.gate + static_cast<size_t>(row) * a.gate_step : nullptr;
@@ -147,18 +177,18 @@ __global__ __launch_bounds__(kThreads<LANES>) void psattn_gn_bwd(Args<E> a) {
             for (int j = 0; j < V; ++j) sums[which][p][j] += x[j];
         }
     };
-    constexpr bool kAhead = PER <= 2 && (WHOLE || !ALL || PER * V < 16 || LANES < 512);  // the next row's loads, where there are registers for them
+    constexpr bool kAhead = PER <= 2 && (WHOLE || !ALL || PER * V < 16);  // the next row's loads, where there are registers for them
     const int step = gridDim.x * kAt;
     int row = blockIdx.x * kAt + own;
     // this lane's first column: the same for all its rows, whose misalignment has to be
-    const int from = lane * V - (WHOLE || (step % V != 0 && hidden % V != 0) || row >= n_rows ? 0 : misalignment(a.S + static_cast<size_t>(row) * hidden));
+    const int from = lane * V - (WHOLE || !shifts<E>(hidden, LANES, PER) || (step % V != 0 && hidden % V != 0) || row >= n_rows ? 0 : misalignment(a.S + static_cast<size_t>(row) * hidden));
     // The weights' groups stay in registers, and with one factor for all rows so does its product of w_post and gate, in fp32.  Of rows of four
     // groups to a lane they are asked for again each time
     constexpr bool kKeep = PER <= 2;
     Place pl[PER];
     u32x4 w_pre[kKeep ? PER : 1], w_post[kKeep ? PER : 1];
     float both[kKeep && !ALL ? PER : 1][V];
-    auto weight = [&](const E* w, int p) { return settled<WHOLE>(raw<WHOLE>(w, pl[p], hidden), pl[p].down); };
+    auto weight = [&](const E* w, int p) { return settled_at<WHOLE, PER>(raw<WHOLE>(w, pl[p], hidden), p, pl[p].down); };
     auto post = [&](int p) {
         float one[V];
 #pragma unroll
@@ -208,11 +238,11 @@ __global__ __launch_bounds__(kThreads<LANES>) void psattn_gn_bwd(Args<E> a) {
         // a lane's values of one group; outside of the row s, b, dy and t are zeros
         float s[V], b[V], dy[V], t[V], g[V], f[V];
         auto unpacked = [&](int p, float (&q)[V]) {
-            unpack(settled<WHOLE>(now.s[p], pl[p].down), s);
-            unpack(settled<WHOLE>(now.b[p], pl[p].down), b);
-            unpack(settled<WHOLE>(now.dy[p], pl[p].down), dy);
-            unpack(settled<WHOLE>(now.ds[p], pl[p].down), t);
-            if constexpr (ALL) unpack(settled<WHOLE>(now.g[p], pl[p].down), g);
+            unpack(now.s[p], s);
+            unpack(now.b[p], b);
+            unpack(now.dy[p], dy);
+            unpack(now.ds[p], t);
+            if constexpr (ALL) unpack(now.g[p], g);
             if constexpr (kKeep) {
                 unpack(w_pre[p], q);
                 if constexpr (ALL) unpack(w_post[p], f);
@@ -234,6 +264,14 @@ __global__ __launch_bounds__(kThreads<LANES>) void psattn_gn_bwd(Args<E> a) {
 #pragma unroll
         for (int p = 0; p < PER; ++p) {
             float q[V], dw[V];
+            if constexpr (!WHOLE) {
+                const int down = pl[p].down;
+                now.s[p] = settled_at<WHOLE, PER>(now.s[p], p, down);
+                now.b[p] = settled_at<WHOLE, PER>(now.b[p], p, down);
+                now.dy[p] = settled_at<WHOLE, PER>(now.dy[p], p, down);
+                now.ds[p] = settled_at<WHOLE, PER>(now.ds[p], p, down);
+                if constexpr (ALL) now.g[p] = settled_at<WHOLE, PER>(now.g[p], p, down);
+            }
             unpacked(p, q);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
@@ -268,7 +306,7 @@ __global__ __launch_bounds__(kThreads<LANES>) void psattn_gn_bwd(Args<E> a) {
                 t[j] = fmaf(-m, s[j], t[j]);
                 o[j] = res * t[j];
             }
-            store<WHOLE>(a.dX + at, c, hidden, o);
+            store_at<WHOLE, PER>(a.dX + at, p, c, hidden, o);
             if (a.B) {
                 float dc[V];
 #pragma unroll
@@ -279,8 +317,8 @@ __global__ __launch_bounds__(kThreads<LANES>) void psattn_gn_bwd(Args<E> a) {
                     if constexpr (ALL) t[j] = f[j] * tb;
                 }
                 collect(1, p, dc);
-                store<WHOLE>(a.dB + at, c, hidden, o);
-                if constexpr (ALL) store<WHOLE>(a.dgate + at, c, hidden, t);
+                store_at<WHOLE, PER>(a.dB + at, p, c, hidden, o);
+                if constexpr (ALL) store_at<WHOLE, PER>(a.dgate + at, p, c, hidden, t);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -436,50 +474,90 @@ __device__ __forceinline__ void group_at(const Args<E>& a, int row, float rs, fl
     }
 }
 
-template <typename E>
+// Rows that are read twice, the second time from the caches: a row to a workgroup of 1 024.  COLUMNS: rows from blockIdx.x on, gridDim.x apart, of 16 384 columns at most, whose sums stand in LDS, each
+// lane's own, and go to part[workgroup] at the end.  Else psattn_gn_columns makes them in a pass over
+// the rows of its own (20 000 rows of 10 001 bf16 with a gate for each 1 673 us, 1 266 by LDS; 10 000 of 10 000 fp32 1 129, 759)
+constexpr int kColumns = 16384;
+template <typename E, bool COLUMNS>
 __global__ __launch_bounds__(1024) void psattn_gn_bwd_wide(Args<E> a) {
     constexpr int V = kVec<E>, kStep = 1024 * V;
-    __shared__ float sm[48];
-    const int row = blockIdx.x, hidden = a.hidden;
-    const size_t at = static_cast<size_t>(row) * hidden;
-    const float rs = a.rstd_s[row], rb = a.w_post ? a.rstd_b[row] : 1.f;
-    float sum[3] = {0.f, 0.f, 0.f};
+    __shared__ float sm[2][48];
+    __shared__ float4 columns[COLUMNS ? 2 * kColumns / 4 : 1];  // [dw_pre, C][group][four of V][lane]
+    const int hidden = a.hidden, step = gridDim.x;
+    const bool shift = COLUMNS && hidden + V - 1 <= kColumns && (step % V == 0 || hidden % V == 0);  // all rows of this workgroup start alike
+    const int from = static_cast<int>(threadIdx.x) * V - (shift ? misalignment(a.S + static_cast<size_t>(blockIdx.x) * hidden) : 0);
+    auto slot = [&](int which, int c, int q) -> float4& { return columns[((which * (kColumns / kStep) + (c - from) / kStep) * (V / 4) + q) * 1024 + threadIdx.x]; };
+    if constexpr (COLUMNS) {
+#pragma unroll
+        for (int i = 0; i < 2 * kColumns / 4096; ++i) columns[i * 1024 + threadIdx.x] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    auto collect = [&](int which, int c, const float (&x)[V]) {
+#pragma unroll
+        for (int q = 0; q < V / 4; ++q) {
+            float4& to = slot(which, c, q);
+            float4 s = to;
+            s.x += x[4 * q], s.y += x[4 * q + 1], s.z += x[4 * q + 2], s.w += x[4 * q + 3];
+            to = s;
+        }
+    };
     Group<V> x;
-    float q[V];
-    for (int c = threadIdx.x * V; c < hidden; c += kStep) {
-        group_at(a, row, rs, rb, c, x, q);
+    float q[V], o[V];
+    int turn = 0;
+    for (int row = blockIdx.x; row < a.n_rows; row += step, turn ^= 1) {
+        const size_t at = static_cast<size_t>(row) * hidden;
+        const float rs = a.rstd_s[row], rb = a.w_post ? a.rstd_b[row] : 1.f;
+        float sum[3] = {0.f, 0.f, 0.f};
+#pragma unroll 1
+        for (int c = from; c < hidden; c += kStep) {
+            group_at(a, row, rs, rb, c, x, q);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const float gwb = x.g[j] * x.wp[j] * x.b[j];
-            sum[0] += q[j] * x.s[j];
-            sum[1] += x.t[j] * gwb;
-            sum[2] += x.s[j] * gwb;
+            for (int j = 0; j < V; ++j) {
+                const float gwb = x.g[j] * x.wp[j] * x.b[j];
+                sum[0] += q[j] * x.s[j];
+                sum[1] += x.t[j] * gwb;
+                sum[2] += x.s[j] * gwb;
+                o[j] = x.dy[j] * x.s[j];
+            }
+            if constexpr (COLUMNS) collect(0, c, o);
         }
+        group_sum<1024>(sum, sm[turn]);
+        const float m = rs * (sum[0] / hidden), mb = (sum[1] - m * sum[2]) / hidden;
+#pragma unroll 1
+        for (int c = from; c < hidden; c += kStep) {
+            group_at(a, row, rs, rb, c, x, q);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                x.t[j] = fmaf(-m, x.s[j], x.t[j]);
+                o[j] = a.B ? a.res * x.t[j] : x.t[j];
+            }
+            store<false>(a.dX + at, c, hidden, o);
+            if (!a.B) continue;
+            if constexpr (COLUMNS) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) o[j] = (a.gate_step ? x.g[j] : 1.f) * (x.t[j] * x.b[j]);
+                collect(1, c, o);
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float d = x.t[j] * (x.g[j] * x.wp[j]);
+                o[j] = a.w_post ? rb * (d - x.b[j] * mb) : d;
+            }
+            store<false>(a.dB + at, c, hidden, o);
+            if (!a.dgate) continue;
+#pragma unroll
+            for (int j = 0; j < V; ++j) o[j] = x.wp[j] * (x.t[j] * x.b[j]);
+            store<false>(a.dgate + at, c, hidden, o);
+        }
+        if (!COLUMNS && threadIdx.x == 0) a.row_m[row] = m;
     }
-    group_sum<1024>(sum, sm);
-    const float m = rs * (sum[0] / hidden), mb = (sum[1] - m * sum[2]) / hidden;
-    for (int c = threadIdx.x * V; c < hidden; c += kStep) {
-        float o[V];
-        group_at(a, row, rs, rb, c, x, q);
+    if constexpr (COLUMNS) {
+        float* const mine = a.part + 2 * static_cast<size_t>(blockIdx.x) * hidden;
+        for (int c = from; c < hidden; c += kStep)
+            for (int which = 0; which < (a.B ? 2 : 1); ++which)
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            x.t[j] = fmaf(-m, x.s[j], x.t[j]);
-            o[j] = a.B ? a.res * x.t[j] : x.t[j];
-        }
-        store<false>(a.dX + at, c, hidden, o);
-        if (!a.B) continue;
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const float d = x.t[j] * (x.g[j] * x.wp[j]);
-            o[j] = a.w_post ? rb * (d - x.b[j] * mb) : d;
-        }
-        store<false>(a.dB + at, c, hidden, o);
-        if (!a.dgate) continue;
-#pragma unroll
-        for (int j = 0; j < V; ++j) o[j] = x.wp[j] * (x.t[j] * x.b[j]);
-        store<false>(a.dgate + at, c, hidden, o);
+                for (int j = 0; j < V; ++j)
+                    if (c + j >= 0 && c + j < hidden) mine[which * hidden + c + j] = reinterpret_cast<const float*>(&slot(which, c, j / 4))[j % 4];
     }
-    if (threadIdx.x == 0) a.row_m[row] = m;
 }
 
 // part[y]: sums of kVec columns to a lane over rows y, y + gridDim.y, ...
@@ -517,7 +595,7 @@ template <typename E, bool BWD, typename F>
 bool sized(int hidden, bool all, F&& f) {
     using std::integral_constant;
     auto go = [&](auto lanes, auto per) { return f(lanes, per), true; };
-    const int64_t g = (static_cast<int64_t>(hidden) + kVec<E> - 1) / kVec<E> + (all ? 0 : 1);  // rows that start off a boundary reach into one more
+    const int64_t g = (static_cast<int64_t>(hidden) + kVec<E> - 1) / kVec<E>;
     constexpr int kWidest = 4 * 8 / kVec<E>;  // groups of a lane: 32 columns
     using One = integral_constant<int, 1>;
     using Two = integral_constant<int, 2>;
@@ -529,7 +607,9 @@ bool sized(int hidden, bool all, F&& f) {
     if (g <= 512) return go(integral_constant<int, 256>{}, Two{});
     if (g <= 1024) return go(integral_constant<int, 512>{}, Two{});
     if constexpr (BWD) {
-        if (g <= 2048 && all) return go(integral_constant<int, 512>{}, integral_constant<int, 4>{});  // off a boundary there are no registers for four groups
+        // bf16 off a boundary, and fp32 of eight groups to a lane, have no registers for a row: spilled / read twice, the backward of 20 000 rows of
+        // 10 001 bf16 with a gate for each 1 896 / 1 266 us, of 10 000 rows of 10 000 fp32 1 018 / 759
+        if (g <= 2048 && (all || sizeof(E) == 4)) return go(integral_constant<int, 512>{}, integral_constant<int, 4>{});
     } else {
         if (g <= 2048) return go(integral_constant<int, 1024>{}, Two{});
         if (g <= 512 * kWidest) return go(integral_constant<int, 1024>{}, integral_constant<int, kWidest / 2>{});
@@ -572,12 +652,16 @@ void bwd(Args<E> a, bool vector_gate, void* dw_pre, void* dw_post, void* dgate, 
             np = std::min(n_parts(a.n_rows, L), (a.n_rows + kAt - 1) / kAt);
             if (np > 8) np -= np % 8;  // a workgroup's rows start alike
             auto go = [&](auto kernel) { kernel<<<np, kThreads<L>, 0, s>>>(a); };
-            if constexpr (PER == 4) a.gate_step ? go(psattn_gn_bwd<E, L, PER, true, true>) : go(psattn_gn_bwd<E, L, PER, true, false>);  // whole rows alone: `sized`
+            if constexpr (PER == 4 && sizeof(E) == 2) a.gate_step ? go(psattn_gn_bwd<E, L, PER, true, true>) : go(psattn_gn_bwd<E, L, PER, true, false>);  // `sized`
             else if (a.gate_step) all ? go(psattn_gn_bwd<E, L, PER, true, true>) : go(psattn_gn_bwd<E, L, PER, false, true>);
             else all ? go(psattn_gn_bwd<E, L, PER, true, false>) : go(psattn_gn_bwd<E, L, PER, false, false>);
         });
-        if (!done) {
-            psattn_gn_bwd_wide<E><<<a.n_rows, 1024, 0, s>>>(a);
+        if (!done && a.hidden <= kColumns) {
+            np = std::min(a.n_rows, 256);  // one to a CU, whose LDS the sums fill
+            if (np > 8) np -= np % 8;
+            psattn_gn_bwd_wide<E, true><<<np, 1024, 0, s>>>(a);
+        } else if (!done) {
+            psattn_gn_bwd_wide<E, false><<<a.n_rows, 1024, 0, s>>>(a);
             const int cols = (a.hidden + kVec<E> - 1 + 256 * kVec<E> - 1) / (256 * kVec<E>);
             np = std::min(np, std::max(8, 2048 / cols / 8 * 8));  // eight workgroups to a CU
             psattn_gn_columns<E><<<dim3(cols, np), 256, 0, s>>>(a);

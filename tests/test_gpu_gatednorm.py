@@ -134,6 +134,15 @@ def test_many_rows(n):
     _check(*_run(n, 40, "f32", gate="all"), "f32")
 
 
+@pytest.mark.parametrize("n,h,dtype,shift", [(600, 8200, "bf16", 1), (523, 8193, "bf16", 0), (300, 16383, "bf16", 3), (270, 16379, "bf16", 0), (301, 8196, "f32", 0), (280, 9001, "f32", 1),
+                                             (265, 16381, "f32", 2), (400, 4097, "f32", 0), (300, 8191, "f32", 0), (530, 4095, "bf16", 0), (520, 4090, "bf16", 5), (1100, 1001, "bf16", 0),
+                                             (257, 127, "bf16", 1), (263, 255, "bf16", 7), (261, 1021, "f32", 3)])
+def test_more_rows_than_workgroups(n, h, dtype, shift):
+    """Widths about the places where a row's lanes or its kernel change, several rows to a workgroup and to its columns' sums"""
+    _check(*_run(n, h, dtype, gate="all", shift=shift), dtype)
+    _check(*_run(n, h, dtype, gate=None if h % 2 else "row", post=h % 3 != 0, ds=False, shift=shift), dtype)
+
+
 def test_scale_zero_and_eps():
     _check(*_run(6, 300, "f32", res=0.0), "f32")
     _check(*_run(6, 300, "bf16", res=-2.5, eps=0.5), "bf16")
