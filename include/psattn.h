@@ -353,7 +353,7 @@ int psattn_meta_copy_positions(const psattn_meta* meta, int32_t* pos /* host [T]
  * (high - low) clamped to [0, 1], r = f * original_positions / 2 pi: what turns `high` times and more over the original context stays,
  * what turns `low` times and less is interpolated.  What a scaling does not name is not looked at.
  * psattn_rope_create_layout: a table as by psattn_rope_create for the first rotary_dim (even) of head_dim dimensions, at most 512, with
- * frequencies from the caller (host) and cosines and sines times `amplitude`.  One with the half layout, head_dim = rotary_dim = 128,
+ * frequencies from the caller (host) and cosines and sines times `amplitude`, computed by the device in double precision; waits as well.  One with the half layout, head_dim = rotary_dim = 128,
  * may be given to every call that takes a psattn_rope; others to psattn_rope_apply alone (PSATTN_EUNSUPPORTED).
  *
  * psattn_rope_apply: Qr = Q and Kr = K, each head's pairs turned by the angles of its token's position, dimensions from

@@ -17,7 +17,4 @@ namespace psattn {
 
 constexpr int32_t kRopeMostDims = 512;  // of a head
 
-int make_rope(int32_t head_dim, int32_t rotary_dim, int32_t layout, const double* inv_freq, double amplitude, int32_t max_positions, void* hip_stream,
-              psattn_rope** out);
-
 }  // namespace psattn

@@ -176,3 +176,28 @@ def test_refusals_of_the_binding():
         ps.psattn_rope_apply(rope, x, x.bfloat16(), positions=pos)
     with pytest.raises(ValueError, match="no K"):
         ps.psattn_rope_apply(rope, x, positions=pos, Kr=x)
+
+
+@pytest.mark.parametrize("rotary,scaling,amp", [(128, "none", 1.0), (64, "base", 1.5), (6, "parts", -0.25)])
+def test_far_positions(rotary, scaling, amp):
+    """Cosines and sines as they stand in the table: half a step of fp32, and of an angle up to 2^20 in 64 bits, rounded once, 2^-33"""
+    most = 1 << 20
+    f = ps.psattn_rope_frequencies(rotary, 500000.0, scaling, factor=8.0, original_positions=8192, low=1.0, high=4.0)
+    rope = ps.Rope(rotary, 500000.0, most, rotary_dim=rotary, layout="half", frequencies=f, amplitude=amp)
+    pos = np.concatenate([np.arange(300), np.random.default_rng(rotary).integers(0, most, 3000), np.arange(most - 50, most)])
+    x = torch.zeros(len(pos), 1, rotary, device="cuda")
+    x[..., : rotary // 2] = 1.0
+    got, _ = ps.psattn_rope_apply(rope, x, x, torch.from_numpy(pos.astype(np.int32)).cuda())
+    a = pos[:, None].astype(np.float64) * f[None, :]
+    want = amp * np.concatenate([np.cos(a), np.sin(a)], 1)
+    close(np64(got)[:, 0], want, EPS32 * np.abs(want) + abs(amp) * 2.0 ** -32, "table")
+
+
+@pytest.mark.parametrize("theta", [10000.0, 500000.0])
+def test_tables_of_both_kinds_are_the_same(theta):
+    n = 20011
+    pos = torch.arange(n, device="cuda", dtype=torch.int32)
+    x = torch.zeros(n, 1, 128, device="cuda")
+    x[..., :64] = 1.0
+    a, b = (ps.psattn_rope_apply(r, x, x, pos)[0] for r in (ps.Rope(128, theta, n), ps.Rope(128, theta, n, layout="half")))
+    assert torch.equal(a, b)
