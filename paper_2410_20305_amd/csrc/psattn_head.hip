@@ -240,23 +240,28 @@ __device__ __forceinline__ void add_token(float at_token, const E* w, int c, int
 }
 
 // dW[token] += sum of dz X over the items of that token: the first of them does it, `lanes` * 4 columns to a workgroup, whose 256 / lanes groups
-// take items in turn.  It looks for the others among all items, n V / 1 024 steps at most beside the products' n V hidden: 160 of 34 400 us
-// for 9 812 items of 128 000 x 4 096.  Items of a single token are the worst: 8 000 of 32 000 x 4 096 take 6.4 ms for 5.3.  The row is rounded a
+// take items in turn.  It looks for the others among all items, n V / 4 096 steps at most beside the products' n V hidden: 209 of 34 400 us
+// for 9 812 items of 128 000 x 4 096.  Items of a single token are the worst: 8 000 of 32 000 x 4 096 take 6.4 ms for 5.4.  The row is rounded a
 // second time, from the first one's sum without the token's own part.
 __global__ __launch_bounds__(256) void psattn_head_dw_tokens(int first, int lanes, int col_blocks, int n_items, int hidden, int64_t ld, const int32_t* target, const float* at_token,
                                                              const uint16_t* x, uint16_t* dW) {
-    constexpr int V = 4, kAtOnce = 8, kSpan = 1024;  // items looked at together: 4 to a thread
-    __shared__ int found[kSpan], count[4];
+    constexpr int V = 4, kAtOnce = 8, kFours = 4, kSpan = 1024 * kFours;  // items looked at together: kFours times 4 to a thread
+    __shared__ int found[kSpan], count[kFours][4];
     __shared__ float4 sums[256];
     const int i = first + static_cast<int>(blockIdx.x) / col_blocks, token = target[i], mine = static_cast<int>(threadIdx.x) * 4, l = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (token < 0) return;
-    auto same = [&](int base, int from, int to) {  // which of the thread's four are in [from, to) and of that token
-        if (base + mine >= n_items) return 0u;
-        const int4 t = *reinterpret_cast<const int4*>(target + base + mine);  // the table's last four are its own: it is of whole 256 bytes
-        const int tok[4] = {t.x, t.y, t.z, t.w};
+    auto same = [&](int base, int from, int to) {  // which of the thread's items are in [from, to) and of that token: four bits to each 1 024 of them
+        int4 t[kFours];
+#pragma unroll
+        for (int u = 0; u < kFours; ++u)  // the table's last four are its own: it is of whole 256 bytes
+            t[u] = base + 1024 * u + mine < n_items ? *reinterpret_cast<const int4*>(target + base + 1024 * u + mine) : make_int4(-1, -1, -1, -1);
         uint32_t yes = 0;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) yes |= tok[k] == token && base + mine + k >= from && base + mine + k < to ? 1u << k : 0u;
+        for (int u = 0; u < kFours; ++u) {
+            const int tok[4] = {t[u].x, t[u].y, t[u].z, t[u].w}, at = base + 1024 * u + mine;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) yes |= tok[k] == token && at + k >= from && at + k < to ? 1u << (4 * u + k) : 0u;
+        }
         return yes;
     };
     const int own = i / kSpan * kSpan;
@@ -268,24 +273,31 @@ __global__ __launch_bounds__(256) void psattn_head_dw_tokens(int first, int lane
     for (int base = own; base < n_items; base += kSpan) {
         const uint32_t yes = same(base, i, n_items);
         if (!__syncthreads_or(yes)) continue;
-        int at = 0, n = 0;
+        int at[kFours] = {}, n = 0;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint64_t votes = __builtin_amdgcn_ballot_w64(yes >> k & 1);
-            at += __builtin_popcountll(votes & ((uint64_t{1} << l) - 1));
-            n += __builtin_popcountll(votes);
+        for (int u = 0; u < kFours; ++u) {
+            int all = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint64_t votes = __builtin_amdgcn_ballot_w64(yes >> (4 * u + k) & 1);
+                at[u] += __builtin_popcountll(votes & ((uint64_t{1} << l) - 1));
+                all += __builtin_popcountll(votes);
+            }
+            if (l == 0) count[u][wave] = all;
         }
-        if (l == 0) count[wave] = n;
         __syncthreads();
-        n = 0;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            at += w < wave ? count[w] : 0;
-            n += count[w];
+        for (int u = 0; u < kFours; ++u) {
+            at[u] += n;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                at[u] += w < wave ? count[u][w] : 0;
+                n += count[u][w];
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (yes >> (4 * u + k) & 1) found[at[u]++] = base + 1024 * u + mine + k;
         }
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (yes >> k & 1) found[at++] = base + mine + k;
         __syncthreads();
         if (c >= hidden) continue;
         auto add = [&](int k, auto COUNT) {  // loads together, sums in order
@@ -324,6 +336,37 @@ __global__ __launch_bounds__(256) void psattn_head_dw_tokens(int first, int lane
 #pragma unroll
     for (int k = 0; k < V; ++k)
         if (c + k < hidden) rows::store1(to + k, rows::to_f32(to[k]) + sum[k]);
+}
+
+// dW of a piece from its parts, four columns to a lane
+template <typename E>
+__global__ __launch_bounds__(256) void psattn_head_dw_join(int n_parts, int cols, int hidden, int64_t ld, const float* parts, int odd, E* dW) {
+    constexpr int V = 4, kAtOnce = 8;
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, per = ld / V, row = i / per, step = cols * ld;
+    const int c = static_cast<int>(i - row * per) * V;
+    if (row >= cols || c >= hidden) return;
+    const float* const from = parts + row * ld + c;
+    float x[V] = {};
+    auto add = [&](int p, auto COUNT) {  // loads together, sums in order
+        constexpr int n = decltype(COUNT)::value;
+        float4 u[n];
+#pragma unroll
+        for (int q = 0; q < n; ++q) u[q] = *reinterpret_cast<const float4*>(from + (p + q) * step);
+#pragma unroll
+        for (int q = 0; q < n; ++q) x[0] += u[q].x, x[1] += u[q].y, x[2] += u[q].z, x[3] += u[q].w;
+    };
+    int p = 0;
+    for (; p + kAtOnce <= n_parts; p += kAtOnce) add(p, std::integral_constant<int, kAtOnce>{});
+    for (; p < n_parts; ++p) add(p, std::integral_constant<int, 1>{});
+    E* const to = dW + row * hidden + c;
+    if (!odd) {  // rows of whole groups on their boundaries
+        if constexpr (sizeof(E) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(psattn::mma::pack2(x[0], x[1]), psattn::mma::pack2(x[2], x[3]));
+        else *reinterpret_cast<float4*>(to) = make_float4(x[0], x[1], x[2], x[3]);
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+        if (c + k < hidden) rows::store1(to + k, x[k]);
 }
 
 // ---- dX of token t: the sums of its items, of all parts of each; `again` rows to a part
@@ -520,6 +563,19 @@ DxTiling dx_tiling(int32_t dt, int64_t n_items, int64_t vocab, int64_t hidden) {
     return {tiling(moved(dt), dz_rows(dt, n_items), hidden, piece, true), false};
 }
 
+// dW of many items and a small vocabulary has few tiles, each with all items for its k: in parts of the items, where a tile alone would take more
+// steps of k than a workgroup's share of the launch, joined by psattn_head_dw_join.  Forward and backward in us, whole / in parts: 9 811 items,
+// 1 200 x 512 bf16 349 / 235, fp32 984 / 613
+int64_t dw_split(int32_t dt, int64_t n_items, int64_t vocab, int64_t hidden) {
+    if (n_items < 1024) return 1;
+    const int64_t piece = piece_rows(dt, n_items, vocab), k = dt == PSATTN_BF16 ? 64 : 32, side = dt == PSATTN_BF16 ? 256 : 128, slots = dt == PSATTN_BF16 ? 256 : 512;
+    const int64_t steps = up64(n_items) / k, tiles = cdiv(piece, side) * cdiv(hidden, side);
+    const int64_t beside = dx_tiling(dt, n_items, vocab, hidden).both ? cdiv(n_items, side) * cdiv(hidden, side) * (piece / k) : 0;
+    const int64_t share = std::max<int64_t>(8, (beside + tiles * steps) / slots);
+    return std::max<int64_t>(1, std::min(steps / share, kPartBytes / (static_cast<int64_t>(sizeof(float)) * piece * up8(hidden))));
+}
+size_t dw_part_bytes(int64_t split, int64_t piece, int64_t hidden) { return split > 1 ? sizeof(float) * split * piece * up8(hidden) : 0; }
+
 struct Room {
     char* p;
     explicit Room(void* base) : p(reinterpret_cast<char*>(align_up(reinterpret_cast<uintptr_t>(base), 256))) {}
@@ -569,7 +625,7 @@ size_t bwd_bytes(const psattn_lp_plan* plan, int32_t dt, int32_t vocab, int32_t 
     const int64_t m = dz_rows(dt, n), piece = piece_rows(dt, n, vocab);
     const size_t sums = m * up8(hidden) * dx_tiling(dt, n, vocab, hidden).split * sizeof(float), parts = logits_bytes(dt, n, vocab, piece, hidden);
     return align_up(up64(m) * up8(hidden) * elem_bytes(dt), 256) + align_up(up64(m) * up8(piece) * elem_bytes(dt), 256) + align_up(sums, 256) + align_up(parts, 256) +
-           4 * align_up(n * 4, 256) + 256;
+           align_up(dw_part_bytes(dw_split(dt, n, vocab, hidden), piece, hidden), 256) + 4 * align_up(n * 4, 256) + 256;
 }
 
 }  // namespace
@@ -655,6 +711,8 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
         char* const dz = room.take<char>(static_cast<size_t>(n_whole) * ldz * e);
         sums = room.take<float>(static_cast<size_t>(again) * ld * parts);
         float* const z_parts = reinterpret_cast<float*>(room.take<char>(logits_bytes(dt, n, vocab, piece, hidden)));
+        const int64_t w_split = dw_split(dt, n, vocab, hidden);
+        float* const w_parts = reinterpret_cast<float*>(room.take<char>(dw_part_bytes(w_split, piece, hidden)));
         char* const rest = again > n ? dz + n * ldz * e : nullptr;
         int32_t* const targets = room.take<int32_t>(n);
         float *const lse = room.take<float>(n), *const weight = room.take<float>(n);
@@ -697,22 +755,31 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
             Product g{};  // dW = dz^T X
             g.p[0] = dz; g.q[0] = x; g.out[0] = static_cast<char*>(dW) + at * hidden * e;
             g.ldp = ldz; g.ldq = ld; g.ldo = hidden;
-            g.M = cols; g.m_load = static_cast<int32_t>(up8(cols)); g.N = hidden; g.n_load = static_cast<int32_t>(ld); g.K = n_whole; g.n_seg = g.n_prod = g.n_split = 1;
+            g.M = cols; g.m_load = static_cast<int32_t>(up8(cols)); g.N = hidden; g.n_load = static_cast<int32_t>(ld); g.K = n_whole; g.n_seg = g.n_prod = 1;
+            g.n_split = static_cast<int32_t>(w_split); g.parts = w_parts; g.ld_part = ld;
             g.odd = !(at16({g.out[0]}) && hidden % (dt == PSATTN_BF16 ? 8 : 4) == 0);
             const bool whole = at16({w}) && hidden % (dt == PSATTN_BF16 ? 8 : 4) == 0;
             if (dx.both && (whole || dt != PSATTN_BF16)) {
-                if ((rc = (dt == PSATTN_BF16 ? head_grads_bf16 : whole ? head_grads_f32_whole : head_grads_f32)(a, g, s)) != PSATTN_OK) return rc;
-                continue;
-            }
-            if ((rc = head_product(dt, kSums, false, dx.size, a, s)) != PSATTN_OK) return rc;
-            if (n_whole <= (dt == PSATTN_BF16 ? 256 : 64)) {
+                rc = (dt == PSATTN_BF16 ? head_grads_bf16 : whole ? head_grads_f32_whole : head_grads_f32)(a, g, s);
+            } else if ((rc = head_product(dt, kSums, false, dx.size, a, s)) != PSATTN_OK) {
+                return rc;
+            } else if (n_whole <= (dt == PSATTN_BF16 ? 256 : 64)) {
                 g.K = again;
                 rc = (dt == PSATTN_BF16 ? head_outer_bf16 : head_outer_f32)(g, s);
             } else {  // bf16: fp32 takes one way or the other above
-                auto us = [&](TileSize t, int64_t side) { return product_us(kWhole, kPlain, t, cdiv(cols, side) * cdiv(hidden, side), n_whole / 64, 1, 0); };
+                auto us = [&](TileSize t, int64_t side) { return product_us(kWhole, kPlain, t, cdiv(cols, side) * cdiv(hidden, side), n_whole / 64, w_split, 0); };
                 rc = product_bf16(kPlain, 0, false, false, cdiv(cols, 256) * cdiv(hidden, 256) >= 256 || us(k256, 256) < us(k128, 128) ? k256 : k128, g, s);
             }
             if (rc != PSATTN_OK) return rc;
+            if (w_split > 1) {
+                const int64_t groups = static_cast<int64_t>(cols) * (ld / 4);
+                auto join = [&](auto* to) {
+                    using E = std::remove_pointer_t<decltype(to)>;
+                    psattn_head_dw_join<E><<<static_cast<uint32_t>(cdiv(groups, 256)), 256, 0, s>>>(static_cast<int>(w_split), cols, hidden, ld, w_parts, g.odd, to);
+                };
+                if (dt == PSATTN_BF16) join(static_cast<uint16_t*>(g.out[0]));
+                else join(static_cast<float*>(g.out[0]));
+            }
         }
     }
     if (apart && n > 0) {

@@ -35,7 +35,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesToSimd) void psattn_head_grad
     __shared__ __attribute__((aligned(1024))) char lds[kLds<S>];
     const int n = x_tiles_m * x_tiles_n, first = n * x.n_split, b = blockIdx.x;
     if (b < first) product_tile<E, ASYNC, true, false, kSums, 0, S>(lds, x, x_tiles_m, x_tiles_n, b % n, b / n);
-    else product_tile<E, ASYNC, false, false, kPlain, 0, S>(lds, w, w_tiles_m, w_tiles_n, b - first, 0);
+    else product_tile<E, ASYNC, false, false, kPlain, 0, S>(lds, w, w_tiles_m, w_tiles_n, (b - first) % (w_tiles_m * w_tiles_n), (b - first) / (w_tiles_m * w_tiles_n));
 }
 
 // dW of few items, a few steps of k: what is written bounds it, and workgroups with one buffer of either operand leave a CU room for four.
@@ -145,7 +145,7 @@ template <typename E, bool ASYNC>
 int launch_grads(const Product& x, const Product& w, hipStream_t s) {
     using S = std::conditional_t<sizeof(E) == 2, Shape<256, 256, 2, 4, 3>, Shape<128, 128, 2, 2, ASYNC ? 3 : 2>>;
     auto tiles = [](int64_t n) { return (n + S::BM - 1) / S::BM; };
-    const int64_t xm = tiles(x.M), xn = tiles(x.N), wm = tiles(w.M), wn = tiles(w.N), n = xm * xn * x.n_split + wm * wn;
+    const int64_t xm = tiles(x.M), xn = tiles(x.N), wm = tiles(w.M), wn = tiles(w.N), n = xm * xn * x.n_split + wm * wn * w.n_split;
     if (n >= (int64_t{1} << 31) / S::kThreads) return PSATTN_EUNSUPPORTED;
     psattn_head_grads<E, ASYNC, S><<<static_cast<uint32_t>(n), S::kThreads, 0, s>>>(x, w, static_cast<int>(xm), static_cast<int>(xn), static_cast<int>(wm), static_cast<int>(wn));
     return hipGetLastError() == hipSuccess ? PSATTN_OK : PSATTN_EHIP;

@@ -314,3 +314,11 @@ def test_tokens_that_come_again(V, h):
     """Rows of dW that sum over items of several thousands, next to others of a single one"""
     a = _inputs("again", V, h, "bf16")
     _check(*a, _call("again", *a[:3], a[4], "bf16"), "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V,h", [(5, 64), (257, 72), (300, 33), (700, 256), (513, 1001)])
+def test_many_items_of_a_small_vocabulary(V, h, dtype):
+    """dW, of few tiles, in parts of the items"""
+    a = _inputs("again", V, h, dtype)
+    _check(*a, _call("again", *a[:3], a[4], dtype, 1 if h == 256 else 0), dtype)
