@@ -429,7 +429,8 @@ int psattn_dpo_loss(int32_t n_pairs, float beta, const float* logp_policy, const
  * psattn_head_logprob_bwd: dX [T, hidden] and dW [vocab, hidden] of dt, both overwritten as a whole (dX is zero for rows that predict
  * nothing): the gradients of sum_j d_resp_logp[j] * resp_logp[j], from the forward's row_lse.  The gradient of the logits is an
  * operand of the matrix cores and is rounded to dt once, from fp32; of bf16 its value at the predicted token, most of its row's
- * weight, is not rounded.  Sums are fp32 in a fixed order.  A response whose d_resp_logp is 0, and a token id outside [0, vocab), give nothing.
+ * weight, is not rounded.  Sums are fp32 in a fixed order, rounded to dt at the end; until then dX may hold other rows.  A response whose
+ * d_resp_logp is 0, and a token id outside [0, vocab), give nothing.
  * Workspaces: the caller's device memory, of at least the bytes that the call of that name gives for the plan (never 0 for valid
  * arguments), contents undefined on entry and exit, one for each call in flight.  The backward's holds the rows and one piece (some
  * 512 MiB, 256 tokens of the vocabulary at least) of the logits' gradient.  No call allocates or blocks, and all may be captured into a graph.

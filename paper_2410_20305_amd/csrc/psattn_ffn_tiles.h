@@ -154,6 +154,16 @@ __device__ __forceinline__ void put8(float* p, const float (&x)[8], int n) {
             if (j < n) p[j] = x[j];
     }
 }
+// what rounding leaves of eight floats, itself rounded
+__device__ __forceinline__ void put_rest(uint16_t* p, const float (&x)[8], int n) {
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t u = mma::pack2(x[2 * j], x[2 * j + 1]);
+        w[j] = mma::pack2(x[2 * j] - __uint_as_float(u << 16), x[2 * j + 1] - __uint_as_float(u & 0xffff0000u));
+    }
+    put8<false>(p, w, n);
+}
 // eight floats as they come from memory
 struct Group {
     float w[8];
@@ -541,6 +551,11 @@ __device__ __forceinline__ void product_tile(char* lds, const Product& d, int ti
         }
         return;
     }
+    int item[PASS == kTokens ? MB : 1];
+    if constexpr (PASS == kTokens) {
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) item[mb] = static_cast<const int32_t*>(d.H)[min(m0 + (wm * MB + mb) * 32 + (le & 31), d.M - 1)];
+    }
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
         const int m = m0 + (wm * MB + mb) * 32, rows = d.M - m;
@@ -570,6 +585,7 @@ __device__ __forceinline__ void product_tile(char* lds, const Product& d, int ti
                                 x[i] = 0.f;
                             }
                         d.parts[at] = at_token;
+                        __hip_atomic_store(d.item_of + t + d.n_load + 4 * (le >> 5), at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // other items' too
                     }
                 }
                 store_out<ASYNC>(static_cast<E*>(d.out[0]) + m * d.ldo + n, d.ldo, rows, cols, chunks(x), le, d.odd);
@@ -627,6 +643,18 @@ __device__ __forceinline__ void product_tile(char* lds, const Product& d, int ti
                 const int n = n0 + (wn * NB + nb) * 32, cols = d.N - n;
                 if (cols <= 0) break;
                 store_out<ASYNC>(static_cast<E*>(d.out[d.n_prod > 1 ? z : 0]) + m * d.ldo + n, d.ldo, rows, cols, chunks(acc[nb][mb]), le, d.odd);
+            }
+        } else if constexpr (PASS == kTokens) {
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                const int n = n0 + (wn * NB + nb) * 32, cols = d.N - n;
+                if (cols <= 0) break;
+                const Chunks x = chunks(acc[nb][mb]);
+                if ((le & 31) < rows && item[mb] >= 0) {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) put_rest(static_cast<uint16_t*>(d.out[1]) + item[mb] * d.ldo + n + 16 * k + 8 * (le >> 5), x.c[k], cols - 16 * k - 8 * (le >> 5));
+                }
+                store_out<ASYNC>(static_cast<E*>(d.out[0]) + m * d.ldo + n, d.ldo, rows, cols, x, le, d.odd);
             }
         }
     }

@@ -31,13 +31,14 @@ enum Pass {
     kLse,     // acc = logits: maximum and sum of exponentials of each tile's part of a row, the logit of the row's token
     kDlogit,  // acc = logits: out = weight (1[n = token] - exp(acc - lse))
     kSums,    // parts = acc in fp32, or what is there and acc
+    kTokens,  // acc = dW of bf16, m a token, k items: out = acc; of tokens that an item predicts also what the rounding leaves
 };
 
 struct Product {
     const void *p[2], *q[2];  // of the segments along k (n_seg), or of two products of one shape (n_prod, p and out only); kGate: q of gate and up
-    void* out[2];             // kPlain: out[product]; kDact: dG, dU; kDlogit: dz and, of bf16 and 32 rows at most, what its rounding leaves (may be null)
+    void* out[2];             // kPlain: out[product]; kDact: dG, dU; kDlogit: dz and, of bf16 and 32 rows at most, what its rounding leaves (may be null); kTokens: dW and [items][ldo], what its rounding leaves
     float *G, *U;             // kGate: written (may be null); kDact: read; kLse: pairs [tile of n][M], logits [M], written; kDlogit: lse, weights [M]
-    void* H;                  // kGate: written; kLse, kDlogit: tokens [M], int32
+    void* H;                  // kGate: written; kLse, kDlogit: tokens [M], int32; kTokens: an item of each token or -1, int32 [M]
     int64_t ldp, ldq, ldo;    // elements from one row in memory to the next
     int64_t ld_kept;          // kDact: of G and U
     int32_t M, N, K;          // K: of one segment
@@ -48,6 +49,7 @@ struct Product {
     int32_t n_split;
     int32_t add;              // kSums: parts hold sums already
     float* parts;             // kDlogit of bf16: [M], dz at the items' tokens, where out gets 0 then (may be null)
+    int32_t* item_of;         // ... and, written too: one of the items of each token
     int64_t ld_part;
 };
 

@@ -14,11 +14,13 @@ int head_product_bf16_any(Pass pass, bool qkc, TileSize size, const Product& d, 
 int head_product_f32_whole(Pass pass, bool qkc, TileSize size, const Product& d, hipStream_t s);
 int head_product_f32(Pass pass, bool qkc, TileSize size, const Product& d, hipStream_t s);
 
-// dX's sums and dW of a piece in one launch, of tiles of 256 x 256, or 128 x 128 of fp32; dz and the rows of X are whole, W may be not in fp32
+// dW of bf16 (kTokens); dz and the rows of X are whole
+int head_tokens_bf16(TileSize size, const Product& w, hipStream_t s);
+// dX's sums and dW (kTokens, of fp32 kPlain) of a piece in one launch, of tiles of 256 x 256, or 128 x 128 of fp32; dz and the rows of X are whole, W may be not in fp32
 int head_grads_bf16(const Product& x, const Product& w, hipStream_t s);
 int head_grads_f32_whole(const Product& x, const Product& w, hipStream_t s);
 int head_grads_f32(const Product& x, const Product& w, hipStream_t s);
-// dW alone, of few items: k is theirs, and behind them stand rows of zeros up to a multiple of 64
+// dW alone, of few items: k is theirs, and behind them stand rows of zeros up to a multiple of 64.  bf16: as kTokens, where there is an out[1]
 int head_outer_bf16(const Product& w, hipStream_t s);
 int head_outer_f32(const Product& w, hipStream_t s);
 

@@ -36,13 +36,15 @@ size_t elem_bytes(int32_t dt) { return dt == PSATTN_BF16 ? 2 : 4; }
 
 // ---- the items' rows, made whole: one workgroup to a row.  Without a token of the vocabulary an item has no gradient, and its row is zeros there.
 // BWD: up to `again` the rows stand there once more (for the second part of dz), and behind them, in dz too, rows of zeros, so that dW's
-// k is whole steps
+// k is whole steps.  item_of: all -1
 template <typename E, bool BWD>
 __global__ __launch_bounds__(256) void psattn_head_rows(int n_items, int again, const int32_t* item_row, const int32_t* item_tok, const int32_t* item_resp,
                                                         const int32_t* token_ids, int vocab, int hidden, const E* X, const float* row_lse, const float* d_logp, E* out,
-                                                        int32_t* target, float* lse, float* weight, float* at_token, E* dz, int64_t ldz) {
+                                                        int32_t* target, float* lse, float* weight, float* at_token, int32_t* item_of, E* dz, int64_t ldz) {
     constexpr int V = rows::kVec<E>;
     const int64_t at = blockIdx.x, ld = (hidden + 7) / 8 * 8;
+    if (BWD && item_of)
+        for (int64_t v = at * 256 + threadIdx.x; v < vocab; v += gridDim.x * 256) item_of[v] = -1;
     if (BWD && at >= again) {
         const rows::u32x4 zero = {0, 0, 0, 0};
         for (int64_t c = threadIdx.x * V; c < ld; c += 256 * V) *reinterpret_cast<rows::u32x4*>(out + at * ld + c) = zero;
@@ -129,7 +131,7 @@ __global__ __launch_bounds__(1024) void psattn_head_parts_lse(int n_items, int n
 // dz of an item, 1 024 columns to a workgroup.  bf16: what its rounding leaves, or its value at the item's token apart, where that is asked for
 template <typename E>
 __global__ __launch_bounds__(256) void psattn_head_parts_dz(int n_items, int n_parts, int first, int cols, int64_t ld, const float* parts, const int32_t* target, const float* lse,
-                                                            const float* weight, E* dz, E* rest, float* at_token, int64_t ldz) {
+                                                            const float* weight, E* dz, E* rest, float* at_token, int32_t* item_of, int64_t ldz) {
     const int64_t i = blockIdx.y;
     const int c = (blockIdx.x * 256 + threadIdx.x) * 4, t = target[i] - first;
     if (c >= cols) return;
@@ -143,7 +145,10 @@ __global__ __launch_bounds__(256) void psattn_head_parts_dz(int n_items, int n_p
         const bool apart = at_token && c + k == t;
         rows::store1(dz + i * ldz + c + k, apart ? 0.f : x);
         if (rest) rows::store1(rest + i * ldz + c + k, x - rows::hold(x, dz));
-        if (apart) at_token[i] = x;
+        if (apart) {
+            at_token[i] = x;
+            __hip_atomic_store(item_of + target[i], static_cast<int32_t>(i), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // other items' too
+        }
     }
 }
 
@@ -230,7 +235,9 @@ __global__ __launch_bounds__(256) void psattn_head_responses(int first, const in
 
 // ---- bf16: dz at an item's own token.  It is most of its row's weight, and its rounding error would be that of all columns of dX and of the
 // token's row of dW alike: it stays in fp32, out of the products, and joins their results here.  (99 items, gradients against 64 bits: dX 2.4e-3
-// in the products, 1.66e-3 apart, which is its own rounding; dW 2.34e-3 and 1.66e-3.)
+// in the products, 1.66e-3 apart, which is its own rounding; dW 2.34e-3 and 1.66e-3.)  The row of a frequent token is a small difference of two
+// large parts: what bf16 leaves of the products' part joins it too (columns of mean 1/3, probabilities up to 0.2, equal weights, a row of dW off
+// by, without that / with it: 9 812 items 1.7e-2 / 1.5e-3, 1 000 8.8e-3 / 1.9e-3, 99 2.4e-3 / 1.9e-3; 16 384 tokens of 128 000 x 4 096 34.55 / 34.3 ms).
 template <typename E>
 __device__ __forceinline__ void add_token(float at_token, const E* w, int c, int hidden, float (&x)[4]) {
     if (at_token == 0.f) return;
@@ -239,18 +246,17 @@ __device__ __forceinline__ void add_token(float at_token, const E* w, int c, int
         if (c + k < hidden) x[k] = fmaf(at_token, rows::to_f32(w[c + k]), x[k]);
 }
 
-// dW[token] += sum of dz X over the items of that token: the first of them does it, `lanes` * 4 columns to a workgroup, whose 256 / lanes groups
-// take items in turn.  It looks for the others among all items, n V / 4 096 steps at most beside the products' n V hidden: 209 of 34 400 us
-// for 9 812 items of 128 000 x 4 096.  Items of a single token are the worst: 8 000 of 32 000 x 4 096 take 6.4 ms for 5.4.  The row is rounded a
-// second time, from the first one's sum without the token's own part.
-__global__ __launch_bounds__(256) void psattn_head_dw_tokens(int first, int lanes, int col_blocks, int n_items, int hidden, int64_t ld, const int32_t* target, const float* at_token,
-                                                             const uint16_t* x, uint16_t* dW) {
+// dW[token] += sum of dz X over the items of that token, and what bf16 has left of the products' row, which stands in `rest` by the item that
+// item_of names.  That item does it, whichever of them it is: it looks for all of them from the first on, so the sum does not depend on it.  `lanes` * 4
+// columns to a workgroup, whose 256 / lanes groups take items in turn; n V / 4 096 steps at most beside the products' n V hidden.
+__global__ __launch_bounds__(256) void psattn_head_dw_tokens(int first, int lanes, int col_blocks, int n_items, int hidden, int64_t ld, const int32_t* target, const int32_t* item_of,
+                                                             const float* at_token, const uint16_t* x, const uint16_t* rest, uint16_t* dW) {
     constexpr int V = 4, kAtOnce = 8, kFours = 4, kSpan = 1024 * kFours;  // items looked at together: kFours times 4 to a thread
     __shared__ int found[kSpan], count[kFours][4];
     __shared__ float4 sums[256];
     const int i = first + static_cast<int>(blockIdx.x) / col_blocks, token = target[i], mine = static_cast<int>(threadIdx.x) * 4, l = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if (token < 0) return;
-    auto same = [&](int base, int from, int to) {  // which of the thread's items are in [from, to) and of that token: four bits to each 1 024 of them
+    if (token < 0 || item_of[token] != i) return;
+    auto same = [&](int base) {  // which of the thread's items are of that token: four bits to each 1 024 of them
         int4 t[kFours];
 #pragma unroll
         for (int u = 0; u < kFours; ++u)  // the table's last four are its own: it is of whole 256 bytes
@@ -260,18 +266,15 @@ __global__ __launch_bounds__(256) void psattn_head_dw_tokens(int first, int lane
         for (int u = 0; u < kFours; ++u) {
             const int tok[4] = {t[u].x, t[u].y, t[u].z, t[u].w}, at = base + 1024 * u + mine;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) yes |= tok[k] == token && at + k >= from && at + k < to ? 1u << (4 * u + k) : 0u;
+            for (int k = 0; k < 4; ++k) yes |= tok[k] == token && at + k < n_items ? 1u << (4 * u + k) : 0u;
         }
         return yes;
     };
-    const int own = i / kSpan * kSpan;
-    for (int base = own; base >= 0; base -= kSpan)  // the nearest first: frequent tokens end here soon
-        if (__syncthreads_or(same(base, 0, i))) return;
     const int lane = static_cast<int>(threadIdx.x) & (lanes - 1), group = static_cast<int>(threadIdx.x) / lanes, groups = 256 / lanes;
     const int c = (static_cast<int>(blockIdx.x) % col_blocks * lanes + lane) * V;
     float sum[V] = {};
-    for (int base = own; base < n_items; base += kSpan) {
-        const uint32_t yes = same(base, i, n_items);
+    for (int base = 0; base < n_items; base += kSpan) {
+        const uint32_t yes = same(base);
         if (!__syncthreads_or(yes)) continue;
         int at[kFours] = {}, n = 0;
 #pragma unroll
@@ -332,15 +335,17 @@ __global__ __launch_bounds__(256) void psattn_head_dw_tokens(int first, int lane
             sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
         }
     }
+    if (c >= hidden) return;
     uint16_t* const to = dW + static_cast<int64_t>(token) * hidden + c;
+    rest += static_cast<int64_t>(i) * hidden + c;
 #pragma unroll
     for (int k = 0; k < V; ++k)
-        if (c + k < hidden) rows::store1(to + k, rows::to_f32(to[k]) + sum[k]);
+        if (c + k < hidden) rows::store1(to + k, rows::to_f32(to[k]) + (rows::to_f32(rest[k]) + sum[k]));
 }
 
-// dW of a piece from its parts, four columns to a lane
+// dW of a piece from its parts, four columns to a lane; item_of and rest as kTokens has them, or null
 template <typename E>
-__global__ __launch_bounds__(256) void psattn_head_dw_join(int n_parts, int cols, int hidden, int64_t ld, const float* parts, int odd, E* dW) {
+__global__ __launch_bounds__(256) void psattn_head_dw_join(int n_parts, int cols, int hidden, int64_t ld, const float* parts, int odd, E* dW, const int32_t* item_of, E* rest) {
     constexpr int V = 4, kAtOnce = 8;
     const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, per = ld / V, row = i / per, step = cols * ld;
     const int c = static_cast<int>(i - row * per) * V;
@@ -359,6 +364,11 @@ __global__ __launch_bounds__(256) void psattn_head_dw_join(int n_parts, int cols
     for (; p + kAtOnce <= n_parts; p += kAtOnce) add(p, std::integral_constant<int, kAtOnce>{});
     for (; p < n_parts; ++p) add(p, std::integral_constant<int, 1>{});
     E* const to = dW + row * hidden + c;
+    if (const int item = item_of ? item_of[row] : -1; item >= 0) {
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            if (c + k < hidden) rows::store1(rest + static_cast<int64_t>(item) * hidden + c + k, x[k] - rows::hold(x[k], dW));
+    }
     if (!odd) {  // rows of whole groups on their boundaries
         if constexpr (sizeof(E) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(psattn::mma::pack2(x[0], x[1]), psattn::mma::pack2(x[2], x[3]));
         else *reinterpret_cast<float4*>(to) = make_float4(x[0], x[1], x[2], x[3]);
@@ -543,6 +553,7 @@ int64_t piece_rows(int32_t dt, int64_t n_items, int64_t vocab) {
 // Few items of bf16: dz as two numbers each, the second what the first one's rounding leaves, as items of their own.  The gradients are as
 // exact as their own rounding then.  Of more items dz at their tokens alone is kept exact (psattn_head_dw_tokens)
 constexpr int64_t kTwice = 32;
+bool dz_apart(int32_t dt, int64_t n_items) { return dt == PSATTN_BF16 && n_items > kTwice; }
 int64_t dz_rows(int32_t dt, int64_t n_items) { return dt == PSATTN_BF16 && n_items <= kTwice ? 2 * n_items : n_items; }
 constexpr int kManyParts = 16;
 // dX's sums: k is a piece of the vocabulary, in parts where the rows' tiles are few.
@@ -625,7 +636,8 @@ size_t bwd_bytes(const psattn_lp_plan* plan, int32_t dt, int32_t vocab, int32_t 
     const int64_t m = dz_rows(dt, n), piece = piece_rows(dt, n, vocab);
     const size_t sums = m * up8(hidden) * dx_tiling(dt, n, vocab, hidden).split * sizeof(float), parts = logits_bytes(dt, n, vocab, piece, hidden);
     return align_up(up64(m) * up8(hidden) * elem_bytes(dt), 256) + align_up(up64(m) * up8(piece) * elem_bytes(dt), 256) + align_up(sums, 256) + align_up(parts, 256) +
-           align_up(dw_part_bytes(dw_split(dt, n, vocab, hidden), piece, hidden), 256) + 4 * align_up(n * 4, 256) + 256;
+           align_up(dw_part_bytes(dw_split(dt, n, vocab, hidden), piece, hidden), 256) + 4 * align_up(n * 4, 256) + 256 +
+           (dz_apart(dt, n) ? align_up(vocab * sizeof(int32_t), 256) : 0);
 }
 
 }  // namespace
@@ -656,7 +668,7 @@ int psattn_head_logprob_fwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
         auto gather = [&](auto* to) {
             using E = std::remove_pointer_t<decltype(to)>;
             psattn_head_rows<E, false><<<n, 256, 0, s>>>(n, n, plan->item_row, plan->item_tok, plan->item_resp, token_ids, vocab, hidden, static_cast<const E*>(X),
-                                                         nullptr, nullptr, to, target, nullptr, nullptr, nullptr, nullptr, 0);
+                                                         nullptr, nullptr, to, target, nullptr, nullptr, nullptr, nullptr, nullptr, 0);
         };
         if (dt == PSATTN_BF16) gather(reinterpret_cast<uint16_t*>(x));
         else gather(reinterpret_cast<float*>(x));
@@ -699,9 +711,10 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
     const int parts = static_cast<int>(dx.split);
     const int64_t ld = up8(hidden), piece = piece_rows(dt, n, vocab), ldz = up8(piece);
     const int again = static_cast<int>(dz_rows(dt, n)), n_whole = static_cast<int>(up64(again));
-    const bool apart = dt == PSATTN_BF16 && again == n;  // dz at the items' tokens
+    const bool apart = dz_apart(dt, n);  // dz at the items' tokens
+    uint16_t* const rest_w = static_cast<uint16_t*>(dX);  // written last, and an item's row in it free until then: there are no more items than tokens
     float *sums = nullptr, *at_token = nullptr;
-    const int32_t* target = nullptr;
+    const int32_t *target = nullptr, *item_of = nullptr;
     const uint16_t* x_rows = nullptr;
     if (n == 0) {  // nothing is predicted: sums over nothing
         psattn_head_zero<<<1024, 256, 0, s>>>(static_cast<uint16_t*>(dW), static_cast<size_t>(vocab) * hidden * e / 2);
@@ -718,10 +731,12 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
         float *const lse = room.take<float>(n), *const weight = room.take<float>(n);
         at_token = room.take<float>(n);
         target = targets;
+        int32_t* const items = apart ? room.take<int32_t>(vocab) : nullptr;
+        item_of = items;
         auto gather = [&](auto* to) {
             using E = std::remove_pointer_t<decltype(to)>;
             psattn_head_rows<E, true><<<n_whole, 256, 0, s>>>(n, again, plan->item_row, plan->item_tok, plan->item_resp, token_ids, vocab, hidden, static_cast<const E*>(X),
-                                                              row_lse, d_resp_logp, to, targets, lse, weight, at_token, reinterpret_cast<E*>(dz), ldz);
+                                                              row_lse, d_resp_logp, to, targets, lse, weight, at_token, items, reinterpret_cast<E*>(dz), ldz);
         };
         if (dt == PSATTN_BF16) gather(reinterpret_cast<uint16_t*>(x));
         else gather(reinterpret_cast<float*>(x));
@@ -730,7 +745,7 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
             const char* const w = static_cast<const char*>(W) + at * hidden * e;
             int rc;
             Product z{};  // dz
-            z.p[0] = x; z.q[0] = w; z.G = lse; z.U = weight; z.H = targets; z.out[0] = dz; z.out[1] = rest; z.parts = apart ? at_token : nullptr;
+            z.p[0] = x; z.q[0] = w; z.G = lse; z.U = weight; z.H = targets; z.out[0] = dz; z.out[1] = rest; z.parts = apart ? at_token : nullptr; z.item_of = items;
             z.ldp = ld; z.ldq = hidden; z.ldo = ldz;
             z.M = n; z.N = cols; z.K = hidden; z.n_seg = z.n_prod = z.n_split = 1;
             z.n_load = static_cast<int32_t>(at);
@@ -741,7 +756,7 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
                 auto go = [&](auto* to) {
                     using E = std::remove_pointer_t<decltype(to)>;
                     psattn_head_parts_dz<E><<<dim3(static_cast<uint32_t>(cdiv(cols, 1024)), n), 256, 0, s>>>(n, z.n_split, static_cast<int>(at), cols, z.ld_part, z_parts, targets, lse,
-                                                                                                            weight, to, reinterpret_cast<E*>(rest), apart ? at_token : nullptr, ldz);
+                                                                                                            weight, to, reinterpret_cast<E*>(rest), apart ? at_token : nullptr, items, ldz);
                 };
                 if (dt == PSATTN_BF16) go(reinterpret_cast<uint16_t*>(dz));
                 else go(reinterpret_cast<float*>(dz));
@@ -757,6 +772,7 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
             g.ldp = ldz; g.ldq = ld; g.ldo = hidden;
             g.M = cols; g.m_load = static_cast<int32_t>(up8(cols)); g.N = hidden; g.n_load = static_cast<int32_t>(ld); g.K = n_whole; g.n_seg = g.n_prod = 1;
             g.n_split = static_cast<int32_t>(w_split); g.parts = w_parts; g.ld_part = ld;
+            if (apart) g.out[1] = rest_w, g.H = items + at;
             g.odd = !(at16({g.out[0]}) && hidden % (dt == PSATTN_BF16 ? 8 : 4) == 0);
             const bool whole = at16({w}) && hidden % (dt == PSATTN_BF16 ? 8 : 4) == 0;
             if (dx.both && (whole || dt != PSATTN_BF16)) {
@@ -768,28 +784,28 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
                 rc = (dt == PSATTN_BF16 ? head_outer_bf16 : head_outer_f32)(g, s);
             } else {  // bf16: fp32 takes one way or the other above
                 auto us = [&](TileSize t, int64_t side) { return product_us(kWhole, kPlain, t, cdiv(cols, side) * cdiv(hidden, side), n_whole / 64, w_split, 0); };
-                rc = product_bf16(kPlain, 0, false, false, cdiv(cols, 256) * cdiv(hidden, 256) >= 256 || us(k256, 256) < us(k128, 128) ? k256 : k128, g, s);
+                rc = head_tokens_bf16(cdiv(cols, 256) * cdiv(hidden, 256) >= 256 || us(k256, 256) < us(k128, 128) ? k256 : k128, g, s);
             }
             if (rc != PSATTN_OK) return rc;
-            if (w_split > 1) {
+            if (w_split > 1) {  // 1 024 items and more
                 const int64_t groups = static_cast<int64_t>(cols) * (ld / 4);
                 auto join = [&](auto* to) {
                     using E = std::remove_pointer_t<decltype(to)>;
-                    psattn_head_dw_join<E><<<static_cast<uint32_t>(cdiv(groups, 256)), 256, 0, s>>>(static_cast<int>(w_split), cols, hidden, ld, w_parts, g.odd, to);
+                    psattn_head_dw_join<E><<<static_cast<uint32_t>(cdiv(groups, 256)), 256, 0, s>>>(static_cast<int>(w_split), cols, hidden, ld, w_parts, g.odd, to, apart ? items + at : nullptr, reinterpret_cast<E*>(rest_w));
                 };
                 if (dt == PSATTN_BF16) join(static_cast<uint16_t*>(g.out[0]));
                 else join(static_cast<float*>(g.out[0]));
             }
         }
     }
-    if (apart && n > 0) {
+    if (apart) {
         int lanes = 4;
         while (lanes < 256 && lanes * 4 < hidden) lanes *= 2;
         const int blocks = static_cast<int>(cdiv(hidden, lanes * 4));
         const int64_t most = ((int64_t{1} << 31) - 1) / 256 / blocks;
         for (int64_t at = 0; at < n; at += most)
-            psattn_head_dw_tokens<<<static_cast<uint32_t>(std::min<int64_t>(most, n - at) * blocks), 256, 0, s>>>(static_cast<int>(at), lanes, blocks, n, hidden, ld, target, at_token,
-                                                                                                                          x_rows, static_cast<uint16_t*>(dW));
+            psattn_head_dw_tokens<<<static_cast<uint32_t>(std::min<int64_t>(most, n - at) * blocks), 256, 0, s>>>(static_cast<int>(at), lanes, blocks, n, hidden, ld, target, item_of, at_token,
+                                                                                                                          x_rows, rest_w, static_cast<uint16_t*>(dW));
     }
     // a row to a workgroup; where they are few, 1 024 columns of one, or with many parts 256
     const bool many = n <= 64 && parts * (again / std::max(n, 1)) >= kManyParts && plan->T < 4096;

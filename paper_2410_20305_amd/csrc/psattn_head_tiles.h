@@ -35,7 +35,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesToSimd) void psattn_head_grad
     __shared__ __attribute__((aligned(1024))) char lds[kLds<S>];
     const int n = x_tiles_m * x_tiles_n, first = n * x.n_split, b = blockIdx.x;
     if (b < first) product_tile<E, ASYNC, true, false, kSums, 0, S>(lds, x, x_tiles_m, x_tiles_n, b % n, b / n);
-    else product_tile<E, ASYNC, false, false, kPlain, 0, S>(lds, w, w_tiles_m, w_tiles_n, (b - first) % (w_tiles_m * w_tiles_n), (b - first) / (w_tiles_m * w_tiles_n));
+    else product_tile<E, ASYNC, false, false, sizeof(E) == 2 ? kTokens : kPlain, 0, S>(lds, w, w_tiles_m, w_tiles_n, (b - first) % (w_tiles_m * w_tiles_n), (b - first) / (w_tiles_m * w_tiles_n));
 }
 
 // dW of few items, a few steps of k: what is written bounds it, and workgroups with one buffer of either operand leave a CU room for four.
@@ -60,6 +60,14 @@ __global__ __launch_bounds__(S::kThreads, 4) void psattn_head_outer(Product d, i
     const LaneRead<E, false> lp(l, wm * MB), lq(l, wn * NB);
     constexpr int kP = decltype(cp)::PER, kQ = decltype(cq)::PER;
     const char *pc = static_cast<const char*>(d.p[0]) + m0 * static_cast<int64_t>(sizeof(E)), *qc = static_cast<const char*>(d.q[0]) + n0 * static_cast<int64_t>(sizeof(E));
+    int item[MB];  // asked for ahead of the copies
+    if constexpr (sizeof(E) == 2) {
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+            const int row = m0 + (wm * MB + mb) * 32 + (l & 31);
+            item[mb] = d.out[1] && row < d.M ? static_cast<const int32_t*>(d.H)[row] : -1;
+        }
+    }
     f32x16 acc[NB][MB] = {};
     for (int k = 0; k < d.K; k += kBK<E>) {
         if (k > 0) __syncthreads();
@@ -94,9 +102,18 @@ __global__ __launch_bounds__(S::kThreads, 4) void psattn_head_outer(Product d, i
     const int nw = n0 + wn * kCols;
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
+        const int m = m0 + (wm * MB + mb) * 32;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             const Chunks x = chunks(acc[nb][mb]);
+            if constexpr (sizeof(E) == 2)
+                if (item[mb] >= 0) {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const int n = nw + nb * 32 + 16 * k + 8 * (l >> 5);
+                        put_rest(static_cast<uint16_t*>(d.out[1]) + item[mb] * d.ldo + n, x.c[k], d.N - n);
+                    }
+                }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 char* const to = mine + (l & 31) * kPitch + (nb * 32 + 16 * k + 8 * (l >> 5)) * static_cast<int>(sizeof(E));
@@ -109,7 +126,6 @@ __global__ __launch_bounds__(S::kThreads, 4) void psattn_head_outer(Product d, i
             }
         }
         __builtin_amdgcn_wave_barrier();
-        const int m = m0 + (wm * MB + mb) * 32;
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
             constexpr int kRow = kCols / EPC;  // chunks of a row
