@@ -34,7 +34,8 @@ constexpr int64_t up64(int64_t n) { return (n + 63) / 64 * 64; }  // a step of k
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 size_t elem_bytes(int32_t dt) { return dt == PSATTN_BF16 ? 2 : 4; }
 
-// ---- the items' rows, made whole: one workgroup to a row.  Without a token of the vocabulary an item has no gradient, and its row is zeros there.
+// ---- the items' rows, made whole: one workgroup to a row.  Without a token of the vocabulary, or with a weight of 0, an item has no gradient, and its
+// row is zeros there: what is not finite in it would reach all of dW by dz = 0.
 // BWD: up to `again` the rows stand there once more (for the second part of dz), and behind them, in dz too, rows of zeros, so that dW's
 // k is whole steps.  item_of: all -1
 template <typename E, bool BWD>
@@ -54,18 +55,19 @@ __global__ __launch_bounds__(256) void psattn_head_rows(int n_items, int again, 
     const int64_t i = at < n_items ? at : at - n_items;
     const int r = item_row[i], row = r < 0 ? ~r : r, id = token_ids[item_tok[i]];
     const bool known = id >= 0 && id < vocab;
+    const float d = BWD && known ? d_logp[item_resp[i]] : 0.f;
     if (threadIdx.x == 0 && at < n_items) {
         target[i] = known ? id : -1;
         if constexpr (BWD) {
             lse[i] = known ? row_lse[row] : 0.f;
-            weight[i] = known ? d_logp[item_resp[i]] : 0.f;
+            weight[i] = d;
             at_token[i] = 0.f;
         }
     }
     const E* const x = X + static_cast<int64_t>(row) * hidden;
     for (int c = threadIdx.x * V; c < ld; c += 256 * V) {
         rows::u32x4 u = {0, 0, 0, 0};
-        if ((!BWD || known) && c < hidden) {
+        if ((!BWD || d != 0.f) && c < hidden) {
             const auto p = rows::place<false, E>(c, hidden);
             u = rows::settled<false>(rows::raw<false>(x, p, hidden), p.down);
         }
@@ -383,7 +385,7 @@ __global__ __launch_bounds__(256) void psattn_head_dw_join(int n_parts, int cols
 template <typename E>
 __global__ __launch_bounds__(256) void psattn_head_dx(int64_t first, int col_blocks, int hidden, int n_items, int again, int n_parts, int64_t ld, const float* parts, const int32_t* row_desc,
                                                       const int32_t* resp_first, const int32_t* resp_len, const int32_t* resp_prev, const int32_t* samp_ptr,
-                                                      const int32_t* item_ptr, const int32_t* target, const float* at_token, const E* W, E* dX) {
+                                                      const int32_t* item_ptr, const int32_t* target, const float* weight, const float* at_token, const E* W, E* dX) {
     constexpr int V = 4;
     const int64_t block = first + blockIdx.x;
     const int row = static_cast<int>(block / col_blocks), desc = row_desc[row];
@@ -396,6 +398,7 @@ __global__ __launch_bounds__(256) void psattn_head_dx(int64_t first, int col_blo
         for (int j = r0; j < r1; ++j) {
             if (resp_len[j] == 0) continue;
             const int i = item_ptr[j] + (desc >= 0 ? row - resp_first[j] + (resp_prev[j] >= 0 ? 1 : 0) : 0);
+            if (weight[i] == 0.f) continue;
             const int64_t step = again * ld;
             for (int64_t row_of = i; row_of < again; row_of += n_items) {  // and its second part's
                 const float* from = parts + row_of * ld + c;
@@ -424,7 +427,7 @@ __global__ __launch_bounds__(256) void psattn_head_dx(int64_t first, int col_blo
 template <typename E>
 __global__ __launch_bounds__(1024) void psattn_head_dx_parts(int64_t first, int col_blocks, int hidden, int n_items, int again, int n_parts, int64_t ld, const float* parts,
                                                              const int32_t* row_desc, const int32_t* resp_first, const int32_t* resp_len, const int32_t* resp_prev,
-                                                             const int32_t* samp_ptr, const int32_t* item_ptr, const int32_t* target, const float* at_token, const E* W, E* dX) {
+                                                             const int32_t* samp_ptr, const int32_t* item_ptr, const int32_t* target, const float* weight, const float* at_token, const E* W, E* dX) {
     constexpr int V = 4, kAtOnce = 4;
     __shared__ float4 sm[16][64];
     const int64_t block = first + blockIdx.x;
@@ -440,6 +443,7 @@ __global__ __launch_bounds__(1024) void psattn_head_dx_parts(int64_t first, int 
         for (int j = r0; j < r1; ++j) {
             if (resp_len[j] == 0) continue;
             const int i = item_ptr[j] + (desc >= 0 ? row - resp_first[j] + (resp_prev[j] >= 0 ? 1 : 0) : 0);
+            if (weight[i] == 0.f) continue;
             for (int64_t row_of = i; row_of < again; row_of += n_items) {
                 const float* const from = parts + row_of * ld + c;
                 int p = w;
@@ -714,6 +718,7 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
     const bool apart = dz_apart(dt, n);  // dz at the items' tokens
     uint16_t* const rest_w = static_cast<uint16_t*>(dX);  // written last, and an item's row in it free until then: there are no more items than tokens
     float *sums = nullptr, *at_token = nullptr;
+    const float* weights = nullptr;
     const int32_t *target = nullptr, *item_of = nullptr;
     const uint16_t* x_rows = nullptr;
     if (n == 0) {  // nothing is predicted: sums over nothing
@@ -731,6 +736,7 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
         float *const lse = room.take<float>(n), *const weight = room.take<float>(n);
         at_token = room.take<float>(n);
         target = targets;
+        weights = weight;
         int32_t* const items = apart ? room.take<int32_t>(vocab) : nullptr;
         item_of = items;
         auto gather = [&](auto* to) {
@@ -815,7 +821,7 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
             using E = std::remove_pointer_t<decltype(to)>;
             auto kernel = many ? psattn_head_dx_parts<E> : psattn_head_dx<E>;
             kernel<<<grid, many ? 1024 : 256, 0, s>>>(at, col_blocks, hidden, n, again, parts, ld, sums, plan->row_desc, plan->resp_first, plan->resp_len, plan->resp_prev,
-                                                     plan->samp_ptr, plan->item_ptr, target, apart ? at_token : nullptr, static_cast<const E*>(W), to);
+                                                     plan->samp_ptr, plan->item_ptr, target, weights, apart ? at_token : nullptr, static_cast<const E*>(W), to);
         };
         if (dt == PSATTN_BF16) go(static_cast<uint16_t*>(dX));
         else go(static_cast<float*>(dX));
