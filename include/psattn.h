@@ -432,8 +432,9 @@ int psattn_dpo_loss(int32_t n_pairs, float beta, const float* logp_policy, const
  * weight, is not rounded.  Sums are fp32 in a fixed order, rounded to dt at the end; until then dX may hold other rows.  A response whose
  * d_resp_logp is 0, and a token id outside [0, vocab), give nothing.
  * Workspaces: the caller's device memory, of at least the bytes that the call of that name gives for the plan (never 0 for valid
- * arguments), contents undefined on entry and exit, one for each call in flight.  The backward's holds the rows and one piece (some
- * 512 MiB, 256 tokens of the vocabulary at least) of the logits' gradient.  No call allocates or blocks, and all may be captured into a graph.
+ * arguments), contents undefined on entry and exit, one for each call in flight.  The forward's holds the rows of X that predict and 8 bytes for
+ * each of them and 128 tokens of the vocabulary; the backward's the rows, their gradient's fp32 sums, of bf16 4 bytes for each token of the vocabulary, and one
+ * piece (512 MiB at most, or 256 tokens of the vocabulary) of the logits' gradient.  No call allocates or blocks, and all may be captured into a graph.
  * PSATTN_EUNSUPPORTED: rows of 2^23 bytes and more, some 2^23 predicted tokens and more, or sizes whose grids would have 2^31
  * threads.  PSATTN_EINVAL also for a plan of another device than the current one.
  */

@@ -546,19 +546,20 @@ int head_product(int32_t dt, Pass pass, bool qkc, TileSize size, Product d, hipS
     return (whole ? head_product_f32_whole : head_product_f32)(pass, qkc, size, d, s);
 }
 
-// dz of a piece of the vocabulary has this much room at most
-constexpr int64_t kPieceBytes = int64_t{512} << 20;
-int64_t piece_rows(int32_t dt, int64_t n_items, int64_t vocab) {
-    const int64_t most = kPieceBytes / static_cast<int64_t>(elem_bytes(dt)) / std::max<int64_t>(n_items, 1) / 256 * 256;
-    if (most >= vocab) return vocab;
-    const int64_t n = cdiv(vocab, std::max<int64_t>(most, 256));
-    return cdiv(cdiv(vocab, n), 256) * 256;
-}
 // Few items of bf16: dz as two numbers each, the second what the first one's rounding leaves, as items of their own.  The gradients are as
 // exact as their own rounding then.  Of more items dz at their tokens alone is kept exact (psattn_head_dw_tokens)
 constexpr int64_t kTwice = 32;
 bool dz_apart(int32_t dt, int64_t n_items) { return dt == PSATTN_BF16 && n_items > kTwice; }
 int64_t dz_rows(int32_t dt, int64_t n_items) { return dt == PSATTN_BF16 && n_items <= kTwice ? 2 * n_items : n_items; }
+// dz of a piece of the vocabulary, whole steps of k for dW, has this much room at most.  A step's rows are then within the 32-bit offsets of
+// the products' copies
+constexpr int64_t kPieceBytes = int64_t{512} << 20;
+int64_t piece_rows(int32_t dt, int64_t n_items, int64_t vocab) {
+    const int64_t most = kPieceBytes / static_cast<int64_t>(elem_bytes(dt)) / std::max<int64_t>(up64(dz_rows(dt, n_items)), 64) / 256 * 256;
+    if (most >= vocab) return vocab;
+    const int64_t n = cdiv(vocab, std::max<int64_t>(most, 256));
+    return cdiv(cdiv(vocab, n), 256) * 256;
+}
 constexpr int kManyParts = 16;
 // dX's sums: k is a piece of the vocabulary, in parts where the rows' tiles are few.
 // `both`: dX and dW of a piece in one launch, no part of k longer than half of what a CU has to do.  A whole step in us, apart / so: bf16, vocabulary
