@@ -18,9 +18,5 @@ struct psattn_lp_plan {
     const int32_t* resp_len = nullptr;     // [n_resp]
     const int32_t* resp_prev = nullptr;    // [n_resp]   last prompt row of its sample, -1 if the prompt is empty
     const int32_t* samp_ptr = nullptr;     // [n_samples + 1] responses of sample i
-    // items: a row and a token that it predicts, response by response
-    const int32_t* item_row = nullptr;     // [n_items]  its row; ~row where an earlier item has the same row
-    const int32_t* item_tok = nullptr;     // [n_items]  place of the token that is predicted
-    const int32_t* item_resp = nullptr;    // [n_items]
-    const int32_t* item_ptr = nullptr;     // [n_resp + 1]
+    const int32_t* item_ptr = nullptr;     // [n_resp + 1] items of response j: a row and the token that it predicts, one after the other
 };

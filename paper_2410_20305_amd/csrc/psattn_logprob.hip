@@ -351,29 +351,16 @@ int psattn_logprob_plan(int32_t n_samples, const int32_t* offset, const int32_t*
         }
         for (int32_t t = 0; t < total_tokens; ++t)
             if (row_desc[t] != -1) rows.push_back(t);
-        std::vector<int32_t> item_row, item_tok, item_resp, item_ptr(static_cast<size_t>(n_resp) + 1);
-        item_row.reserve(n_items), item_tok.reserve(n_items), item_resp.reserve(n_items);
-        int32_t led = -1;  // the last prompt row that has an item already
-        for (int32_t j = 0; j < n_resp; ++j) {
-            item_ptr[j] = static_cast<int32_t>(item_row.size());
-            for (int32_t u = prev[j] < 0 ? 1 : 0; u < len[j]; ++u) {
-                const int32_t row = u == 0 ? prev[j] : first[j] + u - 1;
-                item_row.push_back(u == 0 && led == row ? ~row : row);
-                if (u == 0) led = row;
-                item_tok.push_back(first[j] + u);
-                item_resp.push_back(j);
-            }
-        }
-        item_ptr[n_resp] = static_cast<int32_t>(item_row.size());
+        std::vector<int32_t> item_ptr(static_cast<size_t>(n_resp) + 1);
+        for (int32_t j = 0; j < n_resp; ++j) item_ptr[j + 1] = item_ptr[j] + len[j] - (prev[j] >= 0 || len[j] == 0 ? 0 : 1);
         psattn_lp_plan* pl = new psattn_lp_plan();
         pl->T = total_tokens; pl->n_samples = n_samples; pl->n_resp = n_resp;
         pl->n_rows = static_cast<int32_t>(rows.size()); pl->n_items = n_items;
-        // one blob: rows | row_desc | first | len | prev | samp_ptr | items
+        // one blob: rows | row_desc | first | len | prev | samp_ptr | item_ptr
         size_t off = 0;
         auto take = [&](size_t n) { const size_t o = off; off = align_up(off + n * sizeof(int32_t), 256); return o; };
         const size_t o_rows = take(rows.size()), o_desc = take(row_desc.size()), o_first = take(n_resp), o_len = take(n_resp),
-                     o_prev = take(n_resp), o_ptr = take(static_cast<size_t>(n_samples) + 1), o_irow = take(item_row.size()),
-                     o_itok = take(item_tok.size()), o_iresp = take(item_resp.size()), o_iptr = take(item_ptr.size());
+                     o_prev = take(n_resp), o_ptr = take(static_cast<size_t>(n_samples) + 1), o_iptr = take(item_ptr.size());
         std::vector<char> host(off ? off : 256, 0);
         auto put = [&](size_t o, const int32_t* src, size_t n) { if (n) std::memcpy(host.data() + o, src, n * sizeof(int32_t)); };
         put(o_rows, rows.data(), rows.size());
@@ -382,9 +369,6 @@ int psattn_logprob_plan(int32_t n_samples, const int32_t* offset, const int32_t*
         put(o_len, len.data(), n_resp);
         put(o_prev, prev.data(), n_resp);
         if (n_samples > 0) put(o_ptr, resp_ptr, static_cast<size_t>(n_samples) + 1);
-        put(o_irow, item_row.data(), item_row.size());
-        put(o_itok, item_tok.data(), item_tok.size());
-        put(o_iresp, item_resp.data(), item_resp.size());
         put(o_iptr, item_ptr.data(), item_ptr.size());
         hipStream_t s = static_cast<hipStream_t>(hip_stream);
         if (hipGetDevice(&pl->device) != hipSuccess || hipMalloc(&pl->d_blob, host.size()) != hipSuccess) {
@@ -407,9 +391,6 @@ int psattn_logprob_plan(int32_t n_samples, const int32_t* offset, const int32_t*
         pl->resp_len = reinterpret_cast<const int32_t*>(d + o_len);
         pl->resp_prev = reinterpret_cast<const int32_t*>(d + o_prev);
         pl->samp_ptr = reinterpret_cast<const int32_t*>(d + o_ptr);
-        pl->item_row = reinterpret_cast<const int32_t*>(d + o_irow);
-        pl->item_tok = reinterpret_cast<const int32_t*>(d + o_itok);
-        pl->item_resp = reinterpret_cast<const int32_t*>(d + o_iresp);
         pl->item_ptr = reinterpret_cast<const int32_t*>(d + o_iptr);
         *out = pl;
     } catch (const std::bad_alloc&) {
