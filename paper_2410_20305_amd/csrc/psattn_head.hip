@@ -360,7 +360,10 @@ __global__ __launch_bounds__(256) void psattn_head_dw_tokens(int first, int lane
     rest += static_cast<int64_t>(i) * hidden + c;
 #pragma unroll
     for (int k = 0; k < V; ++k)
-        if (c + k < hidden) rows::store1(to + k, rows::to_f32(to[k]) + (rows::to_f32(rest[k]) + sum[k]));
+        if (c + k < hidden) {
+            const float x = rows::to_f32(to[k]);  // of one beyond bf16's range nothing is left that would be a number
+            rows::store1(to + k, x + (fabsf(x) < INFINITY ? rows::to_f32(rest[k]) + sum[k] : sum[k]));
+        }
 }
 
 // dW of a piece from its parts, four columns to a lane; item_of and rest as kTokens has them, or null

@@ -90,3 +90,26 @@ def test_a_result_does_not_depend_on_who_comes_first():
         got.append(ps.psattn_head_logprob_bwd(plan, tX, tW, tid, lse, d, workspace=ws))
     for g in got[1:]:
         assert torch.equal(g[0], got[0][0]) and torch.equal(g[1], got[0][1])
+
+
+@pytest.mark.parametrize("n,V,h", [(40, 300, 64), (300, 520, 72), (1100, 300, 64)])
+def test_sums_beyond_the_range_of_bf16(n, V, h):
+    """A column of X that holds the largest numbers, a token that many rows find probable and one row is followed by: what the others take away is
+    beyond fp32, the one row's part within it, so dW is infinite there, not NaN, and the other columns are as they are without it."""
+    X, W, ids = _calibrated(n, V, h, 17, 0.5)
+    W[:, 5] = 0
+    ids[ids == 17] = 18
+    ids[n // 2] = 17
+    plan = ps.LogprobPlan([0], [1], [0, 1], [n], n + 1)
+    tW, tid, d = torch.from_numpy(W).bfloat16().cuda(), torch.from_numpy(ids.astype(np.int32)).cuda(), torch.tensor([1.0], device="cuda")
+    got = []
+    for top in (0.0, 3e38):
+        X[:, 5] = top
+        tX = torch.from_numpy(X).bfloat16().cuda()
+        lse, _ = ps.psattn_head_logprob_fwd(plan, tX, tW, tid)
+        got.append(ps.psattn_head_logprob_bwd(plan, tX, tW, tid, lse, d))
+    (dX, dW), (dX2, dW2) = got
+    assert torch.equal(dX, dX2)
+    keep = torch.arange(h, device="cuda") != 5
+    assert torch.equal(dW[:, keep], dW2[:, keep])
+    assert dW2[17, 5] == -float("inf")
