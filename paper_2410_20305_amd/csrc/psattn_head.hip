@@ -12,7 +12,7 @@
 // tokens, do not.  A prompt's last row predicts the first token of every response and takes part once for each.
 //
 // Bound by the matrix cores (four products of 2 items vocab hidden operations in a training step, one of them to make the logits again), for few rows by
-// reading W.  No atomics: every sum has a fixed order.
+// reading W.  Every sum has a fixed order, and none is made by atomics.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
