@@ -33,6 +33,8 @@ constexpr int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
 constexpr int64_t up64(int64_t n) { return (n + 63) / 64 * 64; }  // a step of k of bf16, two of fp32
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 size_t elem_bytes(int32_t dt) { return dt == PSATTN_BF16 ? 2 : 4; }
+// of psattn_head_rows: a lane to 16 bytes, up to four waves
+int row_threads(int32_t dt, int64_t hidden) { return static_cast<int>(std::min<int64_t>(256, up64(cdiv(hidden, dt == PSATTN_BF16 ? 8 : 4)))); }
 
 // ---- items, numbered response by response: which row and which token are the i-th's.  (Tables of them would be most of a plan: with, without 2.2 and
 // 0.95 ms for 2^20 tokens of 512 samples, 136 and 66 us for 65 536 of 64.)
@@ -40,14 +42,27 @@ struct Items {
     int32_t n_resp;
     const int32_t *ptr, *resp_first, *resp_prev;  // a plan's
 };
-__device__ __forceinline__ int response_of(const Items& t, int i) {  // empty ones have no item
-    int lo = 0, hi = t.n_resp;
-    while (hi - lo > 1) {
-        const int mid = lo + (hi - lo) / 2;
-        if (t.ptr[mid] <= i) lo = mid;
-        else hi = mid;
+// The last response that starts at item i or ahead of it (empty ones have no item), by a whole wave, 256 places at a time.  9 812 items of 96 responses
+// and 512 columns, forward's and backward's rows: by halves, seven loads one after the other, in workgroups of 256 12.8 and 16.9 us; so, in as many waves
+// as a row has work for, 7.1 and 7.8
+__device__ __forceinline__ int response_of(const Items& t, int i) {
+    const int l = threadIdx.x & 63;
+    int first = 0, n = t.n_resp;
+    while (n > 1) {
+        const int step = (n - 1) / 256 + 1;
+        bool ahead[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int at = (q * 64 + l) * step;
+            ahead[q] = at < n && t.ptr[first + at] <= i;
+        }
+        int k = -1;  // they ascend
+#pragma unroll
+        for (int q = 0; q < 4; ++q) k += __builtin_popcountll(__builtin_amdgcn_ballot_w64(ahead[q]));
+        first += k * step;
+        n = min(step, n - k * step);
     }
-    return lo;
+    return first;
 }
 
 // ---- the items' rows, made whole: one workgroup to a row.  Without a token of the vocabulary, or with a weight of 0, an item has no gradient, and its
@@ -60,18 +75,20 @@ __global__ __launch_bounds__(256) void psattn_head_rows(int n_items, int again, 
     constexpr int V = rows::kVec<E>;
     const int64_t at = blockIdx.x, ld = (hidden + 7) / 8 * 8;
     if (BWD && item_of)
-        for (int64_t v = at * 256 + threadIdx.x; v < vocab; v += gridDim.x * 256) item_of[v] = -1;
+        for (int64_t v = at * blockDim.x + threadIdx.x; v < vocab; v += gridDim.x * blockDim.x) item_of[v] = -1;
     if (BWD && at >= again) {
         const rows::u32x4 zero = {0, 0, 0, 0};
-        for (int64_t c = threadIdx.x * V; c < ld; c += 256 * V) *reinterpret_cast<rows::u32x4*>(out + at * ld + c) = zero;
-        for (int64_t c = threadIdx.x * V; c < ldz; c += 256 * V) *reinterpret_cast<rows::u32x4*>(dz + at * ldz + c) = zero;
+        for (int64_t c = threadIdx.x * V; c < ld; c += blockDim.x * V) *reinterpret_cast<rows::u32x4*>(out + at * ld + c) = zero;
+        for (int64_t c = threadIdx.x * V; c < ldz; c += blockDim.x * V) *reinterpret_cast<rows::u32x4*>(dz + at * ldz + c) = zero;
         return;
     }
     const int i = static_cast<int>(at < n_items ? at : at - n_items), j = response_of(items, i);
     const int prev = items.resp_prev[j], u = i - items.ptr[j] + (prev < 0 ? 1 : 0), first = items.resp_first[j];
     const int row = u == 0 ? prev : first + u - 1, id = token_ids[first + u];
     const bool known = id >= 0 && id < vocab;
-    const float d = BWD && known ? d_logp[j] : 0.f;
+    const float d_j = BWD ? d_logp[j] : 0.f, d = known ? d_j : 0.f;
+    // an earlier item of this row: the last one, of the response ahead or, behind empty ones, another
+    const bool again_row = !BWD && u == 0 && i > 0 && items.resp_prev[items.ptr[j - 1] < i ? j - 1 : response_of(items, i - 1)] == prev;
     if (threadIdx.x == 0 && at < n_items) {
         target[i] = known ? id : -1;
         if constexpr (BWD) {
@@ -79,16 +96,17 @@ __global__ __launch_bounds__(256) void psattn_head_rows(int n_items, int again, 
             weight[i] = d;
             at_token[i] = 0.f;
         } else {
-            item_row[i] = u == 0 && i > 0 && items.resp_prev[response_of(items, i - 1)] == prev ? ~row : row;
+            item_row[i] = again_row ? ~row : row;
         }
     }
     const E* const x = X + static_cast<int64_t>(row) * hidden;
-    for (int c = threadIdx.x * V; c < ld; c += 256 * V) {
+    for (int c = threadIdx.x * V; c < ld; c += blockDim.x * V) {
         rows::u32x4 u = {0, 0, 0, 0};
-        if ((!BWD || d != 0.f) && c < hidden) {
+        if (c < hidden) {
             const auto p = rows::place<false, E>(c, hidden);
             u = rows::settled<false>(rows::raw<false>(x, p, hidden), p.down);
         }
+        if (BWD && d == 0.f) u = rows::u32x4{0, 0, 0, 0};
         *reinterpret_cast<rows::u32x4*>(out + at * ld + c) = u;
     }
 }
@@ -693,7 +711,7 @@ int psattn_head_logprob_fwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
     if (n > 0) {
         auto gather = [&](auto* to) {
             using E = std::remove_pointer_t<decltype(to)>;
-            psattn_head_rows<E, false><<<n, 256, 0, s>>>(n, n, {plan->n_resp, plan->item_ptr, plan->resp_first, plan->resp_prev}, item_row, token_ids, vocab, hidden, static_cast<const E*>(X),
+            psattn_head_rows<E, false><<<n, row_threads(dt, hidden), 0, s>>>(n, n, {plan->n_resp, plan->item_ptr, plan->resp_first, plan->resp_prev}, item_row, token_ids, vocab, hidden, static_cast<const E*>(X),
                                                          nullptr, nullptr, to, target, nullptr, nullptr, nullptr, nullptr, nullptr, 0);
         };
         if (dt == PSATTN_BF16) gather(reinterpret_cast<uint16_t*>(x));
@@ -763,7 +781,7 @@ int psattn_head_logprob_bwd(const psattn_lp_plan* plan, int32_t dt, int32_t voca
         item_of = items;
         auto gather = [&](auto* to) {
             using E = std::remove_pointer_t<decltype(to)>;
-            psattn_head_rows<E, true><<<n_whole, 256, 0, s>>>(n, again, {plan->n_resp, plan->item_ptr, plan->resp_first, plan->resp_prev}, nullptr, token_ids, vocab, hidden, static_cast<const E*>(X),
+            psattn_head_rows<E, true><<<n_whole, row_threads(dt, hidden), 0, s>>>(n, again, {plan->n_resp, plan->item_ptr, plan->resp_first, plan->resp_prev}, nullptr, token_ids, vocab, hidden, static_cast<const E*>(X),
                                                               row_lse, d_resp_logp, to, targets, lse, weight, at_token, items, reinterpret_cast<E*>(dz), ldz);
         };
         if (dt == PSATTN_BF16) gather(reinterpret_cast<uint16_t*>(x));
